@@ -7,8 +7,8 @@
  * Conventions for every entry point
  *   - Pointers are DEVICE pointers unless the name starts with host_ or the comment says
  *     "host".  The caller owns every buffer it passes; the library allocates device memory
- *     only inside mts_tables_create and mts_cache_create and frees it in the matching
- *     destroy call.
+ *     only inside mts_tables_create, mts_cache_create and mts_adamw_create and frees it in the
+ *     matching destroy call.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Work is
  *     enqueued asynchronously; no entry point synchronises the device except where stated.
  *   - Return value: MTS_OK (0) or a negative MTS_ERR_* code.  Nothing throws, exits, aborts or
@@ -42,6 +42,7 @@ extern "C" {
 
 #define MTS_DTYPE_FP32 0
 #define MTS_DTYPE_FP16 1
+#define MTS_DTYPE_BF16 2        /* dense tensors only: tables and caches hold fp32 or fp16 rows */
 
 #define MTS_POOL_SUM 0
 #define MTS_POOL_MEAN 1
@@ -573,6 +574,132 @@ int mts_cache_import_state(mts_cache* cache, const int64_t* tags, const int64_t*
  * rows of that call are incomplete, the call can simply be repeated.  0 makes every call give up at once:
  * for testing the error path without hanging anything. */
 int mts_cache_set_fetch_wait_limit(mts_cache* cache, int64_t polls);
+
+/* ---------------------------------------------------------------------------------------
+ * The sequence tower beside the tables (the paper trains the dense network next to the embedding
+ * path, Sections 2.1 and 5.9, and does not describe its operators): a gated linear recurrence over
+ * packed ragged histories, the learned relative position bias of the attention over them, and the
+ * AdamW step of the dense parameters.  Sums, states and statistics are fp32 (or wider) whatever
+ * the tensors' type; a value is rounded to its storage type once, to nearest even.  Results are
+ * deterministic: they depend on the inputs and sizes only.
+ * ------------------------------------------------------------------------------------- */
+
+/* Gated linear recurrence.  The tokens of S sequences are packed: sequence s is rows
+ * [offsets[s], offsets[s+1]) of [N, D] arrays (offsets int64 [S+1] on the device, offsets[0] == 0,
+ * offsets[S] == N, the CSR form of the sparse input).  Per channel, with z_t = 1 / (1 + exp(-gate_t)):
+ *   h_t = h_{t-1} + z_t * (value_t - h_{t-1}),   h before a sequence's first token = h0[s] (0 when h0 is NULL)
+ *   gate, value, out : [N, D] of one type (MTS_DTYPE_*), rows *_stride elements apart (>= D), so that gate and
+ *                      value may be column ranges of one projection; out must not overlap the inputs.
+ *   h0, h_final      : fp32 [S, D]; h_final (nullable) receives the state after each sequence's last token, h0 for
+ *                      an empty one.  h_final == h0 is allowed: kept states updated in place (the single-token
+ *                      form is the same call with sequences of length one).
+ *   entry_states     : fp32 [mts_recurrence_chunks(N, D, dtype), D] (nullable; needed by the backward): the
+ *                      state before the first token of each chunk of the token axis.
+ *   workspace        : mts_recurrence_workspace_bytes(N, S, D, dtype) bytes, 256-byte aligned, contents undefined
+ *                      on entry; the same size serves the backward.
+ * Any alignment is accepted; rows that start on 4-element boundaries (D, strides and bases multiples of 4) are fastest.
+ * Offsets that descend or leave [0, N] are clamped (memory-safe, results undefined) and reported by
+ * mts_recurrence_status.  Errors: INVALID_ARG, UNSUPPORTED (N, S >= 2^31 - 2^16 or D > 2^20), WORKSPACE, ALIGNMENT
+ * (workspace), CUDA. */
+int64_t mts_recurrence_chunks(int64_t N, int32_t D, int32_t dtype);
+size_t mts_recurrence_workspace_bytes(int64_t N, int64_t S, int32_t D, int32_t dtype);
+int mts_recurrence_forward(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride,
+                           int32_t dtype, int64_t N, int32_t D, const int64_t* offsets, int64_t S, const float* h0,
+                           void* out, int64_t out_stride, float* h_final, float* entry_states, void* workspace,
+                           size_t workspace_bytes, void* stream);
+/* Its gradient.  With G_t = grad_out_t + (1 - z_{t+1}) G_{t+1} inside a sequence and G_last += grad_final[s]:
+ *   grad_value_t = z_t G_t
+ *   grad_gate_t  = z_t (1 - z_t) (value_t - h_{t-1}) G_t
+ *   grad_h0[s]   = (1 - z_first) G_first   (grad_final[s], or 0, for an empty sequence)
+ * The states h are recomputed from entry_states (as the forward of the same inputs left them), not read back from
+ * the rounded output.  grad_out, grad_gate, grad_value: [N, D] of `dtype`; grad_final, grad_h0: fp32 [S, D], nullable;
+ * h0 as in the forward.  The outputs must not overlap the inputs.  Errors as for the forward. */
+int mts_recurrence_backward(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride,
+                            int32_t dtype, int64_t N, int32_t D, const int64_t* offsets, int64_t S, const float* h0,
+                            const float* entry_states, const void* grad_out, int64_t grad_out_stride,
+                            const float* grad_final, void* grad_gate, int64_t grad_gate_stride, void* grad_value,
+                            int64_t grad_value_stride, float* grad_h0, void* workspace, size_t workspace_bytes,
+                            void* stream);
+/* Status word of the last call on this workspace; synchronises `stream`.  Bit 0: offsets were out of order or out of
+ * range.  Bit 1: a bounded wait inside the kernel ran out (results incomplete; also reported as MTS_ERR_TIMEOUT). */
+int mts_recurrence_status(const void* workspace, int32_t* host_status, void* stream);
+
+/* Learned relative position bias by buckets: a table of [rows, heads] with one row per bucket of the distance
+ * r = key position - query position = j - (i + q_offset), looked up for every (query, key):
+ *   out[h, i, j] = table[bucket(r), h],  or -infinity where causal != 0 and r > 0 (a row may be masked entirely).
+ * host_starts: host, ascending (equal neighbours make an empty bucket), host_starts[0] == 0: bucket k holds the
+ * distances d with host_starts[k] <= d < host_starts[k + 1], the last one all larger ones.  two_sided == 0: d = -r for
+ * keys behind the query, 0 for keys ahead, rows = n; two_sided != 0: d = |r|, keys ahead use rows n + k, rows = 2 n.
+ * table: contiguous, MTS_DTYPE_*; out: MTS_DTYPE_*, element strides between heads and between queries (>= Lk), keys
+ * contiguous.  Lq = 1 with q_offset = position is the single-token form.  Any alignment is accepted.
+ * Errors: INVALID_ARG, UNSUPPORTED (n > MTS_RELPOS_MAX_BUCKETS; heads > 65535; Lq, Lk or |q_offset| >= 2^29), CUDA. */
+#define MTS_RELPOS_MAX_BUCKETS 128
+typedef struct {
+  int32_t n;                    /* distance buckets per side */
+  int32_t two_sided;
+  int32_t causal;
+  const int32_t* host_starts;   /* host [n] */
+} mts_relpos_buckets;
+int mts_relpos_bias_forward(const mts_relpos_buckets* buckets, const void* table, int32_t table_dtype, int32_t heads,
+                            int64_t Lq, int64_t Lk, int64_t q_offset, void* out, int32_t out_dtype,
+                            int64_t out_head_stride, int64_t out_row_stride, void* stream);
+/* Gradient of the table, summed over a batch that shares the bias:
+ *   grad_table[k, h] = sum over b, i, j with bucket(r) = k (and r <= 0 where causal) of grad_out[b, h, i, j]
+ * grad_table: fp32 [rows, heads], overwritten.  Masked places are not read into the sums, whatever they hold.
+ * workspace: mts_relpos_bias_workspace_bytes(buckets, heads) bytes, 256-byte aligned, contents undefined.
+ * Errors: as for the forward, WORKSPACE, ALIGNMENT (workspace). */
+size_t mts_relpos_bias_workspace_bytes(const mts_relpos_buckets* buckets, int32_t heads);
+int mts_relpos_bias_backward(const mts_relpos_buckets* buckets, const void* grad_out, int32_t grad_dtype, int64_t B,
+                             int32_t heads, int64_t Lq, int64_t Lk, int64_t q_offset, int64_t batch_stride,
+                             int64_t head_stride, int64_t row_stride, float* grad_table, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* AdamW over many tensors in one launch.  For every element, at time `step` (1, 2, ...), with g = grad * grad_scale:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32 (the decay only for tensors whose host_decays byte is set; NULL = all).  Parameters: MTS_DTYPE_*; with
+ * host_masters (fp32, one per tensor) the update is made to the master and rounded into the parameter.  Gradients:
+ * MTS_DTYPE_*, a type of their own.  Any pointer alignment is accepted; 32-byte aligned tensors are fastest.
+ * State: one caller-owned device buffer of mts_adamw_state_bytes() bytes, 256-byte aligned, zero-filled before the
+ * first step.  Tensor k owns the elements [first_k, first_k + sizes[k]) of the state, first_k = the sum of the earlier
+ * sizes, each rounded up to MTS_ADAMW_BLOCK; P = mts_adamw_state_elements() counts them with the gaps.
+ *   state_bits 32: float m[P], float v[P].
+ *   state_bits 8:  uint8 m[P], uint8 v[P], float m_scale[P / BLOCK], float v_scale[P / BLOCK].  A code c > 0 stands for
+ *                  scale * (the fp32 number with the bit pattern (c + base) << 20): eight steps per octave, the largest
+ *                  code being 1.  m: bit 7 is the sign, base 0x379 (127 codes), rounded to nearest.  v: base 0x2F9
+ *                  (255 codes), rounded up or down by 16 random bits so that it is kept in the mean: with beta2 near 1
+ *                  a step moves v by less than half a code.  The bits are a hash of (element, seed): another `seed`
+ *                  for every step, the same one gives the same result.  A v that is not 0 keeps at least code 1 (a
+ *                  block whose largest is below 2^-120 is stored as 0).  Moments that are not finite are stored as 0
+ *                  (their parameter shows them) and leave the rest of their block alone.
+ * mts_adamw_create copies the description to the device (synchronous; the only allocation); mts_adamw_set_grads replaces
+ * the gradient pointers (host array) for later steps on `stream`, whose pending steps keep the old ones.
+ * grad_scale: device fp32 scalar, nullable (1): a clipping factor or the inverse of a loss scale.
+ * mts_adamw_export_state / _import_state: the moments as fp32 device arrays [P] (16-byte aligned), out of and into a
+ * state; an 8-bit import rounds both to nearest.
+ * Errors: INVALID_ARG, ALIGNMENT (state), WORKSPACE (state too small), UNSUPPORTED (P >= 2^40), CUDA. */
+#define MTS_ADAMW_BLOCK 256
+typedef struct {
+  int32_t n_tensors;
+  int32_t param_dtype;
+  int32_t grad_dtype;
+  int32_t state_bits;               /* 32 or 8 */
+  const int64_t* host_sizes;        /* host [n_tensors] elements (>= 0) */
+  void* const* host_params;         /* host [n_tensors] device pointers */
+  const void* const* host_grads;
+  float* const* host_masters;       /* nullable */
+  const uint8_t* host_decays;       /* nullable */
+} mts_adamw_desc;
+typedef struct mts_adamw mts_adamw;
+int mts_adamw_create(const mts_adamw_desc* desc, mts_adamw** out);
+int mts_adamw_destroy(mts_adamw* adamw);
+int64_t mts_adamw_state_elements(const mts_adamw* adamw);
+size_t mts_adamw_state_bytes(const mts_adamw* adamw);
+int mts_adamw_set_grads(mts_adamw* adamw, const void* const* host_grads, void* stream);
+int mts_adamw_step(mts_adamw* adamw, void* state, size_t state_bytes, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, int64_t step, const float* grad_scale, uint32_t seed, void* stream);
+int mts_adamw_export_state(mts_adamw* adamw, const void* state, size_t state_bytes, float* m_out, float* v_out, void* stream);
+int mts_adamw_import_state(mts_adamw* adamw, void* state, size_t state_bytes, const float* m, const float* v, void* stream);
 
 #ifdef __cplusplus
 }

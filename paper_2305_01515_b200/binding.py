@@ -17,7 +17,7 @@ LIB_PATH = os.environ.get("MTRAINS_B200_LIB", os.path.join(HERE, "libmtrains_b20
 OK = 0
 ERR_INVALID_ARG, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CAPACITY, ERR_CUDA, ERR_TIMEOUT, ERR_UNSUPPORTED = (
     -1, -2, -3, -4, -5, -6, -7)
-DTYPE_FP32, DTYPE_FP16 = 0, 1
+DTYPE_FP32, DTYPE_FP16, DTYPE_BF16 = 0, 1, 2
 POOL_SUM, POOL_MEAN, POOL_MAX = 0, 1, 2
 POLICY_LRU, POLICY_LFU = 0, 1
 MAX_CACHES, CACHE_WAYS, NUM_COUNTERS, NUM_COUNTERS2 = 8, 32, 10, 20
@@ -40,7 +40,12 @@ EXPORTS = (
     "mts_place_tables",
     "mts_cache_prefetch_misses", "mts_host_gather_rows", "mts_host_scatter_rows", "mts_cache_place_fetched", "mts_cache_save_victims", "mts_mover_create", "mts_mover_submit", "mts_mover_stream_wait_moved", "mts_mover_drain", "mts_mover_stats", "mts_mover_destroy", "mts_cache_writeback_evicted", "mts_cache_refetch_overflowed", "mts_cache_flush",
     "mts_cache_export_state",
+    "mts_recurrence_chunks", "mts_recurrence_workspace_bytes", "mts_recurrence_forward", "mts_recurrence_backward",
+    "mts_recurrence_status", "mts_relpos_bias_forward", "mts_relpos_bias_workspace_bytes", "mts_relpos_bias_backward",
+    "mts_adamw_create", "mts_adamw_destroy", "mts_adamw_state_elements", "mts_adamw_state_bytes", "mts_adamw_set_grads",
+    "mts_adamw_step", "mts_adamw_export_state", "mts_adamw_import_state",
 )
+ADAMW_BLOCK, RELPOS_MAX_BUCKETS = 256, 128
 
 
 class MtsError(RuntimeError):
@@ -55,6 +60,20 @@ class TableDesc(C.Structure):
                 ("host_weight_offset", C.POINTER(C.c_int64)), ("host_cache_id", C.POINTER(C.c_int32)),
                 ("dev_weights", C.c_void_p), ("host_weights_mapped", C.c_void_p),
                 ("momentum", C.c_void_p)]
+
+
+class RelposBucketsDesc(C.Structure):
+    """mts_relpos_buckets of the header."""
+    _fields_ = [("n", C.c_int32), ("two_sided", C.c_int32), ("causal", C.c_int32),
+                ("host_starts", C.POINTER(C.c_int32))]
+
+
+class AdamWDesc(C.Structure):
+    """mts_adamw_desc of the header."""
+    _fields_ = [("n_tensors", C.c_int32), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("state_bits", C.c_int32), ("host_sizes", C.POINTER(C.c_int64)), ("host_params", C.POINTER(C.c_void_p)),
+                ("host_grads", C.POINTER(C.c_void_p)), ("host_masters", C.POINTER(C.c_void_p)),
+                ("host_decays", C.POINTER(C.c_uint8))]
 
 
 _lib = None
@@ -135,6 +154,30 @@ def lib():
         L.mts_cache_set_fetch_wait_limit.argtypes = [vp, i64]
         L.mts_place_tables.argtypes = [i32, C.POINTER(i64), C.POINTER(C.c_double), i64, C.c_double, C.c_double,
                                        C.POINTER(i32), C.POINTER(C.c_double), C.POINTER(i32)]
+        f64, u32 = C.c_double, C.c_uint32
+        L.mts_recurrence_chunks.restype = i64
+        L.mts_recurrence_chunks.argtypes = [i64, i32, i32]
+        L.mts_recurrence_workspace_bytes.restype = sz
+        L.mts_recurrence_workspace_bytes.argtypes = [i64, i64, i32, i32]
+        L.mts_recurrence_forward.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.mts_recurrence_backward.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp,
+                                              i64, vp, vp, sz, vp]
+        L.mts_recurrence_status.argtypes = [vp, C.POINTER(i32), vp]
+        buckets = C.POINTER(RelposBucketsDesc)
+        L.mts_relpos_bias_forward.argtypes = [buckets, vp, i32, i32, i64, i64, i64, vp, i32, i64, i64, vp]
+        L.mts_relpos_bias_workspace_bytes.restype = sz
+        L.mts_relpos_bias_workspace_bytes.argtypes = [buckets, i32]
+        L.mts_relpos_bias_backward.argtypes = [buckets, vp, i32, i64, i32, i64, i64, i64, i64, i64, i64, vp, vp, sz, vp]
+        L.mts_adamw_create.argtypes = [C.POINTER(AdamWDesc), C.POINTER(vp)]
+        L.mts_adamw_destroy.argtypes = [vp]
+        L.mts_adamw_state_elements.restype = i64
+        L.mts_adamw_state_elements.argtypes = [vp]
+        L.mts_adamw_state_bytes.restype = sz
+        L.mts_adamw_state_bytes.argtypes = [vp]
+        L.mts_adamw_set_grads.argtypes = [vp, C.POINTER(vp), vp]
+        L.mts_adamw_step.argtypes = [vp, vp, sz, f64, f64, f64, f64, f64, i64, vp, u32, vp]
+        L.mts_adamw_export_state.argtypes = [vp, vp, sz, vp, vp, vp]
+        L.mts_adamw_import_state.argtypes = [vp, vp, sz, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name)            # raises AttributeError when a declared symbol is missing
         _lib = L
@@ -533,4 +576,125 @@ def cache_set_fetch_wait_limit(cache: Cache, polls: int) -> None:
 
 def cache_export_state(cache: Cache, tags, timestamps, counts, dirty, stream=None) -> None:
     _check(lib().mts_cache_export_state(cache.handle, _ptr(tags), _ptr(timestamps), _ptr(counts), _ptr(dirty),
+                                        _stream(stream)))
+
+
+# ---------------------------------------------------------------------------- the sequence tower beside the tables
+def recurrence_chunks(N: int, D: int, dtype: int) -> int:
+    """Rows of the [chunks, D] fp32 array of entry states that the forward leaves for the backward."""
+    return int(lib().mts_recurrence_chunks(N, D, dtype))
+
+
+def recurrence_workspace_bytes(N: int, S: int, D: int, dtype: int) -> int:
+    return int(lib().mts_recurrence_workspace_bytes(N, S, D, dtype))
+
+
+def recurrence_forward(gate, gate_stride: int, value, value_stride: int, dtype: int, N: int, D: int, offsets, S: int, h0,
+                       out, out_stride: int, h_final, entry_states, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().mts_recurrence_forward(_ptr(gate), gate_stride, _ptr(value), value_stride, dtype, N, D, _ptr(offsets), S,
+                                        _ptr(h0), _ptr(out), out_stride, _ptr(h_final), _ptr(entry_states),
+                                        _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def recurrence_backward(gate, gate_stride: int, value, value_stride: int, dtype: int, N: int, D: int, offsets, S: int, h0,
+                        entry_states, grad_out, grad_out_stride: int, grad_final, grad_gate, grad_gate_stride: int,
+                        grad_value, grad_value_stride: int, grad_h0, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().mts_recurrence_backward(_ptr(gate), gate_stride, _ptr(value), value_stride, dtype, N, D, _ptr(offsets), S,
+                                         _ptr(h0), _ptr(entry_states), _ptr(grad_out), grad_out_stride, _ptr(grad_final),
+                                         _ptr(grad_gate), grad_gate_stride, _ptr(grad_value), grad_value_stride,
+                                         _ptr(grad_h0), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def recurrence_status(workspace, stream=None) -> int:
+    """Status bits of the last recurrence call on this workspace (1: offsets out of order or range); synchronises."""
+    st = C.c_int32(0)
+    _check(lib().mts_recurrence_status(_ptr(workspace), C.byref(st), _stream(stream)))
+    return int(st.value)
+
+
+class RelposBuckets:
+    """The buckets of a relative position bias: mts_relpos_buckets with its host array."""
+
+    def __init__(self, starts: Sequence[int], two_sided: bool = False, causal: bool = False):
+        self.n = len(starts)
+        self.rows = self.n * (2 if two_sided else 1)
+        self._starts = (C.c_int32 * max(self.n, 1))(*[int(x) for x in starts])
+        self.desc = RelposBucketsDesc(self.n, int(two_sided), int(causal), self._starts)
+        self.ref = C.byref(self.desc)
+
+
+def relpos_bias_forward(buckets: RelposBuckets, table, table_dtype: int, heads: int, Lq: int, Lk: int, q_offset: int, out,
+                        out_dtype: int, out_head_stride: int, out_row_stride: int, stream=None) -> None:
+    _check(lib().mts_relpos_bias_forward(buckets.ref, _ptr(table), table_dtype, heads, Lq, Lk, q_offset, _ptr(out),
+                                         out_dtype, out_head_stride, out_row_stride, _stream(stream)))
+
+
+def relpos_bias_workspace_bytes(buckets: RelposBuckets, heads: int) -> int:
+    return int(lib().mts_relpos_bias_workspace_bytes(buckets.ref, heads))
+
+
+def relpos_bias_backward(buckets: RelposBuckets, grad_out, grad_dtype: int, B: int, heads: int, Lq: int, Lk: int,
+                         q_offset: int, batch_stride: int, head_stride: int, row_stride: int, grad_table, workspace,
+                         workspace_bytes: int, stream=None) -> None:
+    _check(lib().mts_relpos_bias_backward(buckets.ref, _ptr(grad_out), grad_dtype, B, heads, Lq, Lk, q_offset, batch_stride,
+                                          head_stride, row_stride, _ptr(grad_table), _ptr(workspace), workspace_bytes,
+                                          _stream(stream)))
+
+
+class AdamW:
+    """Handle returned by mts_adamw_create; keeps the tensors alive."""
+
+    def __init__(self, sizes: Sequence[int], param_dtype: int, grad_dtype: int, state_bits: int, params: Sequence,
+                 grads: Sequence, masters: Optional[Sequence] = None, decays: Optional[Sequence[bool]] = None):
+        n = len(sizes)
+        assert len(params) == n and len(grads) == n, "one parameter and one gradient per size"
+        assert masters is None or len(masters) == n, "one master per parameter"
+        assert decays is None or len(decays) == n, "one flag per parameter"
+        self._keep = (list(params), list(grads), list(masters) if masters is not None else None)
+        self.n = n
+        sz = (C.c_int64 * max(n, 1))(*[int(x) for x in sizes])
+        dec = (C.c_uint8 * max(n, 1))(*[int(bool(x)) for x in decays]) if decays is not None else None
+        d = AdamWDesc(n, param_dtype, grad_dtype, state_bits, sz, _ptr_array(params, n), _ptr_array(grads, n),
+                      _ptr_array(masters, n), dec)
+        h = C.c_void_p()
+        self.handle = None
+        _check(lib().mts_adamw_create(C.byref(d), C.byref(h)))
+        self.handle = h
+        self.state_bits = state_bits
+        self.elements = int(lib().mts_adamw_state_elements(h))
+        self.state_bytes = int(lib().mts_adamw_state_bytes(h))
+
+    def destroy(self):
+        if self.handle:
+            _check(lib().mts_adamw_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def adamw_set_grads(adamw: AdamW, grads: Sequence, stream=None) -> None:
+    assert len(grads) == adamw.n, "one gradient per parameter"
+    _check(lib().mts_adamw_set_grads(adamw.handle, _ptr_array(grads, adamw.n), _stream(stream)))
+    adamw._keep = (adamw._keep[0], list(grads), adamw._keep[2])
+
+
+def adamw_step(adamw: AdamW, state, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int,
+               grad_scale=None, seed: int = 0, stream=None) -> None:
+    """seed: random bits of the 8-bit second moments, another one for every step."""
+    _check(lib().mts_adamw_step(adamw.handle, _ptr(state), state.numel() * state.element_size(), lr, beta1, beta2, eps,
+                                weight_decay, step, _ptr(grad_scale), seed & 0xFFFFFFFF, _stream(stream)))
+
+
+def adamw_export_state(adamw: AdamW, state, m_out, v_out, stream=None) -> None:
+    """The moments as fp32 arrays [adamw.elements]."""
+    _check(lib().mts_adamw_export_state(adamw.handle, _ptr(state), state.numel() * state.element_size(), _ptr(m_out),
+                                        _ptr(v_out), _stream(stream)))
+
+
+def adamw_import_state(adamw: AdamW, state, m, v, stream=None) -> None:
+    _check(lib().mts_adamw_import_state(adamw.handle, _ptr(state), state.numel() * state.element_size(), _ptr(m), _ptr(v),
                                         _stream(stream)))

@@ -30,7 +30,8 @@ static const char* const kKernelNames[K_COUNT] = {
     "tbe_forward_kernel", "linearize_lookups", "digit_histogram", "scan_histogram", "scatter_by_digit",
     "unique_segments", "reduce_chunks", "combine_partials", "cache_prepare_keys", "cache_describe_unique",
     "cache_probe_replace", "cache_lists", "cache_scatter_slots", "cache_save_victims", "cache_fetch_misses",
-    "cache_write_victims", "cache_flush", "other"};
+    "cache_write_victims", "cache_flush", "other", "recurrence_forward", "recurrence_backward", "relpos_bias_forward",
+    "relpos_bias_backward", "adamw_step", "adamw_state"};
 
 struct TraceRecord { int kernel; cudaEvent_t start, stop; };
 
