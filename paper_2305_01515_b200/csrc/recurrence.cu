@@ -2,32 +2,34 @@
 //
 //   z_t = 1 / (1 + exp(-gate_t)),  h_t = z_t value_t + (1 - z_t) h_{t-1}
 //
-// Composition of steps: any run of tokens maps the state before it to B + P * state, P the product of its 1 - z and B the state
-// it reaches from 0; a run that contains a sequence's start forgets what came before it (a cut).  Runs compose, so the token
-// axis is split into chunks of 64 tokens whatever the sequences are: one long sequence and a thousand short ones are the same
-// work.  A block owns a tile (a chunk x a strip of channels): it computes the maps of its 8 runs of 8 tokens, publishes the
-// map of the chunk, gathers the maps before it back to the start of its sequence (at most 15 chunks, 15 groups of 16 chunks and the
-// state after 256 of them), and walks its tokens once more from the state they give.  Everything is read once and written
-// once: memory traffic bounds it.  The association of the maps depends on the offsets alone, so the result is the
-// same in every run.
-//
-// Waiting: published words are single 64-bit stores into memory that was filled with 0xFF; a reader polls the word itself.  All blocks
-// are resident (cooperative launch) and take their tiles in ascending order, and a tile waits for lower ones only: the
-// lowest unfinished tile never waits.  Every poll loop has a limit all the same.
+// Any run of tokens maps the state before it to B + P * state, P the product of its 1 - z and B the state it reaches from 0; a run
+// that contains a sequence's start forgets what came before it (a cut).  Runs compose, so the token axis is cut into chunks
+// whatever the sequences are: one long sequence and a thousand short ones are the same work.  Two passes, a warp per chunk and strip of
+// channels (8 bytes of a row per lane) in each:
+//   maps: the map of every chunk whose last sequence goes on behind it, from that sequence's start on (what lies before it in the
+//         chunk is forgotten).  The last warp of a group of 16 chunks composes the group's map, the last of a span of 16 groups the
+//         span's, the last of all walks the spans: nobody waits.
+//   walk: the state before the chunk from at most a span's state, 15 groups and 15 chunks, then its tokens.
+// The association of the maps depends on the offsets alone, so the result is the same in every run.  Both passes stream at the memory's
+// rate, which bounds them: the inputs are read twice.  The second pass takes the chunks in the opposite order, so that what the first
+// read last is still in the L2 cache.  (Tried before: one pass, whose blocks kept their tokens in shared memory and waited for the
+// maps of the blocks before them.  A word published by one SM is seen by another 1 to 2 us later, and a chain of three such steps per tile
+// outlasts what shared memory can hold back: 424 to 690 us for 524,287 tokens x 256, fp16.)
 #include <type_traits>
 
 #include "dense.cuh"
 
 namespace mts {
 
-constexpr int REC_RUN = 8;                        // tokens of one thread
-constexpr int REC_RUNS = 8;
-constexpr int REC_CHUNK = REC_RUN * REC_RUNS;     // tokens of a tile
+constexpr int REC_WARPS = 4;
+constexpr int REC_CHUNK = 64;                     // tokens of a chunk at most: a bit mask of them is one word
+constexpr int REC_BATCH = 8;                      // tokens loaded together, and between two states kept for the backward
 constexpr int REC_RADIX = 16;                     // chunks per group, groups per span
-constexpr int REC_SPAN = REC_RADIX * REC_RADIX;   // chunks between two published states
-constexpr int REC_STATUS_OFFSETS = 1, REC_STATUS_TIMEOUT = 2;
-constexpr int REC_POLLS = 1 << 21;                // polls of one word before a wait gives up (about a second)
-constexpr uint32_t REC_UNPUBLISHED = 0xFFFFFFFFu;
+constexpr int REC_SPAN = REC_RADIX * REC_RADIX;
+#ifndef MTS_REC_WARPS_WANTED
+#define MTS_REC_WARPS_WANTED 2368
+#endif
+constexpr int REC_STATUS_OFFSETS = 1;
 
 struct RecArgs {
   const void* gate; int64_t gate_stride;
@@ -36,144 +38,378 @@ struct RecArgs {
   const float* h0;
   int64_t N, S;
   int32_t D;
-  int32_t chunks, strips;
-  int32_t wide;                // rows, strides and bases on 16-byte boundaries (else 4-element ones, or none: template)
-  uint32_t* status;            // status bits, inverted: the workspace starts as all ones
-  unsigned long long* chunk_map;   // [chunks, D], [groups, D], [spans, D]
-  unsigned long long* group_map;
-  unsigned long long* span_state;
+  int32_t chunk;               // tokens of a chunk
+  int32_t chunks, strips, groups, spans;
+  uint32_t* status;
+  uint32_t* group_count;       // [groups, strips] chunks done, likewise groups of a span, spans
+  uint32_t* span_count;
+  uint32_t* total_count;
+  int32_t* sequence;           // [chunks] a sequence at or before the chunk's first token
+  float* chunk_P;              // [chunks, D]
+  float* chunk_B;
+  float* chunk_start;          // [chunks, D] state in which the chunk's last sequence starts
+  float* group_P;
+  float* group_B;
+  float* span_P;
+  float* span_B;
+  float* span_state;           // [spans, D] the state before the span
 };
 
-__device__ __forceinline__ void raise_status(const RecArgs& a, int bit) { atomicAnd(a.status, ~(uint32_t)bit); }
+// ------------------------------------------------------------------------------- V channels of a lane
+// fp32 values in pairs, which sm_100 multiplies and adds two at a time.
+template <int V>
+struct Channels {
+  static_assert(V % 2 == 0, "pairs");
+  unsigned long long p[V / 2];
+};
+template <>
+struct Channels<1> { float p[1]; };
 
-// exp through the hardware's 2^x and the reciprocal: a few units of 2^-23, the gate's size times as much for large ones.
-__device__ __forceinline__ float sigmoid_f32(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
-
-// h + z (x - h) as z x + (1 - z) h without rounding 1 - z: x itself for z = 1, h for z = 0.
-__device__ __forceinline__ float blend(float z, float x, float h) { return fmaf(z, x, fmaf(-z, h, h)); }
-
-// A map state -> B + P * state.  P >= 0 is a product of 1 - z; P = -0 marks a cut, whose result is B even if the state before it is
-// infinite or NaN.
-struct Map { float P, B; };
-__device__ __forceinline__ bool is_cut(float P) { return __float_as_int(P) < 0; }
-__device__ __forceinline__ float apply(Map m, float h) { return is_cut(m.P) ? m.B : fmaf(m.P, h, m.B); }
-__device__ __forceinline__ Map then(Map first, Map second) {          // first, then second
-  return Map{is_cut(second.P) ? -0.f : first.P * second.P, apply(second, first.B)};
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
+__device__ __forceinline__ void split(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+
+template <int V>
+__device__ __forceinline__ Channels<V> gathered(const float (&x)[V]) {
+  Channels<V> r;
+  if constexpr (V == 1) r.p[0] = x[0];
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) r.p[k] = pair(x[2 * k], x[2 * k + 1]);
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ void scattered(Channels<V> v, float (&x)[V]) {
+  if constexpr (V == 1) x[0] = v.p[0];
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) split(v.p[k], x[2 * k], x[2 * k + 1]);
+  }
+}
+template <int V>
+__device__ __forceinline__ Channels<V> all(float x) {
+  Channels<V> r;
+  if constexpr (V == 1) r.p[0] = x;
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) r.p[k] = pair(x, x);
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Channels<V> fma(Channels<V> a, Channels<V> b, Channels<V> c) {
+  Channels<V> r;
+  if constexpr (V == 1) r.p[0] = fmaf(a.p[0], b.p[0], c.p[0]);
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.p[k]) : "l"(a.p[k]), "l"(b.p[k]), "l"(c.p[k]));
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Channels<V> operator*(Channels<V> a, Channels<V> b) {
+  Channels<V> r;
+  if constexpr (V == 1) r.p[0] = a.p[0] * b.p[0];
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.p[k]) : "l"(a.p[k]), "l"(b.p[k]));
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Channels<V> operator+(Channels<V> a, Channels<V> b) {
+  Channels<V> r;
+  if constexpr (V == 1) r.p[0] = a.p[0] + b.p[0];
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.p[k]) : "l"(a.p[k]), "l"(b.p[k]));
+  }
+  return r;
+}
+template <int V, typename Fn>
+__device__ __forceinline__ Channels<V> each(Channels<V> a, Fn&& fn) {
+  if constexpr (V == 1) a.p[0] = fn(a.p[0]);
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) {
+      float x, y;
+      split(a.p[k], x, y);
+      a.p[k] = pair(fn(x), fn(y));
+    }
+  }
+  return a;
+}
+
+// -z for gate logits g, through the hardware's 2^x and reciprocal, a few units of 2^-23 each, the gate's size times as much for
+// large ones.  Denormals are flushed: a z below 2^-126.  Exactly -1 and -0 for gates of both infinities.
+template <int V>
+__device__ __forceinline__ Channels<V> minus_sigmoid(Channels<V> g) {
+  const Channels<V> e = each(g * all<V>(-1.4426950408889634f), [](float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+  });
+  return each(fma(e, all<V>(-1.f), all<V>(-1.f)), [](float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+  });
+}
+// z x + (1 - z) h for nz = -z and nx = -x, without rounding 1 - z: x itself for z = 1, h for z = 0.
+template <int V>
+__device__ __forceinline__ Channels<V> blend(Channels<V> nz, Channels<V> nx, Channels<V> h) { return fma(nz, nx, fma(nz, h, h)); }
+
+// V consecutive elements as they lie in memory, in 32-bit words.
+template <typename T, int V>
+struct Raw { uint32_t w[(V * sizeof(T) + 3) / 4]; };
+
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> load_raw(const T* p) {
+  Raw<T, V> r;
+  constexpr int BYTES = V * sizeof(T);
+  if constexpr (BYTES == 16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+  } else if constexpr (BYTES == 8) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = u.x; r.w[1] = u.y;
+  } else if constexpr (BYTES == 4) {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
+    r.w[0] = *reinterpret_cast<const uint16_t*>(p);
+  }
+  return r;
+}
+// NEGATE: minus the values (their sign bits flipped while still packed).
+template <typename T, int V, bool NEGATE = false>
+__device__ __forceinline__ Channels<V> unpack(Raw<T, V> r) {
+  Channels<V> v;
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) v.p[0] = __uint_as_float(r.w[0] ^ (NEGATE ? 0x80000000u : 0u));
+    else v.p[0] = unpack2<T>(r.w[0] ^ (NEGATE ? 0x8000u : 0u)).x;
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k)
+      v.p[k] = pair(__uint_as_float(r.w[2 * k] ^ (NEGATE ? 0x80000000u : 0u)), __uint_as_float(r.w[2 * k + 1] ^ (NEGATE ? 0x80000000u : 0u)));
+  } else {
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) {
+      const float2 f = unpack2<T>(r.w[k] ^ (NEGATE ? 0x80008000u : 0u));
+      v.p[k] = pair(f.x, f.y);
+    }
+  }
+  return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store(T* p, Channels<V> v) {
+  if constexpr (V == 1) {
+    *p = from_f32<T>(v.p[0]);
+  } else {
+    float x[V];
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) split(v.p[k], x[2 * k], x[2 * k + 1]);
+    if constexpr (sizeof(T) == 4 && V == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
+    else if constexpr (V == 4) *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+    else *reinterpret_cast<uint32_t*>(p) = pack2<T>(x[0], x[1]);
+  }
+}
+template <int V>
+__device__ __forceinline__ Channels<V> load_f32(const float* p) { return unpack<float, V>(load_raw<float, V>(p)); }
+// The same in rows of D channels of which `left` begin at p: VEC = D and the row's base allow whole vectors, else one by one.
+template <int V, bool VEC>
+__device__ __forceinline__ Channels<V> get(const float* p, int left) {
+  if (VEC) return left > 0 ? load_f32<V>(p) : all<V>(0.f);
+  float x[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) x[k] = k < left ? p[k] : 0.f;
+  return gathered<V>(x);
+}
+template <int V, bool VEC, typename T>
+__device__ __forceinline__ void put(T* p, int left, Channels<V> v) {
+  if (VEC) {
+    if (left > 0) store(p, v);
+  } else {
+    float x[V];
+    scattered(v, x);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < left) p[k] = from_f32<T>(x[k]);
+  }
+}
+// The V channels of a row of which `left` begin at p (none: 0), as they lie in memory.
+template <typename T, int V, bool VEC>
+__device__ __forceinline__ Raw<T, V> get_raw(const T* p, int left) {
+  Raw<T, V> r = {};
+  if (VEC) {
+    if (left > 0) r = load_raw<T, V>(p);
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) r.w[k] = k < left ? __float_as_uint(p[k]) : 0u;
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < left) r.w[k / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[k] << (16 * (k % 2));
+  }
+  return r;
+}
+// What another warp of the same launch has written: from L2, the L1 cache may hold what was there before.
+template <int V, bool VEC>
+__device__ __forceinline__ Channels<V> load_published(const float* p, int left) {
+  float x[V];
+  if constexpr (VEC && V == 4) {
+    const float4 f = left > 0 ? __ldcg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+  } else if constexpr (VEC && V == 2) {
+    const float2 f = left > 0 ? __ldcg(reinterpret_cast<const float2*>(p)) : make_float2(0.f, 0.f);
+    x[0] = f.x; x[1] = f.y;
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) x[k] = k < left ? __ldcg(p + k) : 0.f;
+  }
+  return gathered<V>(x);
+}
+
+// ------------------------------------------------------------------------------- maps
+// state -> B + P * state.  P >= 0 is a product of 1 - z; P = -0 marks a cut, whose result is B even where the state before it is
+// infinite or NaN.
+template <int V>
+struct Map { Channels<V> P, B; };
 constexpr float CUT = -0.f;
 
-__device__ __forceinline__ void publish(unsigned long long* at, Map m) {
-  uint32_t p = __float_as_uint(m.P);
-  if (p == REC_UNPUBLISHED) p = 0x7FFFFFFFu;                          // a NaN of the one pattern that means "not yet"
-  const unsigned long long w = ((unsigned long long)__float_as_uint(m.B) << 32) | p;
-  asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" :: "l"(at), "l"(w) : "memory");
-}
-__device__ __forceinline__ unsigned long long peek(const unsigned long long* at) {
-  unsigned long long w;
-  asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(w) : "l"(at) : "memory");
-  return w;
-}
-
-__device__ __forceinline__ bool timed_out(const RecArgs& a) {
-  return !(*reinterpret_cast<volatile uint32_t*>(a.status) & REC_STATUS_TIMEOUT);
-}
-
-// Composition of the published maps at[0], at[step], ..., count of them (count <= 16), in that order; waits for those still missing.
-__device__ __forceinline__ Map gather(const RecArgs& a, const unsigned long long* at, int64_t step, int count) {
-  Map m = {1.f, 0.f};
-  for (int i = 0; i < count; i += 8) {
-    unsigned long long w[8];
-    int polls = 0;
-    bool missing;
-    do {
-      missing = false;
+// first, then second; `first` may be a state (P = CUT).
+template <int V>
+__device__ __forceinline__ Map<V> then(Map<V> first, Map<V> second) {
+  float P1[V], B1[V], P2[V], B2[V];
+  scattered(first.P, P1);
+  scattered(first.B, B1);
+  scattered(second.P, P2);
+  scattered(second.B, B2);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = i + k < count ? peek(at + (i + k) * step) : 0ull;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) missing |= (uint32_t)w[k] == REC_UNPUBLISHED;
-      ++polls;                          // once a wait has run out the others give up soon, too
-    } while (missing && polls < REC_POLLS && (polls % 1024 || !timed_out(a)));
-    if (missing) raise_status(a, REC_STATUS_TIMEOUT);
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (i + k < count) m = then(m, Map{__uint_as_float((uint32_t)w[k]), __uint_as_float((uint32_t)(w[k] >> 32))});
+  for (int k = 0; k < V; ++k) {
+    const bool cut = __float_as_int(P2[k]) == (int)0x80000000;
+    B1[k] = cut ? B2[k] : fmaf(P2[k], B1[k], B2[k]);
+    P1[k] = cut || __float_as_int(P1[k]) == (int)0x80000000 ? CUT : P1[k] * P2[k];
   }
+  return Map<V>{gathered<V>(P1), gathered<V>(B1)};
+}
+
+// Composition of n maps from row `lo` of [rows, D] arrays on, after `m`.
+template <int V, bool VEC>
+__device__ __forceinline__ Map<V> compose(const RecArgs& a, const float* P, const float* B, int lo, int n, int c, Map<V> m) {
+  const int left = a.D - c;
+  P += (int64_t)lo * a.D + c;
+  B += (int64_t)lo * a.D + c;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k, P += a.D, B += a.D) m = then(m, Map<V>{load_published<V, VEC>(P, left), load_published<V, VEC>(B, left)});
   return m;
 }
 
-// One channel of a tile, whose maps are counted by `index` in the order of the walk, by two threads.  The near one publishes the tile's own
-// map and returns the composition of those before it in its group; the far one returns (as B) the state before the group.  Both
-// begin at `from`, the tile where the sequence began, and the association is the same whatever is published when.
-__device__ __forceinline__ Map join(const RecArgs& a, int index, int from, bool near, int channel, Map own) {
-  Map m = {1.f, 0.f};
-  if (channel < 0) return m;
-  const int group = index / REC_RADIX, span = index / REC_SPAN;
-  from = min(max(from, 0), index);
-  if (near) {
-    const bool ends_group = index % REC_RADIX == REC_RADIX - 1;
-    if (!ends_group) publish(a.chunk_map + (int64_t)index * a.D + channel, own);
-    const int lo = max(from, group * REC_RADIX);
-    m = gather(a, a.chunk_map + (int64_t)lo * a.D + channel, a.D, index - lo);
-    if (ends_group) publish(a.group_map + (int64_t)group * a.D + channel, then(m, own));
-  } else if (from < group * REC_RADIX) {
-    if (from < span * REC_SPAN) m = gather(a, a.span_state + (int64_t)(span - 1) * a.D + channel, 0, 1);
-    const int lo = max(from / REC_RADIX, span * REC_RADIX);
-    m = then(m, gather(a, a.group_map + (int64_t)lo * a.D + channel, a.D, group - lo));
+// Whether this warp is the last of `members` to get here; if so, what the others wrote before is visible to it.
+__device__ __forceinline__ bool last_of(uint32_t* count, int members) {
+  uint32_t before = 0;
+  __syncwarp();
+  if (lane_id() == 0) {
+    __threadfence();
+    before = atomicAdd(count, 1u);
   }
-  return m;
+  const bool last = __shfl_sync(0xFFFFFFFFu, before, 0) == (uint32_t)members - 1;
+  if (last) __threadfence();
+  return last;
 }
 
-// What a tile knows of the sequences in its chunk.
+// After a chunk's map (counted in the order of the walk) has been written: the maps of the group and span that it completes, and after the
+// last of all the state before every span.
+template <int V, bool VEC>
+__device__ __forceinline__ void complete(const RecArgs& a, int index, int strip, int c) {
+  if (a.groups == 1) return;                                            // the walk composes the chunks' maps itself
+  const Map<V> identity = {all<V>(1.f), all<V>(0.f)};
+  const int left = a.D - c, group = index / REC_RADIX, span = index / REC_SPAN;
+  if (!last_of(a.group_count + (int64_t)group * a.strips + strip, min(REC_RADIX, a.chunks - group * REC_RADIX))) return;
+  Map<V> m = compose<V, VEC>(a, a.chunk_P, a.chunk_B, group * REC_RADIX, min(REC_RADIX, a.chunks - group * REC_RADIX), c, identity);
+  put<V, VEC>(a.group_P + (int64_t)group * a.D + c, left, m.P);
+  put<V, VEC>(a.group_B + (int64_t)group * a.D + c, left, m.B);
+  if (a.spans == 1) return;
+  if (!last_of(a.span_count + (int64_t)span * a.strips + strip, min(REC_RADIX, a.groups - span * REC_RADIX))) return;
+  m = compose<V, VEC>(a, a.group_P, a.group_B, span * REC_RADIX, min(REC_RADIX, a.groups - span * REC_RADIX), c, identity);
+  put<V, VEC>(a.span_P + (int64_t)span * a.D + c, left, m.P);
+  put<V, VEC>(a.span_B + (int64_t)span * a.D + c, left, m.B);
+  if (!last_of(a.total_count + strip, a.spans)) return;
+  m = {all<V>(CUT), all<V>(0.f)};
+#pragma unroll 4
+  for (int k = 0; k < a.spans; ++k) {
+    put<V, VEC>(a.span_state + (int64_t)k * a.D + c, left, m.B);
+    m = compose<V, VEC>(a, a.span_P, a.span_B, k, 1, c, m);
+  }
+}
+
+// The state before tile `index`, whose first sequence (in the order of the walk) began in tile `from` < index.
+template <int V, bool VEC>
+__device__ __forceinline__ Channels<V> state_before(const RecArgs& a, int index, int from, int c) {
+  from = max(0, min(from, index - 1));
+  const int group = index / REC_RADIX, span = index / REC_SPAN, lo = max(from, group * REC_RADIX);
+  Map<V> m = {all<V>(CUT), all<V>(0.f)};
+  if (from < group * REC_RADIX) {
+    if (from < span * REC_SPAN) m.B = load_published<V, VEC>(a.span_state + (int64_t)span * a.D + c, a.D - c);
+    const int glo = max(from / REC_RADIX, span * REC_RADIX);
+    m = compose<V, VEC>(a, a.group_P, a.group_B, glo, group - glo, c, m);
+  }
+  return compose<V, VEC>(a, a.chunk_P, a.chunk_B, lo, index - lo, c, m).B;
+}
+
+// ------------------------------------------------------------------------------- sequences of a chunk
 struct ChunkSequences {
   unsigned long long first, last;      // tokens that begin / end their sequence
-  int64_t far;                         // forward: first token of the sequence that holds the chunk's first token;
-                                       // backward: last token of the one that holds the chunk's last token
-  int32_t first_of[REC_CHUNK];         // sequence that begins at the token
-  int32_t last_of[REC_CHUNK];          // sequence that ends at the token
+  int64_t head_begin;                  // of the sequence that holds the chunk's first token
+  int64_t tail_end;                    // of the one that holds its last token
 };
 
-// One warp: the sequence of the chunk's first token by a search with 32 probes a step, then the sequences up to the chunk's end.  Every
-// index is bounded whatever the offsets hold.
-template <bool BACKWARD>
-__device__ void find_sequences(const RecArgs& a, int chunk, ChunkSequences* out) {
-  const int lane = lane_id();
-  const int64_t t0 = (int64_t)chunk * REC_CHUNK, t1 = min(t0 + REC_CHUNK, a.N);
+// One warp: the sequence of the chunk's first token, by a search with 32 probes a step.  Every index is bounded whatever the offsets hold.
+__device__ __forceinline__ int find_sequence(const RecArgs& a, int64_t t0) {
   int64_t lo = 0, hi = a.S;
   while (hi - lo > 1) {                                               // offsets[lo] <= t0 < offsets[hi]
-    const int64_t step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const int64_t step = (hi - lo + 31) / 32, i = lo + lane_id() * step;
     const int n = __popc(__ballot_sync(0xFFFFFFFFu, i < hi && a.offsets[i] <= t0));
     lo += (int64_t)max(n - 1, 0) * step;
     hi = min(hi, lo + step);
   }
-  unsigned long long first = 0, last = 0;
-  int64_t far = BACKWARD ? t1 - 1 : t0;
+  return (int)lo;
+}
+// The sequences of a chunk from sequence `lo` on; their numbers go to first_of / last_of, by token.
+__device__ __forceinline__ ChunkSequences find_borders(const RecArgs& a, int lo, int64_t t0, int64_t t1, int32_t* first_of, int32_t* last_of) {
+  ChunkSequences q = {0, 0, t0, t1};
   for (int64_t base = lo; base < a.S; base += 32) {
-    const int64_t s = base + lane;
+    const int64_t s = base + lane_id();
     const int64_t b = s < a.S ? a.offsets[s] : a.N, e = s < a.S ? a.offsets[s + 1] : a.N;
-    if (e > b) {
-      if (b >= t0 && b < t1) { first |= 1ull << (b - t0); out->first_of[b - t0] = (int)s; }
-      if (e > t0 && e <= t1) { last |= 1ull << (e - 1 - t0); out->last_of[e - 1 - t0] = (int)s; }
-      if (!BACKWARD && b <= t0 && e > t0) far = b;
-      if (BACKWARD && b < t1 && e >= t1) far = e - 1;
-    }
+    const bool some = e > b;
+    if (some && b >= t0 && b < t1) { q.first |= 1ull << (b - t0); first_of[b - t0] = (int)s; }
+    if (some && e > t0 && e <= t1) { q.last |= 1ull << (e - 1 - t0); last_of[e - 1 - t0] = (int)s; }
+    const unsigned head = __ballot_sync(0xFFFFFFFFu, some && b <= t0 && e > t0), tail = __ballot_sync(0xFFFFFFFFu, some && b < t1 && e >= t1);
+    if (head) q.head_begin = __shfl_sync(0xFFFFFFFFu, b, __ffs(head) - 1);
+    if (tail) q.tail_end = __shfl_sync(0xFFFFFFFFu, e, __ffs(tail) - 1);
     if (__any_sync(0xFFFFFFFFu, b >= t1)) break;
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    first |= __shfl_xor_sync(0xFFFFFFFFu, first, o);
-    last |= __shfl_xor_sync(0xFFFFFFFFu, last, o);
-    const int64_t f = __shfl_xor_sync(0xFFFFFFFFu, far, o);
-    far = BACKWARD ? max(far, f) : min(far, f);
+    q.first |= __shfl_xor_sync(0xFFFFFFFFu, q.first, o);
+    q.last |= __shfl_xor_sync(0xFFFFFFFFu, q.last, o);
   }
-  if (lane == 0) { out->first = first; out->last = last; out->far = far; }
+  q.head_begin = max(q.head_begin, (int64_t)0);
+  q.tail_end = min(q.tail_end, a.N);
+  __syncwarp();
+  return q;
 }
 
-// Offsets in order, from 0 to N (each thread a share of them); `row(s)` for every empty sequence, one warp each.
+// Offsets in order, from 0 to N (each warp a share of them); `row(s)` for every empty sequence.
 template <typename Fn>
-__device__ void check_offsets(const RecArgs& a, Fn&& row) {
-  const int64_t warps = (int64_t)gridDim.x * (blockDim.x / 32);
+__device__ __forceinline__ void check_offsets(const RecArgs& a, Fn&& row) {
+  const int64_t warps = (int64_t)gridDim.x * REC_WARPS;
   bool bad = false;
-  for (int64_t s0 = ((int64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32) * 32; s0 < a.S; s0 += warps * 32) {
+  for (int64_t s0 = ((int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32) * 32; s0 < a.S; s0 += warps * 32) {
     const int64_t s = s0 + lane_id();
     const int64_t b = s < a.S ? a.offsets[s] : 0, e = s < a.S ? a.offsets[s + 1] : 1;
     if (s < a.S) bad |= b < 0 || e < b || (s == 0 && b != 0) || (s == a.S - 1 && e != a.N);
@@ -183,114 +419,88 @@ __device__ void check_offsets(const RecArgs& a, Fn&& row) {
       empty &= empty - 1;
     }
   }
-  if (bad) raise_status(a, REC_STATUS_OFFSETS);
+  if (bad) atomicOr(a.status, (uint32_t)REC_STATUS_OFFSETS);
 }
 
-__device__ __forceinline__ void copy_async(void* smem, const void* global, int bytes, bool wide) {
-  const uint32_t to = (uint32_t)__cvta_generic_to_shared(smem);
-  if (wide) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(global), "r"(bytes) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(to), "l"(global), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+// What a warp works on: chunk (counted from the end where BACKWARD) and strip of channels.
+struct Item {
+  int index, chunk, strip;
+  int64_t t0, t1;
+  __device__ __forceinline__ Item(const RecArgs& a, int64_t item, bool backward) {
+    index = (int)(item / a.strips);
+    strip = (int)(item - (int64_t)index * a.strips);
+    chunk = backward ? a.chunks - 1 - index : index;
+    t0 = (int64_t)chunk * a.chunk;
+    t1 = min(t0 + a.chunk, a.N);
+  }
+};
 
-// Four channels of one row.
-template <typename T>
-__device__ __forceinline__ void read4(const T* p, float (&v)[4]) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y);
-  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-}
-template <>
-__device__ __forceinline__ void read4<float>(const float* p, float (&v)[4]) {
-  const float4 w = *reinterpret_cast<const float4*>(p);
-  v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-}
-template <typename T>
-__device__ __forceinline__ void write4(T* p, const float (&v)[4]) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
-}
-template <>
-__device__ __forceinline__ void write4<float>(float* p, const float (&v)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-}
-// The same in global memory: QUADS = rows begin on 4-element boundaries and D is a multiple of 4, else the first `left` of the
-// four one by one.
-template <bool QUADS, typename T>
-__device__ __forceinline__ void get4(const T* p, int left, float (&v)[4]) {
-  if (QUADS) {
-    if (left > 0) read4(p, v);
-  } else {
+// The rows of a batch of tokens, from row p on; rows that `live` does not name are not read and give 0.
+template <typename T, int V, bool VEC>
+__device__ __forceinline__ void load_rows(const T* p, int64_t stride, uint32_t live, int left, Raw<T, V> (&r)[REC_BATCH]) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < left) v[k] = to_f32(p[k]);
-  }
+  for (int i = 0; i < REC_BATCH; ++i, p += stride) r[i] = (live >> i & 1) ? get_raw<T, V, VEC>(p, left) : Raw<T, V>{};
 }
-template <bool QUADS, typename T>
-__device__ __forceinline__ void put4(T* p, int left, const float (&v)[4]) {
-  if (QUADS) {
-    if (left > 0) write4(p, v);
-  } else {
+template <typename T, int V, bool VEC>
+__device__ __forceinline__ void load_rows(const T* p, int64_t stride, int left, Raw<T, V> (&r)[REC_BATCH]) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < left) p[k] = from_f32<T>(v[k]);
-  }
+  for (int i = 0; i < REC_BATCH; ++i, p += stride) r[i] = get_raw<T, V, VEC>(p, left);
 }
 
-// A tile's [64, 4 LANES] part of an [N, D] array to shared memory; what lies outside reads as 0.
-template <typename T, int LANES, bool QUADS>
-__device__ __forceinline__ void fetch_rows(const RecArgs& a, const void* src, int64_t stride, int64_t t0, int c0, T* to) {
-  constexpr int W = 4 * LANES, THREADS = REC_RUNS * LANES;
-  const T* from = static_cast<const T*>(src);
-  if (QUADS) {
-    const bool wide = sizeof(T) == 4 || a.wide;
-    const int per = wide ? 16 / (int)sizeof(T) : 4;                                  // elements of one copy
-    const int pieces = W / per;
-    for (int i = threadIdx.x; i < REC_CHUNK * pieces; i += THREADS) {
-      const int r = i / pieces, c = (i - r * pieces) * per;
-      const bool in = t0 + r < a.N && c0 + c < a.D;
-      copy_async(to + r * W + c, in ? from + (t0 + r) * stride + c0 + c : from, in ? per * (int)sizeof(T) : 0, wide);
+__device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int64_t rel) { return (uint32_t)(mask >> rel) & ((1u << REC_BATCH) - 1); }
+constexpr uint32_t ALL_LIVE = (1u << REC_BATCH) - 1;
+
+// ------------------------------------------------------------------------------- forward
+template <typename T, int V, bool VEC>
+__global__ void __launch_bounds__(REC_WARPS * 32)
+recurrence_forward_maps(const RecArgs a) {
+  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
+  int32_t* first_of = borders[threadIdx.x / 32][0];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+  const int64_t item = (int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32;
+  if (item >= (int64_t)a.chunks * a.strips) return;
+  const Item it(a, item, false);
+  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
+  const int lo = find_sequence(a, it.t0);
+  if (it.strip == 0 && lane_id() == 0) a.sequence[it.chunk] = lo;
+  const ChunkSequences q = find_borders(a, lo, it.t0, it.t1, first_of, borders[threadIdx.x / 32][1]);
+  Map<V> m = {all<V>(CUT), all<V>(0.f)};
+  if (q.tail_end > it.t1) {                                             // a whole chunk: the sequence goes on
+    int start = 0;
+    if (q.first) {
+      start = 63 - __clzll(q.first);
+      if (a.h0) m.B = get<V, VEC>(a.h0 + (int64_t)first_of[start] * a.D + c, left);
+      put<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left, m.B);
+    } else {
+      m.P = all<V>(1.f);
     }
-  } else {
-    for (int i = threadIdx.x; i < REC_CHUNK * W; i += THREADS) {
-      const int r = i / W, c = i % W;
-      to[i] = t0 + r < a.N && c0 + c < a.D ? from[(t0 + r) * stride + c0 + c] : from_f32<T>(0.f);
+    Raw<T, V> g[REC_BATCH], x[REC_BATCH];
+#pragma unroll 1
+    for (int rel = start & ~(REC_BATCH - 1); rel < a.chunk; rel += REC_BATCH) {
+      load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + (it.t0 + rel) * a.gate_stride + c, a.gate_stride, left, g);
+      load_rows<T, V, VEC>(static_cast<const T*>(a.value) + (it.t0 + rel) * a.value_stride + c, a.value_stride, left, x);
+      const Channels<V> before = m.B;
+#pragma unroll
+      for (int i = 0; i < REC_BATCH; ++i) {
+        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i]));
+        if (rel + i == start) m.B = before;
+        m.B = blend(nz, unpack<T, V, true>(x[i]), m.B);
+        m.P = fma(nz, m.P, m.P);
+      }
     }
+    if (q.first) m.P = all<V>(CUT);
   }
+  put<V, VEC>(a.chunk_P + (int64_t)it.chunk * a.D + c, left, m.P);
+  put<V, VEC>(a.chunk_B + (int64_t)it.chunk * a.D + c, left, m.B);
+  complete<V, VEC>(a, it.index, it.strip, c);
 }
 
-template <int THREADS>
-__device__ __forceinline__ void worker_barrier() { asm volatile("bar.sync 1, %0;" :: "n"(THREADS) : "memory"); }
-
-// Threads: 8 runs x LANES, four channels each, and one more warp that looks up the sequences of the block's next tile.
-template <typename T, int LANES, bool QUADS>
-__global__ void __launch_bounds__(REC_RUNS * LANES + 32)
-recurrence_forward_scan(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
-  constexpr int W = 4 * LANES, WORKERS = REC_RUNS * LANES, TILE = REC_CHUNK * W;
-  extern __shared__ __align__(16) unsigned char smem[];
-  T* rows = reinterpret_cast<T*>(smem);                               // [2 stages][gate, value][64][W]
-  float* run_P = reinterpret_cast<float*>(rows + 4 * TILE);           // [8][W]
-  float* run_B = run_P + REC_RUNS * W;
-  float* near_P = run_B + REC_RUNS * W;                               // [W]: the chunks before this one in its group
-  float* near_B = near_P + W;
-  float* far_h = near_B + W;                                          // [W]: the state before the group
-  ChunkSequences* seqs = reinterpret_cast<ChunkSequences*>(far_h + W);
-  const int tiles = a.chunks * a.strips;
-  const bool worker = threadIdx.x < WORKERS;
-  const int run = threadIdx.x / LANES, lane4 = (threadIdx.x % LANES) * 4;
-
-  auto fetch = [&](int tile, int stage) {
-    if (tile < tiles) {
-      const int64_t t0 = (int64_t)(tile / a.strips) * REC_CHUNK;
-      const int c0 = tile % a.strips * W;
-      fetch_rows<T, LANES, QUADS>(a, a.gate, a.gate_stride, t0, c0, rows + stage * 2 * TILE);
-      fetch_rows<T, LANES, QUADS>(a, a.value, a.value_stride, t0, c0, rows + (stage * 2 + 1) * TILE);
-    }
-    copy_commit();
-  };
-
-  if (worker) fetch(blockIdx.x, 0);
-  else if (blockIdx.x < tiles) find_sequences<false>(a, blockIdx.x / a.strips, &seqs[0]);
+template <typename T, int V, bool VEC>
+__global__ void __launch_bounds__(REC_WARPS * 32)
+recurrence_forward_walk(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
+  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
+  int32_t* first_of = borders[threadIdx.x / 32][0];
+  int32_t* last_of = borders[threadIdx.x / 32][1];
   if (h_final) {
     check_offsets(a, [&](int64_t s) {
       for (int d = lane_id(); d < a.D; d += 32) h_final[s * a.D + d] = a.h0 ? a.h0[s * a.D + d] : 0.f;
@@ -298,149 +508,120 @@ recurrence_forward_scan(const RecArgs a, T* __restrict__ out, int64_t out_stride
   } else {
     check_offsets(a, [](int64_t) {});
   }
-  __syncthreads();
-
-  int stage = 0;
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, stage ^= 1) {
-    const int next = tile + gridDim.x;
-    if (!worker) {
-      if (next < tiles) find_sequences<false>(a, next / a.strips, &seqs[stage ^ 1]);
-      __syncthreads();
-      continue;
-    }
-    fetch(next, stage ^ 1);
-    copy_wait<1>();
-    worker_barrier<WORKERS>();
-
-    const int chunk = tile / a.strips, c0 = tile % a.strips * W;
-    const int64_t t0 = (int64_t)chunk * REC_CHUNK;
-    const ChunkSequences& sq = seqs[stage];
-    const T* gate = rows + stage * 2 * TILE + run * REC_RUN * W + lane4;
-    const T* value = gate + TILE;
-    const uint32_t firsts = (uint32_t)(sq.first >> (run * REC_RUN)) & 0xFF;
-    const int left = a.D - c0 - lane4;                                // channels of this thread that exist
-    const int tokens = (int)min((int64_t)REC_RUN, a.N - t0 - run * REC_RUN);
-
-    // the maps of the runs; z is kept, in its place the state itself where a sequence begins (h0 is read once, before anything
-    // that depends on it is published: h_final may be the same array)
-    float z[REC_RUN][4];
+  const int64_t item = (int64_t)(gridDim.x - 1 - blockIdx.x) * REC_WARPS + threadIdx.x / 32;     // from the end: see above
+  if (item >= (int64_t)a.chunks * a.strips) return;
+  const Item it(a, item, false);
+  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
+  const ChunkSequences q = find_borders(a, a.sequence[it.chunk], it.t0, it.t1, first_of, last_of);
+  // the start of a sequence that goes on behind the chunk was kept by the first pass: h_final may be the same array as h0, and the
+  // warp that writes it does not wait for this one
+  const int kept = q.first && q.tail_end > it.t1 ? 63 - __clzll(q.first) : -1;
+  Channels<V> h = all<V>(0.f);
+  if (!(q.first & 1)) h = state_before<V, VEC>(a, it.index, (int)(q.head_begin / a.chunk), c);
+  const T* gate = static_cast<const T*>(a.gate) + it.t0 * a.gate_stride + c;
+  const T* value = static_cast<const T*>(a.value) + it.t0 * a.value_stride + c;
+  T* to = out + it.t0 * out_stride + c;
+  const int tokens = (int)(it.t1 - it.t0);
+#pragma unroll 1
+  for (int rel = 0; rel < tokens; rel += REC_BATCH, gate += REC_BATCH * a.gate_stride, value += REC_BATCH * a.value_stride, to += REC_BATCH * out_stride) {
+    const uint32_t live = tokens - rel >= REC_BATCH ? ALL_LIVE : (1u << (tokens - rel)) - 1;
+    const uint32_t firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
+    if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
+    Raw<T, V> g[REC_BATCH], x[REC_BATCH];
+    if (live == ALL_LIVE && !(firsts | lasts)) {
+      load_rows<T, V, VEC>(gate, a.gate_stride, left, g);
+      load_rows<T, V, VEC>(value, a.value_stride, left, x);
+      T* row = to;
 #pragma unroll
-    for (int i = 0; i < REC_RUN; ++i) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) z[i][k] = 0.f;
-      if ((firsts >> i & 1) && a.h0) get4<QUADS>(a.h0 + (int64_t)sq.first_of[run * REC_RUN + i] * a.D + c0 + lane4, left, z[i]);
-    }
-    float P[4] = {1.f, 1.f, 1.f, 1.f}, B[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < REC_RUN; ++i) {
-      float g[4], x[4];
-      read4(gate + i * W, g);
-      read4(value + i * W, x);
-      if (firsts >> i & 1) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          B[k] = z[i][k] = blend(sigmoid_f32(g[k]), x[k], z[i][k]);
-          P[k] = CUT;
-        }
-      } else if (i < tokens) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          z[i][k] = sigmoid_f32(g[k]);
-          B[k] = blend(z[i][k], x[k], B[k]);
-          P[k] *= 1.f - z[i][k];
-        }
+      for (int i = 0; i < REC_BATCH; ++i, row += out_stride) {
+        h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
+        put<V, VEC>(row, left, h);
       }
-    }
-    *reinterpret_cast<float4*>(run_P + run * W + lane4) = make_float4(P[0], P[1], P[2], P[3]);
-    *reinterpret_cast<float4*>(run_B + run * W + lane4) = make_float4(B[0], B[1], B[2], B[3]);
-    worker_barrier<WORKERS>();
-
-    const int ch = threadIdx.x % W;
-    const bool near = threadIdx.x < W, exists = c0 + ch < a.D;
-    Map own = {1.f, 0.f};
-    if (near)
-#pragma unroll
-      for (int r = 0; r < REC_RUNS; ++r) own = then(own, Map{run_P[r * W + ch], run_B[r * W + ch]});
-    const int from = sq.first & 1 ? chunk : (int)(sq.far / REC_CHUNK);
-    const Map nearby = join(a, chunk, from, near, exists ? c0 + ch : -1, own);
-    if (near) {
-      near_P[ch] = nearby.P;
-      near_B[ch] = nearby.B;
     } else {
-      far_h[ch] = nearby.B;
-    }
-    worker_barrier<WORKERS>();
-    if (near && exists && (entry || chunk % REC_SPAN == REC_SPAN - 1)) {
-      const float h = apply(nearby, far_h[ch]);
-      if (entry) entry[(int64_t)chunk * a.D + c0 + ch] = h;
-      if (chunk % REC_SPAN == REC_SPAN - 1) publish(a.span_state + (int64_t)(chunk / REC_SPAN) * a.D + c0 + ch, Map{CUT, apply(own, h)});
-    }
-
-    // the state before the run, then its tokens
-    float h[4];
+      load_rows<T, V, VEC>(gate, a.gate_stride, live, left, g);
+      load_rows<T, V, VEC>(value, a.value_stride, live, left, x);
+      T* row = to;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) h[k] = apply(Map{near_P[lane4 + k], near_B[lane4 + k]}, far_h[lane4 + k]);
-    for (int r = 0; r < run; ++r) {
-      const float4 p = *reinterpret_cast<const float4*>(run_P + r * W + lane4);
-      const float4 b = *reinterpret_cast<const float4*>(run_B + r * W + lane4);
-      h[0] = apply(Map{p.x, b.x}, h[0]);
-      h[1] = apply(Map{p.y, b.y}, h[1]);
-      h[2] = apply(Map{p.z, b.z}, h[2]);
-      h[3] = apply(Map{p.w, b.w}, h[3]);
-    }
-    const uint32_t lasts = (uint32_t)(sq.last >> (run * REC_RUN)) & 0xFF;
-    T* to = out + (t0 + run * REC_RUN) * out_stride + c0 + lane4;
+      for (int i0 = 0; i0 < REC_BATCH; i0 += 4) {
+        Channels<V> s[4];
 #pragma unroll
-    for (int i = 0; i < REC_RUN; ++i) {
-      if (i < tokens) {
-        float x[4];
-        read4(value + i * W, x);
+        for (int i = i0; i < i0 + 4; ++i) {
+          s[i - i0] = all<V>(0.f);
+          if (firsts >> i & 1) {
+            if (rel + i == kept) s[i - i0] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
+            else if (a.h0) s[i - i0] = get<V, VEC>(a.h0 + (int64_t)first_of[rel + i] * a.D + c, left);
+          }
+        }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) h[k] = (firsts >> i & 1) ? z[i][k] : blend(z[i][k], x[k], h[k]);
-        put4<QUADS>(to + i * out_stride, left, h);
-        if ((lasts >> i & 1) && h_final) put4<QUADS>(h_final + (int64_t)sq.last_of[run * REC_RUN + i] * a.D + c0 + lane4, left, h);
+        for (int i = i0; i < i0 + 4; ++i, row += out_stride) {
+          if (live >> i & 1) {
+            if (firsts >> i & 1) h = s[i - i0];
+            h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
+            put<V, VEC>(row, left, h);
+            if ((lasts >> i & 1) && h_final) put<V, VEC>(h_final + (int64_t)last_of[rel + i] * a.D + c, left, h);
+          }
+        }
       }
     }
-    __syncthreads();
   }
-  copy_wait<0>();
 }
 
-// The backward walks the chunks from the last to the first.  What a token hands to the one before it, c_t = (1 - z_t) G_t =
-// (1 - z_t) (grad_out_t + c_{t+1}), is the same kind of map; its cut is a sequence's last token, which starts from grad_final.
-// The states come from the forward's entry states, by the runs' forward maps inside the chunk.
-template <typename T, int LANES, bool QUADS>
-__global__ void __launch_bounds__(REC_RUNS * LANES + 32)
-recurrence_backward_scan(const RecArgs a, const float* __restrict__ entry, const T* __restrict__ grad_out, int64_t grad_out_stride,
+// ------------------------------------------------------------------------------- backward
+// What a token hands to the one before it, c_t = (1 - z_t) G_t = (1 - z_t) (grad_out_t + c_{t+1}), is the same kind of map, walked from
+// the last chunk to the first; its cut is a sequence's last token, which starts from grad_final.
+template <typename T, int V, bool VEC>
+__global__ void __launch_bounds__(REC_WARPS * 32)
+recurrence_backward_maps(const RecArgs a, const T* __restrict__ grad_out, int64_t grad_out_stride, const float* __restrict__ grad_final) {
+  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
+  int32_t* last_of = borders[threadIdx.x / 32][1];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
+  const int64_t item = (int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32;
+  if (item >= (int64_t)a.chunks * a.strips) return;
+  const Item it(a, item, true);
+  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
+  const int lo = find_sequence(a, it.t0);
+  if (it.strip == 0 && lane_id() == 0) a.sequence[it.chunk] = lo;
+  const ChunkSequences q = find_borders(a, lo, it.t0, it.t1, borders[threadIdx.x / 32][0], last_of);
+  Map<V> m = {all<V>(CUT), all<V>(0.f)};
+  if (q.head_begin < it.t0) {
+    int end = (int)(it.t1 - it.t0) - 1;
+    if (q.last) {
+      end = __ffsll(q.last) - 1;
+      if (grad_final) m.B = get<V, VEC>(grad_final + (int64_t)last_of[end] * a.D + c, left);
+    } else {
+      m.P = all<V>(1.f);
+    }
+    Raw<T, V> g[REC_BATCH], d[REC_BATCH];
+#pragma unroll 1
+    for (int rel = end & ~(REC_BATCH - 1); rel >= 0; rel -= REC_BATCH) {
+      const uint32_t live = end - rel >= REC_BATCH - 1 ? ALL_LIVE : (1u << (end - rel + 1)) - 1;
+      load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + (it.t0 + rel) * a.gate_stride + c, a.gate_stride, live, left, g);
+      load_rows<T, V, VEC>(grad_out + (it.t0 + rel) * grad_out_stride + c, grad_out_stride, live, left, d);
+#pragma unroll
+      for (int i = REC_BATCH - 1; i >= 0; --i) {
+        if (live >> i & 1) {
+          const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), G = unpack<T, V>(d[i]) + m.B;
+          m.B = fma(nz, G, G);
+          m.P = fma(nz, m.P, m.P);
+        }
+      }
+    }
+    if (q.last) m.P = all<V>(CUT);
+  }
+  put<V, VEC>(a.chunk_P + (int64_t)it.index * a.D + c, left, m.P);
+  put<V, VEC>(a.chunk_B + (int64_t)it.index * a.D + c, left, m.B);
+  complete<V, VEC>(a, it.index, it.strip, c);
+}
+
+// A batch is walked forward from the state that the forward left before it, for -z and the distance from value to state, then backward.
+template <typename T, int V, bool VEC>
+__global__ void __launch_bounds__(REC_WARPS * 32)
+recurrence_backward_walk(const RecArgs a, const float* __restrict__ entry, const T* __restrict__ grad_out, int64_t grad_out_stride,
                          const float* __restrict__ grad_final, T* __restrict__ grad_gate, int64_t grad_gate_stride,
                          T* __restrict__ grad_value, int64_t grad_value_stride, float* __restrict__ grad_h0) {
-  constexpr int W = 4 * LANES, WORKERS = REC_RUNS * LANES, TILE = REC_CHUNK * W;
-  extern __shared__ __align__(16) unsigned char smem[];
-  T* rows = reinterpret_cast<T*>(smem);                               // [2 stages][gate, value, grad_out][64][W]
-  float* run_P = reinterpret_cast<float*>(rows + 6 * TILE);           // [8][W] products of 1 - z
-  float* run_B = run_P + REC_RUNS * W;                                // [8][W] states
-  float* run_C = run_B + REC_RUNS * W;                                // [8][W] what the run hands back
-  float* near_P = run_C + REC_RUNS * W;
-  float* near_B = near_P + W;
-  float* far_c = near_B + W;
-  ChunkSequences* seqs = reinterpret_cast<ChunkSequences*>(far_c + W);
-  const int tiles = a.chunks * a.strips;
-  const bool worker = threadIdx.x < WORKERS;
-  const int run = threadIdx.x / LANES, lane4 = (threadIdx.x % LANES) * 4;
-
-  auto fetch = [&](int tile, int stage) {
-    if (tile < tiles) {
-      const int64_t t0 = (int64_t)(a.chunks - 1 - tile / a.strips) * REC_CHUNK;
-      const int c0 = tile % a.strips * W;
-      fetch_rows<T, LANES, QUADS>(a, a.gate, a.gate_stride, t0, c0, rows + stage * 3 * TILE);
-      fetch_rows<T, LANES, QUADS>(a, a.value, a.value_stride, t0, c0, rows + (stage * 3 + 1) * TILE);
-      fetch_rows<T, LANES, QUADS>(a, grad_out, grad_out_stride, t0, c0, rows + (stage * 3 + 2) * TILE);
-    }
-    copy_commit();
-  };
-
-  if (worker) fetch(blockIdx.x, 0);
-  else if (blockIdx.x < tiles) find_sequences<true>(a, a.chunks - 1 - blockIdx.x / a.strips, &seqs[0]);
+  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
+  int32_t* first_of = borders[threadIdx.x / 32][0];
+  int32_t* last_of = borders[threadIdx.x / 32][1];
   if (grad_h0) {
     check_offsets(a, [&](int64_t s) {
       for (int d = lane_id(); d < a.D; d += 32) grad_h0[s * a.D + d] = grad_final ? grad_final[s * a.D + d] : 0.f;
@@ -448,149 +629,48 @@ recurrence_backward_scan(const RecArgs a, const float* __restrict__ entry, const
   } else {
     check_offsets(a, [](int64_t) {});
   }
-  __syncthreads();
-
-  int stage = 0;
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, stage ^= 1) {
-    const int next = tile + gridDim.x;
-    if (!worker) {
-      if (next < tiles) find_sequences<true>(a, a.chunks - 1 - next / a.strips, &seqs[stage ^ 1]);
-      __syncthreads();
-      continue;
+  const int64_t item = (int64_t)(gridDim.x - 1 - blockIdx.x) * REC_WARPS + threadIdx.x / 32;
+  if (item >= (int64_t)a.chunks * a.strips) return;
+  const Item it(a, item, true);
+  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
+  const ChunkSequences q = find_borders(a, a.sequence[it.chunk], it.t0, it.t1, first_of, last_of);
+  Channels<V> carry = all<V>(0.f);
+  if (!(q.last >> (tokens - 1) & 1))
+    carry = state_before<V, VEC>(a, it.index, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c);
+#pragma unroll 1
+  for (int rel = (tokens - 1) & ~(REC_BATCH - 1); rel >= 0; rel -= REC_BATCH) {
+    const int64_t t = it.t0 + rel;
+    const uint32_t live = tokens - rel >= REC_BATCH ? ALL_LIVE : (1u << (tokens - rel)) - 1;
+    const uint32_t firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
+    Raw<T, V> g[REC_BATCH], x[REC_BATCH], d[REC_BATCH];
+    load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + t * a.gate_stride + c, a.gate_stride, live, left, g);
+    load_rows<T, V, VEC>(static_cast<const T*>(a.value) + t * a.value_stride + c, a.value_stride, live, left, x);
+    load_rows<T, V, VEC>(grad_out + t * grad_out_stride + c, grad_out_stride, live, left, d);
+    Channels<V> h = all<V>(0.f);
+    if (!(firsts & 1)) h = get<V, VEC>(entry + t / REC_BATCH * a.D + c, left);
+    Channels<V> nz[REC_BATCH], away[REC_BATCH];                         // away: - (value - state before the token)
+#pragma unroll
+    for (int i = 0; i < REC_BATCH; ++i) {
+      if (firsts >> i & 1) h = a.h0 ? get<V, VEC>(a.h0 + (int64_t)first_of[rel + i] * a.D + c, left) : all<V>(0.f);
+      const Channels<V> nx = unpack<T, V, true>(x[i]);
+      nz[i] = minus_sigmoid(unpack<T, V>(g[i]));
+      away[i] = nx + h;
+      h = blend(nz[i], nx, h);
     }
-    fetch(next, stage ^ 1);
-    copy_wait<1>();
-    worker_barrier<WORKERS>();
-
-    const int back = tile / a.strips, chunk = a.chunks - 1 - back, c0 = tile % a.strips * W;     // back: chunks from the end
-    const int64_t t0 = (int64_t)chunk * REC_CHUNK;
-    const ChunkSequences& sq = seqs[stage];
-    const T* gate = rows + stage * 3 * TILE + run * REC_RUN * W + lane4;
-    const T* value = gate + TILE;
-    const T* grad = value + TILE;
-    const uint32_t firsts = (uint32_t)(sq.first >> (run * REC_RUN)) & 0xFF, lasts = (uint32_t)(sq.last >> (run * REC_RUN)) & 0xFF;
-    const int left = a.D - c0 - lane4;
-    const int tokens = (int)min((int64_t)REC_RUN, a.N - t0 - run * REC_RUN);
-    auto start_state = [&](int i, float (&h)[4]) {                    // h0 of the sequence that begins at token i of the run
+    T* to_gate = grad_gate + t * grad_gate_stride + c;
+    T* to_value = grad_value + t * grad_value_stride + c;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) h[k] = 0.f;
-      if (a.h0) get4<QUADS>(a.h0 + (int64_t)sq.first_of[run * REC_RUN + i] * a.D + c0 + lane4, left, h);
-    };
-    auto end_gradient = [&](int i, float (&c)[4]) {                   // grad_final of the sequence that ends there
-#pragma unroll
-      for (int k = 0; k < 4; ++k) c[k] = 0.f;
-      if (grad_final) get4<QUADS>(grad_final + (int64_t)sq.last_of[run * REC_RUN + i] * a.D + c0 + lane4, left, c);
-    };
-
-    // the runs' maps in both directions
-    float z[REC_RUN][4], P[4] = {1.f, 1.f, 1.f, 1.f}, h[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f}, before[4] = {0.f, 0.f, 0.f, 0.f};
-    if (entry) get4<QUADS>(entry + (int64_t)chunk * a.D + c0 + lane4, left, before);
-#pragma unroll
-    for (int i = 0; i < REC_RUN; ++i) {
-      float g[4], x[4];
-      read4(gate + i * W, g);
-      read4(value + i * W, x);
-      if (firsts >> i & 1) start_state(i, h);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        z[i][k] = i < tokens ? sigmoid_f32(g[k]) : 0.f;
-        h[k] = blend(z[i][k], x[k], h[k]);
-        P[k] *= 1.f - z[i][k];
+    for (int i = REC_BATCH - 1; i >= 0; --i) {
+      if (live >> i & 1) {
+        if (lasts >> i & 1) carry = grad_final ? get<V, VEC>(grad_final + (int64_t)last_of[rel + i] * a.D + c, left) : all<V>(0.f);
+        const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;          // -z G
+        carry = fma(nz[i], G, G);
+        put<V, VEC>(to_value + i * grad_value_stride, left, nG * all<V>(-1.f));
+        put<V, VEC>(to_gate + i * grad_gate_stride, left, nG * fma(nz[i], away[i], away[i]));
+        if ((firsts >> i & 1) && grad_h0) put<V, VEC>(grad_h0 + (int64_t)first_of[rel + i] * a.D + c, left, carry);
       }
     }
-#pragma unroll
-    for (int i = REC_RUN - 1; i >= 0; --i) {
-      float d[4];
-      read4(grad + i * W, d);
-      if (lasts >> i & 1) end_gradient(i, c);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float G = i < tokens ? d[k] + c[k] : c[k];
-        c[k] = fmaf(-z[i][k], G, G);
-      }
-    }
-    *reinterpret_cast<float4*>(run_P + run * W + lane4) = make_float4(P[0], P[1], P[2], P[3]);
-    *reinterpret_cast<float4*>(run_B + run * W + lane4) = make_float4(h[0], h[1], h[2], h[3]);
-    *reinterpret_cast<float4*>(run_C + run * W + lane4) = make_float4(c[0], c[1], c[2], c[3]);
-    worker_barrier<WORKERS>();
-
-    const int ch = threadIdx.x % W;
-    const bool near = threadIdx.x < W, exists = c0 + ch < a.D;
-    Map own = {1.f, 0.f};
-    if (near)
-#pragma unroll
-      for (int r = REC_RUNS - 1; r >= 0; --r)
-        own = then(own, Map{sq.last >> (r * REC_RUN) & 0xFF ? CUT : run_P[r * W + ch], run_C[r * W + ch]});
-    const int end = (int)(min(t0 + REC_CHUNK, a.N) - 1 - t0);         // the chunk's last token
-    const int from = sq.last >> end & 1 ? back : a.chunks - 1 - (int)min(sq.far / REC_CHUNK, (int64_t)a.chunks - 1);
-    const Map nearby = join(a, back, from, near, exists ? c0 + ch : -1, own);
-    if (near) {
-      near_P[ch] = nearby.P;
-      near_B[ch] = nearby.B;
-    } else {
-      far_c[ch] = nearby.B;
-    }
-
-    // meanwhile the states before the run's tokens: value - h
-    float away[REC_RUN][4];
-    for (int r = 0; r < run; ++r) {
-      const bool cut = sq.first >> (r * REC_RUN) & 0xFF;
-      const float4 p = *reinterpret_cast<const float4*>(run_P + r * W + lane4);
-      const float4 b = *reinterpret_cast<const float4*>(run_B + r * W + lane4);
-      before[0] = cut ? b.x : fmaf(p.x, before[0], b.x);
-      before[1] = cut ? b.y : fmaf(p.y, before[1], b.y);
-      before[2] = cut ? b.z : fmaf(p.z, before[2], b.z);
-      before[3] = cut ? b.w : fmaf(p.w, before[3], b.w);
-    }
-#pragma unroll
-    for (int i = 0; i < REC_RUN; ++i) {
-      float x[4];
-      read4(value + i * W, x);
-      if (firsts >> i & 1) start_state(i, before);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        away[i][k] = x[k] - before[k];
-        before[k] = blend(z[i][k], x[k], before[k]);
-      }
-    }
-    worker_barrier<WORKERS>();
-    if (near && exists && back % REC_SPAN == REC_SPAN - 1)
-      publish(a.span_state + (int64_t)(back / REC_SPAN) * a.D + c0 + ch, Map{CUT, apply(own, apply(nearby, far_c[ch]))});
-
-#pragma unroll
-    for (int k = 0; k < 4; ++k) c[k] = apply(Map{near_P[lane4 + k], near_B[lane4 + k]}, far_c[lane4 + k]);
-    for (int r = REC_RUNS - 1; r > run; --r) {
-      const bool cut = sq.last >> (r * REC_RUN) & 0xFF;
-      const float4 p = *reinterpret_cast<const float4*>(run_P + r * W + lane4);
-      const float4 b = *reinterpret_cast<const float4*>(run_C + r * W + lane4);
-      c[0] = cut ? b.x : fmaf(p.x, c[0], b.x);
-      c[1] = cut ? b.y : fmaf(p.y, c[1], b.y);
-      c[2] = cut ? b.z : fmaf(p.z, c[2], b.z);
-      c[3] = cut ? b.w : fmaf(p.w, c[3], b.w);
-    }
-    T* to_gate = grad_gate + (t0 + run * REC_RUN) * grad_gate_stride + c0 + lane4;
-    T* to_value = grad_value + (t0 + run * REC_RUN) * grad_value_stride + c0 + lane4;
-#pragma unroll
-    for (int i = REC_RUN - 1; i >= 0; --i) {
-      if (i < tokens) {
-        float d[4], gv[4], gg[4];
-        read4(grad + i * W, d);
-        if (lasts >> i & 1) end_gradient(i, c);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float G = d[k] + c[k], keep = 1.f - z[i][k];
-          gv[k] = z[i][k] * G;
-          gg[k] = gv[k] * (keep * away[i][k]);
-          c[k] = fmaf(-z[i][k], G, G);
-        }
-        put4<QUADS>(to_value + i * grad_value_stride, left, gv);
-        put4<QUADS>(to_gate + i * grad_gate_stride, left, gg);
-        if ((firsts >> i & 1) && grad_h0) put4<QUADS>(grad_h0 + (int64_t)sq.first_of[run * REC_RUN + i] * a.D + c0 + lane4, left, c);
-      }
-    }
-    __syncthreads();
   }
-  copy_wait<0>();
 }
 
 }  // namespace mts
@@ -603,7 +683,7 @@ int check_sizes(const char* what, int64_t N, int64_t S, int32_t D, int32_t dtype
   if (N < 0 || S < 0 || D < 1 || !known_dtype(dtype))
     return set_error(MTS_ERR_INVALID_ARG, "%s: N %lld, S %lld, D %d, dtype %d", what, (long long)N, (long long)S, D, dtype);
   if (N >= (1ll << 31) - (1 << 16) || S >= (1ll << 31) - (1 << 16) || D > (1 << 20) ||
-      ceil_div(N, REC_CHUNK) * ceil_div(D, 32) >= (1ll << 30))
+      ceil_div(N, REC_BATCH) * ceil_div(D, 32) >= (1ll << 31))
     return set_error(MTS_ERR_UNSUPPORTED, "%s: N %lld, S %lld, D %d", what, (long long)N, (long long)S, D);
   if (S == 0 && N > 0) return set_error(MTS_ERR_INVALID_ARG, "%s: %lld tokens in no sequence", what, (long long)N);
   return MTS_OK;
@@ -635,61 +715,84 @@ struct Alignment {
   void state(const void* p) { states |= (uintptr_t)p; }
 };
 
+// Tokens of a chunk: 64, fewer where that would leave most of the GPU without a warp (a strip is 256 bytes of a row).
+int chunk_tokens(int64_t N, int32_t D, int32_t dtype) {
+  const int64_t strips = ceil_div((int64_t)D * dtype_bytes(dtype), 256);
+  int chunk = REC_CHUNK;
+  while (chunk > 2 * REC_BATCH && ceil_div(N, chunk) * strips < MTS_REC_WARPS_WANTED) chunk /= 2;
+  return chunk;
+}
+
+// Parts of the workspace, in bytes: status | counters | maps.  Strips of 32 channels are the narrowest.
+struct Workspace {
+  int chunk;
+  int64_t chunks, groups, spans, counters, total;
+  Workspace(int64_t N, int32_t D, int32_t dtype) {
+    chunk = chunk_tokens(N, D, dtype);
+    chunks = ceil_div(N, chunk);
+    groups = ceil_div(chunks, REC_RADIX);
+    spans = ceil_div(groups, REC_RADIX);
+    counters = (int64_t)align_up(256 + 4 * (size_t)(groups + spans + 1) * (size_t)ceil_div(D, 32), 256);
+    total = counters + (int64_t)align_up(4 * (size_t)chunks, 256) + 4 * (3 * chunks + 2 * groups + 3 * spans) * (int64_t)align_up(D, 4);
+  }
+};
+
 RecArgs arguments(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride, const int64_t* offsets, const float* h0,
-                  int64_t N, int64_t S, int32_t D, void* workspace) {
+                  int64_t N, int64_t S, int32_t D, int32_t dtype, int vec, void* workspace) {
   RecArgs a = {gate, gate_stride, value, value_stride, offsets, h0, N, S, D};
-  a.chunks = (int32_t)ceil_div(N, REC_CHUNK);
-  char* w = static_cast<char*>(workspace);
-  a.status = reinterpret_cast<uint32_t*>(w);
-  a.chunk_map = reinterpret_cast<unsigned long long*>(w + 256);
-  a.group_map = a.chunk_map + (int64_t)a.chunks * D;
-  a.span_state = a.group_map + ceil_div(a.chunks, REC_RADIX) * D;
+  const Workspace w(N, D, dtype);
+  a.chunk = w.chunk;
+  a.chunks = (int32_t)w.chunks;
+  a.strips = (int32_t)ceil_div(D, 32 * vec);
+  a.groups = (int32_t)w.groups;
+  a.spans = (int32_t)w.spans;
+  char* p = static_cast<char*>(workspace);
+  a.status = reinterpret_cast<uint32_t*>(p);
+  a.group_count = reinterpret_cast<uint32_t*>(p + 256);
+  a.span_count = a.group_count + w.groups * a.strips;
+  a.total_count = a.span_count + w.spans * a.strips;
+  a.sequence = reinterpret_cast<int32_t*>(p + w.counters);
+  a.chunk_P = reinterpret_cast<float*>(p + w.counters + align_up(4 * (size_t)w.chunks, 256));
+  a.chunk_B = a.chunk_P + w.chunks * D;
+  a.chunk_start = a.chunk_B + w.chunks * D;
+  a.group_P = a.chunk_start + w.chunks * D;
+  a.group_B = a.group_P + w.groups * D;
+  a.span_P = a.group_B + w.groups * D;
+  a.span_B = a.span_P + w.spans * D;
+  a.span_state = a.span_B + w.spans * D;
   return a;
 }
 
-// One block per tile up to what the device holds at once (the blocks of one launch wait for one another).
-template <typename Kernel>
-int launch_scan(const char* what, int trace_id, Kernel kernel, int threads, size_t smem, const RecArgs& a, void** args, cudaStream_t s) {
-  int dev = 0, sms = 0, per_sm = 0;
-  int rc = check_cuda(cudaGetDevice(&dev), "cudaGetDevice");
-  if (rc == MTS_OK) rc = check_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev), "sm count");
-  if (rc == MTS_OK) rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "shared memory size");
-  if (rc == MTS_OK) rc = check_cuda(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem), "occupancy");
-  if (rc != MTS_OK) return rc;
-  const int64_t tiles = (int64_t)a.chunks * a.strips, room = (int64_t)sms * per_sm;
-  const unsigned grid = (unsigned)(tiles < 1 ? 1 : tiles < room ? tiles : room);
+// One warp per chunk and strip, at least one for the check of the offsets.
+template <typename Kernel, typename... Args>
+int launch_pass(const char* what, int trace_id, Kernel kernel, const RecArgs& a, cudaStream_t s, Args... args) {
+  const int64_t blocks = ceil_div((int64_t)a.chunks * a.strips, REC_WARPS);
   LaunchScope scope(trace_id, s);
-  return check_cuda(cudaLaunchCooperativeKernel((const void*)kernel, dim3(grid), dim3(threads), args, smem, s), what);
+  kernel<<<(unsigned)(blocks < 1 ? 1 : blocks), REC_WARPS * 32, 0, s>>>(a, args...);
+  return check_launch(what);
 }
 
-template <typename T, int LANES, bool BACKWARD>
-constexpr size_t scan_smem() {
-  constexpr size_t W = 4 * LANES;
-  return 2 * (BACKWARD ? 3 : 2) * REC_CHUNK * W * sizeof(T) + ((BACKWARD ? 3 : 2) * REC_RUNS + 3) * W * sizeof(float) + 2 * sizeof(ChunkSequences);
-}
-
-// fn(LANES, QUADS) as compile-time constants.  A strip of channels is 256 bytes of a row wide, less for rows that are narrower.
-template <typename T, typename Fn>
-int with_shape(int32_t D, bool quads, Fn&& fn) {
-  using L8 = std::integral_constant<int, 8>;
-  using L16 = std::integral_constant<int, 16>;
-  using L32 = std::integral_constant<int, 32>;
-  if (D <= 32) return quads ? fn(L8(), std::true_type()) : fn(L8(), std::false_type());
-  if constexpr (sizeof(T) == 2)
-    if (D > 64) return quads ? fn(L32(), std::true_type()) : fn(L32(), std::false_type());
-  return quads ? fn(L16(), std::true_type()) : fn(L16(), std::false_type());
+// fn(V, VEC): a lane holds `most` channels, fewer where a row has no use for all lanes.
+template <int MOST, typename Fn>
+int with_channels(int32_t D, const Alignment& al, int bytes, Fn&& fn) {
+  auto vec = [&](int v) { return D % v == 0 && al.rows % (v * bytes) == 0 && al.states % (v * 4) == 0; };
+  if constexpr (MOST >= 4)
+    if (D > 64) return vec(4) ? fn(std::integral_constant<int, 4>(), std::true_type()) : fn(std::integral_constant<int, 4>(), std::false_type());
+  if constexpr (MOST >= 2)
+    if (D > 32) return vec(2) ? fn(std::integral_constant<int, 2>(), std::true_type()) : fn(std::integral_constant<int, 2>(), std::false_type());
+  return fn(std::integral_constant<int, 1>(), std::true_type());
 }
 
 }  // namespace
 
 extern "C" int64_t mts_recurrence_chunks(int64_t N, int32_t D, int32_t dtype) {
-  return N < 0 || D < 1 || !known_dtype(dtype) ? 0 : ceil_div(N, REC_CHUNK);
+  return N < 0 || D < 1 || !known_dtype(dtype) ? 0 : ceil_div(N, REC_BATCH);
 }
 
 extern "C" size_t mts_recurrence_workspace_bytes(int64_t N, int64_t S, int32_t D, int32_t dtype) {
   if (N < 0 || S < 0 || D < 1 || !known_dtype(dtype)) return 0;
-  const int64_t chunks = ceil_div(N, REC_CHUNK);
-  return 256 + sizeof(unsigned long long) * (size_t)(chunks + ceil_div(chunks, REC_RADIX) + ceil_div(chunks, REC_SPAN)) * (size_t)D;
+  const Workspace w(N, D, dtype);
+  return (size_t)w.total;
 }
 
 extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, const void* value, int64_t value_stride, int32_t dtype,
@@ -707,9 +810,9 @@ extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, con
   if (rc == MTS_OK) rc = check_workspace(what, workspace, workspace_bytes, need);
   if (rc != MTS_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  rc = check_cuda(cudaMemsetAsync(workspace, 0xFF, need, s), "cudaMemsetAsync(recurrence maps)");
+  const Workspace w(N, D, dtype);
+  if (w.groups > 1 || S == 0) rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
   if (rc != MTS_OK || S == 0) return rc;
-  RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, workspace);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     Alignment al;
@@ -719,15 +822,13 @@ extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, con
     al.state(h0);
     al.state(h_final);
     al.state(entry_states);
-    a.wide = al.rows % 16 == 0 && D % (16 / (int)sizeof(T)) == 0;
-    const bool quads = al.rows % (4 * sizeof(T)) == 0 && D % 4 == 0 && al.states % 16 == 0;
-    return with_shape<T>(D, quads, [&](auto lanes, auto q) {
-      constexpr int LANES = decltype(lanes)::value;
-      a.strips = (int32_t)ceil_div(D, 4 * LANES);
-      T* o = static_cast<T*>(out);
-      void* args[] = {&a, &o, &out_stride, &h_final, &entry_states};
-      return launch_scan(what, K_RECURRENCE_FWD, recurrence_forward_scan<T, LANES, decltype(q)::value>, REC_RUNS * LANES + 32,
-                         scan_smem<T, LANES, false>(), a, args, s);
+    return with_channels<8 / sizeof(T)>(D, al, sizeof(T), [&](auto v, auto q) {
+      constexpr int V = decltype(v)::value;
+      constexpr bool VEC = decltype(q)::value;
+      const RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, dtype, V, workspace);
+      const int e = launch_pass(what, K_RECURRENCE_FWD, recurrence_forward_maps<T, V, VEC>, a, s);
+      return e != MTS_OK ? e : launch_pass(what, K_RECURRENCE_FWD, recurrence_forward_walk<T, V, VEC>, a, s, static_cast<T*>(out), out_stride,
+                                           h_final, entry_states);
     });
   });
 }
@@ -753,9 +854,9 @@ extern "C" int mts_recurrence_backward(const void* gate, int64_t gate_stride, co
   if (rc == MTS_OK) rc = check_workspace(what, workspace, workspace_bytes, need);
   if (rc != MTS_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  rc = check_cuda(cudaMemsetAsync(workspace, 0xFF, need, s), "cudaMemsetAsync(recurrence maps)");
+  const Workspace w(N, D, dtype);
+  if (w.groups > 1 || S == 0) rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
   if (rc != MTS_OK || S == 0) return rc;
-  RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, workspace);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     Alignment al;
@@ -768,17 +869,15 @@ extern "C" int mts_recurrence_backward(const void* gate, int64_t gate_stride, co
     al.state(entry_states);
     al.state(grad_final);
     al.state(grad_h0);
-    a.wide = al.rows % 16 == 0 && D % (16 / (int)sizeof(T)) == 0;
-    const bool quads = al.rows % (4 * sizeof(T)) == 0 && D % 4 == 0 && al.states % 16 == 0;
-    return with_shape<T>(D, quads, [&](auto lanes, auto q) {
-      constexpr int LANES = decltype(lanes)::value;
-      a.strips = (int32_t)ceil_div(D, 4 * LANES);
-      const T* go = static_cast<const T*>(grad_out);
-      T* gg = static_cast<T*>(grad_gate);
-      T* gv = static_cast<T*>(grad_value);
-      void* args[] = {&a, &entry_states, &go, &grad_out_stride, &grad_final, &gg, &grad_gate_stride, &gv, &grad_value_stride, &grad_h0};
-      return launch_scan(what, K_RECURRENCE_BWD, recurrence_backward_scan<T, LANES, decltype(q)::value>, REC_RUNS * LANES + 32,
-                         scan_smem<T, LANES, true>(), a, args, s);
+    return with_channels<8 / sizeof(T)>(D, al, sizeof(T), [&](auto v, auto q) {
+      constexpr int V = decltype(v)::value;
+      constexpr bool VEC = decltype(q)::value;
+      const RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, dtype, V, workspace);
+      const int e = launch_pass(what, K_RECURRENCE_BWD, recurrence_backward_maps<T, V, VEC>, a, s, static_cast<const T*>(grad_out),
+                                grad_out_stride, grad_final);
+      return e != MTS_OK ? e : launch_pass(what, K_RECURRENCE_BWD, recurrence_backward_walk<T, V, VEC>, a, s, entry_states,
+                                           static_cast<const T*>(grad_out), grad_out_stride, grad_final, static_cast<T*>(grad_gate),
+                                           grad_gate_stride, static_cast<T*>(grad_value), grad_value_stride, grad_h0);
     });
   });
 }
@@ -789,8 +888,6 @@ extern "C" int mts_recurrence_status(const void* workspace, int32_t* host_status
   uint32_t word = 0;
   int rc = check_cuda(cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, s), "cudaMemcpyAsync(status)");
   if (rc == MTS_OK) rc = check_cuda(cudaStreamSynchronize(s), "cudaStreamSynchronize(status)");
-  *host_status = rc == MTS_OK ? (int32_t)~word : 0;
-  if (rc == MTS_OK && (*host_status & REC_STATUS_TIMEOUT))
-    rc = set_error(MTS_ERR_TIMEOUT, "recurrence: a bounded wait ran out, the results of the last call are incomplete");
+  *host_status = rc == MTS_OK ? (int32_t)word : 0;
   return rc;
 }
