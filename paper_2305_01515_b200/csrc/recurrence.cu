@@ -4,32 +4,59 @@
 //
 // Any run of tokens maps the state before it to B + P * state, P the product of its 1 - z and B the state it reaches from 0; a run
 // that contains a sequence's start forgets what came before it (a cut).  Runs compose, so the token axis is cut into chunks
-// whatever the sequences are: one long sequence and a thousand short ones are the same work.  Two passes, a warp per chunk and strip of
-// channels (8 bytes of a row per lane) in each:
-//   maps: the map of every chunk whose last sequence goes on behind it, from that sequence's start on (what lies before it in the
-//         chunk is forgotten).  The last warp of a group of 16 chunks composes the group's map, the last of a span of 16 groups the
-//         span's, the last of all walks the spans: nobody waits.
-//   walk: the state before the chunk from at most a span's state, 15 groups and 15 chunks, then its tokens.
-// The association of the maps depends on the offsets alone, so the result is the same in every run.  Both passes stream at the memory's
-// rate, which bounds them: the inputs are read twice.  The second pass takes the chunks in the opposite order, so that what the first
-// read last is still in the L2 cache.  (Tried before: one pass, whose blocks kept their tokens in shared memory and waited for the
-// maps of the blocks before them.  A word published by one SM is seen by another 1 to 2 us later, and a chain of three such steps per tile
-// outlasts what shared memory can hold back: 424 to 690 us for 524,287 tokens x 256, fp16.)
+// whatever the sequences are: one long sequence and a thousand short ones are the same work.  A chunk x a strip of channels (8 bytes
+// of a row per lane) is two pieces of work for a warp:
+//   map:  the chunk's map, if its last sequence goes on behind it, from that sequence's start on (what lies before it in the chunk is
+//         forgotten).  The last warp of eight neighbours composes their map, and so on; behind every 512 chunks a state is kept.
+//   walk: the state before the chunk from at most seven maps of each of three levels and a kept state, then the chunk's tokens.
+// Warps take the pieces from a counter, a walk some hundreds of pieces behind its chunk's map: by then the maps it needs have long been
+// published (a word written by one SM is seen by another only 1 to 2 us later), and its rows are still in the L2 cache, so memory sees
+// every input once.  The association of the maps depends on the offsets alone: the result is the same in every run.
+//
+// Waiting: a piece waits only for pieces of lower numbers, which running or finished warps have taken, and the lowest unfinished one
+// waits for nothing.  Every wait has a limit all the same, after which the status word says so.
+//
+// Tried before, for 524,287 tokens x 256, fp16: one pass whose blocks kept their tokens in shared memory and waited for the maps of the
+// blocks before them (424 to 690 us: a chain of three publications per tile outlasts what shared memory can hold back); two launches
+// (250 to 280 us: the composition of the maps at the end of the first leaves most SMs idle for 15 us).
 #include <type_traits>
 
 #include "dense.cuh"
 
 namespace mts {
 
-constexpr int REC_WARPS = 4;
-constexpr int REC_CHUNK = 64;                     // tokens of a chunk at most: a bit mask of them is one word
-constexpr int REC_BATCH = 8;                      // tokens loaded together, and between two states kept for the backward
-constexpr int REC_RADIX = 16;                     // chunks per group, groups per span
-constexpr int REC_SPAN = REC_RADIX * REC_RADIX;
-#ifndef MTS_REC_WARPS_WANTED
-#define MTS_REC_WARPS_WANTED 2368
+#ifndef MTS_REC_FWD_BLOCKS
+#define MTS_REC_FWD_BLOCKS 20
 #endif
-constexpr int REC_STATUS_OFFSETS = 1;
+#ifndef MTS_REC_BWD_BLOCKS
+#define MTS_REC_BWD_BLOCKS 12
+#endif
+#ifndef MTS_REC_WARPS_WANTED
+#define MTS_REC_WARPS_WANTED 1776
+#endif
+#ifndef MTS_REC_LAG
+#define MTS_REC_LAG 1024
+#endif
+#ifndef MTS_REC_MAX_CHUNK
+#define MTS_REC_MAX_CHUNK 128
+#endif
+constexpr int REC_CHUNK = MTS_REC_MAX_CHUNK;      // tokens of a chunk at most
+constexpr int REC_PART = 64;                      // tokens whose borders are looked up together: a bit mask of them is one word
+constexpr int REC_BATCH = 8;                      // tokens in registers, and between two states kept for the backward
+constexpr int REC_RADIX_BITS = 3;
+constexpr int REC_RADIX = 1 << REC_RADIX_BITS;    // maps composed into one of the next level
+constexpr int REC_LEVELS = 4;                     // levels of maps, chunks included; a state is kept behind every map of the highest, 512 chunks
+constexpr int REC_STATUS_OFFSETS = 1, REC_STATUS_TIMEOUT = 2;
+constexpr int REC_POLLS = 1 << 21;                // polls before a wait gives up (about a second)
+constexpr uint32_t READY_MAP = 1, READY_CUT = 2;  // a published map, and one that contains a cut
+
+// One level of maps, or (P unused) the kept states.
+struct RecLevel {
+  uint32_t* ready;             // [n, strips]
+  uint32_t* done;              // [n, strips] parts of the map that are ready
+  float* P;                    // [n, D]
+  float* B;
+};
 
 struct RecArgs {
   const void* gate; int64_t gate_stride;
@@ -39,20 +66,12 @@ struct RecArgs {
   int64_t N, S;
   int32_t D;
   int32_t chunk;               // tokens of a chunk
-  int32_t chunks, strips, groups, spans;
+  int32_t chunks, strips;
+  int32_t lag;                 // pieces between the map of a chunk and its walk
   uint32_t* status;
-  uint32_t* group_count;       // [groups, strips] chunks done, likewise groups of a span, spans
-  uint32_t* span_count;
-  uint32_t* total_count;
-  int32_t* sequence;           // [chunks] a sequence at or before the chunk's first token
-  float* chunk_P;              // [chunks, D]
-  float* chunk_B;
+  uint32_t* ticket;
   float* chunk_start;          // [chunks, D] state in which the chunk's last sequence starts
-  float* group_P;
-  float* group_B;
-  float* span_P;
-  float* span_B;
-  float* span_state;           // [spans, D] the state before the span
+  RecLevel level[REC_LEVELS + 1];
 };
 
 // ------------------------------------------------------------------------------- V channels of a lane
@@ -257,140 +276,177 @@ __device__ __forceinline__ Raw<T, V> get_raw(const T* p, int left) {
   }
   return r;
 }
-// What another warp of the same launch has written: from L2, the L1 cache may hold what was there before.
+// What another warp of the same launch has published, after the flag that says so.
 template <int V, bool VEC>
 __device__ __forceinline__ Channels<V> load_published(const float* p, int left) {
   float x[V];
   if constexpr (VEC && V == 4) {
-    const float4 f = left > 0 ? __ldcg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+    if (left <= 0) return all<V>(0.f);
+    asm volatile("ld.relaxed.gpu.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "l"(p) : "memory");
   } else if constexpr (VEC && V == 2) {
-    const float2 f = left > 0 ? __ldcg(reinterpret_cast<const float2*>(p)) : make_float2(0.f, 0.f);
-    x[0] = f.x; x[1] = f.y;
+    if (left <= 0) return all<V>(0.f);
+    asm volatile("ld.relaxed.gpu.global.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "l"(p) : "memory");
   } else {
 #pragma unroll
-    for (int k = 0; k < V; ++k) x[k] = k < left ? __ldcg(p + k) : 0.f;
+    for (int k = 0; k < V; ++k) {
+      x[k] = 0.f;
+      if (k < left) asm volatile("ld.relaxed.gpu.global.f32 %0, [%1];" : "=f"(x[k]) : "l"(p + k) : "memory");
+    }
   }
   return gathered<V>(x);
 }
 
 // ------------------------------------------------------------------------------- maps
-// state -> B + P * state.  P >= 0 is a product of 1 - z; P = -0 marks a cut, whose result is B even where the state before it is
-// infinite or NaN.
 template <int V>
 struct Map { Channels<V> P, B; };
-constexpr float CUT = -0.f;
 
-// first, then second; `first` may be a state (P = CUT).
-template <int V>
-__device__ __forceinline__ Map<V> then(Map<V> first, Map<V> second) {
-  float P1[V], B1[V], P2[V], B2[V];
-  scattered(first.P, P1);
-  scattered(first.B, B1);
-  scattered(second.P, P2);
-  scattered(second.B, B2);
-#pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const bool cut = __float_as_int(P2[k]) == (int)0x80000000;
-    B1[k] = cut ? B2[k] : fmaf(P2[k], B1[k], B2[k]);
-    P1[k] = cut || __float_as_int(P1[k]) == (int)0x80000000 ? CUT : P1[k] * P2[k];
-  }
-  return Map<V>{gathered<V>(P1), gathered<V>(B1)};
-}
-
-// Composition of n maps from row `lo` of [rows, D] arrays on, after `m`.
-template <int V, bool VEC>
-__device__ __forceinline__ Map<V> compose(const RecArgs& a, const float* P, const float* B, int lo, int n, int c, Map<V> m) {
-  const int left = a.D - c;
-  P += (int64_t)lo * a.D + c;
-  B += (int64_t)lo * a.D + c;
-#pragma unroll 4
-  for (int k = 0; k < n; ++k, P += a.D, B += a.D) m = then(m, Map<V>{load_published<V, VEC>(P, left), load_published<V, VEC>(B, left)});
-  return m;
-}
-
-// Whether this warp is the last of `members` to get here; if so, what the others wrote before is visible to it.
-__device__ __forceinline__ bool last_of(uint32_t* count, int members) {
-  uint32_t before = 0;
+// After this warp's writes to what `flag` stands for.
+__device__ __forceinline__ void set_ready(uint32_t* flag, uint32_t how) {
   __syncwarp();
   if (lane_id() == 0) {
     __threadfence();
-    before = atomicAdd(count, 1u);
-  }
-  const bool last = __shfl_sync(0xFFFFFFFFu, before, 0) == (uint32_t)members - 1;
-  if (last) __threadfence();
-  return last;
-}
-
-// After a chunk's map (counted in the order of the walk) has been written: the maps of the group and span that it completes, and after the
-// last of all the state before every span.
-template <int V, bool VEC>
-__device__ __forceinline__ void complete(const RecArgs& a, int index, int strip, int c) {
-  if (a.groups == 1) return;                                            // the walk composes the chunks' maps itself
-  const Map<V> identity = {all<V>(1.f), all<V>(0.f)};
-  const int left = a.D - c, group = index / REC_RADIX, span = index / REC_SPAN;
-  if (!last_of(a.group_count + (int64_t)group * a.strips + strip, min(REC_RADIX, a.chunks - group * REC_RADIX))) return;
-  Map<V> m = compose<V, VEC>(a, a.chunk_P, a.chunk_B, group * REC_RADIX, min(REC_RADIX, a.chunks - group * REC_RADIX), c, identity);
-  put<V, VEC>(a.group_P + (int64_t)group * a.D + c, left, m.P);
-  put<V, VEC>(a.group_B + (int64_t)group * a.D + c, left, m.B);
-  if (a.spans == 1) return;
-  if (!last_of(a.span_count + (int64_t)span * a.strips + strip, min(REC_RADIX, a.groups - span * REC_RADIX))) return;
-  m = compose<V, VEC>(a, a.group_P, a.group_B, span * REC_RADIX, min(REC_RADIX, a.groups - span * REC_RADIX), c, identity);
-  put<V, VEC>(a.span_P + (int64_t)span * a.D + c, left, m.P);
-  put<V, VEC>(a.span_B + (int64_t)span * a.D + c, left, m.B);
-  if (!last_of(a.total_count + strip, a.spans)) return;
-  m = {all<V>(CUT), all<V>(0.f)};
-#pragma unroll 4
-  for (int k = 0; k < a.spans; ++k) {
-    put<V, VEC>(a.span_state + (int64_t)k * a.D + c, left, m.B);
-    m = compose<V, VEC>(a, a.span_P, a.span_B, k, 1, c, m);
+    asm volatile("st.release.gpu.global.u32 [%0], %1;" :: "l"(flag), "r"(how) : "memory");
   }
 }
+// Every lane waits for a flag of its own (null: none) and gets what it says.
+__device__ __forceinline__ uint32_t wait_ready(const RecArgs& a, const uint32_t* flag) {
+  uint32_t v = flag ? 0u : READY_MAP;
+  for (int polls = 1;; ++polls) {
+    if (!v) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(flag) : "memory");
+    if (__all_sync(0xFFFFFFFFu, v != 0)) break;
+    // offsets out of order may name chunks that publish nothing; once a wait has run out the others give up soon, too
+    const uint32_t status = polls % 64 ? 0u : *reinterpret_cast<volatile uint32_t*>(a.status);
+    if (polls >= REC_POLLS || status) {
+      if (lane_id() == 0 && !status) atomicOr(a.status, (uint32_t)REC_STATUS_TIMEOUT);
+      break;
+    }
+  }
+  __syncwarp();
+  return v;
+}
 
-// The state before tile `index`, whose first sequence (in the order of the walk) began in tile `from` < index.
+// Publishes the map of chunk `index` (counted in the order of the walk) and those of the higher levels that it completes.
 template <int V, bool VEC>
-__device__ __forceinline__ Channels<V> state_before(const RecArgs& a, int index, int from, int c) {
+__device__ __forceinline__ void publish(const RecArgs& a, int index, int strip, int c, Map<V> m, bool cut) {
+  const int left = a.D - c;
+#pragma unroll 1
+  for (int l = 0;; ++l) {
+    const RecLevel& to = a.level[l];
+    put<V, VEC>(to.P + (int64_t)index * a.D + c, left, m.P);
+    put<V, VEC>(to.B + (int64_t)index * a.D + c, left, m.B);
+    set_ready(to.ready + (int64_t)index * a.strips + strip, cut ? READY_CUT : READY_MAP);
+    if (l + 1 == REC_LEVELS) break;
+    // the last of eight to come here goes on (a set that the end of the tokens leaves short is never needed)
+    const int parent = index >> REC_RADIX_BITS;
+    uint32_t before = 0;
+    if (lane_id() == 0) {
+      before = atomicAdd(a.level[l + 1].done + (int64_t)parent * a.strips + strip, 1u);
+      __threadfence();
+    }
+    if (__shfl_sync(0xFFFFFFFFu, before, 0) != REC_RADIX - 1) return;
+    __syncwarp();
+    uint32_t how = READY_MAP;
+    if (lane_id() < REC_RADIX) how = *reinterpret_cast<volatile uint32_t*>(to.ready + ((int64_t)parent * REC_RADIX + lane_id()) * a.strips + strip);
+    const uint32_t cuts = __ballot_sync(0xFFFFFFFFu, how == READY_CUT);
+    m = {all<V>(1.f), all<V>(0.f)};
+    const float* P = to.P + (int64_t)parent * REC_RADIX * a.D + c;
+    const float* B = to.B + (int64_t)parent * REC_RADIX * a.D + c;
+#pragma unroll
+    for (int k = 0; k < REC_RADIX; ++k, P += a.D, B += a.D) {
+      const Channels<V> Pk = load_published<V, VEC>(P, left), Bk = load_published<V, VEC>(B, left);
+      if (cuts >> k & 1) m.B = Bk;
+      else m = {Pk * m.P, fma(Pk, m.B, Bk)};
+    }
+    cut = cuts != 0;
+    index = parent;
+  }
+  // the state behind a map of the highest level: the next one kept
+  const RecLevel& kept = a.level[REC_LEVELS];
+  if (!cut && index > 0) {
+    wait_ready(a, lane_id() == 0 ? kept.ready + (int64_t)index * a.strips + strip : nullptr);
+    m.B = fma(m.P, load_published<V, VEC>(kept.B + (int64_t)index * a.D + c, left), m.B);
+  }
+  put<V, VEC>(kept.B + (int64_t)(index + 1) * a.D + c, left, m.B);
+  set_ready(kept.ready + (int64_t)(index + 1) * a.strips + strip, READY_MAP);
+}
+
+// The state before chunk `index`, whose first sequence (in the order of the walk) began in chunk `from` < index.  Also waits for the
+// chunk's own map where `own` says so.
+template <int V, bool VEC>
+__device__ __forceinline__ Channels<V> state_before(const RecArgs& a, int index, int strip, int from, int c, bool want, bool own) {
   from = max(0, min(from, index - 1));
-  const int group = index / REC_RADIX, span = index / REC_SPAN, lo = max(from, group * REC_RADIX);
-  Map<V> m = {all<V>(CUT), all<V>(0.f)};
-  if (from < group * REC_RADIX) {
-    if (from < span * REC_SPAN) m.B = load_published<V, VEC>(a.span_state + (int64_t)span * a.D + c, a.D - c);
-    const int glo = max(from / REC_RADIX, span * REC_RADIX);
-    m = compose<V, VEC>(a, a.group_P, a.group_B, glo, group - glo, c, m);
+  // lane 8 l + k: map k of level l, of those between the start of the next level's map (or `from`) and the chunk, seven at most; lane 31:
+  // the kept state, lane 23: the chunk's own map
+  const int l = lane_id() / REC_RADIX, shift = l * REC_RADIX_BITS, k = lane_id() % REC_RADIX;
+  const int at = index >> shift, parent = at >> REC_RADIX_BITS << REC_RADIX_BITS;
+  // a level is used where the one below does not reach back to `from`
+  const bool used = want && l < REC_LEVELS - 1 && from >> shift < at && (l == 0 || from >> (shift - REC_RADIX_BITS) < (index >> (shift - REC_RADIX_BITS) >> REC_RADIX_BITS << REC_RADIX_BITS));
+  const int lo = max(from >> shift, parent);
+  const bool mine = used && k < REC_RADIX - 1 && lo + k < at;
+  constexpr int TOP = (REC_LEVELS - 1) * REC_RADIX_BITS;
+  const int top = index >> TOP;
+  const bool kept = want && from < top << TOP;
+  const uint32_t* flag = mine ? a.level[l].ready + (int64_t)(lo + k) * a.strips + strip : nullptr;
+  if (lane_id() == 31 && kept) flag = a.level[REC_LEVELS].ready + (int64_t)top * a.strips + strip;
+  if (lane_id() == 23 && own) flag = a.level[0].ready + (int64_t)index * a.strips + strip;
+  const uint32_t how = wait_ready(a, flag);
+  Channels<V> h = all<V>(0.f);
+  if (!want) return h;
+  const uint32_t maps = __ballot_sync(0xFFFFFFFFu, mine), cuts = __ballot_sync(0xFFFFFFFFu, mine && how == READY_CUT);
+  const int left = a.D - c;
+  if (kept) h = load_published<V, VEC>(a.level[REC_LEVELS].B + (int64_t)top * a.D + c, left);
+#pragma unroll
+  for (int i = REC_LEVELS - 2; i >= 0; --i) {
+    const int n = __popc(maps >> (i * REC_RADIX) & 0xFF), first = __shfl_sync(0xFFFFFFFFu, lo, i * REC_RADIX);
+    const float* P = a.level[i].P + (int64_t)first * a.D + c;
+    const float* B = a.level[i].B + (int64_t)first * a.D + c;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j, P += a.D, B += a.D) {
+      const Channels<V> Pj = load_published<V, VEC>(P, left), Bj = load_published<V, VEC>(B, left);
+      h = cuts >> (i * REC_RADIX + j) & 1 ? Bj : fma(Pj, h, Bj);
+    }
   }
-  return compose<V, VEC>(a, a.chunk_P, a.chunk_B, lo, index - lo, c, m).B;
+  return h;
 }
 
-// ------------------------------------------------------------------------------- sequences of a chunk
-struct ChunkSequences {
-  unsigned long long first, last;      // tokens that begin / end their sequence
-  int64_t head_begin;                  // of the sequence that holds the chunk's first token
-  int64_t tail_end;                    // of the one that holds its last token
-};
-
-// One warp: the sequence of the chunk's first token, by a search with 32 probes a step.  Every index is bounded whatever the offsets hold.
-__device__ __forceinline__ int find_sequence(const RecArgs& a, int64_t t0) {
+// ------------------------------------------------------------------------------- sequences
+// One warp: the last sequence that begins at or before token t, by a search with 32 probes a step.  Every index is bounded whatever the
+// offsets hold.
+__device__ __forceinline__ int find_sequence(const RecArgs& a, int64_t t) {
   int64_t lo = 0, hi = a.S;
-  while (hi - lo > 1) {                                               // offsets[lo] <= t0 < offsets[hi]
+  while (hi - lo > 1) {                                               // offsets[lo] <= t < offsets[hi]
     const int64_t step = (hi - lo + 31) / 32, i = lo + lane_id() * step;
-    const int n = __popc(__ballot_sync(0xFFFFFFFFu, i < hi && a.offsets[i] <= t0));
+    const int n = __popc(__ballot_sync(0xFFFFFFFFu, i < hi && a.offsets[i] <= t));
     lo += (int64_t)max(n - 1, 0) * step;
     hi = min(hi, lo + step);
   }
   return (int)lo;
 }
-// The sequences of a chunk from sequence `lo` on; their numbers go to first_of / last_of, by token.
-__device__ __forceinline__ ChunkSequences find_borders(const RecArgs& a, int lo, int64_t t0, int64_t t1, int32_t* first_of, int32_t* last_of) {
-  ChunkSequences q = {0, 0, t0, t1};
+
+// The borders among the tokens [t0, t1) of a part.
+struct Borders {
+  unsigned long long first, last;      // tokens that begin / end their sequence
+  int64_t head_begin;                  // of the sequence that holds the part's first token
+  int64_t tail_end;                    // of the one that holds its last token
+  int32_t lo;                          // in: a sequence at or before the part's first token; out: the one of its last token
+};
+// Looked up by one warp from sequence `lo` on; the sequences' numbers go to first_of / last_of, by token, and those of sequences that
+// begin here and end behind `kept_end` bitwise inverted to first_of.
+__device__ __forceinline__ Borders find_borders(const RecArgs& a, int lo, int64_t t0, int64_t t1, int64_t kept_end, int32_t* first_of, int32_t* last_of) {
+  Borders q = {0, 0, t0, t1, lo};
+  __syncwarp();
   for (int64_t base = lo; base < a.S; base += 32) {
     const int64_t s = base + lane_id();
     const int64_t b = s < a.S ? a.offsets[s] : a.N, e = s < a.S ? a.offsets[s + 1] : a.N;
     const bool some = e > b;
-    if (some && b >= t0 && b < t1) { q.first |= 1ull << (b - t0); first_of[b - t0] = (int)s; }
+    if (some && b >= t0 && b < t1) { q.first |= 1ull << (b - t0); first_of[b - t0] = e > kept_end ? ~(int)s : (int)s; }
     if (some && e > t0 && e <= t1) { q.last |= 1ull << (e - 1 - t0); last_of[e - 1 - t0] = (int)s; }
     const unsigned head = __ballot_sync(0xFFFFFFFFu, some && b <= t0 && e > t0), tail = __ballot_sync(0xFFFFFFFFu, some && b < t1 && e >= t1);
     if (head) q.head_begin = __shfl_sync(0xFFFFFFFFu, b, __ffs(head) - 1);
-    if (tail) q.tail_end = __shfl_sync(0xFFFFFFFFu, e, __ffs(tail) - 1);
+    if (tail) {
+      q.tail_end = __shfl_sync(0xFFFFFFFFu, e, __ffs(tail) - 1);
+      q.lo = (int)base + __ffs(tail) - 1;
+    }
     if (__any_sync(0xFFFFFFFFu, b >= t1)) break;
   }
 #pragma unroll
@@ -404,16 +460,16 @@ __device__ __forceinline__ ChunkSequences find_borders(const RecArgs& a, int lo,
   return q;
 }
 
-// Offsets in order, from 0 to N (each warp a share of them); `row(s)` for every empty sequence.
+// Offsets in order, from 0 to N; `row(s)` for every empty sequence.  Warp `number` of n takes an even share of the sequences.
 template <typename Fn>
-__device__ __forceinline__ void check_offsets(const RecArgs& a, Fn&& row) {
-  const int64_t warps = (int64_t)gridDim.x * REC_WARPS;
+__device__ __forceinline__ void check_offsets(const RecArgs& a, int64_t number, int64_t n, Fn&& row) {
+  const int64_t share = (a.S + n - 1) / n, end = min(a.S, (number + 1) * share);
   bool bad = false;
-  for (int64_t s0 = ((int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32) * 32; s0 < a.S; s0 += warps * 32) {
+  for (int64_t s0 = number * share; s0 < end; s0 += 32) {
     const int64_t s = s0 + lane_id();
-    const int64_t b = s < a.S ? a.offsets[s] : 0, e = s < a.S ? a.offsets[s + 1] : 1;
-    if (s < a.S) bad |= b < 0 || e < b || (s == 0 && b != 0) || (s == a.S - 1 && e != a.N);
-    unsigned empty = __ballot_sync(0xFFFFFFFFu, s < a.S && e <= b);
+    const int64_t b = s < end ? a.offsets[s] : 0, e = s < end ? a.offsets[s + 1] : 1;
+    if (s < end) bad |= b < 0 || e < b || (s == 0 && b != 0) || (s == a.S - 1 && e != a.N);
+    unsigned empty = __ballot_sync(0xFFFFFFFFu, s < end && e <= b);
     while (empty) {
       row(s0 + __ffs(empty) - 1);
       empty &= empty - 1;
@@ -422,125 +478,144 @@ __device__ __forceinline__ void check_offsets(const RecArgs& a, Fn&& row) {
   if (bad) atomicOr(a.status, (uint32_t)REC_STATUS_OFFSETS);
 }
 
-// What a warp works on: chunk (counted from the end where BACKWARD) and strip of channels.
-struct Item {
+// What a warp works on: the map or the walk of a chunk (counted from the end where BACKWARD) and a strip of channels.
+struct Piece {
+  bool walk;
   int index, chunk, strip;
-  int64_t t0, t1;
-  __device__ __forceinline__ Item(const RecArgs& a, int64_t item, bool backward) {
-    index = (int)(item / a.strips);
-    strip = (int)(item - (int64_t)index * a.strips);
+  int64_t t0, t1, number;      // number: of the walk, for the share of the offsets to check
+  __device__ __forceinline__ Piece(const RecArgs& a, bool backward) {
+    uint32_t t = 0;
+    if (lane_id() == 0) t = atomicAdd(a.ticket, 1u);
+    t = __shfl_sync(0xFFFFFFFFu, t, 0);
+    // the first maps; walks and maps in turn; the last walks
+    const int64_t n = (int64_t)a.chunks * a.strips, u = (int64_t)t - a.lag;
+    const bool mixed = u >= 0 && t < 2 * n - a.lag;
+    walk = u >= 0 && (!mixed || u % 2 == 0);
+    number = u < 0 ? t : mixed ? (walk ? u / 2 : a.lag + u / 2) : t - n;
+    index = (int)(number / a.strips);
+    strip = (int)(number - (int64_t)index * a.strips);
     chunk = backward ? a.chunks - 1 - index : index;
     t0 = (int64_t)chunk * a.chunk;
     t1 = min(t0 + a.chunk, a.N);
   }
 };
 
-// The rows of a batch of tokens, from row p on; rows that `live` does not name are not read and give 0.
+// A batch of rows of an [N, D] array: a base that all lanes share, a lane's channels from there as 32-bit offset of bytes, rows `step`
+// bytes apart (the host refuses strides of 2^28 bytes or more).  A lane behind the last channel reads the first ones.
 template <typename T, int V, bool VEC>
-__device__ __forceinline__ void load_rows(const T* p, int64_t stride, uint32_t live, int left, Raw<T, V> (&r)[REC_BATCH]) {
+struct Rows {
+  const char* base;
+  int64_t batch;               // bytes from one batch to the next
+  uint32_t lane, step;
+  int left;
+  __device__ __forceinline__ Rows(const void* p, int64_t stride, int64_t row, int c, int left_)
+      : base(static_cast<const char*>(p) + row * stride * (int64_t)sizeof(T)), batch(REC_BATCH * stride * (int64_t)sizeof(T)),
+        lane(left_ > 0 ? c * (uint32_t)sizeof(T) : 0u), step((uint32_t)stride * (uint32_t)sizeof(T)), left(left_) {}
+  __device__ __forceinline__ Raw<T, V> get(uint32_t offset) const {
+    const T* at = reinterpret_cast<const T*>(base + offset);
+    if (VEC) return load_raw<T, V>(at);
+    return get_raw<T, V, VEC>(at, left);
+  }
+  __device__ __forceinline__ void put(uint32_t offset, Channels<V> v) const {
+    mts::put<V, VEC>(reinterpret_cast<T*>(const_cast<char*>(base) + offset), left, v);
+  }
+  __device__ __forceinline__ void next() { base += batch; }
+  __device__ __forceinline__ void previous() { base -= batch; }
+  // Rows that `live` does not name are not read and give 0.
+  __device__ __forceinline__ void load(uint32_t live, Raw<T, V> (&r)[REC_BATCH]) const {
+    uint32_t at = lane;
 #pragma unroll
-  for (int i = 0; i < REC_BATCH; ++i, p += stride) r[i] = (live >> i & 1) ? get_raw<T, V, VEC>(p, left) : Raw<T, V>{};
-}
-template <typename T, int V, bool VEC>
-__device__ __forceinline__ void load_rows(const T* p, int64_t stride, int left, Raw<T, V> (&r)[REC_BATCH]) {
-#pragma unroll
-  for (int i = 0; i < REC_BATCH; ++i, p += stride) r[i] = get_raw<T, V, VEC>(p, left);
-}
-
-__device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int64_t rel) { return (uint32_t)(mask >> rel) & ((1u << REC_BATCH) - 1); }
+    for (int i = 0; i < REC_BATCH; ++i, at += step) r[i] = (live >> i & 1) ? get(at) : Raw<T, V>{};
+  }
+};
 constexpr uint32_t ALL_LIVE = (1u << REC_BATCH) - 1;
+__device__ __forceinline__ uint32_t live_bits(int tokens) { return tokens >= REC_BATCH ? ALL_LIVE : tokens > 0 ? (1u << tokens) - 1 : 0u; }
+__device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel) { return (uint32_t)(mask >> (rel % REC_PART)) & ALL_LIVE; }
+
+// In all four walks a row's registers take the row one batch ahead as soon as they have been read: a batch is always on its way.
 
 // ------------------------------------------------------------------------------- forward
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(REC_WARPS * 32)
-recurrence_forward_maps(const RecArgs a) {
-  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
-  int32_t* first_of = borders[threadIdx.x / 32][0];
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-  const int64_t item = (int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32;
-  if (item >= (int64_t)a.chunks * a.strips) return;
-  const Item it(a, item, false);
+__device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
-  const int lo = find_sequence(a, it.t0);
-  if (it.strip == 0 && lane_id() == 0) a.sequence[it.chunk] = lo;
-  const ChunkSequences q = find_borders(a, lo, it.t0, it.t1, first_of, borders[threadIdx.x / 32][1]);
-  Map<V> m = {all<V>(CUT), all<V>(0.f)};
-  if (q.tail_end > it.t1) {                                             // a whole chunk: the sequence goes on
-    int start = 0;
-    if (q.first) {
-      start = 63 - __clzll(q.first);
-      if (a.h0) m.B = get<V, VEC>(a.h0 + (int64_t)first_of[start] * a.D + c, left);
-      put<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left, m.B);
-    } else {
-      m.P = all<V>(1.f);
+  const int s = find_sequence(a, it.t1 - 1);
+  const int64_t begin = a.offsets[s], end = min(a.offsets[s + 1], a.N);
+  const bool goes_on = end > it.t1, cut = !goes_on || (begin >= it.t0 && begin < it.t1);
+  Map<V> m = {all<V>(1.f), all<V>(0.f)};
+  if (goes_on) {                                                    // a whole chunk: the sequence goes on
+    const int start = cut ? (int)(begin - it.t0) : 0;
+    Channels<V> from = all<V>(0.f);
+    if (cut) {
+      if (a.h0) from = get<V, VEC>(a.h0 + (int64_t)s * a.D + c, left);
+      put<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left, from);
     }
+    int rel = start & ~(REC_BATCH - 1);
+    Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), value(a.value, a.value_stride, it.t0 + rel, c, left);
     Raw<T, V> g[REC_BATCH], x[REC_BATCH];
+    gate.load(ALL_LIVE, g);
+    value.load(ALL_LIVE, x);
 #pragma unroll 1
-    for (int rel = start & ~(REC_BATCH - 1); rel < a.chunk; rel += REC_BATCH) {
-      load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + (it.t0 + rel) * a.gate_stride + c, a.gate_stride, left, g);
-      load_rows<T, V, VEC>(static_cast<const T*>(a.value) + (it.t0 + rel) * a.value_stride + c, a.value_stride, left, x);
-      const Channels<V> before = m.B;
+    for (; rel < a.chunk; rel += REC_BATCH) {
+      if (rel + REC_BATCH < a.chunk) {                                  // else the last batch once more, unused
+        gate.next();
+        value.next();
+      }
+      uint32_t ga = gate.lane, xa = value.lane;
 #pragma unroll
-      for (int i = 0; i < REC_BATCH; ++i) {
-        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i]));
-        if (rel + i == start) m.B = before;
-        m.B = blend(nz, unpack<T, V, true>(x[i]), m.B);
+      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step) {
+        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
+        g[i] = gate.get(ga);
+        x[i] = value.get(xa);
+        if (rel + i == start) m.B = from;
+        m.B = blend(nz, nx, m.B);
         m.P = fma(nz, m.P, m.P);
       }
     }
-    if (q.first) m.P = all<V>(CUT);
   }
-  put<V, VEC>(a.chunk_P + (int64_t)it.chunk * a.D + c, left, m.P);
-  put<V, VEC>(a.chunk_B + (int64_t)it.chunk * a.D + c, left, m.B);
-  complete<V, VEC>(a, it.index, it.strip, c);
+  publish<V, VEC>(a, it.index, it.strip, c, m, cut);
 }
 
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(REC_WARPS * 32)
-recurrence_forward_walk(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
-  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
-  int32_t* first_of = borders[threadIdx.x / 32][0];
-  int32_t* last_of = borders[threadIdx.x / 32][1];
-  if (h_final) {
-    check_offsets(a, [&](int64_t s) {
+__global__ void __launch_bounds__(32, MTS_REC_FWD_BLOCKS)
+recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
+  __shared__ int32_t first_of[REC_PART], last_of[REC_PART];
+  const Piece it(a, false);
+  if (!it.walk && a.chunks > 0) return forward_map<T, V, VEC>(a, it);
+  const auto empty_row = [&](int64_t s) {
+    if (h_final)
       for (int d = lane_id(); d < a.D; d += 32) h_final[s * a.D + d] = a.h0 ? a.h0[s * a.D + d] : 0.f;
-    });
-  } else {
-    check_offsets(a, [](int64_t) {});
-  }
-  const int64_t item = (int64_t)(gridDim.x - 1 - blockIdx.x) * REC_WARPS + threadIdx.x / 32;     // from the end: see above
-  if (item >= (int64_t)a.chunks * a.strips) return;
-  const Item it(a, item, false);
-  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
-  const ChunkSequences q = find_borders(a, a.sequence[it.chunk], it.t0, it.t1, first_of, last_of);
-  // the start of a sequence that goes on behind the chunk was kept by the first pass: h_final may be the same array as h0, and the
-  // warp that writes it does not wait for this one
-  const int kept = q.first && q.tail_end > it.t1 ? 63 - __clzll(q.first) : -1;
+  };
+  if (a.chunks == 0) return check_offsets(a, blockIdx.x, gridDim.x, empty_row);
+  const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
+  Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0, c, left), value(a.value, a.value_stride, it.t0, c, left), to(out, out_stride, it.t0, c, left);
+  Raw<T, V> g[REC_BATCH], x[REC_BATCH];
+  gate.load(live_bits(tokens), g);
+  value.load(live_bits(tokens), x);
+  check_offsets(a, it.number, (int64_t)a.chunks * a.strips, empty_row);
+  Borders q = {0, 0, 0, 0, find_sequence(a, it.t0)};
   Channels<V> h = all<V>(0.f);
-  if (!(q.first & 1)) h = state_before<V, VEC>(a, it.index, (int)(q.head_begin / a.chunk), c);
-  const T* gate = static_cast<const T*>(a.gate) + it.t0 * a.gate_stride + c;
-  const T* value = static_cast<const T*>(a.value) + it.t0 * a.value_stride + c;
-  T* to = out + it.t0 * out_stride + c;
-  const int tokens = (int)(it.t1 - it.t0);
 #pragma unroll 1
-  for (int rel = 0; rel < tokens; rel += REC_BATCH, gate += REC_BATCH * a.gate_stride, value += REC_BATCH * a.value_stride, to += REC_BATCH * out_stride) {
-    const uint32_t live = tokens - rel >= REC_BATCH ? ALL_LIVE : (1u << (tokens - rel)) - 1;
-    const uint32_t firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
+  for (int rel = 0; rel < tokens; rel += REC_BATCH) {
+    if (rel % REC_PART == 0) {
+      q = find_borders(a, q.lo, it.t0 + rel, min(it.t0 + rel + REC_PART, it.t1), it.t1, first_of, last_of);
+      if (rel == 0) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c, !(q.first & 1), true);
+    }
+    gate.next();
+    value.next();
+    const uint32_t live = live_bits(tokens - rel), firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
     if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
-    Raw<T, V> g[REC_BATCH], x[REC_BATCH];
-    if (live == ALL_LIVE && !(firsts | lasts)) {
-      load_rows<T, V, VEC>(gate, a.gate_stride, left, g);
-      load_rows<T, V, VEC>(value, a.value_stride, left, x);
-      T* row = to;
+    uint32_t ta = to.lane;
+    if (!(firsts | lasts) && tokens - rel >= 2 * REC_BATCH) {
+      uint32_t ga = gate.lane, xa = value.lane;
 #pragma unroll
-      for (int i = 0; i < REC_BATCH; ++i, row += out_stride) {
-        h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
-        put<V, VEC>(row, left, h);
+      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step, ta += to.step) {
+        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
+        g[i] = gate.get(ga);
+        x[i] = value.get(xa);
+        h = blend(nz, nx, h);
+        to.put(ta, h);
       }
     } else {
-      load_rows<T, V, VEC>(gate, a.gate_stride, live, left, g);
-      load_rows<T, V, VEC>(value, a.value_stride, live, left, x);
-      T* row = to;
 #pragma unroll
       for (int i0 = 0; i0 < REC_BATCH; i0 += 4) {
         Channels<V> s[4];
@@ -548,21 +623,27 @@ recurrence_forward_walk(const RecArgs a, T* __restrict__ out, int64_t out_stride
         for (int i = i0; i < i0 + 4; ++i) {
           s[i - i0] = all<V>(0.f);
           if (firsts >> i & 1) {
-            if (rel + i == kept) s[i - i0] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
-            else if (a.h0) s[i - i0] = get<V, VEC>(a.h0 + (int64_t)first_of[rel + i] * a.D + c, left);
+            // the start of a sequence that goes on behind the chunk was kept by the first pass: h_final may be the same array as
+            // h0, and the warp that writes it does not wait for this one
+            const int f = first_of[rel % REC_PART + i];
+            if (f < 0) s[i - i0] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
+            else if (a.h0) s[i - i0] = get<V, VEC>(a.h0 + (int64_t)f * a.D + c, left);
           }
         }
 #pragma unroll
-        for (int i = i0; i < i0 + 4; ++i, row += out_stride) {
+        for (int i = i0; i < i0 + 4; ++i, ta += to.step) {
           if (live >> i & 1) {
             if (firsts >> i & 1) h = s[i - i0];
             h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
-            put<V, VEC>(row, left, h);
-            if ((lasts >> i & 1) && h_final) put<V, VEC>(h_final + (int64_t)last_of[rel + i] * a.D + c, left, h);
+            to.put(ta, h);
+            if ((lasts >> i & 1) && h_final) put<V, VEC>(h_final + (int64_t)last_of[rel % REC_PART + i] * a.D + c, left, h);
           }
         }
       }
+      gate.load(live_bits(tokens - rel - REC_BATCH), g);
+      value.load(live_bits(tokens - rel - REC_BATCH), x);
     }
+    to.next();
   }
 }
 
@@ -570,106 +651,140 @@ recurrence_forward_walk(const RecArgs a, T* __restrict__ out, int64_t out_stride
 // What a token hands to the one before it, c_t = (1 - z_t) G_t = (1 - z_t) (grad_out_t + c_{t+1}), is the same kind of map, walked from
 // the last chunk to the first; its cut is a sequence's last token, which starts from grad_final.
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(REC_WARPS * 32)
-recurrence_backward_maps(const RecArgs a, const T* __restrict__ grad_out, int64_t grad_out_stride, const float* __restrict__ grad_final) {
-  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
-  int32_t* last_of = borders[threadIdx.x / 32][1];
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0;
-  const int64_t item = (int64_t)blockIdx.x * REC_WARPS + threadIdx.x / 32;
-  if (item >= (int64_t)a.chunks * a.strips) return;
-  const Item it(a, item, true);
+__device__ __forceinline__ void backward_map(const RecArgs& a, const Piece& it, const T* grad_out, int64_t grad_out_stride, const float* grad_final) {
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
-  const int lo = find_sequence(a, it.t0);
-  if (it.strip == 0 && lane_id() == 0) a.sequence[it.chunk] = lo;
-  const ChunkSequences q = find_borders(a, lo, it.t0, it.t1, borders[threadIdx.x / 32][0], last_of);
-  Map<V> m = {all<V>(CUT), all<V>(0.f)};
-  if (q.head_begin < it.t0) {
-    int end = (int)(it.t1 - it.t0) - 1;
-    if (q.last) {
-      end = __ffsll(q.last) - 1;
-      if (grad_final) m.B = get<V, VEC>(grad_final + (int64_t)last_of[end] * a.D + c, left);
-    } else {
-      m.P = all<V>(1.f);
-    }
+  const int s = find_sequence(a, it.t0);
+  const int64_t begin = a.offsets[s], end = a.offsets[s + 1];
+  const bool goes_on = begin < it.t0, cut = !goes_on || (end > it.t0 && end <= it.t1);
+  Map<V> m = {all<V>(1.f), all<V>(0.f)};
+  if (goes_on) {
+    const int tokens = (int)((cut ? end : it.t1) - it.t0);
+    if (cut && grad_final) m.B = get<V, VEC>(grad_final + (int64_t)s * a.D + c, left);
+    int rel = (tokens - 1) & ~(REC_BATCH - 1);
+    Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), grad(grad_out, grad_out_stride, it.t0 + rel, c, left);
     Raw<T, V> g[REC_BATCH], d[REC_BATCH];
+    gate.load(live_bits(tokens - rel), g);
+    grad.load(live_bits(tokens - rel), d);
 #pragma unroll 1
-    for (int rel = end & ~(REC_BATCH - 1); rel >= 0; rel -= REC_BATCH) {
-      const uint32_t live = end - rel >= REC_BATCH - 1 ? ALL_LIVE : (1u << (end - rel + 1)) - 1;
-      load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + (it.t0 + rel) * a.gate_stride + c, a.gate_stride, live, left, g);
-      load_rows<T, V, VEC>(grad_out + (it.t0 + rel) * grad_out_stride + c, grad_out_stride, live, left, d);
+    for (; rel >= 0; rel -= REC_BATCH) {
+      const int here = tokens - rel;
+      if (rel > 0) {
+        gate.previous();
+        grad.previous();
+      }
+      uint32_t ga = gate.lane + (REC_BATCH - 1) * gate.step, da = grad.lane + (REC_BATCH - 1) * grad.step;
 #pragma unroll
-      for (int i = REC_BATCH - 1; i >= 0; --i) {
-        if (live >> i & 1) {
-          const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), G = unpack<T, V>(d[i]) + m.B;
+      for (int i = REC_BATCH - 1; i >= 0; --i, ga -= gate.step, da -= grad.step) {
+        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), dv = unpack<T, V>(d[i]);
+        if (rel > 0) {
+          g[i] = gate.get(ga);
+          d[i] = grad.get(da);
+        }
+        if (i < here) {
+          const Channels<V> G = dv + m.B;
           m.B = fma(nz, G, G);
           m.P = fma(nz, m.P, m.P);
         }
       }
     }
-    if (q.last) m.P = all<V>(CUT);
   }
-  put<V, VEC>(a.chunk_P + (int64_t)it.index * a.D + c, left, m.P);
-  put<V, VEC>(a.chunk_B + (int64_t)it.index * a.D + c, left, m.B);
-  complete<V, VEC>(a, it.index, it.strip, c);
+  publish<V, VEC>(a, it.index, it.strip, c, m, cut);
 }
 
 // A batch is walked forward from the state that the forward left before it, for -z and the distance from value to state, then backward.
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(REC_WARPS * 32)
-recurrence_backward_walk(const RecArgs a, const float* __restrict__ entry, const T* __restrict__ grad_out, int64_t grad_out_stride,
-                         const float* __restrict__ grad_final, T* __restrict__ grad_gate, int64_t grad_gate_stride,
-                         T* __restrict__ grad_value, int64_t grad_value_stride, float* __restrict__ grad_h0) {
-  __shared__ int32_t borders[REC_WARPS][2][REC_CHUNK];
-  int32_t* first_of = borders[threadIdx.x / 32][0];
-  int32_t* last_of = borders[threadIdx.x / 32][1];
-  if (grad_h0) {
-    check_offsets(a, [&](int64_t s) {
+__global__ void __launch_bounds__(32, MTS_REC_BWD_BLOCKS)
+recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, const T* __restrict__ grad_out, int64_t grad_out_stride,
+                           const float* __restrict__ grad_final, T* __restrict__ grad_gate, int64_t grad_gate_stride,
+                           T* __restrict__ grad_value, int64_t grad_value_stride, float* __restrict__ grad_h0) {
+  __shared__ int32_t first_of[REC_PART], last_of[REC_PART];
+  const Piece it(a, true);
+  if (!it.walk && a.chunks > 0) return backward_map<T, V, VEC>(a, it, grad_out, grad_out_stride, grad_final);
+  const auto empty_row = [&](int64_t s) {
+    if (grad_h0)
       for (int d = lane_id(); d < a.D; d += 32) grad_h0[s * a.D + d] = grad_final ? grad_final[s * a.D + d] : 0.f;
-    });
-  } else {
-    check_offsets(a, [](int64_t) {});
-  }
-  const int64_t item = (int64_t)(gridDim.x - 1 - blockIdx.x) * REC_WARPS + threadIdx.x / 32;
-  if (item >= (int64_t)a.chunks * a.strips) return;
-  const Item it(a, item, true);
+  };
+  if (a.chunks == 0) return check_offsets(a, blockIdx.x, gridDim.x, empty_row);
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
-  const ChunkSequences q = find_borders(a, a.sequence[it.chunk], it.t0, it.t1, first_of, last_of);
+  int rel = (tokens - 1) & ~(REC_BATCH - 1);
+  Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), value(a.value, a.value_stride, it.t0 + rel, c, left),
+      grad(grad_out, grad_out_stride, it.t0 + rel, c, left), to_gate(grad_gate, grad_gate_stride, it.t0 + rel, c, left),
+      to_value(grad_value, grad_value_stride, it.t0 + rel, c, left);
+  Raw<T, V> g[REC_BATCH], x[REC_BATCH], d[REC_BATCH];
+  gate.load(live_bits(tokens - rel), g);
+  value.load(live_bits(tokens - rel), x);
+  grad.load(live_bits(tokens - rel), d);
+  // the parts from the last: each one's first sequence is found anew, from that of the chunk's first token on
+  check_offsets(a, it.number, (int64_t)a.chunks * a.strips, empty_row);
+  const int lo = find_sequence(a, it.t0);
+  Borders q = {0, 0, 0, 0, lo};
   Channels<V> carry = all<V>(0.f);
-  if (!(q.last >> (tokens - 1) & 1))
-    carry = state_before<V, VEC>(a, it.index, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c);
 #pragma unroll 1
-  for (int rel = (tokens - 1) & ~(REC_BATCH - 1); rel >= 0; rel -= REC_BATCH) {
+  for (bool start = true; rel >= 0; rel -= REC_BATCH, start = false) {
+    if (start || rel % REC_PART == REC_PART - REC_BATCH) {
+      const int64_t p0 = it.t0 + rel / REC_PART * REC_PART;
+      q = find_borders(a, lo, p0, min(p0 + REC_PART, it.t1), INT64_MAX, first_of, last_of);
+      if (start)
+        carry = state_before<V, VEC>(a, it.index, it.strip, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c,
+                                     !(q.last >> ((tokens - 1) % REC_PART) & 1), false);
+    }
     const int64_t t = it.t0 + rel;
-    const uint32_t live = tokens - rel >= REC_BATCH ? ALL_LIVE : (1u << (tokens - rel)) - 1;
-    const uint32_t firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
-    Raw<T, V> g[REC_BATCH], x[REC_BATCH], d[REC_BATCH];
-    load_rows<T, V, VEC>(static_cast<const T*>(a.gate) + t * a.gate_stride + c, a.gate_stride, live, left, g);
-    load_rows<T, V, VEC>(static_cast<const T*>(a.value) + t * a.value_stride + c, a.value_stride, live, left, x);
-    load_rows<T, V, VEC>(grad_out + t * grad_out_stride + c, grad_out_stride, live, left, d);
-    Channels<V> h = all<V>(0.f);
+    const uint32_t live = live_bits(tokens - rel), firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
+    if (rel > 0) {
+      gate.previous();
+      value.previous();
+      grad.previous();
+    }
+    Channels<V> h = all<V>(0.f), nz[REC_BATCH], away[REC_BATCH];        // away: - (value - state before the token)
     if (!(firsts & 1)) h = get<V, VEC>(entry + t / REC_BATCH * a.D + c, left);
-    Channels<V> nz[REC_BATCH], away[REC_BATCH];                         // away: - (value - state before the token)
+    const uint32_t last_row = REC_BATCH - 1;
+    uint32_t va = to_value.lane + last_row * to_value.step, za = to_gate.lane + last_row * to_gate.step;
+    if (!(firsts | lasts) && live == ALL_LIVE && rel > 0) {
+      uint32_t ga = gate.lane, xa = value.lane, da = grad.lane + last_row * grad.step;
 #pragma unroll
-    for (int i = 0; i < REC_BATCH; ++i) {
-      if (firsts >> i & 1) h = a.h0 ? get<V, VEC>(a.h0 + (int64_t)first_of[rel + i] * a.D + c, left) : all<V>(0.f);
-      const Channels<V> nx = unpack<T, V, true>(x[i]);
-      nz[i] = minus_sigmoid(unpack<T, V>(g[i]));
-      away[i] = nx + h;
-      h = blend(nz[i], nx, h);
-    }
-    T* to_gate = grad_gate + t * grad_gate_stride + c;
-    T* to_value = grad_value + t * grad_value_stride + c;
-#pragma unroll
-    for (int i = REC_BATCH - 1; i >= 0; --i) {
-      if (live >> i & 1) {
-        if (lasts >> i & 1) carry = grad_final ? get<V, VEC>(grad_final + (int64_t)last_of[rel + i] * a.D + c, left) : all<V>(0.f);
-        const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;          // -z G
-        carry = fma(nz[i], G, G);
-        put<V, VEC>(to_value + i * grad_value_stride, left, nG * all<V>(-1.f));
-        put<V, VEC>(to_gate + i * grad_gate_stride, left, nG * fma(nz[i], away[i], away[i]));
-        if ((firsts >> i & 1) && grad_h0) put<V, VEC>(grad_h0 + (int64_t)first_of[rel + i] * a.D + c, left, carry);
+      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step) {
+        const Channels<V> nx = unpack<T, V, true>(x[i]);
+        nz[i] = minus_sigmoid(unpack<T, V>(g[i]));
+        g[i] = gate.get(ga);
+        x[i] = value.get(xa);
+        away[i] = nx + h;
+        h = blend(nz[i], nx, h);
       }
+#pragma unroll
+      for (int i = REC_BATCH - 1; i >= 0; --i, da -= grad.step, va -= to_value.step, za -= to_gate.step) {
+        const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;          // -z G
+        d[i] = grad.get(da);
+        carry = fma(nz[i], G, G);
+        to_value.put(va, nG * all<V>(-1.f));
+        to_gate.put(za, nG * fma(nz[i], away[i], away[i]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < REC_BATCH; ++i) {
+        if (firsts >> i & 1) h = a.h0 ? get<V, VEC>(a.h0 + (int64_t)first_of[rel % REC_PART + i] * a.D + c, left) : all<V>(0.f);
+        const Channels<V> nx = unpack<T, V, true>(x[i]);
+        nz[i] = minus_sigmoid(unpack<T, V>(g[i]));
+        away[i] = nx + h;
+        h = blend(nz[i], nx, h);
+      }
+#pragma unroll
+      for (int i = REC_BATCH - 1; i >= 0; --i, va -= to_value.step, za -= to_gate.step) {
+        if (live >> i & 1) {
+          if (lasts >> i & 1) carry = grad_final ? get<V, VEC>(grad_final + (int64_t)last_of[rel % REC_PART + i] * a.D + c, left) : all<V>(0.f);
+          const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;
+          carry = fma(nz[i], G, G);
+          to_value.put(va, nG * all<V>(-1.f));
+          to_gate.put(za, nG * fma(nz[i], away[i], away[i]));
+          if ((firsts >> i & 1) && grad_h0) put<V, VEC>(grad_h0 + (int64_t)first_of[rel % REC_PART + i] * a.D + c, left, carry);
+        }
+      }
+      const uint32_t next = rel > 0 ? ALL_LIVE : 0u;
+      gate.load(next, g);
+      value.load(next, x);
+      grad.load(next, d);
     }
+    to_gate.previous();
+    to_value.previous();
   }
 }
 
@@ -683,7 +798,7 @@ int check_sizes(const char* what, int64_t N, int64_t S, int32_t D, int32_t dtype
   if (N < 0 || S < 0 || D < 1 || !known_dtype(dtype))
     return set_error(MTS_ERR_INVALID_ARG, "%s: N %lld, S %lld, D %d, dtype %d", what, (long long)N, (long long)S, D, dtype);
   if (N >= (1ll << 31) - (1 << 16) || S >= (1ll << 31) - (1 << 16) || D > (1 << 20) ||
-      ceil_div(N, REC_BATCH) * ceil_div(D, 32) >= (1ll << 31))
+      ceil_div(N, 2 * REC_BATCH) * ceil_div(D, 32) >= (1ll << 30))
     return set_error(MTS_ERR_UNSUPPORTED, "%s: N %lld, S %lld, D %d", what, (long long)N, (long long)S, D);
   if (S == 0 && N > 0) return set_error(MTS_ERR_INVALID_ARG, "%s: %lld tokens in no sequence", what, (long long)N);
   return MTS_OK;
@@ -698,6 +813,7 @@ int check_workspace(const char* what, const void* workspace, size_t have, size_t
 // An [N, D] argument: present when there are tokens, rows that do not overlap, elements on their own boundary.
 int check_rows(const char* what, const char* name, const void* p, int64_t stride, int64_t N, int32_t D, int32_t dtype) {
   if (N == 0) return MTS_OK;
+  if (stride >= (1ll << 28) / dtype_bytes(dtype)) return set_error(MTS_ERR_UNSUPPORTED, "%s: %s has rows %lld elements apart", what, name, (long long)stride);
   if (!p || stride < D) return set_error(MTS_ERR_INVALID_ARG, "%s: %s is null or its rows overlap (stride %lld, D %d)", what, name, (long long)stride, D);
   if ((uintptr_t)p % dtype_bytes(dtype)) return set_error(MTS_ERR_ALIGNMENT, "%s: %s is no multiple of its element size", what, name);
   return MTS_OK;
@@ -715,7 +831,7 @@ struct Alignment {
   void state(const void* p) { states |= (uintptr_t)p; }
 };
 
-// Tokens of a chunk: 64, fewer where that would leave most of the GPU without a warp (a strip is 256 bytes of a row).
+// Tokens of a chunk: 256, fewer where that would leave most of the GPU without a warp (a strip is 256 bytes of a row).
 int chunk_tokens(int64_t N, int32_t D, int32_t dtype) {
   const int64_t strips = ceil_div((int64_t)D * dtype_bytes(dtype), 256);
   int chunk = REC_CHUNK;
@@ -723,17 +839,19 @@ int chunk_tokens(int64_t N, int32_t D, int32_t dtype) {
   return chunk;
 }
 
-// Parts of the workspace, in bytes: status | counters | maps.  Strips of 32 channels are the narrowest.
+// Parts of the workspace, in bytes: status and ticket | flags and counts | maps.  Strips of 32 channels are the narrowest.
 struct Workspace {
   int chunk;
-  int64_t chunks, groups, spans, counters, total;
+  int64_t n[REC_LEVELS + 1], counters, total;
   Workspace(int64_t N, int32_t D, int32_t dtype) {
     chunk = chunk_tokens(N, D, dtype);
-    chunks = ceil_div(N, chunk);
-    groups = ceil_div(chunks, REC_RADIX);
-    spans = ceil_div(groups, REC_RADIX);
-    counters = (int64_t)align_up(256 + 4 * (size_t)(groups + spans + 1) * (size_t)ceil_div(D, 32), 256);
-    total = counters + (int64_t)align_up(4 * (size_t)chunks, 256) + 4 * (3 * chunks + 2 * groups + 3 * spans) * (int64_t)align_up(D, 4);
+    n[0] = ceil_div(N, chunk);
+    for (int l = 1; l < REC_LEVELS; ++l) n[l] = ceil_div(n[l - 1], REC_RADIX);
+    n[REC_LEVELS] = n[REC_LEVELS - 1] + 1;
+    int64_t all = 0;
+    for (int l = 0; l <= REC_LEVELS; ++l) all += n[l];
+    counters = (int64_t)align_up(256 + 8 * (size_t)all * (size_t)ceil_div(D, 32), 256);
+    total = counters + 4 * (n[0] + 2 * all) * (int64_t)align_up(D, 4);
   }
 };
 
@@ -742,33 +860,33 @@ RecArgs arguments(const void* gate, int64_t gate_stride, const void* value, int6
   RecArgs a = {gate, gate_stride, value, value_stride, offsets, h0, N, S, D};
   const Workspace w(N, D, dtype);
   a.chunk = w.chunk;
-  a.chunks = (int32_t)w.chunks;
+  a.chunks = (int32_t)w.n[0];
   a.strips = (int32_t)ceil_div(D, 32 * vec);
-  a.groups = (int32_t)w.groups;
-  a.spans = (int32_t)w.spans;
+  const int64_t pieces = w.n[0] * a.strips;
+  a.lag = (int32_t)(pieces < MTS_REC_LAG ? pieces : MTS_REC_LAG);
   char* p = static_cast<char*>(workspace);
   a.status = reinterpret_cast<uint32_t*>(p);
-  a.group_count = reinterpret_cast<uint32_t*>(p + 256);
-  a.span_count = a.group_count + w.groups * a.strips;
-  a.total_count = a.span_count + w.spans * a.strips;
-  a.sequence = reinterpret_cast<int32_t*>(p + w.counters);
-  a.chunk_P = reinterpret_cast<float*>(p + w.counters + align_up(4 * (size_t)w.chunks, 256));
-  a.chunk_B = a.chunk_P + w.chunks * D;
-  a.chunk_start = a.chunk_B + w.chunks * D;
-  a.group_P = a.chunk_start + w.chunks * D;
-  a.group_B = a.group_P + w.groups * D;
-  a.span_P = a.group_B + w.groups * D;
-  a.span_B = a.span_P + w.spans * D;
-  a.span_state = a.span_B + w.spans * D;
+  a.ticket = a.status + 1;
+  uint32_t* flags = reinterpret_cast<uint32_t*>(p + 256);
+  a.chunk_start = reinterpret_cast<float*>(p + w.counters);
+  float* maps = a.chunk_start + w.n[0] * D;
+  for (int l = 0; l <= REC_LEVELS; ++l) {
+    a.level[l].ready = flags;
+    a.level[l].done = flags + w.n[l] * a.strips;
+    flags += 2 * w.n[l] * a.strips;
+    a.level[l].P = maps;
+    a.level[l].B = maps + w.n[l] * D;
+    maps += 2 * w.n[l] * D;
+  }
   return a;
 }
 
-// One warp per chunk and strip, at least one for the check of the offsets.
+// A warp for every piece of work, at least one for the check of the offsets.
 template <typename Kernel, typename... Args>
-int launch_pass(const char* what, int trace_id, Kernel kernel, const RecArgs& a, cudaStream_t s, Args... args) {
-  const int64_t blocks = ceil_div((int64_t)a.chunks * a.strips, REC_WARPS);
+int launch_pieces(const char* what, int trace_id, Kernel kernel, const RecArgs& a, cudaStream_t s, Args... args) {
+  const int64_t warps = 2 * (int64_t)a.chunks * a.strips;
   LaunchScope scope(trace_id, s);
-  kernel<<<(unsigned)(blocks < 1 ? 1 : blocks), REC_WARPS * 32, 0, s>>>(a, args...);
+  kernel<<<(unsigned)(warps < 1 ? 1 : warps), 32, 0, s>>>(a, args...);
   return check_launch(what);
 }
 
@@ -811,7 +929,7 @@ extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, con
   if (rc != MTS_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Workspace w(N, D, dtype);
-  if (w.groups > 1 || S == 0) rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
+  rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
   if (rc != MTS_OK || S == 0) return rc;
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
@@ -826,9 +944,8 @@ extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, con
       constexpr int V = decltype(v)::value;
       constexpr bool VEC = decltype(q)::value;
       const RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, dtype, V, workspace);
-      const int e = launch_pass(what, K_RECURRENCE_FWD, recurrence_forward_maps<T, V, VEC>, a, s);
-      return e != MTS_OK ? e : launch_pass(what, K_RECURRENCE_FWD, recurrence_forward_walk<T, V, VEC>, a, s, static_cast<T*>(out), out_stride,
-                                           h_final, entry_states);
+      return launch_pieces(what, K_RECURRENCE_FWD, recurrence_forward_kernel<T, V, VEC>, a, s, static_cast<T*>(out), out_stride, h_final,
+                           entry_states);
     });
   });
 }
@@ -855,7 +972,7 @@ extern "C" int mts_recurrence_backward(const void* gate, int64_t gate_stride, co
   if (rc != MTS_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Workspace w(N, D, dtype);
-  if (w.groups > 1 || S == 0) rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
+  rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
   if (rc != MTS_OK || S == 0) return rc;
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
@@ -873,11 +990,9 @@ extern "C" int mts_recurrence_backward(const void* gate, int64_t gate_stride, co
       constexpr int V = decltype(v)::value;
       constexpr bool VEC = decltype(q)::value;
       const RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, dtype, V, workspace);
-      const int e = launch_pass(what, K_RECURRENCE_BWD, recurrence_backward_maps<T, V, VEC>, a, s, static_cast<const T*>(grad_out),
-                                grad_out_stride, grad_final);
-      return e != MTS_OK ? e : launch_pass(what, K_RECURRENCE_BWD, recurrence_backward_walk<T, V, VEC>, a, s, entry_states,
-                                           static_cast<const T*>(grad_out), grad_out_stride, grad_final, static_cast<T*>(grad_gate),
-                                           grad_gate_stride, static_cast<T*>(grad_value), grad_value_stride, grad_h0);
+      return launch_pieces(what, K_RECURRENCE_BWD, recurrence_backward_kernel<T, V, VEC>, a, s, entry_states, static_cast<const T*>(grad_out),
+                           grad_out_stride, grad_final, static_cast<T*>(grad_gate), grad_gate_stride, static_cast<T*>(grad_value),
+                           grad_value_stride, grad_h0);
     });
   });
 }
@@ -889,5 +1004,7 @@ extern "C" int mts_recurrence_status(const void* workspace, int32_t* host_status
   int rc = check_cuda(cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, s), "cudaMemcpyAsync(status)");
   if (rc == MTS_OK) rc = check_cuda(cudaStreamSynchronize(s), "cudaStreamSynchronize(status)");
   *host_status = rc == MTS_OK ? (int32_t)word : 0;
+  if (rc == MTS_OK && (*host_status & REC_STATUS_TIMEOUT))
+    rc = set_error(MTS_ERR_TIMEOUT, "recurrence: a bounded wait ran out, the results of the last call are incomplete");
   return rc;
 }
