@@ -35,7 +35,7 @@ namespace mts {
 #define MTS_REC_WARPS_WANTED 1776
 #endif
 #ifndef MTS_REC_LAG
-#define MTS_REC_LAG 1024
+#define MTS_REC_LAG 2048
 #endif
 #ifndef MTS_REC_MAX_CHUNK
 #define MTS_REC_MAX_CHUNK 128

@@ -3,7 +3,9 @@
 //   out[h, i, j] = table[bucket(j - i - q_offset), h]
 //   grad_table[k, h] = sum over b and the (i, j) of bucket k of grad_out[b, h, i, j]
 //
-// The bucket depends on the diagonal alone.
+// The bucket depends on the diagonal j - i alone.  Forward: a head's matrix is one vector of Lq + Lk - 1 values of which every row
+// shows a window; what bounds it is writing the rows.  Gradient: the sum of each diagonal first, then of the diagonals of a
+// bucket; what bounds it is reading the gradient.
 #include <math.h>
 
 #include "dense.cuh"
@@ -37,75 +39,218 @@ struct BiasGeometry {
   int32_t heads, Lq, Lk, q_offset;
 };
 
-// One element per thread and step.
+__device__ __forceinline__ float bias_value(const Buckets& b, const BiasGeometry& g, const void* table, int table_dtype, int h, int r) {
+  return b.causal && r > 0 ? -INFINITY : table_value(table, table_dtype, (int64_t)bucket_row(b, r) * g.heads + h);
+}
+
+// Few queries: one element per thread and step.
 template <typename T>
 __global__ void __launch_bounds__(256)
-relpos_forward_direct(Buckets b, BiasGeometry g, const void* __restrict__ table, int table_dtype, T* __restrict__ out,
+relpos_forward_direct(const __grid_constant__ Buckets b, BiasGeometry g, const void* __restrict__ table, int table_dtype, T* __restrict__ out,
                       int64_t head_stride, int64_t row_stride) {
   const int h = blockIdx.z;
-  for (int i = blockIdx.y; i < g.Lq; i += gridDim.y) {
-    for (int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; j < g.Lk; j += (int64_t)gridDim.x * blockDim.x) {
-      const int r = (int)j - i - g.q_offset;
-      const float v = b.causal && r > 0 ? -INFINITY : table_value(table, table_dtype, (int64_t)bucket_row(b, r) * g.heads + h);
-      out[h * head_stride + i * row_stride + j] = from_f32<T>(v);
+  for (int i = blockIdx.y; i < g.Lq; i += gridDim.y)
+    for (int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; j < g.Lk; j += (int64_t)gridDim.x * blockDim.x)
+      out[h * head_stride + i * row_stride + j] = from_f32<T>(bias_value(b, g, table, table_dtype, h, (int)j - i - g.q_offset));
+}
+
+// A block writes `rows` queries x up to FWD_COLS keys of one head.  It holds their part of the vector in shared memory once for each of the
+// 16 / sizeof(T) positions that a 16-byte boundary can have in it, so that every row is one bulk copy to global memory from an
+// aligned place of one of the copies, whatever its window and the alignment of the row; up to 15 bytes at either end of a row are
+// stored by threads.
+#ifndef MTS_RELPOS_DIRECT
+#define MTS_RELPOS_DIRECT 8
+#endif
+constexpr int FWD_COLS = 2048;
+constexpr int FWD_THREADS = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(FWD_THREADS)
+relpos_forward_rows(const __grid_constant__ Buckets b, BiasGeometry g, const void* __restrict__ table, int table_dtype, T* __restrict__ out,
+                    int64_t head_stride, int64_t row_stride, int rows, int pitch) {
+  constexpr int COPIES = 16 / (int)sizeof(T);
+  extern __shared__ __align__(16) unsigned char smem[];
+  T* line = reinterpret_cast<T*>(smem);                                 // [COPIES][pitch]: copy s holds element e at e - s
+  const int h = blockIdx.z, i0 = blockIdx.y * rows, j0 = blockIdx.x * FWD_COLS;
+  const int nr = min(rows, g.Lq - i0), nc = min(FWD_COLS, g.Lk - j0), n = nr + nc - 1;
+  // element e: distance of the last query of the block to key j0, plus e
+  const int r0 = j0 - (i0 + nr - 1) - g.q_offset;
+  for (int e = threadIdx.x; e < n; e += FWD_THREADS) {
+    const T v = from_f32<T>(bias_value(b, g, table, table_dtype, h, r0 + e));
+#pragma unroll
+    for (int s = 0; s < COPIES; ++s)
+      if (e >= s) line[s * pitch + e - s] = v;
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the copies below read what these stores wrote
+  __syncthreads();
+  T* to = out + h * head_stride + (int64_t)i0 * row_stride + j0;
+  for (int i = threadIdx.x; i < nr; i += FWD_THREADS) {
+    T* row = to + i * row_stride;
+    const int w = nr - 1 - i;                                           // the row's window: elements [w, w + nc)
+    const int head = min(nc, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)), body = (nc - head) / COPIES * COPIES;
+    const int s = (w + head) % COPIES;
+    if (body > 0) {
+      const uint32_t from = (uint32_t)__cvta_generic_to_shared(line + s * pitch + (w + head - s));
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" :: "l"(row + head), "r"(from), "r"(body * (int)sizeof(T)) : "memory");
     }
   }
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  for (int k = threadIdx.x; k < nr * 2 * COPIES; k += FWD_THREADS) {      // the ends of the rows
+    const int i = k / (2 * COPIES), e = k % (2 * COPIES);
+    T* row = to + i * row_stride;
+    const int head = min(nc, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)), body = (nc - head) / COPIES * COPIES;
+    const int j = e < COPIES ? e : head + body + e - COPIES;
+    if (e < COPIES ? j < head : j < nc) row[j] = line[nr - 1 - i + j];
+  }
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // shared memory stays until it has been read
 }
 
 constexpr int GRAD_CTAS = 592;            // blocks over all heads; also bounds the partial sums kept in the workspace
 constexpr int GRAD_WARPS = 8;
-constexpr int GRAD_ROWS = 256;            // queries of one piece of work
+constexpr int GRAD_ROWS = 8;              // rows of a patch
+constexpr int GRAD_STEPS = 32;            // patches of a piece of work: at most 256 terms of a diagonal are added in fp32
 inline int grad_ctas_per_head(int heads) { return (int)ceil_div(GRAD_CTAS, heads); }
 
-// A warp takes 32 neighbouring diagonals, one per lane, and walks down GRAD_ROWS queries of one batch entry.  The sums of a piece of
-// work are added per bucket, in a fixed order, to the warp's own row of accumulators.
-template <typename T>
-__global__ void __launch_bounds__(GRAD_WARPS * 32)
-relpos_backward_partial(Buckets b, BiasGeometry g, int64_t B, const T* __restrict__ grad, int64_t batch_stride, int64_t head_stride,
-                        int64_t row_stride, double* __restrict__ partial) {
-  __shared__ double acc[GRAD_WARPS][2 * MTS_RELPOS_MAX_BUCKETS];
-  const int rows = b.two_sided ? 2 * b.n : b.n, w = threadIdx.x / 32, lane = lane_id(), h = blockIdx.y;
-  for (int k = lane; k < rows; k += 32) acc[w][k] = 0.0;
-  __syncwarp();
-  // diagonal c: distance r = c - (Lq - 1) - q_offset, key j = i + c - (Lq - 1)
-  const int64_t bands = ((int64_t)g.Lq + g.Lk - 1 + 31) / 32, pieces = (g.Lq + GRAD_ROWS - 1) / GRAD_ROWS;
-  for (int64_t item = (int64_t)blockIdx.x * GRAD_WARPS + w; item < bands * pieces * B; item += (int64_t)gridDim.x * GRAD_WARPS) {
-    const int c = (int)(item % bands) * 32 + lane;
-    const int piece = (int)(item / bands % pieces);
-    const int64_t batch = item / (bands * pieces);
-    const int shift = c - (g.Lq - 1), r = shift - g.q_offset;
-    const bool counts = !(b.causal && r > 0) && c < g.Lq + g.Lk - 1;
-    const int i0 = max(piece * GRAD_ROWS, -shift), i1 = min(min(piece * GRAD_ROWS + GRAD_ROWS, g.Lq), g.Lk - shift);
-    float sum = 0.f;
-    if (counts)
-      for (int i = i0; i < i1; ++i) sum += to_f32(grad[batch * batch_stride + h * head_stride + i * row_stride + (i + shift)]);
-    const int row = counts ? bucket_row(b, r) : -1;
+// Sums of n neighbouring diagonals (distances r0, r0 + 1, ... in shared memory) to the warp's bucket sums, in a fixed order.
+__device__ __forceinline__ void add_to_buckets(const Buckets& b, const float* diagonals, int n, int r0, int valid_lo, int valid_hi, double* acc) {
+  for (int base = 0; base < n; base += 32) {
+    const int d = base + lane_id();
+    const bool counts = d < n && r0 + d >= valid_lo && r0 + d < valid_hi && !(b.causal && r0 + d > 0);
+    const float sum = counts ? diagonals[d] : 0.f;
+    const int row = counts ? bucket_row(b, r0 + d) : -1;
     unsigned left = __ballot_sync(0xFFFFFFFFu, counts);
     while (left) {
       const int k = __shfl_sync(0xFFFFFFFFu, row, __ffs(left) - 1);
       const bool mine = row == k;
       float s = mine ? sum : 0.f;
+#pragma unroll
       for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-      if (lane == 0) acc[w][k] += (double)s;
+      if (lane_id() == 0) acc[k] += (double)s;
       left &= ~__ballot_sync(0xFFFFFFFFu, mine);
     }
+  }
+  __syncwarp();
+}
+
+// A warp walks down a band of neighbouring diagonals in patches of 8 rows; the columns move with the rows, so each accumulator stays on its
+// diagonal for all patches of a piece of work.
+//   VECTOR: a lane holds 16 bytes of each row (E neighbouring columns): an 8 x E patch has E + 7 diagonals.  Rows on 16-byte
+//           boundaries, Lk a multiple of E.
+//   else:   a lane holds every 32nd column (E = 4 of them): one diagonal for each of its 8 E elements.  Any alignment.
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(GRAD_WARPS * 32)
+relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64_t B, const T* __restrict__ grad, int64_t batch_stride,
+                        int64_t head_stride, int64_t row_stride, double* __restrict__ partial) {
+  constexpr int E = VECTOR ? 16 / (int)sizeof(T) : 4, BAND = 32 * E, ROWS = GRAD_ROWS, SHIFT = ROWS - 1;
+  __shared__ double sums[GRAD_WARPS][2 * MTS_RELPOS_MAX_BUCKETS];
+  __shared__ float lines[GRAD_WARPS][BAND + ROWS];
+  const int rows = b.two_sided ? 2 * b.n : b.n, w = threadIdx.x / 32, lane = lane_id(), h = blockIdx.y;
+  double* acc = sums[w];
+  float* line = lines[w];
+  for (int k = lane; k < rows; k += 32) acc[k] = 0.0;
+  __syncwarp();
+  const int steps = (g.Lq + ROWS - 1) / ROWS;                           // patches down a column of them
+  const int below = steps * ROWS;                                       // bands begin at column -below of row 0
+  const int bands = (below + g.Lk + BAND - 1) / BAND;
+  const int64_t pieces = (B * steps + GRAD_STEPS - 1) / GRAD_STEPS;
+  for (int64_t item = (int64_t)blockIdx.x * GRAD_WARPS + w; item < bands * pieces; item += (int64_t)gridDim.x * GRAD_WARPS) {
+    const int c0 = (int)(item % bands) * BAND - below;                  // column of row 0 on the band's first diagonal
+    // diagonals c0 - 7 ... c0 + BAND - 1 are touched; nothing to do where all are masked
+    if (b.causal && c0 - SHIFT - g.q_offset > 0) continue;
+    const int64_t p0 = item / bands * GRAD_STEPS, p1 = min(p0 + GRAD_STEPS, B * steps);
+    float sum[VECTOR ? E + SHIFT : E * ROWS];
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(sum) / 4); ++k) sum[k] = 0.f;
+    bool any = false;
+    int64_t batch = p0 / steps;
+    int step = (int)(p0 - batch * steps);
+    for (int64_t p = p0; p < p1; ++p) {
+      const int i = step * ROWS, j = i + c0;                            // the patch: rows i..., columns j... of all lanes
+      if (j + BAND > 0 && j < g.Lk) {
+        any = true;
+        const T* at = grad + batch * batch_stride + h * head_stride + (int64_t)i * row_stride;
+        const int n = min(ROWS, g.Lq - i);
+        if constexpr (VECTOR) {
+          const int col = j + lane * E;
+          const bool in = col >= 0 && col < g.Lk && !(b.causal && c0 + lane * E - SHIFT - g.q_offset > 0);
+          uint4 v[ROWS];
+#pragma unroll
+          for (int k = 0; k < ROWS; ++k)
+            v[k] = in && k < n ? __ldcs(reinterpret_cast<const uint4*>(at + (int64_t)k * row_stride + col)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int k = 0; k < ROWS; ++k) {
+            const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if constexpr (sizeof(T) == 4) {
+                sum[q - k + SHIFT] += __uint_as_float(u[q]);
+              } else {
+                const float2 f = unpack2<T>(u[q]);
+                sum[2 * q - k + SHIFT] += f.x;
+                sum[2 * q + 1 - k + SHIFT] += f.y;
+              }
+            }
+          }
+        } else {
+          T v[ROWS][E];
+#pragma unroll
+          for (int k = 0; k < ROWS; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const int col = j + lane + 32 * e;
+              const bool in = k < n && col >= 0 && col < g.Lk && !(b.causal && c0 + lane + 32 * e - k - g.q_offset > 0);
+              v[k][e] = in ? at[(int64_t)k * row_stride + col] : from_f32<T>(0.f);
+            }
+#pragma unroll
+          for (int k = 0; k < ROWS; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e * ROWS + k] += to_f32(v[k][e]);
+        }
+      }
+      if (++step == steps) { step = 0; ++batch; }
+    }
+    if (!any) continue;
+    // line[d]: the sum of diagonal c0 - 7 + d; lanes add to it one after the other where their diagonals overlap
+    for (int d = lane; d < BAND + ROWS; d += 32) line[d] = 0.f;
+    __syncwarp();
+    if constexpr (VECTOR) {
+#pragma unroll
+      for (int k = 0; k < E + SHIFT; k += E) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (k + e < E + SHIFT) line[lane * E + k + e] += sum[k + e];
+        __syncwarp();
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) line[lane + 32 * e - k + SHIFT] += sum[e * ROWS + k];
+        __syncwarp();
+      }
+    }
+    add_to_buckets(b, line, BAND + SHIFT, c0 - SHIFT - g.q_offset, -(g.Lq - 1) - g.q_offset, g.Lk - g.q_offset, acc);
   }
   __syncthreads();
   for (int k = threadIdx.x; k < rows; k += blockDim.x) {
     double s = 0.0;
-    for (int v = 0; v < GRAD_WARPS; ++v) s += acc[v][k];
+    for (int v = 0; v < GRAD_WARPS; ++v) s += sums[v][k];
     partial[((int64_t)h * gridDim.x + blockIdx.x) * rows + k] = s;
   }
 }
 
-// grad_table[k, h] = the sum of the blocks' partial sums, in the order of the blocks.
-__global__ void relpos_backward_combine(const double* __restrict__ partial, int ctas, int rows, int heads, float* __restrict__ grad_table) {
-  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+// grad_table[k, h] = the sum of the blocks' partial sums, a warp each, in a fixed order.
+__global__ void __launch_bounds__(128)
+relpos_backward_combine(const double* __restrict__ partial, int ctas, int rows, int heads, float* __restrict__ grad_table) {
+  const int i = blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
   if (i >= rows * heads) return;
   const int h = i / rows, k = i % rows;
   double s = 0.0;
-  for (int c = 0; c < ctas; ++c) s += partial[((int64_t)h * ctas + c) * rows + k];
-  grad_table[k * heads + h] = (float)s;
+#pragma unroll 4
+  for (int c = lane_id(); c < ctas; c += 32) s += partial[((int64_t)h * ctas + c) * rows + k];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if (lane_id() == 0) grad_table[k * heads + h] = (float)s;
 }
 
 }  // namespace mts
@@ -161,8 +306,23 @@ extern "C" int mts_relpos_bias_forward(const mts_relpos_buckets* buckets, const 
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
     LaunchScope scope(K_RELPOS_FWD, s);
-    const dim3 grid((unsigned)ceil_div(Lk, 256), (unsigned)(Lq < 65535 ? Lq : 65535), (unsigned)heads);
-    relpos_forward_direct<T><<<grid, 256, 0, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride);
+    if (Lq < MTS_RELPOS_DIRECT) {
+      const dim3 grid((unsigned)ceil_div(Lk, 256), (unsigned)Lq, (unsigned)heads);
+      relpos_forward_direct<T><<<grid, 256, 0, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride);
+      return check_launch(what);
+    }
+    // rows of a block: as many as leave the GPU four blocks per SM, 128 at most (the vector is made once for all of them), and not
+    // more blocks down than a grid has room for
+    const int64_t strips = ceil_div(Lk, FWD_COLS);
+    int rows = 128;
+    while (rows > 8 && ceil_div(Lq, rows) * strips * heads < 148 * 4) rows /= 2;
+    while (ceil_div(Lq, rows) > 65535) rows *= 2;
+    const int pitch = (int)align_up((size_t)(Lk < FWD_COLS ? Lk : FWD_COLS) + (size_t)rows, 16);
+    const size_t smem = (size_t)pitch * 16;
+    int e = check_cuda(cudaFuncSetAttribute(relpos_forward_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "shared memory size");
+    if (e != MTS_OK) return e;
+    const dim3 grid((unsigned)strips, (unsigned)ceil_div(Lq, rows), (unsigned)heads);
+    relpos_forward_rows<T><<<grid, FWD_THREADS, smem, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride, rows, pitch);
     return check_launch(what);
   });
 }
@@ -198,13 +358,18 @@ extern "C" int mts_relpos_bias_backward(const mts_relpos_buckets* buckets, const
     using T = decltype(t);
     {
       LaunchScope scope(K_RELPOS_BWD, s);
-      relpos_backward_partial<T><<<dim3(ctas, heads), GRAD_WARPS * 32, 0, s>>>(b, g, B, static_cast<const T*>(grad_out), batch_stride, head_stride,
-                                                                              row_stride, static_cast<double*>(workspace));
+      const uintptr_t bits = (uintptr_t)grad_out | (uintptr_t)((batch_stride | head_stride | row_stride | Lk) * (int64_t)sizeof(T));
+      if (bits % 16 == 0)
+        relpos_backward_partial<T, true><<<dim3(ctas, heads), GRAD_WARPS * 32, 0, s>>>(b, g, B, static_cast<const T*>(grad_out), batch_stride, head_stride,
+                                                                                     row_stride, static_cast<double*>(workspace));
+      else
+        relpos_backward_partial<T, false><<<dim3(ctas, heads), GRAD_WARPS * 32, 0, s>>>(b, g, B, static_cast<const T*>(grad_out), batch_stride, head_stride,
+                                                                                      row_stride, static_cast<double*>(workspace));
     }
     int e = check_launch(what);
     if (e != MTS_OK) return e;
     LaunchScope scope(K_RELPOS_BWD, s);
-    relpos_backward_combine<<<(unsigned)ceil_div((int64_t)rows * heads, 128), 128, 0, s>>>(static_cast<const double*>(workspace), ctas, rows, heads, grad_table);
+    relpos_backward_combine<<<(unsigned)ceil_div((int64_t)rows * heads, 4), 128, 0, s>>>(static_cast<const double*>(workspace), ctas, rows, heads, grad_table);
     return check_launch(what);
   });
 }
