@@ -6,6 +6,7 @@
 // The bucket depends on the diagonal j - i alone.  Forward: a head's matrix is one vector of Lq + Lk - 1 values of which every row
 // shows a window; what bounds it is writing the rows.  Gradient: the sum of each diagonal first, then of the diagonals of a
 // bucket; what bounds it is reading the gradient.
+#include <limits.h>
 #include <math.h>
 
 #include "dense.cuh"
@@ -105,40 +106,56 @@ relpos_forward_rows(const __grid_constant__ Buckets b, BiasGeometry g, const voi
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // shared memory stays until it has been read
 }
 
+#ifndef MTS_RELPOS_GRAD_BLOCKS
+#define MTS_RELPOS_GRAD_BLOCKS 4
+#endif
 constexpr int GRAD_CTAS = 592;            // blocks over all heads; also bounds the partial sums kept in the workspace
 constexpr int GRAD_WARPS = 8;
 constexpr int GRAD_ROWS = 8;              // rows of a patch
-constexpr int GRAD_STEPS = 32;            // patches of a piece of work: at most 256 terms of a diagonal are added in fp32
-inline int grad_ctas_per_head(int heads) { return (int)ceil_div(GRAD_CTAS, heads); }
+constexpr int GRAD_PATCHES = 96;          // patches of a warp after which the diagonals' fp32 sums are handed on (768 terms)
+inline int grad_ctas_per_head(int heads) { return heads < GRAD_CTAS ? GRAD_CTAS / heads : 1; }
 
-// Sums of n neighbouring diagonals (distances r0, r0 + 1, ... in shared memory) to the warp's bucket sums, in a fixed order.
-__device__ __forceinline__ void add_to_buckets(const Buckets& b, const float* diagonals, int n, int r0, int valid_lo, int valid_hi, double* acc) {
-  for (int base = 0; base < n; base += 32) {
-    const int d = base + lane_id();
-    const bool counts = d < n && r0 + d >= valid_lo && r0 + d < valid_hi && !(b.causal && r0 + d > 0);
-    const float sum = counts ? diagonals[d] : 0.f;
-    const int row = counts ? bucket_row(b, r0 + d) : -1;
-    unsigned left = __ballot_sync(0xFFFFFFFFu, counts);
-    while (left) {
-      const int k = __shfl_sync(0xFFFFFFFFu, row, __ffs(left) - 1);
-      const bool mine = row == k;
-      float s = mine ? sum : 0.f;
+// A diagonal per lane, at distance r, to the warp's bucket sums, in a fixed order.
+__device__ __forceinline__ void add_to_buckets(const Buckets& b, float sum, int r, bool counts, double* acc) {
+  const int row = counts ? bucket_row(b, r) : -1;
+  unsigned left = __ballot_sync(0xFFFFFFFFu, counts);
+  while (left) {
+    const int k = __shfl_sync(0xFFFFFFFFu, row, __ffs(left) - 1);
+    const bool mine = row == k;
+    float s = mine ? sum : 0.f;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-      if (lane_id() == 0) acc[k] += (double)s;
-      left &= ~__ballot_sync(0xFFFFFFFFu, mine);
-    }
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (lane_id() == 0) acc[k] += (double)s;
+    left &= ~__ballot_sync(0xFFFFFFFFu, mine);
   }
-  __syncwarp();
 }
 
-// A warp walks down a band of neighbouring diagonals in patches of 8 rows; the columns move with the rows, so each accumulator stays on its
-// diagonal for all patches of a piece of work.
+// Bands of neighbouring diagonals, BAND wide, and the patches of 8 rows down each of them that hold anything.
+struct Bands {
+  int32_t band, count, steps, below, Lk, first_masked;
+  __device__ __forceinline__ Bands(const Buckets& b, const BiasGeometry& g, int band_)
+      : band(band_), steps((g.Lq + GRAD_ROWS - 1) / GRAD_ROWS), below(steps * GRAD_ROWS), Lk(g.Lk) {
+    count = (below + g.Lk + band - 1) / band;                           // the first begins at column -below of row 0
+    // causal: diagonals from q_offset + 1 on are masked, a band's lowest is 7 below its first column
+    first_masked = b.causal ? g.q_offset + GRAD_ROWS : INT_MAX;
+  }
+  __device__ __forceinline__ int column(int k) const { return k * band - below; }       // of row 0
+  __device__ __forceinline__ int first(int k) const { return max(0, (-band - column(k)) / GRAD_ROWS + 1); }
+  __device__ __forceinline__ int patches(int k) const {
+    const int c = column(k);
+    if (k >= count || c >= first_masked) return 0;
+    return max(0, min(steps, (Lk - c + GRAD_ROWS - 1) / GRAD_ROWS) - first(k));
+  }
+};
+
+// A warp walks down a band in patches of 8 rows; the columns move with the rows, so each accumulator stays on its diagonal.  The patches
+// of all bands and batch entries of a head, band by band, are dealt out evenly in runs to the blocks, whose warps take them in turn;
+// where the band changes the block adds up its warps' diagonals and hands them on to the buckets.
 //   VECTOR: a lane holds 16 bytes of each row (E neighbouring columns): an 8 x E patch has E + 7 diagonals.  Rows on 16-byte
 //           boundaries, Lk a multiple of E.
 //   else:   a lane holds every 32nd column (E = 4 of them): one diagonal for each of its 8 E elements.  Any alignment.
 template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(GRAD_WARPS * 32)
+__global__ void __launch_bounds__(GRAD_WARPS * 32, MTS_RELPOS_GRAD_BLOCKS)
 relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64_t B, const T* __restrict__ grad, int64_t batch_stride,
                         int64_t head_stride, int64_t row_stride, double* __restrict__ partial) {
   constexpr int E = VECTOR ? 16 / (int)sizeof(T) : 4, BAND = 32 * E, ROWS = GRAD_ROWS, SHIFT = ROWS - 1;
@@ -149,67 +166,85 @@ relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64
   float* line = lines[w];
   for (int k = lane; k < rows; k += 32) acc[k] = 0.0;
   __syncwarp();
-  const int steps = (g.Lq + ROWS - 1) / ROWS;                           // patches down a column of them
-  const int below = steps * ROWS;                                       // bands begin at column -below of row 0
-  const int bands = (below + g.Lk + BAND - 1) / BAND;
-  const int64_t pieces = (B * steps + GRAD_STEPS - 1) / GRAD_STEPS;
-  for (int64_t item = (int64_t)blockIdx.x * GRAD_WARPS + w; item < bands * pieces; item += (int64_t)gridDim.x * GRAD_WARPS) {
-    const int c0 = (int)(item % bands) * BAND - below;                  // column of row 0 on the band's first diagonal
-    // diagonals c0 - 7 ... c0 + BAND - 1 are touched; nothing to do where all are masked
-    if (b.causal && c0 - SHIFT - g.q_offset > 0) continue;
-    const int64_t p0 = item / bands * GRAD_STEPS, p1 = min(p0 + GRAD_STEPS, B * steps);
+  const Bands bands(b, g, BAND);
+  int64_t total = 0;
+  for (int k0 = 0; k0 < bands.count; k0 += 32) total += __reduce_add_sync(0xFFFFFFFFu, bands.patches(k0 + lane));
+  total *= B;
+  // this block's run of patches, counted from the first band's first
+  int64_t at = blockIdx.x * total / gridDim.x;
+  const int64_t stop = (blockIdx.x + 1) * total / gridDim.x;
+  int band = 0;
+  int64_t skip = at;                                                    // patches of band `band` before the run
+
+  while (at < stop) {
+    const int n = bands.patches(band);
+    if (skip >= B * n) { skip -= B * n; ++band; continue; }
+    const int c0 = bands.column(band);
+    const int run = (int)min(min(stop - at, B * n - skip), (int64_t)GRAD_PATCHES * GRAD_WARPS);
+    const int end = bands.first(band) + n;
+    int64_t batch = (skip + w) / n;
+    int step = bands.first(band) + (int)(skip + w - batch * n);
     float sum[VECTOR ? E + SHIFT : E * ROWS];
 #pragma unroll
     for (int k = 0; k < (int)(sizeof(sum) / 4); ++k) sum[k] = 0.f;
-    bool any = false;
-    int64_t batch = p0 / steps;
-    int step = (int)(p0 - batch * steps);
-    for (int64_t p = p0; p < p1; ++p) {
-      const int i = step * ROWS, j = i + c0;                            // the patch: rows i..., columns j... of all lanes
-      if (j + BAND > 0 && j < g.Lk) {
-        any = true;
-        const T* at = grad + batch * batch_stride + h * head_stride + (int64_t)i * row_stride;
-        const int n = min(ROWS, g.Lq - i);
-        if constexpr (VECTOR) {
-          const int col = j + lane * E;
-          const bool in = col >= 0 && col < g.Lk && !(b.causal && c0 + lane * E - SHIFT - g.q_offset > 0);
-          uint4 v[ROWS];
+#pragma unroll 1
+    for (int p = w; p < run; p += GRAD_WARPS) {
+      const int i = step * ROWS, j = i + c0, here = min(ROWS, g.Lq - i);     // the patch: rows i..., columns j... of all lanes
+      const T* from = grad + batch * batch_stride + h * head_stride + (int64_t)i * row_stride + j;
+      // nothing of the patch outside the matrix, no lane behind the mask: no tests
+      const bool whole = here == ROWS && j >= 0 && j + BAND <= g.Lk && c0 + BAND - 1 < bands.first_masked;
+      if constexpr (VECTOR) {
+        const int col = j + lane * E;
+        const bool in = col >= 0 && col < g.Lk && c0 + lane * E < bands.first_masked;
+        const T* mine = from + lane * E;
+        uint4 v[ROWS];
+        if (whole) {
 #pragma unroll
-          for (int k = 0; k < ROWS; ++k)
-            v[k] = in && k < n ? __ldcs(reinterpret_cast<const uint4*>(at + (int64_t)k * row_stride + col)) : make_uint4(0u, 0u, 0u, 0u);
+          for (int k = 0; k < ROWS; ++k, mine += row_stride) v[k] = __ldcs(reinterpret_cast<const uint4*>(mine));
+        } else {
 #pragma unroll
-          for (int k = 0; k < ROWS; ++k) {
-            const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          for (int k = 0; k < ROWS; ++k, mine += row_stride)
+            v[k] = in && k < here ? __ldcs(reinterpret_cast<const uint4*>(mine)) : make_uint4(0u, 0u, 0u, 0u);
+        }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if constexpr (sizeof(T) == 4) {
-                sum[q - k + SHIFT] += __uint_as_float(u[q]);
-              } else {
-                const float2 f = unpack2<T>(u[q]);
-                sum[2 * q - k + SHIFT] += f.x;
-                sum[2 * q + 1 - k + SHIFT] += f.y;
-              }
+        for (int k = 0; k < ROWS; ++k) {
+          const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if constexpr (sizeof(T) == 4) {
+              sum[q - k + SHIFT] += __uint_as_float(u[q]);
+            } else {
+              const float2 f = unpack2<T>(u[q]);
+              sum[2 * q - k + SHIFT] += f.x;
+              sum[2 * q + 1 - k + SHIFT] += f.y;
             }
           }
-        } else {
-          T v[ROWS][E];
+        }
+      } else {
+        bool in[E];
 #pragma unroll
-          for (int k = 0; k < ROWS; ++k)
+        for (int e = 0; e < E; ++e) {
+          const int col = j + lane + 32 * e;
+          in[e] = col >= 0 && col < g.Lk && c0 + lane + 32 * e < bands.first_masked;
+        }
+        const T* mine = from + lane;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const int col = j + lane + 32 * e;
-              const bool in = k < n && col >= 0 && col < g.Lk && !(b.causal && c0 + lane + 32 * e - k - g.q_offset > 0);
-              v[k][e] = in ? at[(int64_t)k * row_stride + col] : from_f32<T>(0.f);
-            }
+        for (int k0 = 0; k0 < ROWS; k0 += ROWS / 2) {                     // half the rows at a time: 64 registers, 32 warps per SM
+          T v[ROWS / 2][E];
 #pragma unroll
-          for (int k = 0; k < ROWS; ++k)
+          for (int k = 0; k < ROWS / 2; ++k, mine += row_stride)
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e * ROWS + k] += to_f32(v[k][e]);
+            for (int e = 0; e < E; ++e) v[k][e] = whole || (in[e] && k0 + k < here) ? __ldcs(mine + 32 * e) : from_f32<T>(0.f);
+#pragma unroll
+          for (int k = 0; k < ROWS / 2; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e * ROWS + k0 + k] += to_f32(v[k][e]);
         }
       }
-      if (++step == steps) { step = 0; ++batch; }
+      for (step += GRAD_WARPS; step >= end; step -= n) ++batch;
     }
-    if (!any) continue;
+    at += run;
+    skip += run;
     // line[d]: the sum of diagonal c0 - 7 + d; lanes add to it one after the other where their diagonals overlap
     for (int d = lane; d < BAND + ROWS; d += 32) line[d] = 0.f;
     __syncwarp();
@@ -229,7 +264,16 @@ relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64
         __syncwarp();
       }
     }
-    add_to_buckets(b, line, BAND + SHIFT, c0 - SHIFT - g.q_offset, -(g.Lq - 1) - g.q_offset, g.Lk - g.q_offset, acc);
+    __syncthreads();
+    for (int d = threadIdx.x; d < (BAND + SHIFT + 31) / 32 * 32; d += GRAD_WARPS * 32) {
+      const int r = c0 - SHIFT + d - g.q_offset;
+      const bool counts = d < BAND + SHIFT && r > -g.Lq - g.q_offset && r < g.Lk - g.q_offset && !(b.causal && r > 0);
+      float s = 0.f;
+#pragma unroll
+      for (int v = 0; v < GRAD_WARPS; ++v) s += counts ? lines[v][d] : 0.f;
+      add_to_buckets(b, s, r, counts, acc);
+    }
+    __syncthreads();
   }
   __syncthreads();
   for (int k = threadIdx.x; k < rows; k += blockDim.x) {
