@@ -26,7 +26,7 @@
 namespace mts {
 
 #ifndef MTS_REC_FWD_BLOCKS
-#define MTS_REC_FWD_BLOCKS 20
+#define MTS_REC_FWD_BLOCKS 24
 #endif
 #ifndef MTS_REC_BWD_BLOCKS
 #define MTS_REC_BWD_BLOCKS 12
@@ -339,14 +339,10 @@ __device__ __forceinline__ void publish(const RecArgs& a, int index, int strip, 
     // the last of eight to come here goes on (a set that the end of the tokens leaves short is never needed)
     const int parent = index >> REC_RADIX_BITS;
     uint32_t before = 0;
-    if (lane_id() == 0) {
-      before = atomicAdd(a.level[l + 1].done + (int64_t)parent * a.strips + strip, 1u);
-      __threadfence();
-    }
+    if (lane_id() == 0)
+      asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.level[l + 1].done + (int64_t)parent * a.strips + strip) : "memory");
     if (__shfl_sync(0xFFFFFFFFu, before, 0) != REC_RADIX - 1) return;
-    __syncwarp();
-    uint32_t how = READY_MAP;
-    if (lane_id() < REC_RADIX) how = *reinterpret_cast<volatile uint32_t*>(to.ready + ((int64_t)parent * REC_RADIX + lane_id()) * a.strips + strip);
+    const uint32_t how = wait_ready(a, lane_id() < REC_RADIX ? to.ready + ((int64_t)parent * REC_RADIX + lane_id()) * a.strips + strip : nullptr);
     const uint32_t cuts = __ballot_sync(0xFFFFFFFFu, how == READY_CUT);
     m = {all<V>(1.f), all<V>(0.f)};
     const float* P = to.P + (int64_t)parent * REC_RADIX * a.D + c;
@@ -500,41 +496,37 @@ struct Piece {
   }
 };
 
-// A batch of rows of an [N, D] array: a base that all lanes share, a lane's channels from there as 32-bit offset of bytes, rows `step`
-// bytes apart (the host refuses strides of 2^28 bytes or more).  A lane behind the last channel reads the first ones.
+// A lane's channels of the rows of an [N, D] array, from one row on, walked up or down by a pointer.  A lane behind the last channel
+// reads the first ones: no test where rows are read.
 template <typename T, int V, bool VEC>
 struct Rows {
-  const char* base;
-  int64_t batch;               // bytes from one batch to the next
-  uint32_t lane, step;
+  T* at;
+  int64_t stride;
   int left;
-  __device__ __forceinline__ Rows(const void* p, int64_t stride, int64_t row, int c, int left_)
-      : base(static_cast<const char*>(p) + row * stride * (int64_t)sizeof(T)), batch(REC_BATCH * stride * (int64_t)sizeof(T)),
-        lane(left_ > 0 ? c * (uint32_t)sizeof(T) : 0u), step((uint32_t)stride * (uint32_t)sizeof(T)), left(left_) {}
-  __device__ __forceinline__ Raw<T, V> get(uint32_t offset) const {
-    const T* at = reinterpret_cast<const T*>(base + offset);
-    if (VEC) return load_raw<T, V>(at);
-    return get_raw<T, V, VEC>(at, left);
-  }
-  __device__ __forceinline__ void put(uint32_t offset, Channels<V> v) const {
-    mts::put<V, VEC>(reinterpret_cast<T*>(const_cast<char*>(base) + offset), left, v);
-  }
-  __device__ __forceinline__ void next() { base += batch; }
-  __device__ __forceinline__ void previous() { base -= batch; }
-  // Rows that `live` does not name are not read and give 0.
-  __device__ __forceinline__ void load(uint32_t live, Raw<T, V> (&r)[REC_BATCH]) const {
-    uint32_t at = lane;
+  __device__ __forceinline__ Rows(const void* p, int64_t stride_, int64_t row, int c, int left_)
+      : at(static_cast<T*>(const_cast<void*>(p)) + row * stride_ + (left_ > 0 ? c : 0)), stride(stride_), left(left_) {}
+  __device__ __forceinline__ void move(int rows) { at += rows * stride; }
+  __device__ __forceinline__ Raw<T, V> get() const { return VEC ? load_raw<T, V>(at) : get_raw<T, V, VEC>(at, left); }
+  __device__ __forceinline__ Raw<T, V> next() { const Raw<T, V> r = get(); at += stride; return r; }
+  __device__ __forceinline__ Raw<T, V> previous() { at -= stride; return get(); }
+  __device__ __forceinline__ void put(Channels<V> v) const { mts::put<V, VEC>(at, left, v); }
+  // A batch of n rows from here on, the first `live` of them; the others give 0.  Moves behind the batch.
+  template <int N>
+  __device__ __forceinline__ void load(int live, Raw<T, V> (&r)[N]) {
 #pragma unroll
-    for (int i = 0; i < REC_BATCH; ++i, at += step) r[i] = (live >> i & 1) ? get(at) : Raw<T, V>{};
+    for (int i = 0; i < N; ++i, at += stride) r[i] = i < live ? get() : Raw<T, V>{};
   }
 };
-constexpr uint32_t ALL_LIVE = (1u << REC_BATCH) - 1;
-__device__ __forceinline__ uint32_t live_bits(int tokens) { return tokens >= REC_BATCH ? ALL_LIVE : tokens > 0 ? (1u << tokens) - 1 : 0u; }
-__device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel) { return (uint32_t)(mask >> (rel % REC_PART)) & ALL_LIVE; }
+// Bits of n tokens from token `rel` of a part on.
+template <int N>
+__device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel) { return (uint32_t)(mask >> (rel % REC_PART)) & ((1u << N) - 1); }
 
 // In all four walks a row's registers take the row one batch ahead as soon as they have been read: a batch is always on its way.
 
 // ------------------------------------------------------------------------------- forward
+constexpr int FWD_BATCH = 4;           // rows on their way: with 8 the registers leave room for fewer warps
+static_assert(REC_BATCH == 2 * FWD_BATCH, "a state is kept where a batch begins");
+
 template <typename T, int V, bool VEC>
 __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c;
@@ -549,27 +541,43 @@ __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
       if (a.h0) from = get<V, VEC>(a.h0 + (int64_t)s * a.D + c, left);
       put<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left, from);
     }
-    int rel = start & ~(REC_BATCH - 1);
+    int rel = start & ~(FWD_BATCH - 1);
     Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), value(a.value, a.value_stride, it.t0 + rel, c, left);
-    Raw<T, V> g[REC_BATCH], x[REC_BATCH];
-    gate.load(ALL_LIVE, g);
-    value.load(ALL_LIVE, x);
-#pragma unroll 1
-    for (; rel < a.chunk; rel += REC_BATCH) {
-      if (rel + REC_BATCH < a.chunk) {                                  // else the last batch once more, unused
-        gate.next();
-        value.next();
-      }
-      uint32_t ga = gate.lane, xa = value.lane;
+    Raw<T, V> g[FWD_BATCH], x[FWD_BATCH];
+    gate.load(FWD_BATCH, g);
+    value.load(FWD_BATCH, x);
+    // the batch with the start: what is before it there is forgotten
+    const int later = a.chunk - rel - FWD_BATCH;                        // tokens behind this batch
 #pragma unroll
-      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step) {
-        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
-        g[i] = gate.get(ga);
-        x[i] = value.get(xa);
-        if (rel + i == start) m.B = from;
-        m.B = blend(nz, nx, m.B);
-        m.P = fma(nz, m.P, m.P);
+    for (int i = 0; i < FWD_BATCH; ++i) {
+      const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
+      if (rel + i == start) m = {all<V>(1.f), from};
+      m.B = blend(nz, nx, m.B);
+      m.P = fma(nz, m.P, m.P);
+    }
+    gate.load(later, g);
+    value.load(later, x);
+    const auto step = [&](int i) {
+      const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
+      m.B = blend(nz, nx, m.B);
+      m.P = fma(nz, m.P, m.P);
+    };
+    rel = later;                                                        // tokens to go, FWD_BATCH of them in registers
+#pragma unroll 1
+    for (; rel >= 3 * FWD_BATCH; rel -= 2 * FWD_BATCH) {
+#pragma unroll
+      for (int i = 0; i < 2 * FWD_BATCH; ++i) {
+        step(i % FWD_BATCH);
+        g[i % FWD_BATCH] = gate.next();
+        x[i % FWD_BATCH] = value.next();
       }
+    }
+#pragma unroll 1
+    for (; rel > 0; rel -= FWD_BATCH) {
+#pragma unroll
+      for (int i = 0; i < FWD_BATCH; ++i) step(i);
+      gate.load(rel - FWD_BATCH, g);
+      value.load(rel - FWD_BATCH, x);
     }
   }
   publish<V, VEC>(a, it.index, it.strip, c, m, cut);
@@ -588,62 +596,63 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
   if (a.chunks == 0) return check_offsets(a, blockIdx.x, gridDim.x, empty_row);
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
   Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0, c, left), value(a.value, a.value_stride, it.t0, c, left), to(out, out_stride, it.t0, c, left);
-  Raw<T, V> g[REC_BATCH], x[REC_BATCH];
-  gate.load(live_bits(tokens), g);
-  value.load(live_bits(tokens), x);
+  Raw<T, V> g[FWD_BATCH], x[FWD_BATCH];
+  gate.load(tokens, g);
+  value.load(tokens, x);
   check_offsets(a, it.number, (int64_t)a.chunks * a.strips, empty_row);
   Borders q = {0, 0, 0, 0, find_sequence(a, it.t0)};
   Channels<V> h = all<V>(0.f);
 #pragma unroll 1
-  for (int rel = 0; rel < tokens; rel += REC_BATCH) {
+  for (int rel = 0; rel < tokens;) {
     if (rel % REC_PART == 0) {
       q = find_borders(a, q.lo, it.t0 + rel, min(it.t0 + rel + REC_PART, it.t1), it.t1, first_of, last_of);
       if (rel == 0) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c, !(q.first & 1), true);
     }
-    gate.next();
-    value.next();
-    const uint32_t live = live_bits(tokens - rel), firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
-    if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
-    uint32_t ta = to.lane;
-    if (!(firsts | lasts) && tokens - rel >= 2 * REC_BATCH) {
-      uint32_t ga = gate.lane, xa = value.lane;
+    // tokens of the part before the next border; twice FWD_BATCH at a time as long as the next FWD_BATCH exist
+    const unsigned long long ahead = (q.first | q.last) >> (rel % REC_PART);
+    const int clear = min(ahead ? __ffsll(ahead) - 1 : REC_PART - rel % REC_PART, tokens - rel - FWD_BATCH);
+    if (clear >= 2 * FWD_BATCH && rel % (2 * FWD_BATCH) == 0) {
+#pragma unroll 1
+      for (const int end = rel + clear / (2 * FWD_BATCH) * (2 * FWD_BATCH); rel < end; rel += 2 * FWD_BATCH) {
+        if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
 #pragma unroll
-      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step, ta += to.step) {
-        const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), nx = unpack<T, V, true>(x[i]);
-        g[i] = gate.get(ga);
-        x[i] = value.get(xa);
-        h = blend(nz, nx, h);
-        to.put(ta, h);
+        for (int i = 0; i < 2 * FWD_BATCH; ++i, to.at += to.stride) {
+          const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i % FWD_BATCH])), nx = unpack<T, V, true>(x[i % FWD_BATCH]);
+          g[i % FWD_BATCH] = gate.next();
+          x[i % FWD_BATCH] = value.next();
+          h = blend(nz, nx, h);
+          to.put(h);
+        }
       }
     } else {
+      const uint32_t firsts = batch_bits<FWD_BATCH>(q.first, rel), lasts = batch_bits<FWD_BATCH>(q.last, rel);
+      if (entry && rel % REC_BATCH == 0) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
+      const int live = tokens - rel;
+      Channels<V> s[FWD_BATCH];
 #pragma unroll
-      for (int i0 = 0; i0 < REC_BATCH; i0 += 4) {
-        Channels<V> s[4];
-#pragma unroll
-        for (int i = i0; i < i0 + 4; ++i) {
-          s[i - i0] = all<V>(0.f);
-          if (firsts >> i & 1) {
-            // the start of a sequence that goes on behind the chunk was kept by the first pass: h_final may be the same array as
-            // h0, and the warp that writes it does not wait for this one
-            const int f = first_of[rel % REC_PART + i];
-            if (f < 0) s[i - i0] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
-            else if (a.h0) s[i - i0] = get<V, VEC>(a.h0 + (int64_t)f * a.D + c, left);
-          }
-        }
-#pragma unroll
-        for (int i = i0; i < i0 + 4; ++i, ta += to.step) {
-          if (live >> i & 1) {
-            if (firsts >> i & 1) h = s[i - i0];
-            h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
-            to.put(ta, h);
-            if ((lasts >> i & 1) && h_final) put<V, VEC>(h_final + (int64_t)last_of[rel % REC_PART + i] * a.D + c, left, h);
-          }
+      for (int i = 0; i < FWD_BATCH; ++i) {
+        s[i] = all<V>(0.f);
+        if (firsts >> i & 1) {
+          // the start of a sequence that goes on behind the chunk was kept with the chunk's map: h_final may be the same array as h0,
+          // and the warp that writes it does not wait for this one
+          const int f = first_of[rel % REC_PART + i];
+          if (f < 0) s[i] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
+          else if (a.h0) s[i] = get<V, VEC>(a.h0 + (int64_t)f * a.D + c, left);
         }
       }
-      gate.load(live_bits(tokens - rel - REC_BATCH), g);
-      value.load(live_bits(tokens - rel - REC_BATCH), x);
+#pragma unroll
+      for (int i = 0; i < FWD_BATCH; ++i, to.at += to.stride) {
+        if (i < live) {
+          if (firsts >> i & 1) h = s[i];
+          h = blend(minus_sigmoid(unpack<T, V>(g[i])), unpack<T, V, true>(x[i]), h);
+          to.put(h);
+          if ((lasts >> i & 1) && h_final) put<V, VEC>(h_final + (int64_t)last_of[rel % REC_PART + i] * a.D + c, left, h);
+        }
+      }
+      gate.load(live - FWD_BATCH, g);
+      value.load(live - FWD_BATCH, x);
+      rel += FWD_BATCH;
     }
-    to.next();
   }
 }
 
@@ -663,22 +672,19 @@ __device__ __forceinline__ void backward_map(const RecArgs& a, const Piece& it, 
     int rel = (tokens - 1) & ~(REC_BATCH - 1);
     Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), grad(grad_out, grad_out_stride, it.t0 + rel, c, left);
     Raw<T, V> g[REC_BATCH], d[REC_BATCH];
-    gate.load(live_bits(tokens - rel), g);
-    grad.load(live_bits(tokens - rel), d);
+    gate.load(tokens - rel, g);
+    grad.load(tokens - rel, d);
+    gate.move(-REC_BATCH);                                              // to the batch's first row: rows before it come next
+    grad.move(-REC_BATCH);
 #pragma unroll 1
     for (; rel >= 0; rel -= REC_BATCH) {
       const int here = tokens - rel;
-      if (rel > 0) {
-        gate.previous();
-        grad.previous();
-      }
-      uint32_t ga = gate.lane + (REC_BATCH - 1) * gate.step, da = grad.lane + (REC_BATCH - 1) * grad.step;
 #pragma unroll
-      for (int i = REC_BATCH - 1; i >= 0; --i, ga -= gate.step, da -= grad.step) {
+      for (int i = REC_BATCH - 1; i >= 0; --i) {
         const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i])), dv = unpack<T, V>(d[i]);
         if (rel > 0) {
-          g[i] = gate.get(ga);
-          d[i] = grad.get(da);
+          g[i] = gate.previous();
+          d[i] = grad.previous();
         }
         if (i < here) {
           const Channels<V> G = dv + m.B;
@@ -708,13 +714,15 @@ recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, con
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
   int rel = (tokens - 1) & ~(REC_BATCH - 1);
   Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0 + rel, c, left), value(a.value, a.value_stride, it.t0 + rel, c, left),
-      grad(grad_out, grad_out_stride, it.t0 + rel, c, left), to_gate(grad_gate, grad_gate_stride, it.t0 + rel, c, left),
-      to_value(grad_value, grad_value_stride, it.t0 + rel, c, left);
+      grad(grad_out, grad_out_stride, it.t0 + rel, c, left), to_gate(grad_gate, grad_gate_stride, it.t0 + rel + REC_BATCH, c, left),
+      to_value(grad_value, grad_value_stride, it.t0 + rel + REC_BATCH, c, left);
   Raw<T, V> g[REC_BATCH], x[REC_BATCH], d[REC_BATCH];
-  gate.load(live_bits(tokens - rel), g);
-  value.load(live_bits(tokens - rel), x);
-  grad.load(live_bits(tokens - rel), d);
-  // the parts from the last: each one's first sequence is found anew, from that of the chunk's first token on
+  gate.load(tokens - rel, g);
+  value.load(tokens - rel, x);
+  grad.load(tokens - rel, d);
+  gate.move(-2 * REC_BATCH);                                            // to the batch before; the gradient to the first row of this one
+  value.move(-2 * REC_BATCH);
+  grad.move(-REC_BATCH);
   check_offsets(a, it.number, (int64_t)a.chunks * a.strips, empty_row);
   const int lo = find_sequence(a, it.t0);
   Borders q = {0, 0, 0, 0, lo};
@@ -729,35 +737,32 @@ recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, con
                                      !(q.last >> ((tokens - 1) % REC_PART) & 1), false);
     }
     const int64_t t = it.t0 + rel;
-    const uint32_t live = live_bits(tokens - rel), firsts = batch_bits(q.first, rel), lasts = batch_bits(q.last, rel);
-    if (rel > 0) {
-      gate.previous();
-      value.previous();
-      grad.previous();
-    }
+    const int live = tokens - rel;
+    const uint32_t firsts = batch_bits<REC_BATCH>(q.first, rel), lasts = batch_bits<REC_BATCH>(q.last, rel);
     Channels<V> h = all<V>(0.f), nz[REC_BATCH], away[REC_BATCH];        // away: - (value - state before the token)
     if (!(firsts & 1)) h = get<V, VEC>(entry + t / REC_BATCH * a.D + c, left);
-    const uint32_t last_row = REC_BATCH - 1;
-    uint32_t va = to_value.lane + last_row * to_value.step, za = to_gate.lane + last_row * to_gate.step;
-    if (!(firsts | lasts) && live == ALL_LIVE && rel > 0) {
-      uint32_t ga = gate.lane, xa = value.lane, da = grad.lane + last_row * grad.step;
+    if (!(firsts | lasts) && live >= REC_BATCH && rel > 0) {
 #pragma unroll
-      for (int i = 0; i < REC_BATCH; ++i, ga += gate.step, xa += value.step) {
+      for (int i = 0; i < REC_BATCH; ++i) {
         const Channels<V> nx = unpack<T, V, true>(x[i]);
         nz[i] = minus_sigmoid(unpack<T, V>(g[i]));
-        g[i] = gate.get(ga);
-        x[i] = value.get(xa);
+        g[i] = gate.next();
+        x[i] = value.next();
         away[i] = nx + h;
         h = blend(nz[i], nx, h);
       }
 #pragma unroll
-      for (int i = REC_BATCH - 1; i >= 0; --i, da -= grad.step, va -= to_value.step, za -= to_gate.step) {
+      for (int i = REC_BATCH - 1; i >= 0; --i) {
         const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;          // -z G
-        d[i] = grad.get(da);
+        d[i] = grad.previous();
         carry = fma(nz[i], G, G);
-        to_value.put(va, nG * all<V>(-1.f));
-        to_gate.put(za, nG * fma(nz[i], away[i], away[i]));
+        to_value.at -= to_value.stride;
+        to_gate.at -= to_gate.stride;
+        to_value.put(nG * all<V>(-1.f));
+        to_gate.put(nG * fma(nz[i], away[i], away[i]));
       }
+      gate.move(-2 * REC_BATCH);
+      value.move(-2 * REC_BATCH);
     } else {
 #pragma unroll
       for (int i = 0; i < REC_BATCH; ++i) {
@@ -768,23 +773,27 @@ recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, con
         h = blend(nz[i], nx, h);
       }
 #pragma unroll
-      for (int i = REC_BATCH - 1; i >= 0; --i, va -= to_value.step, za -= to_gate.step) {
-        if (live >> i & 1) {
+      for (int i = REC_BATCH - 1; i >= 0; --i) {
+        to_value.at -= to_value.stride;
+        to_gate.at -= to_gate.stride;
+        if (i < live) {
           if (lasts >> i & 1) carry = grad_final ? get<V, VEC>(grad_final + (int64_t)last_of[rel % REC_PART + i] * a.D + c, left) : all<V>(0.f);
           const Channels<V> G = unpack<T, V>(d[i]) + carry, nG = nz[i] * G;
           carry = fma(nz[i], G, G);
-          to_value.put(va, nG * all<V>(-1.f));
-          to_gate.put(za, nG * fma(nz[i], away[i], away[i]));
+          to_value.put(nG * all<V>(-1.f));
+          to_gate.put(nG * fma(nz[i], away[i], away[i]));
           if ((firsts >> i & 1) && grad_h0) put<V, VEC>(grad_h0 + (int64_t)first_of[rel % REC_PART + i] * a.D + c, left, carry);
         }
       }
-      const uint32_t next = rel > 0 ? ALL_LIVE : 0u;
+      const int next = rel > 0 ? REC_BATCH : 0;
+      grad.move(-REC_BATCH);
       gate.load(next, g);
       value.load(next, x);
       grad.load(next, d);
+      gate.move(-2 * REC_BATCH);
+      value.move(-2 * REC_BATCH);
+      grad.move(-REC_BATCH);
     }
-    to_gate.previous();
-    to_value.previous();
   }
 }
 
@@ -813,7 +822,6 @@ int check_workspace(const char* what, const void* workspace, size_t have, size_t
 // An [N, D] argument: present when there are tokens, rows that do not overlap, elements on their own boundary.
 int check_rows(const char* what, const char* name, const void* p, int64_t stride, int64_t N, int32_t D, int32_t dtype) {
   if (N == 0) return MTS_OK;
-  if (stride >= (1ll << 28) / dtype_bytes(dtype)) return set_error(MTS_ERR_UNSUPPORTED, "%s: %s has rows %lld elements apart", what, name, (long long)stride);
   if (!p || stride < D) return set_error(MTS_ERR_INVALID_ARG, "%s: %s is null or its rows overlap (stride %lld, D %d)", what, name, (long long)stride, D);
   if ((uintptr_t)p % dtype_bytes(dtype)) return set_error(MTS_ERR_ALIGNMENT, "%s: %s is no multiple of its element size", what, name);
   return MTS_OK;

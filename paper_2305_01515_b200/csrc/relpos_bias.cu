@@ -59,6 +59,9 @@ relpos_forward_direct(const __grid_constant__ Buckets b, BiasGeometry g, const v
 // 16 / sizeof(T) positions that a 16-byte boundary can have in it, so that every row is one bulk copy to global memory from an
 // aligned place of one of the copies, whatever its window and the alignment of the row; up to 15 bytes at either end of a row are
 // stored by threads.
+#ifndef MTS_RELPOS_BLOCKS
+#define MTS_RELPOS_BLOCKS (148 * 2)
+#endif
 #ifndef MTS_RELPOS_DIRECT
 #define MTS_RELPOS_DIRECT 8
 #endif
@@ -355,16 +358,18 @@ extern "C" int mts_relpos_bias_forward(const mts_relpos_buckets* buckets, const 
       relpos_forward_direct<T><<<grid, 256, 0, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride);
       return check_launch(what);
     }
-    // rows of a block: as many as leave the GPU four blocks per SM, 128 at most (the vector is made once for all of them), and not
+    // rows of a block: as many as leave the GPU two blocks per SM, 128 at most (the vector is made once for all of them), and not
     // more blocks down than a grid has room for
     const int64_t strips = ceil_div(Lk, FWD_COLS);
     int rows = 128;
-    while (rows > 8 && ceil_div(Lq, rows) * strips * heads < 148 * 4) rows /= 2;
+    while (rows > 8 && ceil_div(Lq, rows) * strips * heads < MTS_RELPOS_BLOCKS) rows /= 2;
     while (ceil_div(Lq, rows) > 65535) rows *= 2;
     const int pitch = (int)align_up((size_t)(Lk < FWD_COLS ? Lk : FWD_COLS) + (size_t)rows, 16);
     const size_t smem = (size_t)pitch * 16;
-    int e = check_cuda(cudaFuncSetAttribute(relpos_forward_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "shared memory size");
-    if (e != MTS_OK) return e;
+    if (smem > 48 * 1024) {
+      const int e = check_cuda(cudaFuncSetAttribute(relpos_forward_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), "shared memory size");
+      if (e != MTS_OK) return e;
+    }
     const dim3 grid((unsigned)strips, (unsigned)ceil_div(Lq, rows), (unsigned)heads);
     relpos_forward_rows<T><<<grid, FWD_THREADS, smem, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride, rows, pitch);
     return check_launch(what);
