@@ -56,24 +56,23 @@ constexpr uint32_t CODE_ONE = 0x3F8;                    // 1.0f >> 20
 constexpr uint32_t BASE_M = CODE_ONE - 127, BASE_V = CODE_ONE - 255;
 constexpr uint32_t SMALLEST_TOP = 0x03800000;           // 2^-120: below it the inverse of the scale would overflow
 
-__device__ __forceinline__ float decode_first(uint32_t code, float scale) {
-  const uint32_t mag = code & 0x7F;
-  const float x = mag ? __fmul_rn(__uint_as_float((mag + BASE_M) << 20), scale) : 0.f;
-  return (code & 0x80) ? -x : x;
+__device__ __forceinline__ float decode_first(uint32_t code, float scale) {      // -0 for code 0x80
+  const uint32_t mag = code & 0x7F, bits = mag ? (mag + BASE_M) << 20 : 0u;
+  return __fmul_rn(__uint_as_float(bits | ((code << 24) & 0x80000000u)), scale);
 }
 __device__ __forceinline__ float decode_second(uint32_t code, float scale) {
-  return code ? __fmul_rn(__uint_as_float((code + BASE_V) << 20), scale) : 0.f;
+  return __fmul_rn(__uint_as_float(code ? (code + BASE_V) << 20 : 0u), scale);
 }
-// inv: 1 / the block's largest magnitude.  Rounded to nearest (halves away from zero).
+// inv: 1 / the block's largest magnitude, so that |x| inv is 1 at most, or the number after it.  Rounded to nearest (halves away from
+// zero): half a step is put on top of the 20 dropped bits.
 __device__ __forceinline__ uint32_t encode_first(float x, float inv) {
-  const uint32_t q = min((__float_as_uint(__fmul_rn(fabsf(x), inv)) + 0x80000u) >> 20, CODE_ONE);
-  const uint32_t code = q > BASE_M ? q - BASE_M : 0u;
-  return code | ((__float_as_uint(x) >> 24) & (code ? 0x80u : 0u));
+  const uint32_t bits = __float_as_uint(__fmul_rn(x, inv));
+  return (max(((bits & 0x7FFFFFFFu) + 0x80000u) >> 20, BASE_M) - BASE_M) | ((bits >> 24) & 0x80u);
 }
-// add: what is put on top of the 20 dropped bits: half a step, or random bits below a whole step.
+// add: half a step, or random bits below a whole step.  Not 0 for x > 0.
 __device__ __forceinline__ uint32_t encode_second(float x, float inv, uint32_t add) {
-  const uint32_t q = min((__float_as_uint(__fmul_rn(x, inv)) + add) >> 20, CODE_ONE);
-  return x > 0.f ? max(q, BASE_V + 1u) - BASE_V : 0u;
+  const uint32_t q = max((__float_as_uint(__fmul_rn(x, inv)) + add) >> 20, BASE_V + 1u) - BASE_V;
+  return x > 0.f ? q : 0u;
 }
 // 16 random bits of (element, seed) in the upper half of the word: two rounds of multiply and shift.
 __device__ __forceinline__ uint32_t mix(uint32_t element, uint32_t seed_word) {
@@ -82,36 +81,49 @@ __device__ __forceinline__ uint32_t mix(uint32_t element, uint32_t seed_word) {
   w = (w ^ (w >> 12)) * 0x297A2D39u;
   return w;
 }
-// Bits of |x|, 0 for infinities and NaN: fp32 magnitudes compare like their bits.
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
-}
-
-// A warp's block of moments to codes and scales.  RANDOM: second moments by random bits, else to nearest.
+// A warp's block of moments to codes and scales.  RANDOM: second moments by random bits, else to nearest.  fp32 magnitudes compare like
+// their bits; what is not finite is above all others.
 template <bool RANDOM>
-__device__ __forceinline__ void encode_block(const float (&m)[8], const float (&v)[8], int64_t block, uint32_t seed_word,
-                                             const AdamState& st) {
+__device__ __forceinline__ void encode_block(float (&m)[8], float (&v)[8], int64_t block, uint32_t seed_word, const AdamState& st) {
+  constexpr uint32_t NOT_FINITE = 0x7F800000u;
   uint32_t tm = 0, tv = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    tm = max(tm, finite_bits(m[k]));
-    tv = max(tv, finite_bits(v[k]));
+    tm = max(tm, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+    tv = max(tv, __float_as_uint(v[k]));
   }
   tm = __reduce_max_sync(0xFFFFFFFFu, tm);
   tv = __reduce_max_sync(0xFFFFFFFFu, tv);
-  if (tm < SMALLEST_TOP) tm = 0;
-  if (tv < SMALLEST_TOP) tv = 0;
-  const float inv_m = __frcp_rn(__uint_as_float(tm)), inv_v = __frcp_rn(__uint_as_float(tv));
+  if (max(tm, tv) >= NOT_FINITE) {                                      // the whole warp: stored as 0, the rest by the largest of them
+    tm = tv = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if ((__float_as_uint(m[k]) & 0x7FFFFFFFu) >= NOT_FINITE) m[k] = 0.f;
+      if (__float_as_uint(v[k]) >= NOT_FINITE) v[k] = 0.f;
+      tm = max(tm, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+      tv = max(tv, __float_as_uint(v[k]));
+    }
+    tm = __reduce_max_sync(0xFFFFFFFFu, tm);
+    tv = __reduce_max_sync(0xFFFFFFFFu, tv);
+  }
   const int64_t at = block * ADAM_BLOCK + lane_id() * 8;
   uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
+  if (tm >= SMALLEST_TOP) {
+    const float inv = __frcp_rn(__uint_as_float(tm));
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t add = RANDOM ? (mix((uint32_t)at + k, seed_word) >> 16) << 4 : 0x80000u;
-    const uint32_t a = (tm && finite_bits(m[k])) ? encode_first(m[k], inv_m) : 0u;
-    const uint32_t b = (tv && finite_bits(v[k])) ? encode_second(v[k], inv_v, add) : 0u;
-    cm[k / 4] |= a << (8 * (k % 4));
-    cv[k / 4] |= b << (8 * (k % 4));
+    for (int k = 0; k < 8; ++k) cm[k / 4] |= encode_first(m[k], inv) << (8 * (k % 4));
+  } else {
+    tm = 0;
+  }
+  if (tv >= SMALLEST_TOP) {
+    const float inv = __frcp_rn(__uint_as_float(tv));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t add = RANDOM ? (mix((uint32_t)at + k, seed_word) >> 12) & 0xFFFF0u : 0x80000u;
+      cv[k / 4] |= encode_second(v[k], inv, add) << (8 * (k % 4));
+    }
+  } else {
+    tv = 0;
   }
   *reinterpret_cast<uint2*>(st.m8 + at) = make_uint2(cm[0], cm[1]);
   *reinterpret_cast<uint2*>(st.v8 + at) = make_uint2(cv[0], cv[1]);
@@ -184,8 +196,11 @@ adamw_step_kernel(const AdamTensor* __restrict__ tensors, const void* const* __r
     const float gk = __fmul_rn(g[k], scale);
     m[k] = __fadd_rn(__fmul_rn(m[k], c.beta1), __fmul_rn(gk, c.one_minus_beta1));
     v[k] = __fadd_rn(__fmul_rn(v[k], c.beta2), __fmul_rn(__fmul_rn(gk, gk), c.one_minus_beta2));
-    const float root = fmaf(__fsqrt_rn(v[k]), c.inv_root2, c.eps);
-    p[k] = fmaf(-c.rate, __fdividef(m[k], root), fmaf(-decay, p[k], p[k]));
+    // hardware root and reciprocal: an update's last two units of 2^-23
+    float root, inv;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[k]));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(root, c.inv_root2, c.eps)));
+    p[k] = fmaf(-c.rate, m[k] * inv, fmaf(-decay, p[k], p[k]));
   }
   if (t.master) store_some(t.master + e, count, p);
   store_some(param, count, p);
@@ -206,12 +221,8 @@ adamw_export_kernel(AdamState st, int64_t blocks, float* __restrict__ m_out, flo
   float m[8], v[8];
   decode_block(*reinterpret_cast<const uint2*>(st.m8 + at), *reinterpret_cast<const uint2*>(st.v8 + at),
                st.m_scale[block], st.v_scale[block], m, v);
-  float4* mo = reinterpret_cast<float4*>(m_out + at);
-  float4* vo = reinterpret_cast<float4*>(v_out + at);
-  mo[0] = make_float4(m[0], m[1], m[2], m[3]);
-  mo[1] = make_float4(m[4], m[5], m[6], m[7]);
-  vo[0] = make_float4(v[0], v[1], v[2], v[3]);
-  vo[1] = make_float4(v[4], v[5], v[6], v[7]);
+  store_some(m_out + at, 8, m);
+  store_some(v_out + at, 8, v);
 }
 
 __global__ void __launch_bounds__(ADAM_WARPS * 32)
