@@ -1,0 +1,122 @@
+"""The tower's functions inside torch's autograd, against the same formulas in torch (64 bits), and the example that trains a table and a
+tower together."""
+import os
+import sys
+
+import pytest
+import torch
+
+from paper_2305_01515_b200 import binding as mb
+from paper_2305_01515_b200 import sequence as sq
+
+pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+
+def recurrence_64(gate, value, offsets, h0):
+    h, out, final = None, [], []
+    for s in range(len(offsets) - 1):
+        h = h0[s]
+        for t in range(offsets[s], offsets[s + 1]):
+            h = h + torch.sigmoid(gate[t]) * (value[t] - h)
+            out.append(h)
+        final.append(h)
+    return torch.stack(out), torch.stack(final)
+
+
+def test_gated_recurrence_in_autograd():
+    g = torch.Generator(device="cuda").manual_seed(0)
+    off = [0, 5, 5, 30, 31]
+    both = torch.randn(31, 2 * 24, generator=g, device="cuda").requires_grad_()
+    h0 = torch.randn(4, 24, generator=g, device="cuda").requires_grad_()
+    w, wf = torch.randn(31, 24, generator=g, device="cuda"), torch.randn(4, 24, generator=g, device="cuda")
+    out, final = sq.gated_recurrence(*both.chunk(2, dim=1), torch.tensor(off, device="cuda"), h0)
+    got = torch.autograd.grad((out * w).sum() + (final * wf).sum(), (both, h0))
+    b64, h64 = both.detach().double().requires_grad_(), h0.detach().double().requires_grad_()
+    o64, f64 = recurrence_64(*b64.chunk(2, dim=1), off, h64)
+    want = torch.autograd.grad((o64 * w.double()).sum() + (f64 * wf.double()).sum(), (b64, h64))
+    # 25 steps of values around 4 at most: a few hundred units of 2^-24 of sums of 25 terms
+    assert float((out.double() - o64).abs().max()) < 1e-4 and float((final.double() - f64).abs().max()) < 1e-4
+    for x, y in zip(got, want):
+        assert float((x.double() - y).abs().max()) < 2e-3 * float(y.abs().max())
+
+
+def test_relpos_bias_in_autograd():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    buckets = mb.RelposBuckets(sq.log_bucket_starts(8, 20), two_sided=True)
+    table = torch.randn(buckets.rows, 3, generator=g, device="cuda").requires_grad_()
+    scores = torch.randn(5, 3, 33, 40, generator=g, device="cuda").requires_grad_()
+    w = torch.randn(5, 3, 33, 40, generator=g, device="cuda")
+    bias = sq.relpos_bias(table, buckets, 33, 40, q_offset=7)
+    (a,) = torch.autograd.grad(((scores.detach() + bias) * w).sum(), table)
+    d_scores, b = torch.autograd.grad((sq.add_relpos_bias(scores, table, buckets, q_offset=7) * w).sum(), (scores, table))
+    assert torch.equal(d_scores, w)
+    one = torch.zeros(buckets.rows, 3, dtype=torch.float64, device="cuda")
+    for k in range(buckets.rows):            # every bucket on its own: the bias is linear in the table
+        t = torch.zeros(buckets.rows, 3, device="cuda")
+        t[k] = 1.0
+        one[k] = (sq.relpos_bias(t, buckets, 33, 40, q_offset=7).double() * w.double().sum(0)).sum((1, 2))
+    for x in (a, b):                         # sums of up to 6600 terms of size 4 at most, rounded in fp32 along the way
+        assert float((x.double() - one).abs().max()) < 6600 * 4 * 1e-6
+
+
+def test_log_bucket_starts():
+    assert sq.log_bucket_starts(32, 128)[:17] == list(range(17)) and sq.log_bucket_starts(32, 128)[-1] == 128
+    for n, far in ((1, 5), (2, 1), (8, 20), (16, 64), (33, 1000)):
+        s = sq.log_bucket_starts(n, far)
+        assert len(s) == n and s[0] == 0 and s == sorted(s) and (n < 3 or s[-1] == far)
+    with pytest.raises(ValueError):
+        sq.log_bucket_starts(32, 8)
+
+
+@pytest.mark.parametrize("bits,masters,dtype", [(32, False, torch.float32), (8, False, torch.float32), (32, True, torch.bfloat16)])
+def test_adamw_against_torch(bits, masters, dtype):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    params = [torch.randn(*s, generator=g, device="cuda").to(dtype).requires_grad_() for s in ((300, 7), (11,), (64, 64))]
+    other = [p.detach().double().requires_grad_() for p in params]
+    mine = sq.AdamW(params, lr=1e-2, weight_decay=0.1, state_bits=bits, masters=masters)
+    theirs = torch.optim.AdamW([dict(params=[p for p in other if p.dim() > 1]), dict(params=[p for p in other if p.dim() == 1], weight_decay=0.0)],
+                               lr=1e-2, weight_decay=0.1)
+    for k in range(5):
+        for p, o in zip(params, other):
+            p.grad = torch.randn(p.shape, generator=g, device="cuda").to(dtype)          # new gradient tensors every step
+            o.grad = p.grad.double()
+        mine.step()
+        theirs.step()
+    for k, (p, o) in enumerate(zip(params, other)):
+        got = mine.masters[k].double() if masters else p.double()
+        # 8 bits: an update of at most lr is off by half a code of m and of the root of v a step, about an eighth of it
+        assert float((got.detach() - o.detach()).abs().max()) < (5 * 1e-2 * 0.2 if bits == 8 else 1e-5)
+
+
+def test_refusals():
+    x = torch.zeros(4, 8, device="cuda")
+    off = torch.tensor([0, 4], device="cuda")
+    for args in ((x, x[:, :4], off), (x, x.half(), off), (x, x, off.int()), (x, x, off.cpu()), (x, x, off, torch.zeros(2, 8, device="cuda"))):
+        with pytest.raises(ValueError):
+            sq.gated_recurrence(*args)
+    with pytest.raises(TypeError):
+        sq.gated_recurrence(x.double(), x.double(), off)
+    with pytest.raises(ValueError):
+        sq.relpos_bias(x, mb.RelposBuckets([0, 1]), 3, 3)
+    with pytest.raises(ValueError):
+        sq.AdamW([x.requires_grad_(), torch.zeros(3, device="cuda").half()])
+
+
+def test_example_trains_a_table_and_a_tower():
+    import history_tower
+
+    tower = history_tower.HistoryTower(rows=3000, S=16, L=40, seed=3)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    indices = torch.randint(3000, (16 * 40,), generator=g, device="cuda")
+    target = torch.randn(16, tower.D, generator=g, device="cuda")
+    before = tower.table.weights_numpy()
+    losses = [float(tower.step(indices, target)) for _ in range(25)]
+    after = tower.table.weights_numpy()
+    assert losses[-1] < 0.5 * losses[0], losses
+    assert (before != after).any() and tower.table.tables.status() == 0
+    touched = set(indices.cpu().tolist())
+    rows = (before.reshape(3000, -1) != after.reshape(3000, -1)).any(1)
+    assert all(not rows[r] for r in range(3000) if r not in touched)
+    tower.close()
