@@ -26,7 +26,7 @@
 namespace mts {
 
 #ifndef MTS_REC_FWD_BLOCKS
-#define MTS_REC_FWD_BLOCKS 24
+#define MTS_REC_FWD_BLOCKS 16
 #endif
 #ifndef MTS_REC_BWD_BLOCKS
 #define MTS_REC_BWD_BLOCKS 12
@@ -35,10 +35,10 @@ namespace mts {
 #define MTS_REC_WARPS_WANTED 1776
 #endif
 #ifndef MTS_REC_LAG
-#define MTS_REC_LAG 2048
+#define MTS_REC_LAG 4096
 #endif
 #ifndef MTS_REC_MAX_CHUNK
-#define MTS_REC_MAX_CHUNK 128
+#define MTS_REC_MAX_CHUNK 256
 #endif
 constexpr int REC_CHUNK = MTS_REC_MAX_CHUNK;      // tokens of a chunk at most
 constexpr int REC_PART = 64;                      // tokens whose borders are looked up together: a bit mask of them is one word
@@ -524,8 +524,12 @@ __device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel)
 // In all four walks a row's registers take the row one batch ahead as soon as they have been read: a batch is always on its way.
 
 // ------------------------------------------------------------------------------- forward
-constexpr int FWD_BATCH = 4;           // rows on their way: with 8 the registers leave room for fewer warps
-static_assert(REC_BATCH == 2 * FWD_BATCH, "a state is kept where a batch begins");
+#ifndef MTS_REC_FWD_BATCH
+#define MTS_REC_FWD_BATCH 8
+#endif
+constexpr int FWD_BATCH = MTS_REC_FWD_BATCH;           // rows on their way
+constexpr int FWD_STEP = REC_BATCH;    // tokens of one turn of the inner loops
+static_assert(FWD_STEP % FWD_BATCH == 0, "a state is kept where a batch begins");
 
 template <typename T, int V, bool VEC>
 __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
@@ -564,9 +568,9 @@ __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
     };
     rel = later;                                                        // tokens to go, FWD_BATCH of them in registers
 #pragma unroll 1
-    for (; rel >= 3 * FWD_BATCH; rel -= 2 * FWD_BATCH) {
+    for (; rel >= FWD_STEP + FWD_BATCH; rel -= FWD_STEP) {
 #pragma unroll
-      for (int i = 0; i < 2 * FWD_BATCH; ++i) {
+      for (int i = 0; i < FWD_STEP; ++i) {
         step(i % FWD_BATCH);
         g[i % FWD_BATCH] = gate.next();
         x[i % FWD_BATCH] = value.next();
@@ -608,15 +612,15 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
       q = find_borders(a, q.lo, it.t0 + rel, min(it.t0 + rel + REC_PART, it.t1), it.t1, first_of, last_of);
       if (rel == 0) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c, !(q.first & 1), true);
     }
-    // tokens of the part before the next border; twice FWD_BATCH at a time as long as the next FWD_BATCH exist
+    // tokens of the part before the next border; FWD_STEP at a time as long as the FWD_BATCH behind them exist
     const unsigned long long ahead = (q.first | q.last) >> (rel % REC_PART);
     const int clear = min(ahead ? __ffsll(ahead) - 1 : REC_PART - rel % REC_PART, tokens - rel - FWD_BATCH);
-    if (clear >= 2 * FWD_BATCH && rel % (2 * FWD_BATCH) == 0) {
+    if (clear >= FWD_STEP && rel % FWD_STEP == 0) {
 #pragma unroll 1
-      for (const int end = rel + clear / (2 * FWD_BATCH) * (2 * FWD_BATCH); rel < end; rel += 2 * FWD_BATCH) {
+      for (const int end = rel + clear / FWD_STEP * FWD_STEP; rel < end; rel += FWD_STEP) {
         if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
 #pragma unroll
-        for (int i = 0; i < 2 * FWD_BATCH; ++i, to.at += to.stride) {
+        for (int i = 0; i < FWD_STEP; ++i, to.at += to.stride) {
           const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i % FWD_BATCH])), nx = unpack<T, V, true>(x[i % FWD_BATCH]);
           g[i % FWD_BATCH] = gate.next();
           x[i % FWD_BATCH] = value.next();
