@@ -211,8 +211,8 @@ def _check(rc: int) -> None:
 
 
 def _ptr(x):
-    if x is None:
-        return None
+    if x is None or type(x) is int:
+        return x
     if isinstance(x, int):
         return x
     return x.data_ptr()

@@ -43,6 +43,7 @@ namespace mts {
 constexpr int REC_CHUNK = MTS_REC_MAX_CHUNK;      // tokens of a chunk at most
 constexpr int REC_PART = 64;                      // tokens whose borders are looked up together: a bit mask of them is one word
 constexpr int REC_BATCH = 8;                      // tokens in registers, and between two states kept for the backward
+constexpr int REC_SHORT = 4096;                   // tokens of a call that threads may walk one by one
 constexpr int REC_RADIX_BITS = 3;
 constexpr int REC_RADIX = 1 << REC_RADIX_BITS;    // maps composed into one of the next level
 constexpr int REC_LEVELS = 4;                     // levels of maps, chunks included; a state is kept behind every map of the highest, 512 chunks
@@ -366,28 +367,25 @@ __device__ __forceinline__ void publish(const RecArgs& a, int index, int strip, 
   set_ready(kept.ready + (int64_t)(index + 1) * a.strips + strip, READY_MAP);
 }
 
-// The state before chunk `index`, whose first sequence (in the order of the walk) began in chunk `from` < index.  Also waits for the
-// chunk's own map where `own` says so.
+// The state before chunk `index`, whose first sequence (in the order of the walk) began in chunk `from` < index.
 template <int V, bool VEC>
-__device__ __forceinline__ Channels<V> state_before(const RecArgs& a, int index, int strip, int from, int c, bool want, bool own) {
+__device__ __forceinline__ Channels<V> state_before(const RecArgs& a, int index, int strip, int from, int c) {
   from = max(0, min(from, index - 1));
   // lane 8 l + k: map k of level l, of those between the start of the next level's map (or `from`) and the chunk, seven at most; lane 31:
-  // the kept state, lane 23: the chunk's own map
+  // the kept state
   const int l = lane_id() / REC_RADIX, shift = l * REC_RADIX_BITS, k = lane_id() % REC_RADIX;
   const int at = index >> shift, parent = at >> REC_RADIX_BITS << REC_RADIX_BITS;
   // a level is used where the one below does not reach back to `from`
-  const bool used = want && l < REC_LEVELS - 1 && from >> shift < at && (l == 0 || from >> (shift - REC_RADIX_BITS) < (index >> (shift - REC_RADIX_BITS) >> REC_RADIX_BITS << REC_RADIX_BITS));
+  const bool used = l < REC_LEVELS - 1 && from >> shift < at && (l == 0 || from >> (shift - REC_RADIX_BITS) < (index >> (shift - REC_RADIX_BITS) >> REC_RADIX_BITS << REC_RADIX_BITS));
   const int lo = max(from >> shift, parent);
   const bool mine = used && k < REC_RADIX - 1 && lo + k < at;
   constexpr int TOP = (REC_LEVELS - 1) * REC_RADIX_BITS;
   const int top = index >> TOP;
-  const bool kept = want && from < top << TOP;
+  const bool kept = from < top << TOP;
   const uint32_t* flag = mine ? a.level[l].ready + (int64_t)(lo + k) * a.strips + strip : nullptr;
   if (lane_id() == 31 && kept) flag = a.level[REC_LEVELS].ready + (int64_t)top * a.strips + strip;
-  if (lane_id() == 23 && own) flag = a.level[0].ready + (int64_t)index * a.strips + strip;
   const uint32_t how = wait_ready(a, flag);
   Channels<V> h = all<V>(0.f);
-  if (!want) return h;
   const uint32_t maps = __ballot_sync(0xFFFFFFFFu, mine), cuts = __ballot_sync(0xFFFFFFFFu, mine && how == READY_CUT);
   const int left = a.D - c;
   if (kept) h = load_published<V, VEC>(a.level[REC_LEVELS].B + (int64_t)top * a.D + c, left);
@@ -610,7 +608,7 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
   for (int rel = 0; rel < tokens;) {
     if (rel % REC_PART == 0) {
       q = find_borders(a, q.lo, it.t0 + rel, min(it.t0 + rel + REC_PART, it.t1), it.t1, first_of, last_of);
-      if (rel == 0) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c, !(q.first & 1), true);
+      if (rel == 0 && !(q.first & 1)) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c);
     }
     // tokens of the part before the next border; FWD_STEP at a time as long as the FWD_BATCH behind them exist
     const unsigned long long ahead = (q.first | q.last) >> (rel % REC_PART);
@@ -640,8 +638,10 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
           // the start of a sequence that goes on behind the chunk was kept with the chunk's map: h_final may be the same array as h0,
           // and the warp that writes it does not wait for this one
           const int f = first_of[rel % REC_PART + i];
-          if (f < 0) s[i] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
-          else if (a.h0) s[i] = get<V, VEC>(a.h0 + (int64_t)f * a.D + c, left);
+          if (f < 0) {
+            wait_ready(a, lane_id() == 0 ? a.level[0].ready + (int64_t)it.index * a.strips + it.strip : nullptr);
+            s[i] = load_published<V, VEC>(a.chunk_start + (int64_t)it.chunk * a.D + c, left);
+          } else if (a.h0) s[i] = get<V, VEC>(a.h0 + (int64_t)f * a.D + c, left);
         }
       }
 #pragma unroll
@@ -657,6 +657,37 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
       value.load(live - FWD_BATCH, x);
       rel += FWD_BATCH;
     }
+  }
+}
+
+// Single tokens: a thread for every channel of every sequence.  One launch, no counters to clear, and no search: 192 sequences of one token
+// x 128 take a third of the pieces' time.  A long sequence among empty ones would be walked token by token, so the host takes this only
+// where sequences hold one token on average and REC_SHORT in all.
+template <typename T>
+__global__ void __launch_bounds__(128)
+recurrence_forward_short(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
+  if (blockIdx.x == 0 && blockIdx.y == 0) {
+    bool bad = false;
+    for (int64_t s = threadIdx.x; s < a.S; s += blockDim.x) {
+      const int64_t b = a.offsets[s], e = a.offsets[s + 1];
+      bad |= b < 0 || e < b || (s == 0 && b != 0) || (s == a.S - 1 && e != a.N);
+    }
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *a.status = any ? (uint32_t)REC_STATUS_OFFSETS : 0u;
+  }
+  const int c = blockIdx.x * blockDim.x + threadIdx.x;
+  if (c >= a.D) return;
+  for (int64_t s = blockIdx.y; s < a.S; s += gridDim.y) {
+    const int64_t begin = min(max(a.offsets[s], (int64_t)0), a.N), end = min(max(a.offsets[s + 1], begin), a.N);
+    Channels<1> h = {{a.h0 ? a.h0[s * a.D + c] : 0.f}};
+    const T* gate = static_cast<const T*>(a.gate) + begin * a.gate_stride + c;
+    const T* value = static_cast<const T*>(a.value) + begin * a.value_stride + c;
+    for (int64_t t = begin; t < end; ++t, gate += a.gate_stride, value += a.value_stride) {
+      if (entry && t % REC_BATCH == 0) entry[t / REC_BATCH * a.D + c] = h.p[0];
+      h = blend(minus_sigmoid(Channels<1>{{to_f32(*gate)}}), Channels<1>{{-to_f32(*value)}}, h);
+      out[t * out_stride + c] = from_f32<T>(h.p[0]);
+    }
+    if (h_final) h_final[s * a.D + c] = h.p[0];
   }
 }
 
@@ -736,9 +767,8 @@ recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, con
     if (start || rel % REC_PART == REC_PART - REC_BATCH) {
       const int64_t p0 = it.t0 + rel / REC_PART * REC_PART;
       q = find_borders(a, lo, p0, min(p0 + REC_PART, it.t1), INT64_MAX, first_of, last_of);
-      if (start)
-        carry = state_before<V, VEC>(a, it.index, it.strip, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c,
-                                     !(q.last >> ((tokens - 1) % REC_PART) & 1), false);
+      if (start && !(q.last >> ((tokens - 1) % REC_PART) & 1))
+        carry = state_before<V, VEC>(a, it.index, it.strip, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c);
     }
     const int64_t t = it.t0 + rel;
     const int live = tokens - rel;
@@ -940,6 +970,16 @@ extern "C" int mts_recurrence_forward(const void* gate, int64_t gate_stride, con
   if (rc == MTS_OK) rc = check_workspace(what, workspace, workspace_bytes, need);
   if (rc != MTS_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (N <= S && N <= REC_SHORT && S > 0) {
+    const RecArgs a = arguments(gate, gate_stride, value, value_stride, offsets, h0, N, S, D, dtype, 1, workspace);
+    return with_dtype(dtype, [&](auto t) {
+      using T = decltype(t);
+      LaunchScope scope(K_RECURRENCE_FWD, s);
+      recurrence_forward_short<T><<<dim3((unsigned)ceil_div(D, 128), (unsigned)(S < 65535 ? S : 65535)), 128, 0, s>>>(a, static_cast<T*>(out), out_stride,
+                                                                                                                  h_final, entry_states);
+      return check_launch(what);
+    });
+  }
   const Workspace w(N, D, dtype);
   rc = check_cuda(cudaMemsetAsync(workspace, 0, (size_t)w.counters, s), "cudaMemsetAsync(recurrence counters)");
   if (rc != MTS_OK || S == 0) return rc;
