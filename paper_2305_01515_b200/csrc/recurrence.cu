@@ -9,38 +9,35 @@
 //   map:  the chunk's map, if its last sequence goes on behind it, from that sequence's start on (what lies before it in the chunk is
 //         forgotten).  The last warp of eight neighbours composes their map, and so on; behind every 512 chunks a state is kept.
 //   walk: the state before the chunk from at most seven maps of each of three levels and a kept state, then the chunk's tokens.
-// Warps take the pieces from a counter, a walk some hundreds of pieces behind its chunk's map: by then the maps it needs have long been
-// published (a word written by one SM is seen by another only 1 to 2 us later), and its rows are still in the L2 cache, so memory sees
-// every input once.  The association of the maps depends on the offsets alone: the result is the same in every run.
+// Warps take the pieces from a counter, a walk some thousands of pieces behind its chunk's map: by then the maps it needs have long been
+// published (a word written by one SM is seen by another only 1 to 2 us later).  The association of the maps depends on the
+// offsets alone: the result is the same in every run.
+//
+// What bounds it: memory.  A chunk's rows are read for its map and again for its walk (in the backward: gate and gradient, then all
+// three), which the L2 cache does not hold in between.  524,287 tokens x 256 in fp16, one sequence: 233 us, 5.8 TB/s of what is
+// moved, 3.5 TB/s of each input once; 1,000 histories of 120,007 tokens in bf16: 71 us; forward and backward of 2,048 histories,
+// 250,001 x 200: 113 + 168 us.  Ragged calls of that size are one wave of warps, whose tokens go one after the other.
 //
 // Waiting: a piece waits only for pieces of lower numbers, which running or finished warps have taken, and the lowest unfinished one
 // waits for nothing.  Every wait has a limit all the same, after which the status word says so.
 //
-// Tried before, for 524,287 tokens x 256, fp16: one pass whose blocks kept their tokens in shared memory and waited for the maps of the
-// blocks before them (424 to 690 us: a chain of three publications per tile outlasts what shared memory can hold back); two launches
-// (250 to 280 us: the composition of the maps at the end of the first leaves most SMs idle for 15 us).
+// Tried before (524,287 x 256): one pass that keeps its rows in shared memory, with maps gathered over levels of groups by every tile
+// (424 to 690 us: three publications in a row per tile outlast what shared memory can hold back), or linked in order by dedicated
+// warps (321 us: 40 ns a link); two launches, maps and walks (250 us: the composition at the end of the first leaves SMs idle).
 #include <type_traits>
 
 #include "dense.cuh"
 
 namespace mts {
 
-#ifndef MTS_REC_FWD_BLOCKS
-#define MTS_REC_FWD_BLOCKS 16
-#endif
-#ifndef MTS_REC_BWD_BLOCKS
-#define MTS_REC_BWD_BLOCKS 12
-#endif
-#ifndef MTS_REC_WARPS_WANTED
-#define MTS_REC_WARPS_WANTED 1776
-#endif
-#ifndef MTS_REC_LAG
-#define MTS_REC_LAG 4096
-#endif
-#ifndef MTS_REC_MAX_CHUNK
-#define MTS_REC_MAX_CHUNK 256
-#endif
-constexpr int REC_CHUNK = MTS_REC_MAX_CHUNK;      // tokens of a chunk at most
+// Measured on 250,001 tokens x 200 and 524,287 x 256 (16-bit): 12, 16, 20, 24 blocks of one warp per SM take 129 / 114 / 122 / 128 us and
+// 242 / 233 / 264 / 278 us in the forward (fewer registers spill, fewer warps wait); 10, 12, 14 take 177 / 168 / 184 us in the backward.
+constexpr int FWD_BLOCKS = 16, BWD_BLOCKS = 12;
+constexpr int REC_WARPS_WANTED = 2368;            // chunks are halved until there are so many pieces of a kind: 16 per SM
+// Pieces between a chunk's map and its walk.  512 to 100 million were tried: the map's readers must not wait (below 2,048 the backward
+// takes a tenth longer), and no lag keeps the rows in the L2 cache until the walk (memory reads are 1.7 to 2 times the inputs at all of them).
+constexpr int REC_LAG = 4096;
+constexpr int REC_CHUNK = 256;                    // tokens of a chunk at most
 constexpr int REC_PART = 64;                      // tokens whose borders are looked up together: a bit mask of them is one word
 constexpr int REC_BATCH = 8;                      // tokens in registers, and between two states kept for the backward
 constexpr int REC_SHORT = 4096;                   // tokens of a call that threads may walk one by one
@@ -522,10 +519,7 @@ __device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel)
 // In all four walks a row's registers take the row one batch ahead as soon as they have been read: a batch is always on its way.
 
 // ------------------------------------------------------------------------------- forward
-#ifndef MTS_REC_FWD_BATCH
-#define MTS_REC_FWD_BATCH 8
-#endif
-constexpr int FWD_BATCH = MTS_REC_FWD_BATCH;           // rows on their way
+constexpr int FWD_BATCH = 8;           // rows on their way; 4 leave room for more warps and take as long
 constexpr int FWD_STEP = REC_BATCH;    // tokens of one turn of the inner loops
 static_assert(FWD_STEP % FWD_BATCH == 0, "a state is kept where a batch begins");
 
@@ -586,7 +580,7 @@ __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
 }
 
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(32, MTS_REC_FWD_BLOCKS)
+__global__ void __launch_bounds__(32, FWD_BLOCKS)
 recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
   __shared__ int32_t first_of[REC_PART], last_of[REC_PART];
   const Piece it(a, false);
@@ -734,7 +728,7 @@ __device__ __forceinline__ void backward_map(const RecArgs& a, const Piece& it, 
 
 // A batch is walked forward from the state that the forward left before it, for -z and the distance from value to state, then backward.
 template <typename T, int V, bool VEC>
-__global__ void __launch_bounds__(32, MTS_REC_BWD_BLOCKS)
+__global__ void __launch_bounds__(32, BWD_BLOCKS)
 recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, const T* __restrict__ grad_out, int64_t grad_out_stride,
                            const float* __restrict__ grad_final, T* __restrict__ grad_gate, int64_t grad_gate_stride,
                            T* __restrict__ grad_value, int64_t grad_value_stride, float* __restrict__ grad_h0) {
@@ -877,7 +871,7 @@ struct Alignment {
 int chunk_tokens(int64_t N, int32_t D, int32_t dtype) {
   const int64_t strips = ceil_div((int64_t)D * dtype_bytes(dtype), 256);
   int chunk = REC_CHUNK;
-  while (chunk > 2 * REC_BATCH && ceil_div(N, chunk) * strips < MTS_REC_WARPS_WANTED) chunk /= 2;
+  while (chunk > 2 * REC_BATCH && ceil_div(N, chunk) * strips < REC_WARPS_WANTED) chunk /= 2;
   return chunk;
 }
 
@@ -905,7 +899,7 @@ RecArgs arguments(const void* gate, int64_t gate_stride, const void* value, int6
   a.chunks = (int32_t)w.n[0];
   a.strips = (int32_t)ceil_div(D, 32 * vec);
   const int64_t pieces = w.n[0] * a.strips;
-  a.lag = (int32_t)(pieces < MTS_REC_LAG ? pieces : MTS_REC_LAG);
+  a.lag = (int32_t)(pieces < REC_LAG ? pieces : REC_LAG);
   char* p = static_cast<char*>(workspace);
   a.status = reinterpret_cast<uint32_t*>(p);
   a.ticket = a.status + 1;
