@@ -44,7 +44,7 @@ __device__ __forceinline__ float bias_value(const Buckets& b, const BiasGeometry
   return b.causal && r > 0 ? -INFINITY : table_value(table, table_dtype, (int64_t)bucket_row(b, r) * g.heads + h);
 }
 
-// Few queries: one element per thread and step.
+// Few rows: one element per thread and step.
 template <typename T>
 __global__ void __launch_bounds__(256)
 relpos_forward_direct(const __grid_constant__ Buckets b, BiasGeometry g, const void* __restrict__ table, int table_dtype, T* __restrict__ out,
@@ -55,17 +55,20 @@ relpos_forward_direct(const __grid_constant__ Buckets b, BiasGeometry g, const v
       out[h * head_stride + i * row_stride + j] = from_f32<T>(bias_value(b, g, table, table_dtype, h, (int)j - i - g.q_offset));
 }
 
-// A block writes `rows` queries x up to FWD_COLS keys of one head.  It holds their part of the vector in shared memory once for each of the
+// A block writes `rows` queries x up to FWD_COLS keys of one head: bound by the bytes it writes.  It holds their part of the vector in shared memory once for each of the
 // 16 / sizeof(T) positions that a 16-byte boundary can have in it, so that every row is one bulk copy to global memory from an
 // aligned place of one of the copies, whatever its window and the alignment of the row; up to 15 bytes at either end of a row are
-// stored by threads.
-#ifndef MTS_RELPOS_BLOCKS
-#define MTS_RELPOS_BLOCKS (148 * 2)
-#endif
-#ifndef MTS_RELPOS_DIRECT
-#define MTS_RELPOS_DIRECT 8
-#endif
+// stored by threads.  16 x 4,096 x 4,096 in bf16: 88.6 us, 6.06 TB/s, 93% of the copy rate (a thread per element: 1,320 us, a search of
+// the buckets each); 12 x 1,023 x 1,023: 10.2 us.
+//
+// Blocks a call is cut into, where it has the rows.  148, 296, 592 and 1,184 take 12.4 / 12.4 / 16.4 / 16.4 us for 4 x 2,048 x 2,048 in bf16 (each
+// block makes its vector) and 10.4 / 10.4 / 10.4 / 12.7 us for 12 x 1,023 x 1,023.
+constexpr int FWD_WANTED = 148 * 2;
 constexpr int FWD_COLS = 2048;
+// Rows of up to FWD_COLS keys below which a call's elements are written one by one.  Direct / by rows in bf16: 16 heads x 2,048 keys with 1, 8,
+// 12, 16 and 32 queries 2.0 / 4.7, 3.5 / 5.7, 4.1 / 5.7, 4.9 / 5.7 and 8.2 / 5.9 us; 8 x 300 with 16 and 32 queries 2.3 / 2.9 and 2.5 / 2.9 us;
+// 32 x 8,192 with 1, 2 and 4 queries 3.5 / 5.1, 4.8 / 5.5 and 8.0 / 5.6 us.
+constexpr int FWD_DIRECT = 256;
 constexpr int FWD_THREADS = 256;
 
 template <typename T>
@@ -109,9 +112,6 @@ relpos_forward_rows(const __grid_constant__ Buckets b, BiasGeometry g, const voi
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // shared memory stays until it has been read
 }
 
-#ifndef MTS_RELPOS_GRAD_BLOCKS
-#define MTS_RELPOS_GRAD_BLOCKS 4
-#endif
 constexpr int GRAD_CTAS = 592;            // blocks over all heads; also bounds the partial sums kept in the workspace
 constexpr int GRAD_WARPS = 8;
 constexpr int GRAD_ROWS = 8;              // rows of a patch
@@ -157,8 +157,11 @@ struct Bands {
 //   VECTOR: a lane holds 16 bytes of each row (E neighbouring columns): an 8 x E patch has E + 7 diagonals.  Rows on 16-byte
 //           boundaries, Lk a multiple of E.
 //   else:   a lane holds every 32nd column (E = 4 of them): one diagonal for each of its 8 E elements.  Any alignment.
+// Vectors / single elements for the same aligned input: 60.1 / 117.1 us for 16 x 8 x 1,024 x 1,024 in bf16 (4.5 TB/s, 68% of the copy rate),
+// 39.2 / 50.4 us for 5 x 12 x 776 x 1,000 in fp32.  Bound by the reads that are in flight: 64 registers a thread (four blocks per SM) hold
+// eight 16-byte rows, and a warp waits for its patch before it asks for the next.
 template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(GRAD_WARPS * 32, MTS_RELPOS_GRAD_BLOCKS)
+__global__ void __launch_bounds__(GRAD_WARPS * 32, 4)
 relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64_t B, const T* __restrict__ grad, int64_t batch_stride,
                         int64_t head_stride, int64_t row_stride, double* __restrict__ partial) {
   constexpr int E = VECTOR ? 16 / (int)sizeof(T) : 4, BAND = 32 * E, ROWS = GRAD_ROWS, SHIFT = ROWS - 1;
@@ -353,16 +356,16 @@ extern "C" int mts_relpos_bias_forward(const mts_relpos_buckets* buckets, const 
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
     LaunchScope scope(K_RELPOS_FWD, s);
-    if (Lq < MTS_RELPOS_DIRECT) {
+    const int64_t strips = ceil_div(Lk, FWD_COLS);
+    if (heads * Lq * strips < FWD_DIRECT) {
       const dim3 grid((unsigned)ceil_div(Lk, 256), (unsigned)Lq, (unsigned)heads);
       relpos_forward_direct<T><<<grid, 256, 0, s>>>(b, g, table, table_dtype, static_cast<T*>(out), out_head_stride, out_row_stride);
       return check_launch(what);
     }
     // rows of a block: as many as leave the GPU two blocks per SM, 128 at most (the vector is made once for all of them), and not
     // more blocks down than a grid has room for
-    const int64_t strips = ceil_div(Lk, FWD_COLS);
     int rows = 128;
-    while (rows > 8 && ceil_div(Lq, rows) * strips * heads < MTS_RELPOS_BLOCKS) rows /= 2;
+    while (rows > 8 && ceil_div(Lq, rows) * strips * heads < FWD_WANTED) rows /= 2;
     while (ceil_div(Lq, rows) > 65535) rows *= 2;
     const int pitch = (int)align_up((size_t)(Lk < FWD_COLS ? Lk : FWD_COLS) + (size_t)rows, 16);
     const size_t smem = (size_t)pitch * 16;

@@ -50,6 +50,21 @@ def test_forward(H, Lq, Lk, off, two_sided, causal, dtype):
     assert torch.equal(out, want)
 
 
+# Enough rows that a block writes several of them by whole windows of the vector.
+@pytest.mark.parametrize("H,Lq,Lk,off,pad,shift", [(7, 61, 131, 0, 0, 0), (3, 129, 2049, 1900, 3, 1), (1, 300, 77, -5, 0, 3), (33, 8, 8, 0, 0, 0), (9, 31, 1, 3, 0, 0),
+                                                   (2, 131, 4100, 4000, 12, 4), (260, 1, 40, 39, 1, 2), (40, 8, 4, 0, 5, 7)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_forward_of_many_rows(H, Lq, Lk, off, pad, shift, causal, dtype):
+    table = torch.randn(2 * len(STARTS), H, device=DEV)
+    out, room = forward(STARTS, True, causal, H, Lq, Lk, off, table, dtype, pad, shift)
+    k = torch.from_numpy(bucket_table(STARTS, True, causal, Lq, Lk, off)).to(DEV)
+    assert torch.equal(out, torch.where(k < 0, float("-inf"), table.t()[:, k.clamp(min=0)]).to(dtype))
+    touched = torch.zeros_like(room, dtype=torch.bool)
+    torch.as_strided(touched, out.shape, out.stride(), shift).fill_(True)
+    assert bool((room[~touched] == 5.0).all())
+
+
 @pytest.mark.parametrize("pad,shift", [(0, 1), (3, 0), (8, 8), (1, 5), (0, 4)])
 @pytest.mark.parametrize("table_dtype", [torch.float32, torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
