@@ -8,6 +8,11 @@
 // consecutive ones per lane (one 16- or 32-byte access per array); in 8 bits the block is also the unit that shares a scale, so its
 // largest moment is one warp reduction and nothing leaves the registers.  A block of threads owns eight such blocks of
 // one tensor, found through a map made once, so that tensors of any number and size share one launch.
+//
+// Parameters in 16 bits with fp32 masters and moments, 120 M elements of 28 bytes: 521 us, 6.45 TB/s, 98.6% of the copy rate.  8-bit moments with
+// fp32 parameters and bf16 gradients, 100 M elements of 14 bytes: step 320 us, 4.4 TB/s: 80 instructions per element, a third of them for
+// the codes, keep the integer units busy (113 with correctly rounded root and quotient and the check for finite values by element:
+// 437 us); their export, 10 bytes per element, 152 us at the copy rate.
 #include <math.h>
 
 #include <new>
@@ -196,7 +201,7 @@ adamw_step_kernel(const AdamTensor* __restrict__ tensors, const void* const* __r
     const float gk = __fmul_rn(g[k], scale);
     m[k] = __fadd_rn(__fmul_rn(m[k], c.beta1), __fmul_rn(gk, c.one_minus_beta1));
     v[k] = __fadd_rn(__fmul_rn(v[k], c.beta2), __fmul_rn(__fmul_rn(gk, gk), c.one_minus_beta2));
-    // hardware root and reciprocal: an update's last two units of 2^-23
+    // hardware root and reciprocal: an update's last two units of 2^-23, far below the fp32 parameter's own rounding of the sum
     float root, inv;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[k]));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(root, c.inv_root2, c.eps)));

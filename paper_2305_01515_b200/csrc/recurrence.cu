@@ -14,9 +14,9 @@
 // offsets alone: the result is the same in every run.
 //
 // What bounds it: memory.  A chunk's rows are read for its map and again for its walk (in the backward: gate and gradient, then all
-// three), which the L2 cache does not hold in between.  524,287 tokens x 256 in fp16, one sequence: 233 us, 5.8 TB/s of what is
-// moved, 3.5 TB/s of each input once; 1,000 histories of 120,007 tokens in bf16: 71 us; forward and backward of 2,048 histories,
-// 250,001 x 200: 113 + 168 us.  Ragged calls of that size are one wave of warps, whose tokens go one after the other.
+// three), which the L2 cache does not hold in between.  524,287 tokens x 256 in fp16, one sequence: 219 us, 6.1 TB/s of what is
+// moved, 3.7 TB/s of each input once; 1,000 histories of 120,007 tokens in bf16: 70 us; forward and backward of 2,048 histories,
+// 250,001 x 200: 108 + 164 us.  Ragged calls of that size are one wave of warps, whose tokens go one after the other.
 //
 // Waiting: a piece waits only for pieces of lower numbers, which running or finished warps have taken, and the lowest unfinished one
 // waits for nothing.  Every wait has a limit all the same, after which the status word says so.
@@ -30,8 +30,8 @@
 
 namespace mts {
 
-// Measured on 250,001 tokens x 200 and 524,287 x 256 (16-bit): 12, 16, 20, 24 blocks of one warp per SM take 129 / 114 / 122 / 128 us and
-// 242 / 233 / 264 / 278 us in the forward (fewer registers spill, fewer warps wait); 10, 12, 14 take 177 / 168 / 184 us in the backward.
+// Measured on 250,001 tokens x 200 and 524,287 x 256 (16-bit): 12, 14, 16 blocks of one warp per SM take 120 / 109 / 108 us and 223 / 219 / 219 us
+// in the forward, 20 and 24 of them a tenth more than 16 (registers spill); 10, 11, 12, 14 take 177 / 167 / 168 / 184 us in the backward.
 constexpr int FWD_BLOCKS = 16, BWD_BLOCKS = 12;
 constexpr int REC_WARPS_WANTED = 2368;            // chunks are halved until there are so many pieces of a kind: 16 per SM
 // Pieces between a chunk's map and its walk.  512 to 100 million were tried: the map's readers must not wait (below 2,048 the backward
@@ -240,11 +240,14 @@ __device__ __forceinline__ Channels<V> load_f32(const float* p) { return unpack<
 // The same in rows of D channels of which `left` begin at p: VEC = D and the row's base allow whole vectors, else one by one.
 template <int V, bool VEC>
 __device__ __forceinline__ Channels<V> get(const float* p, int left) {
-  if (VEC) return left > 0 ? load_f32<V>(p) : all<V>(0.f);
-  float x[V];
+  if constexpr (VEC) {
+    return left > 0 ? load_f32<V>(p) : all<V>(0.f);
+  } else {
+    float x[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) x[k] = k < left ? p[k] : 0.f;
-  return gathered<V>(x);
+    for (int k = 0; k < V; ++k) x[k] = k < left ? p[k] : 0.f;
+    return gathered<V>(x);
+  }
 }
 template <int V, bool VEC, typename T>
 __device__ __forceinline__ void put(T* p, int left, Channels<V> v) {
@@ -512,6 +515,22 @@ struct Rows {
     for (int i = 0; i < N; ++i, at += stride) r[i] = i < live ? get() : Raw<T, V>{};
   }
 };
+// Brings rows 8 to 15 behind where two arrays stand towards the L2 cache: every lane asks for half a strip of one row.  The registers
+// hold a batch on its way, which is less than the memory's latency needs: 524,287 tokens x 256 take 219 us with it, 233 without, 226 from eight rows
+// further on.  In the backward it costs as much as it gives (169 / 168 us), but for the kept states (164).
+template <typename T, int V, bool VEC>
+struct Ahead {
+  using R = Rows<T, V, VEC>;
+  int64_t by;
+  bool second;
+  __device__ __forceinline__ Ahead(const R& a, const R& b, int c, int D) : second(lane_id() & 1) {
+    const int own = a.left > 0 ? c : 0, half = min(c - lane_id() * V + (lane_id() >> 1 & 1) * 16 * V, D - 1), row = 8 + (lane_id() >> 2);
+    by = row * (second ? b.stride : a.stride) + half - own;
+  }
+  __device__ __forceinline__ void operator()(const R& a, const R& b) const {
+    asm volatile("prefetch.global.L2 [%0];" :: "l"((second ? b.at : a.at) + by));
+  }
+};
 // Bits of n tokens from token `rel` of a part on.
 template <int N>
 __device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel) { return (uint32_t)(mask >> (rel % REC_PART)) & ((1u << N) - 1); }
@@ -522,6 +541,7 @@ __device__ __forceinline__ uint32_t batch_bits(unsigned long long mask, int rel)
 constexpr int FWD_BATCH = 8;           // rows on their way; 4 leave room for more warps and take as long
 constexpr int FWD_STEP = REC_BATCH;    // tokens of one turn of the inner loops
 static_assert(FWD_STEP % FWD_BATCH == 0, "a state is kept where a batch begins");
+static_assert(FWD_STEP == 8 && FWD_BATCH == 8, "eight rows are asked for ahead");
 
 template <typename T, int V, bool VEC>
 __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
@@ -559,8 +579,10 @@ __device__ __forceinline__ void forward_map(const RecArgs& a, const Piece& it) {
       m.P = fma(nz, m.P, m.P);
     };
     rel = later;                                                        // tokens to go, FWD_BATCH of them in registers
+    const Ahead<T, V, VEC> ahead(gate, value, c, a.D);
 #pragma unroll 1
     for (; rel >= FWD_STEP + FWD_BATCH; rel -= FWD_STEP) {
+      if (rel >= FWD_STEP + 2 * FWD_BATCH) ahead(gate, value);
 #pragma unroll
       for (int i = 0; i < FWD_STEP; ++i) {
         step(i % FWD_BATCH);
@@ -596,6 +618,7 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
   gate.load(tokens, g);
   value.load(tokens, x);
   check_offsets(a, it.number, (int64_t)a.chunks * a.strips, empty_row);
+  const Ahead<T, V, VEC> ahead(gate, value, c, a.D);
   Borders q = {0, 0, 0, 0, find_sequence(a, it.t0)};
   Channels<V> h = all<V>(0.f);
 #pragma unroll 1
@@ -605,12 +628,13 @@ recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stri
       if (rel == 0 && !(q.first & 1)) h = state_before<V, VEC>(a, it.index, it.strip, (int)(q.head_begin / a.chunk), c);
     }
     // tokens of the part before the next border; FWD_STEP at a time as long as the FWD_BATCH behind them exist
-    const unsigned long long ahead = (q.first | q.last) >> (rel % REC_PART);
-    const int clear = min(ahead ? __ffsll(ahead) - 1 : REC_PART - rel % REC_PART, tokens - rel - FWD_BATCH);
+    const unsigned long long borders = (q.first | q.last) >> (rel % REC_PART);
+    const int clear = min(borders ? __ffsll(borders) - 1 : REC_PART - rel % REC_PART, tokens - rel - FWD_BATCH);
     if (clear >= FWD_STEP && rel % FWD_STEP == 0) {
 #pragma unroll 1
       for (const int end = rel + clear / FWD_STEP * FWD_STEP; rel < end; rel += FWD_STEP) {
         if (entry) put<V, VEC>(entry + ((it.t0 + rel) / REC_BATCH) * a.D + c, left, h);
+        if (rel + FWD_STEP + 2 * FWD_BATCH <= tokens) ahead(gate, value);
 #pragma unroll
         for (int i = 0; i < FWD_STEP; ++i, to.at += to.stride) {
           const Channels<V> nz = minus_sigmoid(unpack<T, V>(g[i % FWD_BATCH])), nx = unpack<T, V, true>(x[i % FWD_BATCH]);
@@ -764,11 +788,12 @@ recurrence_backward_kernel(const RecArgs a, const float* __restrict__ entry, con
       if (start && !(q.last >> ((tokens - 1) % REC_PART) & 1))
         carry = state_before<V, VEC>(a, it.index, it.strip, a.chunks - 1 - (int)min((q.tail_end - 1) / a.chunk, (int64_t)a.chunks - 1), c);
     }
-    const int64_t t = it.t0 + rel;
     const int live = tokens - rel;
     const uint32_t firsts = batch_bits<REC_BATCH>(q.first, rel), lasts = batch_bits<REC_BATCH>(q.last, rel);
     Channels<V> h = all<V>(0.f), nz[REC_BATCH], away[REC_BATCH];        // away: - (value - state before the token)
-    if (!(firsts & 1)) h = get<V, VEC>(entry + t / REC_BATCH * a.D + c, left);
+    const float* kept = entry + (it.t0 + rel) / REC_BATCH * a.D + c;
+    if (!(firsts & 1)) h = get<V, VEC>(kept, left);
+    if (rel >= 2 * REC_BATCH && left > 0) asm volatile("prefetch.global.L2 [%0];" :: "l"(kept - 2 * a.D));     // registers for it are not to be had
     if (!(firsts | lasts) && live >= REC_BATCH && rel > 0) {
 #pragma unroll
       for (int i = 0; i < REC_BATCH; ++i) {
@@ -926,7 +951,8 @@ int launch_pieces(const char* what, int trace_id, Kernel kernel, const RecArgs& 
   return check_launch(what);
 }
 
-// fn(V, VEC): a lane holds `most` channels, fewer where a row has no use for all lanes.
+// fn(V, VEC): a lane holds MOST channels, fewer where a row has no use for all lanes: 200,000 tokens in bf16 with 32 and 64 channels take 34.9
+// and 40.7 us with one and two of them a lane, 51.1 and 52.6 us with four.
 template <int MOST, typename Fn>
 int with_channels(int32_t D, const Alignment& al, int bytes, Fn&& fn) {
   auto vec = [&](int v) { return D % v == 0 && al.rows % (v * bytes) == 0 && al.states % (v * 4) == 0; };
