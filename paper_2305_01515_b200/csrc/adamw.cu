@@ -9,7 +9,7 @@
 // largest moment is one warp reduction and nothing leaves the registers.  A block of threads owns eight such blocks of
 // one tensor, found through a map made once, so that tensors of any number and size share one launch.
 //
-// Parameters in 16 bits with fp32 masters and moments, 120 M elements of 28 bytes: 521 us, 6.45 TB/s, 98.6% of the copy rate.  8-bit moments with
+// Parameters in 16 bits with fp32 masters and moments, 120 M elements of 28 bytes: 521 to 533 us on different GPUs, 96 to 98.6% of the copy rate.  8-bit moments with
 // fp32 parameters and bf16 gradients, 100 M elements of 14 bytes: step 320 us, 4.4 TB/s: 80 instructions per element, a third of them for
 // the codes, keep the integer units busy (113 with correctly rounded root and quotient and the check for finite values by element:
 // 437 us); their export, 10 bytes per element, 152 us at the copy rate.
