@@ -23,8 +23,7 @@ inline int check_launch(const char* what) { return check_cuda(cudaGetLastError()
 enum KernelId {
   K_FORWARD = 0, K_LINEARIZE, K_SORT_HISTOGRAM, K_SORT_SCAN, K_SORT_SCATTER, K_UNIQUE, K_REDUCE_CHUNKS,
   K_COMBINE_PARTIALS, K_CACHE_PREPARE, K_CACHE_DESCRIBE, K_CACHE_PROBE_REPLACE, K_CACHE_LISTS, K_CACHE_SCATTER_SLOTS,
-  K_CACHE_SAVE_VICTIMS, K_CACHE_FETCH_MISSES, K_CACHE_WRITE_VICTIMS, K_CACHE_FLUSH, K_OTHER,
-  K_RECURRENCE_FWD, K_RECURRENCE_BWD, K_RELPOS_FWD, K_RELPOS_BWD, K_ADAMW, K_ADAMW_STATE, K_COUNT
+  K_CACHE_SAVE_VICTIMS, K_CACHE_FETCH_MISSES, K_CACHE_WRITE_VICTIMS, K_CACHE_FLUSH, K_OTHER, K_COUNT
 };
 
 struct LaunchScope {

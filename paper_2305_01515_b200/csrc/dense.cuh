@@ -8,6 +8,10 @@
 
 namespace mts {
 
+// Kernels of the dense operators in the launch trace, behind those of the tables and caches (whose header stands in the profiler captures'
+// hash and does not change with these).
+enum DenseKernelId { K_RECURRENCE_FWD = K_COUNT, K_RECURRENCE_BWD, K_RELPOS_FWD, K_RELPOS_BWD, K_ADAMW, K_ADAMW_STATE, K_ALL_COUNT };
+
 inline bool known_dtype(int32_t dtype) {
   return dtype == MTS_DTYPE_FP32 || dtype == MTS_DTYPE_FP16 || dtype == MTS_DTYPE_BF16;
 }

@@ -6,7 +6,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "common.cuh"
+#include "dense.cuh"
 
 namespace mts {
 
@@ -26,7 +26,7 @@ int check_cuda(cudaError_t e, const char* what) {
 }
 
 // ------------------------------------------------------------------------------- instrumentation
-static const char* const kKernelNames[K_COUNT] = {
+static const char* const kKernelNames[K_ALL_COUNT] = {
     "tbe_forward_kernel", "linearize_lookups", "digit_histogram", "scan_histogram", "scatter_by_digit",
     "unique_segments", "reduce_chunks", "combine_partials", "cache_prepare_keys", "cache_describe_unique",
     "cache_probe_replace", "cache_lists", "cache_scatter_slots", "cache_save_victims", "cache_fetch_misses",
@@ -78,15 +78,15 @@ extern "C" int mts_trace_enable(int32_t enable) {
   return MTS_OK;
 }
 
-extern "C" int32_t mts_trace_kernel_count(void) { return K_COUNT; }
+extern "C" int32_t mts_trace_kernel_count(void) { return K_ALL_COUNT; }
 
 extern "C" const char* mts_trace_kernel_name(int32_t kernel) {
-  return (kernel >= 0 && kernel < K_COUNT) ? kKernelNames[kernel] : "";
+  return (kernel >= 0 && kernel < K_ALL_COUNT) ? kKernelNames[kernel] : "";
 }
 
 extern "C" int mts_trace_report(double* host_total_ms, int64_t* host_launches, int32_t n) {
-  if (!host_total_ms || !host_launches || n < K_COUNT)
-    return set_error(MTS_ERR_INVALID_ARG, "trace_report: need %d entries", (int)K_COUNT);
+  if (!host_total_ms || !host_launches || n < K_ALL_COUNT)
+    return set_error(MTS_ERR_INVALID_ARG, "trace_report: need %d entries", (int)K_ALL_COUNT);
   std::lock_guard<std::mutex> lk(g_trace_mu);
   for (int k = 0; k < n; ++k) { host_total_ms[k] = 0.0; host_launches[k] = 0; }
   for (size_t i = 0; i < g_used; ++i) {
