@@ -252,6 +252,7 @@ struct mts_adamw {
   int32_t param_dtype = 0, grad_dtype = 0, bits = 32;
   int64_t elements = 0;          // P: with every tensor rounded up to whole blocks
   int64_t n_chunks = 0;
+  std::vector<int64_t> sizes;
   void* block = nullptr;         // the one device allocation: tensors, gradient pointers, chunks
   mts::AdamTensor* d_tensors = nullptr;
   const void** d_grads = nullptr;
@@ -342,6 +343,7 @@ extern "C" int mts_adamw_create(const mts_adamw_desc* d, mts_adamw** out) {
     h->bits = d->state_bits;
     h->elements = elements;
     h->n_chunks = n_chunks;
+    h->sizes.assign(d->host_sizes, d->host_sizes + d->n_tensors);
     const size_t tb = align_up(sizeof(AdamTensor) * tensors.size(), 256), pbytes = align_up(sizeof(void*) * grads.size(), 256);
     char* blk = nullptr;
     int rc = check_cuda(cudaMalloc(&blk, tb + pbytes + sizeof(AdamChunk) * chunks.size() + 256), "cudaMalloc(adamw)");
@@ -380,9 +382,11 @@ extern "C" size_t mts_adamw_state_bytes(const mts_adamw* h) { return h ? state_b
 extern "C" int mts_adamw_set_grads(mts_adamw* h, const void* const* host_grads, void* stream) {
   if (!h || !host_grads) return set_error(MTS_ERR_INVALID_ARG, "adamw_set_grads: null argument");
   const int gb = dtype_bytes(h->grad_dtype);
-  for (int k = 0; k < h->n_tensors; ++k)
-    if ((uintptr_t)host_grads[k] % gb)
+  for (int k = 0; k < h->n_tensors; ++k) {
+    if (h->sizes[k] > 0 && !host_grads[k]) return set_error(MTS_ERR_INVALID_ARG, "adamw_set_grads: null gradient of tensor %d", k);
+    if (h->sizes[k] > 0 && (uintptr_t)host_grads[k] % gb)
       return set_error(MTS_ERR_ALIGNMENT, "adamw_set_grads: gradient %d is no multiple of its element size", k);
+  }
   return check_cuda(cudaMemcpyAsync(h->d_grads, host_grads, sizeof(void*) * (size_t)h->n_tensors, cudaMemcpyHostToDevice,
                                     static_cast<cudaStream_t>(stream)), "cudaMemcpyAsync(adamw gradients)");
 }

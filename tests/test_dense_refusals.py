@@ -117,3 +117,18 @@ def test_adamw_handle_refusals():
         mb.adamw_set_grads(h, [])
     refused(mb.ERR_ALIGNMENT, mb.adamw_set_grads, h, [x.data_ptr() + 1])
     assert float(x.abs().sum()) == 0.0
+
+
+@pytest.mark.gpu
+def test_adamw_refuses_null_gradients_of_tensors_that_have_elements():
+    import torch
+
+    x, g = torch.ones(300, device="cuda:0"), torch.ones(300, device="cuda:0")
+    h = mb.AdamW((0, 300), 0, 0, 32, (None, x), (None, g))
+    refused(mb.ERR_INVALID_ARG, mb.adamw_set_grads, h, [None, None])
+    refused(mb.ERR_INVALID_ARG, mb.adamw_set_grads, h, [g, None])
+    state = torch.zeros(h.state_bytes, dtype=torch.uint8, device="cuda:0")
+    mb.adamw_set_grads(h, [None, g])                       # nothing is read of an empty tensor
+    mb.adamw_step(h, state, 0.1, 0.9, 0.999, 1e-8, 0.0, 1)
+    torch.cuda.synchronize()
+    assert float((x - 0.9).abs().max()) < 1e-6             # the first step of equal gradients is lr
