@@ -673,7 +673,8 @@ int mts_relpos_bias_backward(const mts_relpos_buckets* buckets, const void* grad
  *                  block whose largest is below 2^-120 is stored as 0).  Moments that are not finite are stored as 0
  *                  (their parameter shows them) and leave the rest of their block alone.
  * mts_adamw_create copies the description to the device (synchronous; the only allocation); mts_adamw_set_grads replaces
- * the gradient pointers (host array) for later steps on `stream`, whose pending steps keep the old ones.
+ * the gradient pointers (host array, read before the call returns) for later steps on `stream`, whose pending steps keep
+ * the old ones; a stream that is being captured into a graph is refused (UNSUPPORTED): set them before the capture.
  * grad_scale: device fp32 scalar, nullable (1): a clipping factor or the inverse of a loss scale.
  * mts_adamw_export_state / _import_state: the moments as fp32 device arrays [P] (16-byte aligned), out of and into a
  * state; an 8-bit import rounds both to nearest.

@@ -381,6 +381,11 @@ extern "C" size_t mts_adamw_state_bytes(const mts_adamw* h) { return h ? state_b
 
 extern "C" int mts_adamw_set_grads(mts_adamw* h, const void* const* host_grads, void* stream) {
   if (!h || !host_grads) return set_error(MTS_ERR_INVALID_ARG, "adamw_set_grads: null argument");
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const int rc = check_cuda(cudaStreamIsCapturing(static_cast<cudaStream_t>(stream), &capture), "cudaStreamIsCapturing(adamw gradients)");
+  if (rc != MTS_OK) return rc;
+  // a captured copy would read the caller's array at every replay, long after this call
+  if (capture != cudaStreamCaptureStatusNone) return set_error(MTS_ERR_UNSUPPORTED, "adamw_set_grads: the stream is being captured");
   const int gb = dtype_bytes(h->grad_dtype);
   for (int k = 0; k < h->n_tensors; ++k) {
     if (h->sizes[k] > 0 && !host_grads[k]) return set_error(MTS_ERR_INVALID_ARG, "adamw_set_grads: null gradient of tensor %d", k);

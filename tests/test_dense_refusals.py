@@ -132,3 +132,24 @@ def test_adamw_refuses_null_gradients_of_tensors_that_have_elements():
     mb.adamw_step(h, state, 0.1, 0.9, 0.999, 1e-8, 0.0, 1)
     torch.cuda.synchronize()
     assert float((x - 0.9).abs().max()) < 1e-6             # the first step of equal gradients is lr
+
+
+@pytest.mark.gpu
+def test_adamw_refuses_new_gradients_on_a_stream_under_capture():
+    """A captured copy would read the host array of pointers when the graph runs, after it is gone.  The step itself can be captured."""
+    import torch
+
+    x, g = torch.zeros(300, device="cuda:0"), torch.ones(300, device="cuda:0")
+    h = mb.AdamW((300,), 0, 0, 32, (x,), (g.clone(),))
+    state = torch.zeros(h.state_bytes, dtype=torch.uint8, device="cuda:0")
+    mb.adamw_set_grads(h, [g], torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        refused(mb.ERR_UNSUPPORTED, mb.adamw_set_grads, h, [g.data_ptr()], torch.cuda.current_stream())
+        mb.adamw_step(h, state, 0.1, 0.9, 0.999, 1e-8, 0.0, 1, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert float(x.abs().max()) == 0.0
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float((x + 0.1).abs().max()) < 1e-6
