@@ -355,6 +355,8 @@ extern "C" int mts_adamw_create(const mts_adamw_desc* d, mts_adamw** out) {
       rc = upload("cudaMemcpy(adamw tensors)", h->d_tensors, tensors.data(), sizeof(AdamTensor) * tensors.size());
       if (rc == MTS_OK) rc = upload("cudaMemcpy(adamw gradients)", h->d_grads, grads.data(), sizeof(void*) * grads.size());
       if (rc == MTS_OK) rc = upload("cudaMemcpy(adamw chunks)", h->d_chunks, chunks.data(), sizeof(AdamChunk) * chunks.size());
+      // a copy from pageable memory returns once it is staged; streams that do not wait for the default one may run the first step
+      if (rc == MTS_OK) rc = check_cuda(cudaStreamSynchronize(cudaStreamLegacy), "cudaStreamSynchronize(adamw)");
     }
     if (rc != MTS_OK) {
       if (h->block) cudaFree(h->block);

@@ -242,3 +242,19 @@ def test_new_gradient_pointers_and_a_side_stream():
     q.step()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(p.params, q.params))
+
+
+def test_first_step_on_a_stream_that_does_not_wait_for_the_default_one():
+    """The description is on the device when create returns: 3,000 tensors, the first step at once on a stream of its own."""
+    sizes = [300] * 3000
+    params, grads = torch.zeros(3000, 300, device=DEV), torch.ones(3000, 300, device=DEV)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        params.zero_()
+        state = torch.zeros(3000 * 512 * 8, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        h = mb.AdamW(sizes, 0, 0, 32, params.unbind(0), grads.unbind(0))
+        assert h.state_bytes == state.numel()
+        mb.adamw_step(h, state, 0.1, 0.9, 0.999, 1e-8, 0.0, 1, stream=side)
+        torch.cuda.synchronize()
+        assert float((params + 0.1).abs().max()) < 1e-6
