@@ -20,6 +20,11 @@ def _kind(t: torch.Tensor, what: str) -> int:
     return KIND[t.dtype]
 
 
+def _same_device(t: torch.Tensor, device: torch.device, what: str) -> None:
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+
+
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """An [N, D] tensor whose channels are contiguous and whose rows do not overlap (a column range of a wider one is)."""
     return t if t.stride(1) == 1 and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]) else t.contiguous()
@@ -38,6 +43,9 @@ class _GatedRecurrence(torch.autograd.Function):
             raise ValueError("offsets: contiguous int64 [S + 1] on the GPU")
         N, D, S = gate.shape[0], gate.shape[1], offsets.numel() - 1
         kind = _kind(gate, "gate")
+        for t, what in ((value, "value"), (offsets, "offsets"), (h0, "h0")):
+            if t is not None:
+                _same_device(t, gate.device, what)
         if h0 is not None and (h0.dtype != torch.float32 or tuple(h0.shape) != (S, D)):
             raise ValueError(f"h0: fp32 {(S, D)}, not {h0.dtype} {tuple(h0.shape)}")
         gate, value, h0 = _rows(gate), _rows(value), None if h0 is None else h0.contiguous()

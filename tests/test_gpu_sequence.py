@@ -120,3 +120,11 @@ def test_example_trains_a_table_and_a_tower():
     rows = (before.reshape(3000, -1) != after.reshape(3000, -1)).any(1)
     assert all(not rows[r] for r in range(3000) if r not in touched)
     tower.close()
+
+
+def test_recurrence_refuses_arguments_on_another_device():
+    x, off = torch.zeros(4, 8, device="cuda"), torch.tensor([0, 4], device="cuda")
+    for args in ((x, x.cpu(), off), (x.cpu(), x, off), (x, x, off, torch.zeros(1, 8)), (x.cpu(), x.cpu(), off)):
+        with pytest.raises(ValueError):
+            sq.gated_recurrence(*args)
+    sq.gated_recurrence(x, x, off, torch.zeros(1, 8, device="cuda"))
