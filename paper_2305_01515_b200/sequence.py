@@ -157,6 +157,8 @@ class AdamW:
         if not self.params or any(p.dtype != self.params[0].dtype or not p.is_contiguous() for p in self.params):
             raise ValueError("parameters: contiguous, of one type")
         kind = _kind(self.params[0], "parameters")
+        for k, p in enumerate(self.params):
+            _same_device(p, self.params[0].device, f"parameter {k}")
         self.lr, self.betas, self.eps, self.weight_decay, self.steps = lr, betas, eps, weight_decay, 0
         for p in self.params:
             if p.grad is None:
@@ -173,6 +175,11 @@ class AdamW:
         for p, g in zip(self.params, grads):
             if g is None or g.dtype != p.dtype or not g.is_contiguous():
                 raise ValueError("every parameter needs a contiguous gradient of its own type")
+            _same_device(g, self.params[0].device, "a gradient")
+        if grad_scale is not None:
+            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
+                raise ValueError(f"grad_scale: one fp32 number, not {grad_scale.dtype} {tuple(grad_scale.shape)}")
+            _same_device(grad_scale, self.params[0].device, "grad_scale")
         stream = torch.cuda.current_stream()
         if any(g.data_ptr() != o.data_ptr() for g, o in zip(grads, self._grads)):
             mb.adamw_set_grads(self.handle, grads, stream)

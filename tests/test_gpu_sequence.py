@@ -128,3 +128,21 @@ def test_recurrence_refuses_arguments_on_another_device():
         with pytest.raises(ValueError):
             sq.gated_recurrence(*args)
     sq.gated_recurrence(x, x, off, torch.zeros(1, 8, device="cuda"))
+
+
+def test_adamw_refuses_arguments_that_the_kernel_cannot_read():
+    w = torch.ones(5, 8, device="cuda").requires_grad_()
+    with pytest.raises(ValueError):
+        sq.AdamW([w, torch.zeros(3)])
+    with pytest.raises(ValueError):
+        sq.AdamW([torch.zeros(3), w])
+    opt = sq.AdamW([w], lr=0.1, weight_decay=0.0)
+    w.grad = torch.ones_like(w)
+    for bad in (torch.tensor(0.5), torch.tensor(0.5, dtype=torch.float64, device="cuda"), torch.tensor(0.5, dtype=torch.float16, device="cuda"),
+                torch.ones(2, device="cuda"), torch.ones(0, device="cuda")):
+        with pytest.raises(ValueError):
+            opt.step(grad_scale=bad)
+    assert opt.steps == 0 and torch.equal(w.detach(), torch.ones_like(w))
+    opt.step(grad_scale=torch.tensor(0.5, device="cuda"))
+    opt.step(grad_scale=torch.tensor([0.25], device="cuda"))
+    assert opt.steps == 2 and float((w.detach() - 0.8).abs().max()) < 0.05
