@@ -95,6 +95,8 @@ def log_bucket_starts(n: int, far: int) -> List[int]:
 
 def _bias(table, buckets, Lq, Lk, q_offset, dtype):
     kind = _kind(table, "table")
+    if dtype not in KIND:
+        raise TypeError(f"bias: {dtype} (fp32, fp16 or bf16)")
     if table.dim() != 2 or table.shape[0] != buckets.rows:
         raise ValueError(f"table {tuple(table.shape)}: one row for each of {buckets.rows} buckets")
     table, H = table.contiguous(), table.shape[1]
@@ -133,6 +135,9 @@ def relpos_bias(table: torch.Tensor, buckets: mb.RelposBuckets, Lq: int, Lk: int
 class _AddRelposBias(torch.autograd.Function):
     @staticmethod
     def forward(ctx, scores, table, buckets, q_offset):
+        if scores.dim() != 4:
+            raise ValueError(f"scores {tuple(scores.shape)}: [B, H, Lq, Lk]")
+        _same_device(scores, table.device, "scores")
         ctx.args = (buckets, q_offset, table.dtype)
         return scores + _bias(table, buckets, scores.shape[2], scores.shape[3], q_offset, scores.dtype)
 

@@ -146,3 +146,30 @@ def test_adamw_refuses_arguments_that_the_kernel_cannot_read():
     opt.step(grad_scale=torch.tensor(0.5, device="cuda"))
     opt.step(grad_scale=torch.tensor([0.25], device="cuda"))
     assert opt.steps == 2 and float((w.detach() - 0.8).abs().max()) < 0.05
+
+
+def test_bias_refuses_scores_that_do_not_fit():
+    b = mb.RelposBuckets([0, 1, 2])
+    table = torch.zeros(3, 2, device="cuda")
+    with pytest.raises(TypeError):
+        sq.relpos_bias(table, b, 4, 4, dtype=torch.float64)
+    with pytest.raises(TypeError):
+        sq.add_relpos_bias(torch.zeros(1, 2, 4, 4, device="cuda", dtype=torch.float64), table, b)
+    for scores in (torch.zeros(2, 4, 4, device="cuda"), torch.zeros(1, 2, 4, 4)):
+        with pytest.raises(ValueError):
+            sq.add_relpos_bias(scores, table, b)
+
+
+def test_gradients_of_broadcast_heads():
+    """One head's table for all heads, and one head's scores for all tables: the gradients are summed over what was broadcast."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    b = mb.RelposBuckets([0, 1, 3], two_sided=True)
+    w = torch.randn(2, 3, 9, 10, generator=g, device="cuda")
+    for hs, ht in ((3, 1), (1, 3)):
+        scores = torch.randn(2, hs, 9, 10, generator=g, device="cuda").requires_grad_()
+        table = torch.randn(b.rows, ht, generator=g, device="cuda").requires_grad_()
+        ds, dt = torch.autograd.grad((sq.add_relpos_bias(scores, table, b) * w).sum(), (scores, table))
+        full = torch.zeros(b.rows, 3, device="cuda").requires_grad_()
+        (df,) = torch.autograd.grad((sq.add_relpos_bias(torch.zeros_like(w), full, b) * w).sum(), full)
+        assert torch.equal(ds, w if hs == 3 else w.sum(1, keepdim=True))
+        assert dt.shape == table.shape and torch.equal(dt, df if ht == 3 else df.sum(1, keepdim=True))
