@@ -1,6 +1,6 @@
 """Torch plumbing for the sequence tower beside the tables: the gated recurrence and the relative position bias as
 differentiable functions, AdamW over a list of parameters.  Nothing here computes anything on its own; every step is a call into
-libmtrains_b200.so on torch's current stream."""
+libmtrains_b200.so on torch's current stream of the tensors' device."""
 from __future__ import annotations
 
 from typing import List, Optional, Sequence
@@ -54,8 +54,9 @@ class _GatedRecurrence(torch.autograd.Function):
         need = any(ctx.needs_input_grad)
         entry = torch.empty(mb.recurrence_chunks(N, D, kind), D, dtype=torch.float32, device=gate.device) if need else None
         ws = torch.empty(mb.recurrence_workspace_bytes(N, S, D, kind), dtype=torch.uint8, device=gate.device)
-        mb.recurrence_forward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, out, D, final, entry, ws,
-                              ws.numel(), torch.cuda.current_stream())
+        with torch.cuda.device(gate.device):
+            mb.recurrence_forward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, out, D, final, entry, ws,
+                                  ws.numel(), torch.cuda.current_stream(gate.device))
         ctx.save_for_backward(gate, value, offsets, h0, entry)
         return out, final
 
@@ -67,8 +68,9 @@ class _GatedRecurrence(torch.autograd.Function):
         d_gate, d_value = (torch.empty(N, D, dtype=gate.dtype, device=gate.device) for _ in range(2))
         d_h0 = torch.empty(S, D, dtype=torch.float32, device=gate.device) if h0 is not None else None
         ws = torch.empty(mb.recurrence_workspace_bytes(N, S, D, kind), dtype=torch.uint8, device=gate.device)
-        mb.recurrence_backward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, entry, grad_out, _stride(grad_out),
-                               grad_final, d_gate, D, d_value, D, d_h0, ws, ws.numel(), torch.cuda.current_stream())
+        with torch.cuda.device(gate.device):
+            mb.recurrence_backward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, entry, grad_out, _stride(grad_out),
+                                   grad_final, d_gate, D, d_value, D, d_h0, ws, ws.numel(), torch.cuda.current_stream(gate.device))
         return d_gate, d_value, None, d_h0
 
 
@@ -101,7 +103,8 @@ def _bias(table, buckets, Lq, Lk, q_offset, dtype):
         raise ValueError(f"table {tuple(table.shape)}: one row for each of {buckets.rows} buckets")
     table, H = table.contiguous(), table.shape[1]
     out = torch.empty(H, Lq, Lk, dtype=dtype, device=table.device)
-    mb.relpos_bias_forward(buckets, table, kind, H, Lq, Lk, q_offset, out, KIND[dtype], Lq * Lk, Lk, torch.cuda.current_stream())
+    with torch.cuda.device(table.device):
+        mb.relpos_bias_forward(buckets, table, kind, H, Lq, Lk, q_offset, out, KIND[dtype], Lq * Lk, Lk, torch.cuda.current_stream(table.device))
     return out
 
 
@@ -110,8 +113,9 @@ def _table_gradient(buckets, grad, q_offset):
     B, H, Lq, Lk = grad.shape
     out = torch.empty(buckets.rows, H, dtype=torch.float32, device=grad.device)
     ws = torch.empty(mb.relpos_bias_workspace_bytes(buckets, H), dtype=torch.uint8, device=grad.device)
-    mb.relpos_bias_backward(buckets, grad, _kind(grad, "gradient"), B, H, Lq, Lk, q_offset, *grad.stride()[:3], out, ws, ws.numel(),
-                            torch.cuda.current_stream())
+    with torch.cuda.device(grad.device):
+        mb.relpos_bias_backward(buckets, grad, _kind(grad, "gradient"), B, H, Lq, Lk, q_offset, *grad.stride()[:3], out, ws, ws.numel(),
+                                torch.cuda.current_stream(grad.device))
     return out
 
 
@@ -170,8 +174,9 @@ class AdamW:
                 p.grad = torch.zeros_like(p)
         self.masters = [p.detach().float() for p in self.params] if masters else None
         self._grads = [p.grad for p in self.params]
-        self.handle = mb.AdamW([p.numel() for p in self.params], kind, kind, state_bits, [p.detach() for p in self.params], self._grads,
-                               self.masters, decays=[p.dim() > 1 for p in self.params])
+        with torch.cuda.device(self.params[0].device):
+            self.handle = mb.AdamW([p.numel() for p in self.params], kind, kind, state_bits, [p.detach() for p in self.params], self._grads,
+                                   self.masters, decays=[p.dim() > 1 for p in self.params])
         self.state = torch.zeros(self.handle.state_bytes, dtype=torch.uint8, device=self.params[0].device)
 
     @torch.no_grad()
@@ -185,12 +190,13 @@ class AdamW:
             if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
                 raise ValueError(f"grad_scale: one fp32 number, not {grad_scale.dtype} {tuple(grad_scale.shape)}")
             _same_device(grad_scale, self.params[0].device, "grad_scale")
-        stream = torch.cuda.current_stream()
-        if any(g.data_ptr() != o.data_ptr() for g, o in zip(grads, self._grads)):
-            mb.adamw_set_grads(self.handle, grads, stream)
-        self._grads = grads
-        self.steps += 1
-        mb.adamw_step(self.handle, self.state, self.lr, *self.betas, self.eps, self.weight_decay, self.steps, grad_scale, self.steps, stream)
+        stream = torch.cuda.current_stream(self.params[0].device)
+        with torch.cuda.device(self.params[0].device):
+            if any(g.data_ptr() != o.data_ptr() for g, o in zip(grads, self._grads)):
+                mb.adamw_set_grads(self.handle, grads, stream)
+            self._grads = grads
+            self.steps += 1
+            mb.adamw_step(self.handle, self.state, self.lr, *self.betas, self.eps, self.weight_decay, self.steps, grad_scale, self.steps, stream)
 
     def zero_grad(self) -> None:
         for p in self.params:

@@ -173,3 +173,38 @@ def test_gradients_of_broadcast_heads():
         (df,) = torch.autograd.grad((sq.add_relpos_bias(torch.zeros_like(w), full, b) * w).sum(), full)
         assert torch.equal(ds, w if hs == 3 else w.sum(1, keepdim=True))
         assert dt.shape == table.shape and torch.equal(dt, df if ht == 3 else df.sum(1, keepdim=True))
+
+
+def test_calls_go_to_the_tensors_device(monkeypatch):
+    """Stream and device of every call are those of the tensors, not the current ones (seen on the host: one GPU is enough)."""
+    asked, entered = [], []
+    current, guard = torch.cuda.current_stream, torch.cuda.device
+
+    class Guard(guard):
+        def __init__(self, device):
+            entered.append(device)
+            super().__init__(device)
+
+    def current_stream(device=None):
+        asked.append(device)
+        return current(device)
+
+    x = torch.zeros(4, 8, device="cuda").requires_grad_()
+    table = torch.zeros(2, 3, device="cuda").requires_grad_()
+    scores, off, b = torch.zeros(1, 3, 4, 4, device="cuda"), torch.tensor([0, 4], device="cuda"), mb.RelposBuckets([0, 1])
+    monkeypatch.setattr(torch.cuda, "current_stream", current_stream)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+
+    def seen(fn):
+        del asked[:], entered[:]
+        result = fn()
+        assert entered and all(d == x.device for d in asked + entered), (asked, entered)
+        return result
+
+    h, _ = seen(lambda: sq.gated_recurrence(x, x.detach(), off))
+    seen(lambda: h.sum().backward())
+    bias = seen(lambda: sq.add_relpos_bias(scores, table, b))
+    seen(lambda: bias.sum().backward())
+    opt = seen(lambda: sq.AdamW([x, table]))
+    seen(opt.step)
+    assert asked == [x.device]
