@@ -6,6 +6,7 @@ from __future__ import annotations
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as mb
 
@@ -61,6 +62,7 @@ class _GatedRecurrence(torch.autograd.Function):
         return out, final
 
     @staticmethod
+    @once_differentiable                     # a second derivative has no kernel: torch raises where one is asked for
     def backward(ctx, grad_out, grad_final):
         gate, value, offsets, h0, entry = ctx.saved_tensors
         N, D, S, kind = gate.shape[0], gate.shape[1], offsets.numel() - 1, KIND[gate.dtype]

@@ -208,3 +208,12 @@ def test_calls_go_to_the_tensors_device(monkeypatch):
     opt = seen(lambda: sq.AdamW([x, table]))
     seen(opt.step)
     assert asked == [x.device]
+
+
+def test_second_derivative_of_the_recurrence_is_refused():
+    """Its gradient has no graph; a penalty on it must not vanish without a word."""
+    x = torch.randn(6, 8, device="cuda").requires_grad_()
+    h, _ = sq.gated_recurrence(x, x, torch.tensor([0, 6], device="cuda"))
+    (d,) = torch.autograd.grad(h.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (h.sum() + d.square().sum()).backward()
