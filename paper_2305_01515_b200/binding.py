@@ -622,6 +622,10 @@ class RelposBuckets:
         self.desc = RelposBucketsDesc(self.n, int(two_sided), int(causal), self._starts)
         self.ref = C.byref(self.desc)
 
+    def without_mask(self) -> "RelposBuckets":
+        """The same buckets for all keys, those ahead of the query too."""
+        return RelposBuckets(self._starts[:self.n], bool(self.desc.two_sided), False) if self.desc.causal else self
+
 
 def relpos_bias_forward(buckets: RelposBuckets, table, table_dtype: int, heads: int, Lq: int, Lk: int, q_offset: int, out,
                         out_dtype: int, out_head_stride: int, out_row_stride: int, stream=None) -> None:

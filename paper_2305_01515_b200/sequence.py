@@ -130,7 +130,22 @@ class _RelposBias(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         buckets, q_offset, dtype = ctx.args
-        return _table_gradient(buckets, grad.unsqueeze(0), q_offset).to(dtype), None, None, None, None, None
+        return _TableGradient.apply(grad.unsqueeze(0), buckets, q_offset).to(dtype), None, None, None, None, None
+
+
+class _TableGradient(torch.autograd.Function):
+    """Linear in the gradient of the scores, so that its own derivative is the bias again, with 0 where keys are masked."""
+
+    @staticmethod
+    def forward(ctx, grad, buckets, q_offset):
+        ctx.args = (buckets, q_offset, grad.shape, grad.dtype)
+        return _table_gradient(buckets, grad, q_offset)
+
+    @staticmethod
+    def backward(ctx, way):
+        buckets, q_offset, shape, dtype = ctx.args
+        bias = _RelposBias.apply(way, buckets.without_mask(), shape[2], shape[3], q_offset, dtype)
+        return (bias.tril(q_offset) if buckets.desc.causal else bias).expand(shape), None, None
 
 
 def relpos_bias(table: torch.Tensor, buckets: mb.RelposBuckets, Lq: int, Lk: int, q_offset: int = 0, dtype: torch.dtype = torch.float32):
@@ -150,7 +165,7 @@ class _AddRelposBias(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         buckets, q_offset, dtype = ctx.args
-        return grad, _table_gradient(buckets, grad, q_offset).to(dtype), None, None
+        return grad, _TableGradient.apply(grad, buckets, q_offset).to(dtype), None, None
 
 
 def add_relpos_bias(scores: torch.Tensor, table: torch.Tensor, buckets: mb.RelposBuckets, q_offset: int = 0):

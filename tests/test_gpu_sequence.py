@@ -217,3 +217,48 @@ def test_second_derivative_of_the_recurrence_is_refused():
     (d,) = torch.autograd.grad(h.square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (h.sum() + d.square().sum()).backward()
+
+
+@pytest.mark.parametrize("two_sided,causal", [(True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("added", [True, False])
+def test_second_derivatives_of_the_bias(two_sided, causal, added):
+    """A loss with a penalty on the gradients of the table and of the scores, against the same bias by indexing in 64 bits.  2 heads x 2 x 7 x 9 places of
+    values around 3 at most: sums of a few hundred terms below 100, u = 2^-24 each, pass through at most three products."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    starts, off, Lq, Lk = [0, 1, 2, 4], 3, 7, 9
+    b = mb.RelposBuckets(starts, two_sided, causal)
+    r = torch.arange(Lk)[None, :] - torch.arange(Lq)[:, None] - off
+    d = r.abs() if two_sided else (-r).clamp(min=0)
+    k = torch.bucketize(d, torch.tensor(starts), right=True) - 1
+    k = (torch.where(r > 0, k + 4, k) if two_sided else k).cuda()
+    seen = torch.ones_like(k, dtype=torch.bool) if not causal else (r <= 0).cuda()
+    scores = torch.randn(2, 2, Lq, Lk, generator=g, device="cuda").requires_grad_()
+    table = torch.randn(b.rows, 2, generator=g, device="cuda").requires_grad_()
+    s64, t64 = scores.detach().double().requires_grad_(), table.detach().double().requires_grad_()
+
+    def loss(s, t, own):
+        if own:
+            x = sq.add_relpos_bias(s, t, b, off) if added else s + sq.relpos_bias(t, b, Lq, Lk, off)
+        else:
+            x = s + torch.where(seen, t.t()[:, k], float("-inf"))
+        x = torch.where(seen, x, 0.0)
+        ds, dt = torch.autograd.grad(x.square().sum() + x.sum(), (s, t), create_graph=True)
+        return x.sum() + dt.square().sum() * 0.01 + ds.square().sum()
+
+    got = torch.autograd.grad(loss(scores, table, True), (scores, table))
+    want = torch.autograd.grad(loss(s64, t64, False), (s64, t64))
+    for x, y in zip(got, want):
+        assert float((x.double() - y).abs().max()) <= 1e-4 * max(1.0, float(y.abs().max()))
+    assert float(want[1].abs().max()) > 1.0
+
+
+def test_gradient_of_the_tables_gradient_in_16_bits():
+    """What the mask hides gets 0, whatever the direction holds; values are the direction's, rounded once."""
+    b = mb.RelposBuckets([0, 2], causal=True)
+    grad = torch.randn(3, 1, 5, 6, device="cuda").bfloat16().requires_grad_()
+    dt = sq._TableGradient.apply(grad, b, 1)
+    way = torch.tensor([[float("inf")], [0.3]], device="cuda")
+    (dd,) = torch.autograd.grad(dt, grad, way)
+    r = torch.arange(6)[None, :] - torch.arange(5)[:, None] - 1
+    want = torch.where(r > 0, 0.0, torch.where(r > -2, float("inf"), 0.3)).bfloat16().cuda()
+    assert dd.dtype == torch.bfloat16 and torch.equal(dd, want.expand(3, 1, 5, 6))
