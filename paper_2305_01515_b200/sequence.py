@@ -175,45 +175,75 @@ def add_relpos_bias(scores: torch.Tensor, table: torch.Tensor, buckets: mb.Relpo
 
 class AdamW:
     """AdamW over a list of parameters in one launch a step; the gradients are p.grad at the time of the step.  state_bits: 32 or 8; masters:
-    keep fp32 copies of 16-bit parameters.  Tensors of one dimension (biases, scales) take no weight decay."""
+    keep fp32 copies of 16-bit parameters.  Tensors of one dimension (biases, scales) take no weight decay.  A parameter whose storage was
+    replaced by another of its size and type (p.data = ..., module.to(...)) is found at the next step and updated where it is then."""
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  state_bits: int = 32, masters: bool = False):
         self.params = list(params)
-        if not self.params or any(p.dtype != self.params[0].dtype or not p.is_contiguous() for p in self.params):
-            raise ValueError("parameters: contiguous, of one type")
-        kind = _kind(self.params[0], "parameters")
-        for k, p in enumerate(self.params):
-            _same_device(p, self.params[0].device, f"parameter {k}")
+        if not self.params:
+            raise ValueError("no parameters")
+        self._kind, self._dtype, self._device = _kind(self.params[0], "parameters"), self.params[0].dtype, self.params[0].device
+        self._sizes, self._state_bits = [p.numel() for p in self.params], state_bits
+        self._check_params()
         self.lr, self.betas, self.eps, self.weight_decay, self.steps = lr, betas, eps, weight_decay, 0
         for p in self.params:
             if p.grad is None:
                 p.grad = torch.zeros_like(p)
         self.masters = [p.detach().float() for p in self.params] if masters else None
-        self._grads = [p.grad for p in self.params]
-        with torch.cuda.device(self.params[0].device):
-            self.handle = mb.AdamW([p.numel() for p in self.params], kind, kind, state_bits, [p.detach() for p in self.params], self._grads,
-                                   self.masters, decays=[p.dim() > 1 for p in self.params])
-        self.state = torch.zeros(self.handle.state_bytes, dtype=torch.uint8, device=self.params[0].device)
+        self._make_handle([p.grad for p in self.params])
+        self.state = torch.zeros(self.handle.state_bytes, dtype=torch.uint8, device=self._device)
+
+    def _check_params(self) -> None:
+        for k, (p, n) in enumerate(zip(self.params, self._sizes)):
+            if p.dtype is not self._dtype or p.numel() != n or not p.is_contiguous():
+                raise ValueError(f"parameter {k}: parameters are contiguous, of one type, and keep their sizes")
+            _same_device(p, self._device, f"parameter {k}")
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("a parameter is given twice, or two of them share memory")
+
+    def _make_handle(self, grads: List[torch.Tensor]) -> None:
+        with torch.cuda.device(self._device):
+            self.handle = mb.AdamW(self._sizes, self._kind, self._kind, self._state_bits, [p.detach() for p in self.params], grads, self.masters,
+                                   decays=[p.dim() > 1 for p in self.params])
+        self._grads = grads                                 # the handle holds their addresses: they stay until it has others
+        self._param_at, self._grad_at = [p.data_ptr() for p in self.params], [g.data_ptr() for g in grads]
+
+    @torch.no_grad()
+    def refresh_masters(self) -> None:
+        """After new values were written into the parameters (loaded weights): a master that does not round to its parameter takes its value."""
+        for p, m in zip(self.params, self.masters or []):
+            m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))
 
     @torch.no_grad()
     def step(self, grad_scale: Optional[torch.Tensor] = None) -> None:
         grads = [p.grad for p in self.params]
-        for p, g in zip(self.params, grads):
-            if g is None or g.dtype != p.dtype or not g.is_contiguous():
+        for g, n in zip(grads, self._sizes):
+            if g is None or g.dtype is not self._dtype or g.numel() != n or not g.is_contiguous():
                 raise ValueError("every parameter needs a contiguous gradient of its own type")
-            _same_device(g, self.params[0].device, "a gradient")
+        # the handle holds addresses: what lies elsewhere now is looked at and handed over
+        param_at, grad_at = [p.data_ptr() for p in self.params], [g.data_ptr() for g in grads]
+        moved, renewed = param_at != self._param_at, grad_at != self._grad_at
+        if moved:
+            self._check_params()
+        if renewed and {g.get_device() for g in grads} != {self._device.index}:
+            raise ValueError(f"a gradient is not on {self._device}")
         if grad_scale is not None:
             if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
                 raise ValueError(f"grad_scale: one fp32 number, not {grad_scale.dtype} {tuple(grad_scale.shape)}")
-            _same_device(grad_scale, self.params[0].device, "grad_scale")
-        stream = torch.cuda.current_stream(self.params[0].device)
-        with torch.cuda.device(self.params[0].device):
-            if any(g.data_ptr() != o.data_ptr() for g, o in zip(grads, self._grads)):
-                mb.adamw_set_grads(self.handle, grads, stream)
-            self._grads = grads
-            self.steps += 1
-            mb.adamw_step(self.handle, self.state, self.lr, *self.betas, self.eps, self.weight_decay, self.steps, grad_scale, self.steps, stream)
+            _same_device(grad_scale, self._device, "grad_scale")
+        stream = torch.cuda.current_stream(self._device)
+        if moved:
+            torch.cuda.synchronize(self._device)            # steps that still use the old description
+            self.refresh_masters()
+            self._make_handle(grads)
+        with torch.cuda.device(self._device):
+            if renewed:
+                mb.adamw_set_grads(self.handle, grad_at, stream)
+            self._grads, self._grad_at = grads, grad_at
+            mb.adamw_step(self.handle, self.state, self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1, grad_scale, self.steps + 1, stream)
+        self.steps += 1
 
     def zero_grad(self) -> None:
         for p in self.params:

@@ -262,3 +262,61 @@ def test_gradient_of_the_tables_gradient_in_16_bits():
     r = torch.arange(6)[None, :] - torch.arange(5)[:, None] - 1
     want = torch.where(r > 0, 0.0, torch.where(r > -2, float("inf"), 0.3)).bfloat16().cuda()
     assert dd.dtype == torch.bfloat16 and torch.equal(dd, want.expand(3, 1, 5, 6))
+
+
+@pytest.mark.parametrize("masters,dtype", [(False, torch.float32), (True, torch.bfloat16)])
+def test_adamw_follows_a_parameter_whose_storage_is_replaced(masters, dtype):
+    """The same steps with and without moving a parameter between them: the same values, and the old storage stays as it was."""
+    results = []
+    for move in (False, True):
+        g = torch.Generator(device="cuda").manual_seed(5)
+        params = [torch.randn(40, 9, generator=g, device="cuda").to(dtype).requires_grad_() for _ in range(3)]
+        opt = sq.AdamW(params, lr=1e-2, masters=masters)
+        for k in range(4):
+            if move and k == 2:
+                old = params[1].data
+                params[1].data = old.clone()
+                kept = old.clone()
+            for p in params:
+                p.grad.copy_(torch.randn(40, 9, generator=g, device="cuda"))
+            opt.step()
+        if move:
+            assert torch.equal(old, kept) and not torch.equal(params[1].data, kept)
+        results.append([p.detach().clone() for p in params] + (opt.masters or []))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_adamw_takes_loaded_weights_into_its_masters():
+    w = torch.randn(30, 8, device="cuda").bfloat16().requires_grad_()
+    opt = sq.AdamW([w], lr=1e-3, weight_decay=0.0, masters=True)
+    w.grad.fill_(1.0)
+    for _ in range(3):
+        opt.step()
+    fine = opt.masters[0].clone()
+    opt.refresh_masters()
+    assert torch.equal(opt.masters[0], fine)               # they round to the parameter: nothing to take
+    with torch.no_grad():
+        w[:10] = 5.0                                       # in place
+        opt.refresh_masters()
+    assert bool((opt.masters[0][:10] == 5.0).all()) and torch.equal(opt.masters[0][10:], fine[10:])
+    w.data = torch.full_like(w, 7.0)                       # other storage: taken at the next step
+    opt.step()
+    assert float((opt.masters[0] - 7.0).abs().max()) < 2e-3
+
+
+def test_adamw_refuses_shared_and_changed_parameters():
+    w = torch.ones(6, 8, device="cuda")
+    a, b = w[:4].detach(), w[3:].detach()
+    for params in ([w, w], [a, b], [w, a]):
+        with pytest.raises(ValueError):
+            sq.AdamW([p.requires_grad_() for p in params])
+    p = torch.ones(6, 8, device="cuda").requires_grad_()
+    q = torch.ones(6, 8, device="cuda").requires_grad_()
+    opt = sq.AdamW([p, q])
+    for bad in (torch.ones(5, 8, device="cuda"), torch.ones(8, 6, device="cuda").t(), q.data):
+        p.grad = None
+        p.data = bad
+        p.grad = torch.ones_like(bad)
+        with pytest.raises(ValueError):
+            opt.step()
+    assert opt.steps == 0 and bool((q == 1.0).all())
