@@ -670,14 +670,17 @@ int mts_relpos_bias_backward(const mts_relpos_buckets* buckets, const void* grad
  *                  (255 codes), rounded up or down by 16 random bits so that it is kept in the mean: with beta2 near 1
  *                  a step moves v by less than half a code.  The bits are a hash of (element, seed): another `seed`
  *                  for every step, the same one gives the same result.  A v that is not 0 keeps at least code 1 (a
- *                  block whose largest is below 2^-120 is stored as 0).  Moments that are not finite are stored as 0
- *                  (their parameter shows them) and leave the rest of their block alone.
+ *                  block whose largest is below 2^-120 is stored as 0).  An element of which either moment is not finite
+ *                  has both stored as 0 and leaves the rest of its block alone.
+ * A gradient that is not finite shows in its parameter.  A finite one whose square is not (from 1.8e19 on) moves the parameter by
+ * the decay alone in that step; after it the element starts anew with 8 bits and keeps v = infinity (no more updates) with 32.
+ * An eps below 2^-126 counts as 0.
  * mts_adamw_create copies the description to the device (synchronous; the only allocation); mts_adamw_set_grads replaces
  * the gradient pointers (host array, read before the call returns) for later steps on `stream`, whose pending steps keep
  * the old ones; a stream that is being captured into a graph is refused (UNSUPPORTED): set them before the capture.
  * grad_scale: device fp32 scalar, nullable (1): a clipping factor or the inverse of a loss scale.
  * mts_adamw_export_state / _import_state: the moments as fp32 device arrays [P] (16-byte aligned), out of and into a
- * state; an 8-bit import rounds both to nearest.
+ * state; an 8-bit import rounds both to nearest, negative second moments count as 0.
  * Errors: INVALID_ARG, ALIGNMENT (state), WORKSPACE (state too small), UNSUPPORTED (P >= 2^40), CUDA. */
 #define MTS_ADAMW_BLOCK 256
 typedef struct {

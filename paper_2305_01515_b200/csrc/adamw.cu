@@ -99,12 +99,11 @@ __device__ __forceinline__ void encode_block(float (&m)[8], float (&v)[8], int64
   }
   tm = __reduce_max_sync(0xFFFFFFFFu, tm);
   tv = __reduce_max_sync(0xFFFFFFFFu, tv);
-  if (max(tm, tv) >= NOT_FINITE) {                                      // the whole warp: stored as 0, the rest by the largest of them
-    tm = tv = 0;
+  if (max(tm, tv) >= NOT_FINITE) {                                      // the whole warp: both moments of such an element are stored as 0
+    tm = tv = 0;                                                        // (one without the other is a step of its own size), the rest by the largest
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if ((__float_as_uint(m[k]) & 0x7FFFFFFFu) >= NOT_FINITE) m[k] = 0.f;
-      if (__float_as_uint(v[k]) >= NOT_FINITE) v[k] = 0.f;
+      if (max(__float_as_uint(m[k]) & 0x7FFFFFFFu, __float_as_uint(v[k])) >= NOT_FINITE) m[k] = v[k] = 0.f;
       tm = max(tm, __float_as_uint(m[k]) & 0x7FFFFFFFu);
       tv = max(tv, __float_as_uint(v[k]));
     }
@@ -242,6 +241,8 @@ adamw_import_kernel(AdamState st, int64_t blocks, const float* __restrict__ m_in
     m[4 * h] = a.x; m[4 * h + 1] = a.y; m[4 * h + 2] = a.z; m[4 * h + 3] = a.w;
     v[4 * h] = b.x; v[4 * h + 1] = b.y; v[4 * h + 2] = b.z; v[4 * h + 3] = b.w;
   }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = v[k] <= 0.f ? 0.f : v[k];          // -0 among them: the codes have no sign
   encode_block<false>(m, v, block, 0u, st);
 }
 

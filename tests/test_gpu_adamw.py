@@ -258,3 +258,60 @@ def test_first_step_on_a_stream_that_does_not_wait_for_the_default_one():
         mb.adamw_step(h, state, 0.1, 0.9, 0.999, 1e-8, 0.0, 1, stream=side)
         torch.cuda.synchronize()
         assert float((params + 0.1).abs().max()) < 1e-6
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_gradient_whose_square_overflows(bits, grad):
+    """One step with gradients of 1e20 and -3e38, then ordinary ones: a step of Adam moves a parameter by lr * sqrt(10) at most here ((1 - beta1) / sqrt(1 - beta2)
+    = 0.1 / 0.0316, of corrected moments less), so ten of them stay within 32 lr.  The rest of the block is as without them."""
+    p, q = (Problem([1000], grad=grad, bits=bits, seed=9, lr=1e-2, decay=0.0) for _ in range(2))
+    hit = [10, 300, 301]
+    rest = torch.ones(1000, dtype=torch.bool, device=DEV)
+    rest[hit] = False
+    start = p.params[0].clone()
+    for k in range(10):
+        g = torch.randn(1000, device=DEV, generator=torch.Generator(device=DEV).manual_seed(k)).to(grad)
+        for x in (p, q):
+            x.grads[0].copy_(g)
+            x.grads[0][hit] = 0.0
+        if k == 2:
+            p.grads[0][hit] = torch.tensor([1e20, -3e38, 2e19], device=DEV).to(grad)
+        if k > 2:
+            p.grads[0][hit] = g[hit]
+        p.step(seed=k)
+        q.step(seed=k)
+        moved = (p.params[0] - start).abs()
+        assert float(moved.max()) <= 32 * 1e-2, (k, float(moved[hit].max()))
+        if k == 2:
+            assert torch.equal(p.params[0][hit], start[hit])
+    assert torch.equal(p.params[0][rest], q.params[0][rest])
+    m, v = p.moments()
+    if bits == 8:
+        assert np.isfinite(m).all() and np.isfinite(v).all() and (v[hit] > 0).all()
+        assert float(moved[hit].min()) > 0
+    else:
+        assert np.isinf(v[hit]).all() and float(moved[hit].max()) == 0.0
+
+
+def test_import_of_moments_that_are_not_finite():
+    """Either one of an element: both are 0, the others as without it."""
+    p = Problem([700], bits=8, seed=10)
+    m = torch.randn(p.h.elements, device=DEV)
+    v = torch.rand(p.h.elements, device=DEV)
+    clean = [x.clone() for x in (m, v)]
+    hit = [3, 4, 300, 301]
+    for x in clean:
+        x[hit] = 0.0
+    m[3], m[300], v[4], v[301] = float("inf"), float("nan"), float("inf"), float("nan")
+    mb.adamw_import_state(p.h, p.state, m, v)
+    got = p.moments()
+    mb.adamw_import_state(p.h, p.state, *clean)
+    want = p.moments()
+    assert all(np.array_equal(a, b) for a, b in zip(got, want))
+    v[[3, 4, 300, 301, 600]], m[[3, 4, 300, 301]] = torch.tensor([0.0, -0.0, -1.0, -float("inf"), -0.0], device=DEV), 0.0
+    clean[1][600] = 0.0
+    mb.adamw_import_state(p.h, p.state, m, v)
+    got = p.moments()
+    mb.adamw_import_state(p.h, p.state, *clean)
+    assert got[0][600] != 0 and all(np.array_equal(a, b) for a, b in zip(got, p.moments()))
