@@ -35,9 +35,16 @@ def _stride(t: torch.Tensor) -> int:
     return max(t.stride(0), t.shape[1])
 
 
+def _check_status(workspace: torch.Tensor) -> None:
+    """Waits for the call that used this workspace; offsets out of order or range raise, a wait that ran out does in the binding."""
+    with torch.cuda.device(workspace.device):
+        if mb.recurrence_status(workspace, torch.cuda.current_stream(workspace.device)):
+            raise ValueError("offsets do not run from 0 to N in order: the rows that they leave out hold nothing")
+
+
 class _GatedRecurrence(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, gate, value, offsets, h0):
+    def forward(ctx, gate, value, offsets, h0, check):
         if gate.dim() != 2 or gate.shape != value.shape or gate.dtype != value.dtype:
             raise ValueError(f"gate {tuple(gate.shape)} {gate.dtype} and value {tuple(value.shape)} {value.dtype} must be alike, [N, D]")
         if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_cuda or not offsets.is_contiguous():
@@ -58,6 +65,9 @@ class _GatedRecurrence(torch.autograd.Function):
         with torch.cuda.device(gate.device):
             mb.recurrence_forward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, out, D, final, entry, ws,
                                   ws.numel(), torch.cuda.current_stream(gate.device))
+        if check:
+            _check_status(ws)
+        ctx.check = check
         ctx.save_for_backward(gate, value, offsets, h0, entry)
         return out, final
 
@@ -73,12 +83,16 @@ class _GatedRecurrence(torch.autograd.Function):
         with torch.cuda.device(gate.device):
             mb.recurrence_backward(gate, _stride(gate), value, _stride(value), kind, N, D, offsets, S, h0, entry, grad_out, _stride(grad_out),
                                    grad_final, d_gate, D, d_value, D, d_h0, ws, ws.numel(), torch.cuda.current_stream(gate.device))
-        return d_gate, d_value, None, d_h0
+        if ctx.check:
+            _check_status(ws)
+        return d_gate, d_value, None, d_h0, None
 
 
-def gated_recurrence(gate: torch.Tensor, value: torch.Tensor, offsets: torch.Tensor, h0: Optional[torch.Tensor] = None):
-    """h_t = h_{t-1} + sigmoid(gate_t) (value_t - h_{t-1}) over packed sequences: (h [N, D], state after each sequence fp32 [S, D])."""
-    return _GatedRecurrence.apply(gate, value, offsets, h0)
+def gated_recurrence(gate: torch.Tensor, value: torch.Tensor, offsets: torch.Tensor, h0: Optional[torch.Tensor] = None, check: bool = False):
+    """h_t = h_{t-1} + sigmoid(gate_t) (value_t - h_{t-1}) over packed sequences: (h [N, D], state after each sequence fp32 [S, D]).
+    First derivatives only.  The offsets are on the GPU and are trusted: they have to run from 0 to N in order, else rows of the results are
+    undefined.  check: wait for the call, and for its backward, and raise where they do not."""
+    return _GatedRecurrence.apply(gate, value, offsets, h0, check)
 
 
 def log_bucket_starts(n: int, far: int) -> List[int]:

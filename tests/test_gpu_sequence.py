@@ -320,3 +320,21 @@ def test_adamw_refuses_shared_and_changed_parameters():
         with pytest.raises(ValueError):
             opt.step()
     assert opt.steps == 0 and bool((q == 1.0).all())
+
+
+@pytest.mark.parametrize("S", [3, 80])                      # by chunks, and a thread for every channel of a sequence
+def test_recurrence_reports_offsets_that_do_not_fit(S):
+    x = torch.randn(60, 16, device="cuda").requires_grad_()
+    good = torch.linspace(0, 60, S + 1).long().cuda()
+    for k, bad in ((S, 59), (S, 61), (0, 1), (1, -3), (1, 45)):
+        off = good.clone()
+        off[k] = bad
+        with pytest.raises(ValueError):
+            sq.gated_recurrence(x, x, off, check=True)
+    h, _ = sq.gated_recurrence(x, x, good, check=True)
+    h.sum().backward()
+    off = good.clone()                                     # changed between the two: the backward says so
+    h, _ = sq._GatedRecurrence.apply(x, x, off, None, True)
+    off.data[1] = 45
+    with pytest.raises(ValueError):
+        h.sum().backward()
