@@ -366,7 +366,7 @@ extern "C" int mts_relpos_bias_forward(const mts_relpos_buckets* buckets, const 
     // more blocks down than a grid has room for
     int rows = 128;
     while (rows > 8 && ceil_div(Lq, rows) * strips * heads < FWD_WANTED) rows /= 2;
-    while (ceil_div(Lq, rows) > 65535) rows *= 2;
+    if (ceil_div(Lq, rows) > 65535) rows = (int)ceil_div(Lq, 65535);      // 8,193 at most: 164 KB of shared memory
     const int pitch = (int)align_up((size_t)(Lk < FWD_COLS ? Lk : FWD_COLS) + (size_t)rows, 16);
     const size_t smem = (size_t)pitch * 16;
     if (smem > 48 * 1024) {

@@ -191,3 +191,14 @@ def test_gradient_is_the_same_every_time_and_on_a_side_stream():
         torch.cuda.synchronize()
         results.append(out)
     assert all(torch.equal(results[0], r) for r in results)
+
+
+@pytest.mark.parametrize("Lq", [65535 * 128 + 5, (1 << 29) - 1])
+def test_forward_of_as_many_queries_as_there_may_be(Lq):
+    """One key: the column is the table's rows by distance, then the last one to the end."""
+    table = torch.tensor([[1.0], [2.0], [3.0]], device=DEV)
+    b = mb.RelposBuckets([0, 1, 70])
+    out = torch.zeros(Lq, dtype=torch.bfloat16, device=DEV)
+    mb.relpos_bias_forward(b, table, mb.DTYPE_FP32, 1, Lq, 1, 0, out, mb.DTYPE_BF16, Lq, 1)
+    torch.cuda.synchronize()
+    assert float(out[0]) == 1.0 and bool((out[1:70] == 2.0).all()) and bool((out[70:] == 3.0).all())
