@@ -312,7 +312,7 @@ extern "C" int mts_adamw_create(const mts_adamw_desc* d, mts_adamw** out) {
   for (int k = 0; k < d->n_tensors; ++k) {
     const int64_t n = d->host_sizes[k];
     if (n < 0) return set_error(MTS_ERR_INVALID_ARG, "adamw_create: tensor %d has %lld elements", k, (long long)n);
-    if (n >= (1ll << 40) || elements >= (1ll << 40))
+    if (n >= (1ll << 40) || elements + ceil_div(n, ADAM_BLOCK) * ADAM_BLOCK >= (1ll << 40))
       return set_error(MTS_ERR_UNSUPPORTED, "adamw_create: 2^40 elements or more");
     if (n > 0 && (!d->host_params[k] || !d->host_grads[k] || (d->host_masters && !d->host_masters[k])))
       return set_error(MTS_ERR_INVALID_ARG, "adamw_create: null pointer of tensor %d", k);

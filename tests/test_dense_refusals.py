@@ -119,6 +119,12 @@ def test_adamw_handle_refusals():
     assert float(x.abs().sum()) == 0.0
 
 
+def test_adamw_counts_the_last_tensor_too():
+    half = 1 << 39
+    for sizes in ((half, half), (half, half - 1), ((1 << 40) - 1,)):     # with the gaps up to whole blocks 2^40 elements each
+        refused(mb.ERR_UNSUPPORTED, mb.AdamW, sizes, 0, 0, 32, (P,) * len(sizes), (P,) * len(sizes))
+
+
 @pytest.mark.gpu
 def test_adamw_refuses_null_gradients_of_tensors_that_have_elements():
     import torch
