@@ -618,6 +618,8 @@ class RelposBuckets:
     def __init__(self, starts: Sequence[int], two_sided: bool = False, causal: bool = False):
         self.n = len(starts)
         self.rows = self.n * (2 if two_sided else 1)
+        if any(not -(1 << 31) <= int(x) < 1 << 31 for x in starts):
+            raise ValueError("bucket starts are 32-bit numbers")            # ctypes would drop the upper bits
         self._starts = (C.c_int32 * max(self.n, 1))(*[int(x) for x in starts])
         self.desc = RelposBucketsDesc(self.n, int(two_sided), int(causal), self._starts)
         self.ref = C.byref(self.desc)

@@ -58,6 +58,13 @@ def test_relpos_buckets():
     call(Lk=0)
 
 
+def test_relpos_bucket_starts_that_do_not_fit():
+    for far in (1 << 31, (1 << 32) + 5, -(1 << 31) - 1):
+        with pytest.raises(ValueError):
+            mb.RelposBuckets((0, far))
+    assert list(mb.RelposBuckets((0, (1 << 31) - 1))._starts) == [0, (1 << 31) - 1]
+
+
 def test_relpos_gradient():
     b = mb.RelposBuckets((0, 1, 2), two_sided=True)
     need = mb.relpos_bias_workspace_bytes(b, 2)
