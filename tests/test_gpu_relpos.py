@@ -202,3 +202,22 @@ def test_forward_of_as_many_queries_as_there_may_be(Lq):
     mb.relpos_bias_forward(b, table, mb.DTYPE_FP32, 1, Lq, 1, 0, out, mb.DTYPE_BF16, Lq, 1)
     torch.cuda.synchronize()
     assert float(out[0]) == 1.0 and bool((out[1:70] == 2.0).all()) and bool((out[70:] == 3.0).all())
+
+
+# Blocks with long runs of patches (8 rows x 32 lanes of 16 bytes, or of four columns): several for every warp, runs that go on from one batch entry to the
+# next, and bands of more than 768, after which the sums are handed on.  592 blocks are shared by the heads; from 297 heads on each has one.
+@pytest.mark.parametrize("B,H,Lq,Lk,off,heads_alike", [(3, 5, 1000, 1200, 100, False), (3, 5, 997, 1203, 100, False), (17, 297, 400, 400, 0, True),
+                                                     (17, 297, 397, 403, 10, True), (130, 297, 64, 136, -20, True), (900, 300, 9, 33, 5, True)])
+@pytest.mark.parametrize("two_sided,causal", [(True, False), (False, True)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_many_patches(B, H, Lq, Lk, off, heads_alike, two_sided, causal, dtype):
+    grad = torch.randn(B, 1 if heads_alike else H, Lq, Lk, device=DEV).to(dtype)
+    got = backward(STARTS, two_sided, causal, off, grad.expand(B, H, Lq, Lk)).double()
+    k = torch.from_numpy(bucket_table(STARTS, two_sided, causal, Lq, Lk, off)).to(DEV).reshape(-1)
+    rows = len(STARTS) * (2 if two_sided else 1)
+    for h in range(grad.shape[1]):
+        g = grad[:, h].double().reshape(B, -1)
+        total = torch.zeros(rows + 1, dtype=torch.float64, device=DEV).index_add_(0, k % (rows + 1), g.sum(0))[:rows]
+        size = torch.zeros(rows + 1, dtype=torch.float64, device=DEV).index_add_(0, k % (rows + 1), g.abs().sum(0))[:rows]
+        for x in (got if heads_alike else got[:, h:h + 1]).unbind(1):
+            assert bool(((x - total).abs() <= 1024 * U * size + U * total.abs()).all()), float((x - total).abs().max())
