@@ -606,12 +606,11 @@ __global__ void __launch_bounds__(32, FWD_BLOCKS)
 recurrence_forward_kernel(const RecArgs a, T* __restrict__ out, int64_t out_stride, float* h_final, float* __restrict__ entry) {
   __shared__ int32_t first_of[REC_PART], last_of[REC_PART];
   const Piece it(a, false);
-  if (!it.walk && a.chunks > 0) return forward_map<T, V, VEC>(a, it);
+  if (!it.walk) return forward_map<T, V, VEC>(a, it);
   const auto empty_row = [&](int64_t s) {
     if (h_final)
       for (int d = lane_id(); d < a.D; d += 32) h_final[s * a.D + d] = a.h0 ? a.h0[s * a.D + d] : 0.f;
   };
-  if (a.chunks == 0) return check_offsets(a, blockIdx.x, gridDim.x, empty_row);
   const int c = (it.strip * 32 + lane_id()) * V, left = a.D - c, tokens = (int)(it.t1 - it.t0);
   Rows<T, V, VEC> gate(a.gate, a.gate_stride, it.t0, c, left), value(a.value, a.value_stride, it.t0, c, left), to(out, out_stride, it.t0, c, left);
   Raw<T, V> g[FWD_BATCH], x[FWD_BATCH];
@@ -942,7 +941,7 @@ RecArgs arguments(const void* gate, int64_t gate_stride, const void* value, int6
   return a;
 }
 
-// A warp for every piece of work, at least one for the check of the offsets.
+// A warp for every piece of work; without tokens (the backward's, the forward then takes the single-token kernel) one for the offsets.
 template <typename Kernel, typename... Args>
 int launch_pieces(const char* what, int trace_id, Kernel kernel, const RecArgs& a, cudaStream_t s, Args... args) {
   const int64_t warps = 2 * (int64_t)a.chunks * a.strips;
