@@ -588,6 +588,7 @@ int mts_cache_set_fetch_wait_limit(mts_cache* cache, int64_t polls);
  * [offsets[s], offsets[s+1]) of [N, D] arrays (offsets int64 [S+1] on the device, offsets[0] == 0,
  * offsets[S] == N, the CSR form of the sparse input).  Per channel, with z_t = 1 / (1 + exp(-gate_t)):
  *   h_t = h_{t-1} + z_t * (value_t - h_{t-1}),   h before a sequence's first token = h0[s] (0 when h0 is NULL)
+ * (an infinite state is NaN from the next token on, as the formula's infinity - infinity; other sequences are not touched)
  *   gate, value, out : [N, D] of one type (MTS_DTYPE_*), rows *_stride elements apart (>= D), so that gate and
  *                      value may be column ranges of one projection; out must not overlap the inputs.
  *   h0, h_final      : fp32 [S, D]; h_final (nullable) receives the state after each sequence's last token, h0 for

@@ -10,7 +10,7 @@
 // one tensor, found through a map made once, so that tensors of any number and size share one launch.
 //
 // Parameters in 16 bits with fp32 masters and moments, 120 M elements of 28 bytes: 521 to 533 us on different GPUs, 96 to 98.6% of the copy rate.  8-bit moments with
-// fp32 parameters and bf16 gradients, 100 M elements of 14 bytes: step 320 us, 4.4 TB/s: 80 instructions per element, a third of them for
+// fp32 parameters and bf16 gradients, 100 M elements of 14 bytes: step 320 to 325 us, 4.4 TB/s: 80 instructions per element, a third of them for
 // the codes, keep the integer units busy (113 with correctly rounded root and quotient and the check for finite values by element:
 // 437 us); their export, 10 bytes per element, 152 us at the copy rate.
 #include <math.h>
@@ -79,7 +79,8 @@ __device__ __forceinline__ uint32_t encode_second(float x, float inv, uint32_t a
   const uint32_t q = max((__float_as_uint(__fmul_rn(x, inv)) + add) >> 20, BASE_V + 1u) - BASE_V;
   return x > 0.f ? q : 0u;
 }
-// 16 random bits of (element, seed) in the upper half of the word: two rounds of multiply and shift.
+// 16 random bits of (element, seed) in the upper half of the word: two rounds of multiply and shift, with the 32-bit pair of multipliers and
+// shifts that C. Wellons published in "Prospecting for Hash Functions" (2018).
 __device__ __forceinline__ uint32_t mix(uint32_t element, uint32_t seed_word) {
   uint32_t w = element * 0x9E3779B1u + seed_word;
   w = (w ^ (w >> 15)) * 0x2C1B3C6Du;

@@ -9,14 +9,17 @@
 //   map:  the chunk's map, if its last sequence goes on behind it, from that sequence's start on (what lies before it in the chunk is
 //         forgotten).  The last warp of eight neighbours composes their map, and so on; behind every 512 chunks a state is kept.
 //   walk: the state before the chunk from at most seven maps of each of three levels and a kept state, then the chunk's tokens.
-// Warps take the pieces from a counter, a walk some thousands of pieces behind its chunk's map: by then the maps it needs have long been
-// published (a word written by one SM is seen by another only 1 to 2 us later).  The association of the maps depends on the
+// Warps take the pieces from a counter: all maps, then all walks in calls of up to REC_LAG pieces of a kind, else in turn, a walk REC_LAG
+// pieces behind its chunk's map.  By then the maps it needs have long been published (a word written by one SM is seen by another only 1 to
+// 2 us later).  The association of the maps depends on the
 // offsets alone: the result is the same in every run.
 //
 // What bounds it: memory.  A chunk's rows are read for its map and again for its walk (in the backward: gate and gradient, then all
-// three), which the L2 cache does not hold in between.  524,287 tokens x 256 in fp16, one sequence: 219 us, 6.1 TB/s of what is
-// moved, 3.7 TB/s of each input once; 1,000 histories of 120,007 tokens in bf16: 70 us; forward and backward of 2,048 histories,
-// 250,001 x 200: 108 + 164 us.  Ragged calls of that size are one wave of warps, whose tokens go one after the other.
+// three), which the L2 cache does not hold in between.  524,287 tokens x 256 in fp16, one sequence: 218 to 228 us on different GPUs, 5.9 to
+// 6.1 TB/s of what is moved (reads from memory are twice the inputs), 3.5 to 3.7 TB/s of each input once; 1,000 histories of 120,007 tokens
+// in bf16: 69 us (1.8 times the inputs); forward and backward of 2,048 histories, 250,001 x 200: 106 + 160 us (1.7 and 1.4 times).  In all of
+// these every map comes before the walks; 262,143 x 1,024 in bf16, in turn: 420 us.  Ragged calls of that size are one wave of warps, whose
+// tokens go one after the other.
 //
 // Waiting: a piece waits only for pieces of lower numbers, which running or finished warps have taken, and the lowest unfinished one
 // waits for nothing.  Every wait has a limit all the same, after which the status word says so.
@@ -34,8 +37,10 @@ namespace mts {
 // in the forward, 20 and 24 of them a tenth more than 16 (registers spill); 10, 11, 12, 14 take 177 / 167 / 168 / 184 us in the backward.
 constexpr int FWD_BLOCKS = 16, BWD_BLOCKS = 12;
 constexpr int REC_WARPS_WANTED = 2368;            // chunks are halved until there are so many pieces of a kind: 16 per SM
-// Pieces between a chunk's map and its walk.  512 to 100 million were tried: the map's readers must not wait (below 2,048 the backward
-// takes a tenth longer), and no lag keeps the rows in the L2 cache until the walk (memory reads are 1.7 to 2 times the inputs at all of them).
+// Pieces between a chunk's map and its walk; calls with fewer of a kind take all maps first.  512, 2,048, 4,096 and all of them: one sequence of
+// 524,287 x 256 in bf16 (4,096 of a kind) 255 / 227 / 218 / 218 us, with its backward 640 / 581 / 566 / 566; 262,143 x 1,024 (8,192) 460 / 424 / 420 / 427
+// and 1,198 / 1,102 / 1,090 / 1,095; 1,048,575 x 256 (8,192) 469 / 428 / 420 / 426: a walk must not wait for its maps, and a short way does not
+// keep the rows in the L2 cache.
 constexpr int REC_LAG = 4096;
 constexpr int REC_CHUNK = 256;                    // tokens of a chunk at most
 constexpr int REC_PART = 64;                      // tokens whose borders are looked up together: a bit mask of them is one word
@@ -516,7 +521,7 @@ struct Rows {
   }
 };
 // Brings rows 8 to 15 behind where two arrays stand towards the L2 cache: every lane asks for half a strip of one row.  The registers
-// hold a batch on its way, which is less than the memory's latency needs: 524,287 tokens x 256 take 219 us with it, 233 without, 226 from eight rows
+// hold a batch on its way, which is less than the memory's latency needs: 524,287 tokens x 256 take 219 us with it, on the same GPU 233 without and 226 from eight rows
 // further on.  In the backward it costs as much as it gives (169 / 168 us), but for the kept states (164).
 template <typename T, int V, bool VEC>
 struct Ahead {

@@ -58,7 +58,7 @@ relpos_forward_direct(const __grid_constant__ Buckets b, BiasGeometry g, const v
 // A block writes `rows` queries x up to FWD_COLS keys of one head: bound by the bytes it writes.  It holds their part of the vector in shared memory once for each of the
 // 16 / sizeof(T) positions that a 16-byte boundary can have in it, so that every row is one bulk copy to global memory from an
 // aligned place of one of the copies, whatever its window and the alignment of the row; up to 15 bytes at either end of a row are
-// stored by threads.  16 x 4,096 x 4,096 in bf16: 88.6 us, 6.06 TB/s, 93% of the copy rate (a thread per element: 1,320 us, a search of
+// stored by threads.  16 x 4,096 x 4,096 in bf16: 88.6 to 89.7 us, 6.0 TB/s, 92% of the copy rate (a thread per element: 1,320 us, a search of
 // the buckets each); 12 x 1,023 x 1,023: 10.2 us.
 //
 // Blocks a call is cut into, where it has the rows.  148, 296, 592 and 1,184 take 12.4 / 12.4 / 16.4 / 16.4 us for 4 x 2,048 x 2,048 in bf16 (each
@@ -157,9 +157,11 @@ struct Bands {
 //   VECTOR: a lane holds 16 bytes of each row (E neighbouring columns): an 8 x E patch has E + 7 diagonals.  Rows on 16-byte
 //           boundaries, Lk a multiple of E.
 //   else:   a lane holds every 32nd column (E = 4 of them): one diagonal for each of its 8 E elements.  Any alignment.
-// Vectors / single elements for the same aligned input: 60.1 / 117.1 us for 16 x 8 x 1,024 x 1,024 in bf16 (4.5 TB/s, 68% of the copy rate),
-// 39.2 / 50.4 us for 5 x 12 x 776 x 1,000 in fp32.  Bound by the reads that are in flight: 64 registers a thread (four blocks per SM) hold
-// eight 16-byte rows, and a warp waits for its patch before it asks for the next.
+// Vectors / single elements for the same input: 64 / 121 us for 16 x 8 x 1,024 x 1,024 in bf16 (4.2 TB/s, 64% of the copy rate by vectors), 33 / 41 us
+// for 5 x 12 x 776 x 1,000 in fp32 causal, 44 / 56 us without the mask; 777 x 1,001, which has no vectors, 39 to 41 and 57 us.  The width of the loads is
+// a quarter of the odd call.  What bounds both forms is the reads in flight: 64 registers a thread (four blocks per SM) hold eight 16-byte
+// rows, and a warp waits for its patch before it asks for the next: 17 of them in a row in the first call, 7 of two waits each in the odd one.  One
+// call of 8 heads x 256 x 256 takes 14 us, mostly the emptying of the bands and the second kernel.
 template <typename T, bool VECTOR>
 __global__ void __launch_bounds__(GRAD_WARPS * 32, 4)
 relpos_backward_partial(const __grid_constant__ Buckets b, BiasGeometry g, int64_t B, const T* __restrict__ grad, int64_t batch_stride,

@@ -97,7 +97,9 @@ def gated_recurrence(gate: torch.Tensor, value: torch.Tensor, offsets: torch.Ten
 
 def log_bucket_starts(n: int, far: int) -> List[int]:
     """First distances of n buckets: half of them hold one distance each, the others grow evenly in the logarithm, the last begins at
-    `far`.  In whole numbers, so that no rounded logarithm moves a border."""
+    `far`.  In whole numbers, so that no rounded logarithm moves a border.  A spacing of its own: the common formula, which cuts the
+    logarithm up to `far` into n / 2 parts, has its last bucket begin before `far` (32 buckets up to 128: 16, 19, 21, 24, 27, 31, ..., 99, 113, here
+    16, 19, 22, 25, 28, 32, ..., 112, 128).  A table trained with other buckets needs their starts, which RelposBuckets takes as they are."""
     exact = max(n // 2, 1)
     if far < exact:
         raise ValueError(f"the last of {n} buckets cannot begin at {far}")
