@@ -146,7 +146,7 @@ class _RelposBias(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         buckets, q_offset, dtype = ctx.args
-        return _TableGradient.apply(grad.unsqueeze(0), buckets, q_offset).to(dtype), None, None, None, None, None
+        return _gradient_of_table(grad.unsqueeze(0), buckets, q_offset).to(dtype), None, None, None, None, None
 
 
 class _TableGradient(torch.autograd.Function):
@@ -162,6 +162,11 @@ class _TableGradient(torch.autograd.Function):
         buckets, q_offset, shape, dtype = ctx.args
         bias = _RelposBias.apply(way, buckets.without_mask(), shape[2], shape[3], q_offset, dtype)
         return (bias.tril(q_offset) if buckets.desc.causal else bias).expand(shape), None, None
+
+
+def _gradient_of_table(grad, buckets, q_offset):
+    """With a graph of its own only where a second derivative may be asked for: the graph's node costs 10 us a call."""
+    return _TableGradient.apply(grad, buckets, q_offset) if torch.is_grad_enabled() else _table_gradient(buckets, grad, q_offset)
 
 
 def relpos_bias(table: torch.Tensor, buckets: mb.RelposBuckets, Lq: int, Lk: int, q_offset: int = 0, dtype: torch.dtype = torch.float32):
@@ -181,7 +186,7 @@ class _AddRelposBias(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad):
         buckets, q_offset, dtype = ctx.args
-        return grad, _TableGradient.apply(grad, buckets, q_offset).to(dtype), None, None
+        return grad, _gradient_of_table(grad, buckets, q_offset).to(dtype), None, None
 
 
 def add_relpos_bias(scores: torch.Tensor, table: torch.Tensor, buckets: mb.RelposBuckets, q_offset: int = 0):
