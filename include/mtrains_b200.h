@@ -706,6 +706,94 @@ int mts_adamw_step(mts_adamw* adamw, void* state, size_t state_bytes, double lr,
 int mts_adamw_export_state(mts_adamw* adamw, const void* state, size_t state_bytes, float* m_out, float* v_out, void* stream);
 int mts_adamw_import_state(mts_adamw* adamw, void* state, size_t state_bytes, const float* m, const float* v, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The head of the tower: the norm of the residual stream between its layers, and the scores of the next event over a catalogue
+ * of V items (a softmax over a row of scores), of which a user wants the log probability of the event that came, the entropy, the
+ * best alternatives, and the loss against a larger tower's best items.  Sums and statistics are fp32, a value is rounded to its storage
+ * type once, results are deterministic.  Rows are *_stride elements apart (>= their length), elements of a row contiguous; any
+ * alignment is accepted, rows that start on 16-byte boundaries are fastest.  Unless stated otherwise outputs must not overlap inputs.
+ * ------------------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of the residual stream.  Per row of [N, D]:
+ *   r = round(x + residual)  (x itself when residual is NULL),   c = 1 / sqrt(mean_j r_j^2 + eps),   out_j = r_j c weight_j
+ * What is normalised is the stream as it is stored: the sum is rounded to the tensors' type first and written to sum_out.
+ *   x, residual, sum_out, out : [N, D] of one type (MTS_DTYPE_*); residual and sum_out are both given or both NULL; sum_out may be the
+ *                               memory of x or of residual (same stride): the stream updated in place.
+ *   weight  : [D] contiguous, MTS_DTYPE_* of its own.       inv_rms : fp32 [N], nullable (needed by the backward): c.
+ * N = 0 is allowed.  The sum of squares is taken in fp32: it overflows (output 0) for rows of values around 1e19 and more.
+ * Errors: INVALID_ARG (eps negative or not finite too), UNSUPPORTED (D > MTS_RMS_NORM_MAX_D, N >= 2^31), ALIGNMENT, CUDA. */
+#define MTS_RMS_NORM_MAX_D 32768
+int mts_rms_norm_forward(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                         int32_t weight_dtype, int32_t dtype, int64_t N, int32_t D, float eps, void* sum_out, int64_t sum_stride,
+                         void* out, int64_t out_stride, float* inv_rms, void* stream);
+/* The same with out in 8 bits: groups of `group` columns (32, 64, 128 or 256, counted from column 0, the last may be shorter; 0: the whole
+ * row) share a scale = max(max_j |y_j|, 2^-100) / 448, codes_j = e4m3(y_j * (448 / max)), rounded to nearest even (NaN stays NaN).
+ * codes: uint8 [N, D] (the bits of e4m3 numbers); scales: fp32 [N, ceil(D / group)] contiguous ([N] where group is 0).  Forward only: for serving,
+ * or with a backward that takes the rounding as the identity.  Errors as above. */
+int mts_rms_norm_forward_8bit(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                              int32_t weight_dtype, int32_t dtype, int64_t N, int32_t D, float eps, void* sum_out, int64_t sum_stride,
+                              uint8_t* codes, int64_t codes_stride, float* scales, int32_t group, float* inv_rms, void* stream);
+/* The values that codes and scales stand for: out[n, j] = code * scale, rounded to out_dtype.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int mts_rows_from_8bit(const uint8_t* codes, int64_t codes_stride, const float* scales, int32_t group, int64_t N, int32_t D, void* out,
+                       int32_t out_dtype, int64_t out_stride, void* stream);
+/* Gradient of the norm.  x is what was normalised (sum_out, or x where there was no residual), inv_rms as the forward left it; with
+ * a = inv_rms^2 mean_j(grad_out_j weight_j x_j):
+ *   grad_x_j = grad_sum_j + inv_rms (grad_out_j weight_j - x_j a)      (of x and of residual alike)
+ *   grad_weight_j = sum over rows of grad_out_j x_j inv_rms            (fp32 [D], overwritten; nullable)
+ * grad_sum: [N, D], the gradient that reaches sum_out by other ways, nullable.  grad_x may be the memory of grad_out or of grad_sum (same stride).
+ * workspace: mts_rms_norm_workspace_bytes(N, D) bytes, 256-byte aligned, contents undefined; NULL where grad_weight is.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
+size_t mts_rms_norm_workspace_bytes(int64_t N, int32_t D);
+int mts_rms_norm_backward(const void* x, int64_t x_stride, const void* weight, int32_t weight_dtype, int32_t dtype, int64_t N, int32_t D,
+                          const float* inv_rms, const void* grad_out, int64_t grad_out_stride, const void* grad_sum,
+                          int64_t grad_sum_stride, void* grad_x, int64_t grad_x_stride, float* grad_weight, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Log probabilities under p = softmax(scale * logits[n, :]), scale > 0 (the inverse of a temperature).  All outputs are nullable:
+ *   logp      : fp32 [N], log p of targets[n] (int64 [N]); 0 where the target is negative (no event: padding), NaN where it is >= V.
+ *   entropy   : fp32 [N], -sum_v p_v log p_v.
+ *   top_index : int64 [N, top_k], the top_k <= MTS_LOGPROBS_MAX_TOP largest scores, the lowest index first among equals;
+ *   top_logp  : fp32 [N, top_k], their log probabilities.
+ *   stats     : fp32 [N, 2], for the backward: the largest score m, and log sum_v exp(scale (x_v - m)).
+ * A score of -infinity rules an item out: p = 0, log p = -infinity, nothing in the entropy.  A row in which every item is ruled out has p = 0
+ * everywhere, log p = -infinity, entropy 0 (its stats are {0, 0}).  A row with a NaN or +infinity has NaN for logp, entropy and top_logp;
+ * its alternatives are picked among its numbers, NaN coming last.
+ * Errors: INVALID_ARG (top_k > V, scale not positive and finite too), UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V,
+ * top_k > MTS_LOGPROBS_MAX_TOP), ALIGNMENT, CUDA. */
+#define MTS_SCORES_MAX_N 100000000
+#define MTS_SCORES_MAX_V 1000000000
+#define MTS_LOGPROBS_MAX_TOP 32
+int mts_logprobs_forward(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale,
+                         const int64_t* targets, int32_t top_k, float* logp, float* entropy, float* stats, int64_t* top_index,
+                         float* top_logp, void* stream);
+/* Its gradient, for gradients of logp and of entropy (fp32 [N], either may be NULL: 0):
+ *   grad_logits[n, v] = scale (grad_logp ([v = target] - p_v) - grad_entropy p_v (log p_v + entropy))
+ * stats and entropy as the forward left them (entropy may be NULL without grad_entropy).  A row without a target takes grad_logp as 0.  A row
+ * whose gradients are 0 gets zeros whatever its scores hold.  grad_logits may be the memory of logits (same stride).  Errors as above. */
+int mts_logprobs_backward(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale,
+                          const int64_t* targets, const float* stats, const float* entropy, const float* grad_logp,
+                          const float* grad_entropy, void* grad_logits, int64_t grad_stride, void* stream);
+
+/* Loss of a student's scores against a teacher's best K items, and its gradient in the same pass.  For each row, with
+ *   q   = softmax over the listed items k of scale * teacher_logits[n, k], and over one more place of weight exp(teacher_rest[n]) for all
+ *         items that are not listed (teacher_rest: the logarithm of sum exp(scale * t) over them; NULL or -infinity: nothing),
+ *   p   = softmax(scale * logits[n, :]),   p_rest = the sum of p over the items not listed:
+ *   loss[n] = sum_k q_k (log q_k - log p_{index_k})  [ + q_rest (log q_rest - log p_rest) ]
+ *   grad_logits[n, v] = weights[n] * scale * (p_v - q_v) for listed items, weights[n] * scale * p_v (1 - q_rest / p_rest) for others
+ * loss fp32 [N] (not weighted); grad_logits [N, V] of the scores' type, nullable (loss alone); weights fp32 [N], NULL = 1: the gradient of the
+ * loss that is made of these rows.  teacher_index int64 [N, K], teacher_logits [N, K] of a type of their own, both contiguous.
+ * A negative index leaves its place out (rows with fewer than K); an index >= V makes the row's loss and gradient NaN; an index given
+ * more than once has the sum of its places' q, its item counting once in p_rest.  Where nothing is left of the teacher's row, loss and gradient are 0.  A
+ * score of -infinity is an item that the student rules out: infinite loss where the teacher gives it any weight, the gradient stays
+ * finite (p = 0; everywhere in a row in which every item is ruled out).  A row of weight 0 has gradient 0 whatever it holds.  No factor
+ * 1 / scale^2 is put in.  grad_logits may be the memory of logits (same stride).
+ * Errors: INVALID_ARG, UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V, K > MTS_DISTILL_MAX_K), ALIGNMENT, CUDA. */
+#define MTS_DISTILL_MAX_K 256
+int mts_distill_loss(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale,
+                     const int64_t* teacher_index, const void* teacher_logits, int32_t teacher_dtype, int32_t K,
+                     const float* teacher_rest, const float* weights, float* loss, void* grad_logits, int64_t grad_stride,
+                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

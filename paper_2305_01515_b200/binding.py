@@ -44,8 +44,11 @@ EXPORTS = (
     "mts_recurrence_status", "mts_relpos_bias_forward", "mts_relpos_bias_workspace_bytes", "mts_relpos_bias_backward",
     "mts_adamw_create", "mts_adamw_destroy", "mts_adamw_state_elements", "mts_adamw_state_bytes", "mts_adamw_set_grads",
     "mts_adamw_step", "mts_adamw_export_state", "mts_adamw_import_state",
+    "mts_rms_norm_forward", "mts_rms_norm_forward_8bit", "mts_rows_from_8bit", "mts_rms_norm_workspace_bytes", "mts_rms_norm_backward",
+    "mts_logprobs_forward", "mts_logprobs_backward", "mts_distill_loss",
 )
 ADAMW_BLOCK, RELPOS_MAX_BUCKETS = 256, 128
+RMS_NORM_MAX_D, LOGPROBS_MAX_TOP, DISTILL_MAX_K = 32768, 32, 256
 
 
 class MtsError(RuntimeError):
@@ -178,6 +181,17 @@ def lib():
         L.mts_adamw_step.argtypes = [vp, vp, sz, f64, f64, f64, f64, f64, i64, vp, u32, vp]
         L.mts_adamw_export_state.argtypes = [vp, vp, sz, vp, vp, vp]
         L.mts_adamw_import_state.argtypes = [vp, vp, sz, vp, vp, vp]
+        norm_in = [vp, i64, vp, i64, vp, i32, i32, i64, i32, f32, vp, i64]
+        L.mts_rms_norm_forward.argtypes = norm_in + [vp, i64, vp, vp]
+        L.mts_rms_norm_forward_8bit.argtypes = norm_in + [vp, i64, vp, i32, vp, vp]
+        L.mts_rows_from_8bit.argtypes = [vp, i64, vp, i32, i64, i32, vp, i32, i64, vp]
+        L.mts_rms_norm_workspace_bytes.restype = sz
+        L.mts_rms_norm_workspace_bytes.argtypes = [i64, i32]
+        L.mts_rms_norm_backward.argtypes = [vp, i64, vp, i32, i32, i64, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        scores = [vp, i64, i32, i64, i64, f32]
+        L.mts_logprobs_forward.argtypes = scores + [vp, i32] + [vp] * 6
+        L.mts_logprobs_backward.argtypes = scores + [vp] * 6 + [i64, vp]
+        L.mts_distill_loss.argtypes = scores + [vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
         for name in EXPORTS:
             getattr(L, name)            # raises AttributeError when a declared symbol is missing
         _lib = L
@@ -704,3 +718,51 @@ def adamw_export_state(adamw: AdamW, state, m_out, v_out, stream=None) -> None:
 def adamw_import_state(adamw: AdamW, state, m, v, stream=None) -> None:
     _check(lib().mts_adamw_import_state(adamw.handle, _ptr(state), state.numel() * state.element_size(), _ptr(m), _ptr(v),
                                         _stream(stream)))
+
+
+# ---------------------------------------------------------------------------- the head of the tower
+def rms_norm_forward(x, x_stride: int, residual, residual_stride: int, weight, weight_dtype: int, dtype: int, N: int, D: int, eps: float, sum_out,
+                     sum_stride: int, out, out_stride: int, inv_rms, stream=None) -> None:
+    _check(lib().mts_rms_norm_forward(_ptr(x), x_stride, _ptr(residual), residual_stride, _ptr(weight), weight_dtype, dtype, N, D, eps,
+                                      _ptr(sum_out), sum_stride, _ptr(out), out_stride, _ptr(inv_rms), _stream(stream)))
+
+
+def rms_norm_forward_8bit(x, x_stride: int, residual, residual_stride: int, weight, weight_dtype: int, dtype: int, N: int, D: int, eps: float,
+                          sum_out, sum_stride: int, codes, codes_stride: int, scales, group: int, inv_rms, stream=None) -> None:
+    """group: columns that share a scale, 0 for the whole row."""
+    _check(lib().mts_rms_norm_forward_8bit(_ptr(x), x_stride, _ptr(residual), residual_stride, _ptr(weight), weight_dtype, dtype, N, D, eps,
+                                           _ptr(sum_out), sum_stride, _ptr(codes), codes_stride, _ptr(scales), group, _ptr(inv_rms),
+                                           _stream(stream)))
+
+
+def rows_from_8bit(codes, codes_stride: int, scales, group: int, N: int, D: int, out, out_dtype: int, out_stride: int, stream=None) -> None:
+    _check(lib().mts_rows_from_8bit(_ptr(codes), codes_stride, _ptr(scales), group, N, D, _ptr(out), out_dtype, out_stride, _stream(stream)))
+
+
+def rms_norm_workspace_bytes(N: int, D: int) -> int:
+    return int(lib().mts_rms_norm_workspace_bytes(N, D))
+
+
+def rms_norm_backward(x, x_stride: int, weight, weight_dtype: int, dtype: int, N: int, D: int, inv_rms, grad_out, grad_out_stride: int, grad_sum,
+                      grad_sum_stride: int, grad_x, grad_x_stride: int, grad_weight, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().mts_rms_norm_backward(_ptr(x), x_stride, _ptr(weight), weight_dtype, dtype, N, D, _ptr(inv_rms), _ptr(grad_out),
+                                       grad_out_stride, _ptr(grad_sum), grad_sum_stride, _ptr(grad_x), grad_x_stride, _ptr(grad_weight),
+                                       _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def logprobs_forward(logits, row_stride: int, dtype: int, N: int, V: int, scale: float, targets, top_k: int, logp, entropy, stats, top_index,
+                     top_logp, stream=None) -> None:
+    _check(lib().mts_logprobs_forward(_ptr(logits), row_stride, dtype, N, V, scale, _ptr(targets), top_k, _ptr(logp), _ptr(entropy),
+                                      _ptr(stats), _ptr(top_index), _ptr(top_logp), _stream(stream)))
+
+
+def logprobs_backward(logits, row_stride: int, dtype: int, N: int, V: int, scale: float, targets, stats, entropy, grad_logp, grad_entropy,
+                      grad_logits, grad_stride: int, stream=None) -> None:
+    _check(lib().mts_logprobs_backward(_ptr(logits), row_stride, dtype, N, V, scale, _ptr(targets), _ptr(stats), _ptr(entropy),
+                                       _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad_logits), grad_stride, _stream(stream)))
+
+
+def distill_loss(logits, row_stride: int, dtype: int, N: int, V: int, scale: float, teacher_index, teacher_logits, teacher_dtype: int, K: int,
+                 teacher_rest, weights, loss, grad_logits, grad_stride: int, stream=None) -> None:
+    _check(lib().mts_distill_loss(_ptr(logits), row_stride, dtype, N, V, scale, _ptr(teacher_index), _ptr(teacher_logits), teacher_dtype, K,
+                                  _ptr(teacher_rest), _ptr(weights), _ptr(loss), _ptr(grad_logits), grad_stride, _stream(stream)))

@@ -31,7 +31,8 @@ static const char* const kKernelNames[K_ALL_COUNT] = {
     "unique_segments", "reduce_chunks", "combine_partials", "cache_prepare_keys", "cache_describe_unique",
     "cache_probe_replace", "cache_lists", "cache_scatter_slots", "cache_save_victims", "cache_fetch_misses",
     "cache_write_victims", "cache_flush", "other", "recurrence_forward", "recurrence_backward", "relpos_bias_forward",
-    "relpos_bias_backward", "adamw_step", "adamw_state"};
+    "relpos_bias_backward", "adamw_step", "adamw_state", "rms_norm_forward", "rms_norm_backward", "logprobs_forward",
+    "logprobs_backward", "distill_loss"};
 
 struct TraceRecord { int kernel; cudaEvent_t start, stop; };
 
