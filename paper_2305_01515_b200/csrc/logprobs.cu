@@ -8,6 +8,8 @@
 namespace mts {
 
 constexpr int LOGP_THREADS = 256;
+constexpr int LOGP_MAX_PARTS = 8;              // blocks of a cluster that share a row
+constexpr int LOGP_UNROLL = 4;                 // batches on their way for a thread
 
 struct LogprobsOut {
   float* logp;
@@ -17,79 +19,232 @@ struct LogprobsOut {
   float* top_logp;
 };
 
-template <int THREADS>
-__device__ __forceinline__ uint64_t block_max64(uint64_t x, uint64_t* room) {
+// Statistics of a set of scores: the largest, and relative to it the sums of p = 2^(c (x - m)) and of p log2 p.
+struct RowStats {
+  float m, S, P;
+  // those of two sets together
+  __device__ __forceinline__ void join(const RowStats& o, float c) {
+    const float top = fmaxf(m, o.m), base = top == -INFINITY ? 0.f : top;
+    const float a = exponent((m - base) * c), b = exponent((o.m - base) * c), fa = exp2_fast(a), fb = exp2_fast(b);
+    P = fa * (P + S * a) + fb * (o.P + o.S * b);
+    S = fa * S + fb * o.S;
+    m = top;
+  }
+};
+
+// Those of the first LANES lanes (a power of two) together, in all lanes.
+template <int LANES>
+__device__ __forceinline__ RowStats join_lanes(RowStats st, float c) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-  __syncthreads();
-  if (lane_id() == 0) room[threadIdx.x / 32] = x;
-  __syncthreads();
-  x = room[0];
-  for (int w = 1; w < THREADS / 32; ++w) x = max(x, room[w]);
-  return x;
+  for (int o = LANES / 2; o; o >>= 1) {
+    const RowStats other = {__shfl_xor_sync(0xFFFFFFFFu, st.m, o), __shfl_xor_sync(0xFFFFFFFFu, st.S, o), __shfl_xor_sync(0xFFFFFFFFu, st.P, o)};
+    st.join(other, c);
+  }
+  if constexpr (LANES < 32) st = {__shfl_sync(0xFFFFFFFFu, st.m, 0), __shfl_sync(0xFFFFFFFFu, st.S, 0), __shfl_sync(0xFFFFFFFFu, st.P, 0)};
+  return st;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(LOGP_THREADS)
-logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, LogprobsOut out) {
-  __shared__ float room[LOGP_THREADS / 32];
-  __shared__ uint64_t room64[LOGP_THREADS / 32];
-  const int64_t n = blockIdx.x;
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Address in the first block of the cluster of a variable of this block.
+__device__ __forceinline__ uint32_t in_first_block(const void* p) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)));
+  return a;
+}
+
+// A row by a cluster of blocks, each a run of batches, each thread every THREADS-th of them.  One pass over the scores:
+//   Sums: a thread keeps the running maximum of its scores and the sums relative to it; where a group of batches has a larger score the sums are
+//   scaled (rare after the first few).  They are joined over warp, block and cluster.
+//   Best k: nothing is kept but the batch in which each thread's maximum came first.  With (score, index) ordered so that the lowest index comes first
+//   among equals, a thread's order is at least that of all its scores, and the k-th largest of the 32 largest orders of groups of threads is a
+//   bound that k scores reach.  Only the few threads whose order reaches it can hold more of them: a warp reads each such thread's batches again
+//   (k / THREADS of the row about), collects the scores that reach the bound, and a score's place is the number of those before it.  Where the bound
+//   lets too many pass (a row made for it) or too few (NaN), the block finds its best one after the other.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, int parts,
+                 LogprobsOut out) {
+  constexpr int E = RowBatches<T>::E, WARPS = THREADS / 32, CAP = THREADS < 64 ? 256 : 512;
+  __shared__ RowStats warp_stats[WARPS], part_stats[LOGP_MAX_PARTS];
+  __shared__ uint64_t room64[32], found[CAP], part_best[LOGP_MAX_PARTS * MTS_LOGPROBS_MAX_TOP], best[MTS_LOGPROBS_MAX_TOP];
+  __shared__ int count;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+  const int64_t n = blockIdx.x / parts;
+  const int part = blockIdx.x % parts;
+  if (parts > 1) cluster_arrive();                                      // the first block has begun before others write to it
   const RowBatches<T> r(logits + n * row_stride, V);
-  constexpr int E = RowBatches<T>::E;
+  const int32_t b0 = (int32_t)((int64_t)r.count * part / parts), b1 = (int32_t)((int64_t)r.count * (part + 1) / parts);
   const float c = scale * LOG2E;
-  float m = -INFINITY, v[E];
-  for (int b = threadIdx.x; b < r.count; b += LOGP_THREADS) {
-    r.load(b, v);
-#pragma unroll
-    for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
+  int64_t target = -1;
+  float target_score = 0.f;
+  if (part == 0 && tid == 0 && out.logp) {
+    target = targets[n];
+    if (target >= 0 && target < V) target_score = to_f32(r.row[target]);
   }
-  m = block_max<LOGP_THREADS>(m, room);
-  const float base = m == -INFINITY ? 0.f : m;
-  float S = 0.f, P = 0.f;
-  for (int b = threadIdx.x; b < r.count; b += LOGP_THREADS) {
-    r.load(b, v);
+  if (tid == 0) count = 0;
+
+  float m = -INFINITY, base = 0.f;
+  Pair S(0.f, 0.f), P(0.f, 0.f);
+  const Pair c2(c, c);
+  int32_t best_batch = b0 + tid;
+  for (int32_t g = b0; g < b1; g += THREADS * LOGP_UNROLL) {
+    uint4 w[LOGP_UNROLL];
+    const int32_t b = g + tid;
+    if (g > 0 && g + THREADS * LOGP_UNROLL < r.count && g + THREADS * LOGP_UNROLL <= b1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float d = exponent((v[e] - base) * c), p = exp2_fast(d);
-      S += p;
-      P += p * d;
+      for (int u = 0; u < LOGP_UNROLL; ++u) w[u] = __ldg(reinterpret_cast<const uint4*>(r.row + r.first(b + u * THREADS)));
+    } else {
+#pragma unroll
+      for (int u = 0; u < LOGP_UNROLL; ++u) w[u] = r.raw(b + u * THREADS < b1 ? b + u * THREADS : r.count);
+    }
+    float top[LOGP_UNROLL];
+#pragma unroll
+    for (int u = 0; u < LOGP_UNROLL; ++u) top[u] = max_of<T>(w[u]);
+    float most = top[0];
+#pragma unroll
+    for (int u = 1; u < LOGP_UNROLL; ++u) most = fmaxf(most, top[u]);
+    if (most > m) {
+      const float a = exponent((m - most) * c), f = exp2_fast(a);
+      P = (P + S * Pair(a, a)) * Pair(f, f);
+      S = S * Pair(f, f);
+#pragma unroll
+      for (int u = LOGP_UNROLL - 1; u >= 0; --u)
+        if (top[u] == most) best_batch = b + u * THREADS;
+      m = base = most;
+    }
+    const Pair minus(-base, -base);
+#pragma unroll
+    for (int u = 0; u < LOGP_UNROLL; ++u) {
+      float v[E];
+      RowBatches<T>::unpack(w[u], v);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 d = ((Pair(v[e], v[e + 1]) + minus) * c2).get();
+        const float d0 = exponent(d.x), d1 = exponent(d.y);
+        const Pair p(exp2_fast(d0), exp2_fast(d1));
+        S = S + p;
+        P = fma2(p, Pair(d0, d1), P);
+      }
     }
   }
-  S = block_sum<LOGP_THREADS>(S, room);
+  RowStats st = {m, S.get().x + S.get().y, P.get().x + P.get().y};
+  st = join_lanes<32>(st, c);
+  // the thread's order, and the largest of its group of THREADS / 32 threads
+  uint64_t order = 0;
+  if (b0 + tid < b1) order = score_order(m, max(r.first(best_batch), 0));
+  uint64_t group = order;
+#pragma unroll
+  for (int o = THREADS / 64; o; o >>= 1) group = max(group, __shfl_xor_sync(0xFFFFFFFFu, group, o));
+  if (lane % (THREADS / 32) == 0) room64[tid / (THREADS / 32)] = group;
+  if (lane == 0) warp_stats[warp] = st;
   __syncthreads();
-  P = block_sum<LOGP_THREADS>(P, room);
-  const float log_s = S > 0.f ? logf(S) : S == 0.f ? 0.f : NAN;
-  const float nothing = S == 0.f ? -INFINITY : 0.f;
-  if (threadIdx.x == 0) {
-    if (out.logp) {
-      const int64_t t = targets[n];
-      out.logp[n] = t < 0 ? 0.f : t >= V ? NAN : (to_f32(r.row[t]) - base) * scale - log_s + nothing;
+
+  const int k = min((int64_t)top_k, (int64_t)V);
+  if (k > 0) {
+    // the k-th largest of the 32
+    const uint64_t mine = room64[lane];
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const uint64_t o = room64[i];
+      before += o > mine || (o == mine && i < lane);
     }
-    if (out.entropy) out.entropy[n] = S == 0.f ? 0.f : log_s - P / S * LN2;
+    const unsigned kth = __ballot_sync(0xFFFFFFFFu, before == k - 1);
+    uint64_t bound = __shfl_sync(0xFFFFFFFFu, mine, __ffs(kth) - 1);
+    bound = bound > E ? bound - (E - 1) : 0;                            // the score itself lies up to E - 1 places behind its batch's first
+    unsigned winners = __ballot_sync(0xFFFFFFFFu, order >= bound && b0 + tid < b1);
+    while (winners) {
+      const int w = __ffs(winners) - 1;
+      winners &= winners - 1;
+      for (int32_t b = b0 + warp * 32 + w + lane * THREADS; b < b1; b += 32 * THREADS) {
+        float v[E];
+        RowBatches<T>::unpack(r.raw(b), v);
+        const int32_t i = r.first(b);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const uint64_t o = score_order(v[e], i + e);
+          if (o >= bound && i + e >= 0 && i + e < V) {
+            const int at = atomicAdd(&count, 1);
+            if (at < CAP) found[at] = o;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const int have = count;
+    if (have <= CAP && (have >= k || bound == 0)) {
+      if (tid < k) best[tid] = 0;
+      __syncthreads();
+      for (int i = tid; i < have; i += THREADS) {
+        const uint64_t o = found[i];
+        int place = 0;
+        for (int j = 0; j < have; ++j) place += found[j] > o;
+        if (place < k) best[place] = o;
+      }
+    } else {
+      uint64_t last = ~0ull;
+      for (int q = 0; q < k; ++q) {
+        uint64_t top = 0;
+        for (int32_t b = b0 + tid; b < b1; b += THREADS) {
+          float v[E];
+          RowBatches<T>::unpack(r.raw(b), v);
+          const int32_t i = r.first(b);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const uint64_t o = score_order(v[e], i + e);
+            if (i + e >= 0 && i + e < V && o < last && o > top) top = o;
+          }
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        __syncthreads();
+        if (lane == 0) room64[warp] = top;
+        __syncthreads();
+        for (int w = 0; w < WARPS; ++w) top = max(top, room64[w]);
+        last = top;
+        if (tid == 0) best[q] = top;
+      }
+    }
+    __syncthreads();
+  }
+  const RowStats nobody = {-INFINITY, 0.f, 0.f};
+  st = join_lanes<WARPS>(lane < WARPS ? warp_stats[lane] : nobody, c);
+
+  if (parts > 1) {
+    // to the first block, which joins them
+    cluster_wait();
+    const uint32_t to = in_first_block(&part_stats[part]);
+    if (tid == 0)
+      asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;" :: "r"(to), "f"(st.m), "f"(st.S), "f"(st.P) : "memory");
+    if (tid < k) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(in_first_block(&part_best[part * k + tid])), "l"(best[tid]) : "memory");
+    cluster_arrive();
+    cluster_wait();
+    if (part != 0) return;
+    st = join_lanes<LOGP_MAX_PARTS>(lane < parts ? part_stats[lane] : nobody, c);
+    for (int i = tid; i < parts * k; i += THREADS) {
+      const uint64_t o = part_best[i];
+      int place = 0;
+      for (int j = 0; j < parts * k; ++j) place += part_best[j] > o;
+      if (place < k && o != 0) best[place] = o;
+    }
+    __syncthreads();
+  }
+  base = st.m == -INFINITY ? 0.f : st.m;
+  const float log_s = st.S > 0.f ? logf(st.S) : st.S == 0.f ? 0.f : NAN;
+  const float nothing = st.S == 0.f ? -INFINITY : 0.f;
+  if (tid == 0) {
+    if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - base) * scale - log_s + nothing;
+    if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_s - st.P / st.S * LN2;
     if (out.stats) {
       out.stats[2 * n] = base;
       out.stats[2 * n + 1] = log_s;
     }
   }
-  uint64_t last = ~0ull;
-  for (int k = 0; k < top_k; ++k) {
-    uint64_t best = 0;
-    for (int b = threadIdx.x; b < r.count; b += LOGP_THREADS) {
-      r.load(b, v);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int i = r.first(b) + e;
-        const uint64_t o = score_order(v[e], i);
-        if (i >= 0 && i < V && o < last && o > best) best = o;
-      }
-    }
-    last = block_max64<LOGP_THREADS>(best, room64);
-    if (threadIdx.x == 0) {
-      const int i = order_index(last);
-      if (out.top_index) out.top_index[n * top_k + k] = i;
-      if (out.top_logp) out.top_logp[n * top_k + k] = (to_f32(r.row[i]) - base) * scale - log_s + nothing;
-    }
+  if (tid < k) {
+    const uint64_t o = best[tid];
+    if (out.top_index) out.top_index[n * top_k + tid] = order_index(o);
+    if (out.top_logp) out.top_logp[n * top_k + tid] = (order_score(o) - base) * scale - log_s + nothing;
   }
 }
 
@@ -129,6 +284,23 @@ int check_logits(const char* what, const void* logits, int64_t row_stride, int32
   return check_rows(what, "logits", logits, dtype, N, V, row_stride);
 }
 
+template <typename T, int THREADS>
+int launch_forward(const char* what, const T* logits, int64_t row_stride, int64_t N, int64_t V, float scale, const int64_t* targets, int top_k, int parts,
+                   const LogprobsOut& out, cudaStream_t s) {
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = (unsigned)parts;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3((unsigned)(N * parts));
+  config.blockDim = dim3(THREADS);
+  config.stream = s;
+  config.attrs = &cluster;
+  config.numAttrs = parts > 1 ? 1 : 0;
+  LaunchScope scope(K_LOGPROBS_FWD, s);
+  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, THREADS>, logits, row_stride, (int32_t)V, scale, targets, top_k, parts, out), what);
+}
+
 }  // namespace
 
 extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale, const int64_t* targets,
@@ -147,9 +319,18 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
   const LogprobsOut out = {logp, entropy, stats, top_index, top_logp};
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    LaunchScope scope(K_LOGPROBS_FWD, s);
-    logprobs_forward<T><<<(unsigned)N, LOGP_THREADS, 0, s>>>(static_cast<const T*>(logits), row_stride, (int32_t)V, scale, targets, top_k, out);
-    return check_launch(what);
+    const int64_t batches = ceil_div(V, RowBatches<T>::E);
+    int threads = 32, parts = 1;
+    while (threads < 512 && batches >= 8 * threads) threads *= 2;
+    while (parts < LOGP_MAX_PARTS && N * parts < 296 && batches >= 1024 * parts) parts *= 2;
+    const T* x = static_cast<const T*>(logits);
+    switch (threads) {
+      case 32: return launch_forward<T, 32>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
+      case 64: return launch_forward<T, 64>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
+      case 128: return launch_forward<T, 128>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
+      case 256: return launch_forward<T, 256>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
+      default: return launch_forward<T, 512>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
+    }
   });
 }
 

@@ -49,6 +49,20 @@ struct RowBatches {
       for (int e = 0; e < E; ++e) v[e] = i + e >= 0 && i + e < V ? to_f32(row[i + e]) : -INFINITY;
     }
   }
+  // The batch as it is stored, -infinity outside the row.
+  __device__ __forceinline__ uint4 raw(int32_t b) const {
+    const int32_t i = first(b);
+    if (i >= 0 && i <= V - E) return __ldg(reinterpret_cast<const uint4*>(row + i));
+    const uint32_t low = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __half) ? 0xFC00FC00u : 0xFF80FF80u);
+    uint4 w = make_uint4(low, low, low, low);
+    if (i > -E && i < V) {
+      T* const e = reinterpret_cast<T*>(&w);
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (i + k >= 0 && i + k < V) e[k] = row[i + k];
+    }
+    return w;
+  }
   static __device__ __forceinline__ void unpack(const uint4& w, float (&v)[E]) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -73,6 +87,54 @@ __device__ __forceinline__ uint64_t score_order(float x, int32_t index) {
   return (uint64_t)score_key(x) << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ int32_t order_index(uint64_t o) { return (int32_t)~(uint32_t)o; }
+
+__device__ __forceinline__ float order_score(uint64_t o) {
+  const uint32_t k = (uint32_t)(o >> 32);
+  return k == 0u ? NAN : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+// Pairs of fp32 numbers in one instruction.
+struct Pair {
+  unsigned long long bits;
+  __device__ __forceinline__ Pair() {}
+  __device__ __forceinline__ Pair(float x, float y) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(x), "f"(y)); }
+  __device__ __forceinline__ float2 get() const {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(bits));
+    return f;
+  }
+};
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+  return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+  return r;
+}
+
+// Largest of the elements of 16 bytes (numbers only: NaN counts as -infinity).
+template <typename T>
+__device__ __forceinline__ float max_of(const uint4& w) {
+  if constexpr (sizeof(T) == 4) {
+    return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+  } else {
+    uint32_t m;
+    if constexpr (sizeof(T) == 2 && !__is_same(T, __half))
+      asm("{\n\t.reg .b32 a, b;\n\tmax.bf16x2 a, %1, %2;\n\tmax.bf16x2 b, %3, %4;\n\tmax.bf16x2 %0, a, b;\n\t}" : "=r"(m) : "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w));
+    else
+      asm("{\n\t.reg .b32 a, b;\n\tmax.f16x2 a, %1, %2;\n\tmax.f16x2 b, %3, %4;\n\tmax.f16x2 %0, a, b;\n\t}" : "=r"(m) : "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w));
+    const float2 f = unpack2<T>(m);
+    return fmaxf(fmaxf(f.x, f.y), -INFINITY);
+  }
+}
 
 // Sum and maximum over a block of THREADS in a fixed order; every thread gets the result.  `room`: shared, [THREADS / 32]; free again at the
 // next barrier of the block.
