@@ -3,13 +3,19 @@
 //   z = scale x,  m = max x,  S = sum_v exp(scale (x_v - m)),  log p_v = scale (x_v - m) - log S
 //   entropy = -sum_v p_v log p_v = log S - (sum_v exp(scale (x_v - m)) scale (x_v - m)) / S
 //   dx_v = scale (g_logp ([v = target] - p_v) - g_entropy p_v (log p_v + entropy))
+#include <stdlib.h>
 #include "rows.cuh"
 
 namespace mts {
 
 constexpr int LOGP_THREADS = 256;
+constexpr int LOGP_WARPS = 16;                 // of a block that works on a row
+constexpr int LOGP_ROWS = 4;                   // rows of a block whose warps have one each
 constexpr int LOGP_MAX_PARTS = 8;              // blocks of a cluster that share a row
-constexpr int LOGP_UNROLL = 4;                 // batches on their way for a thread
+constexpr int LOGP_HELD = 8;                   // batches that a thread holds of a row that is held in registers
+constexpr int LOGP_UNROLL = 8;                 // batches on their way for a thread otherwise
+constexpr int LOGP_LISTED = 64;                // batches that can hold a score which reaches the bound
+constexpr int LOGP_FOUND = 512;                // scores that can reach it
 
 struct LogprobsOut {
   float* logp;
@@ -19,29 +25,22 @@ struct LogprobsOut {
   float* top_logp;
 };
 
-// Statistics of a set of scores: the largest, and relative to it the sums of p = 2^(c (x - m)) and of p log2 p.
-struct RowStats {
-  float m, S, P;
-  // those of two sets together
-  __device__ __forceinline__ void join(const RowStats& o, float c) {
-    const float top = fmaxf(m, o.m), base = top == -INFINITY ? 0.f : top;
-    const float a = exponent((m - base) * c), b = exponent((o.m - base) * c), fa = exp2_fast(a), fb = exp2_fast(b);
-    P = fa * (P + S * a) + fb * (o.P + o.S * b);
-    S = fa * S + fb * o.S;
-    m = top;
-  }
-};
+// Exponents are taken relative to the largest score m: c x - base with base = c m rounded (its error is put right at the end), which is one
+// instruction; where base is no finite number (scores of about 2e38 and more, or none but the lowest of their type) it is c (x - m).
+// Statistics of a set of scores: the largest, and the sums of p = 2^exponent and of p log2 p.
+struct RowStats { float m, S, P; };
 
-// Those of the first LANES lanes (a power of two) together, in all lanes.
-template <int LANES>
-__device__ __forceinline__ RowStats join_lanes(RowStats st, float c) {
-#pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) {
-    const RowStats other = {__shfl_xor_sync(0xFFFFFFFFu, st.m, o), __shfl_xor_sync(0xFFFFFFFFu, st.S, o), __shfl_xor_sync(0xFFFFFFFFu, st.P, o)};
-    st.join(other, c);
-  }
-  if constexpr (LANES < 32) st = {__shfl_sync(0xFFFFFFFFu, st.m, 0), __shfl_sync(0xFFFFFFFFu, st.S, 0), __shfl_sync(0xFFFFFFFFu, st.P, 0)};
-  return st;
+__device__ __forceinline__ float base_of(float m, float c) { return m == -INFINITY ? 0.f : m * c; }
+__device__ __forceinline__ bool ordinary(float base) { return fabsf(base) < INFINITY; }
+__device__ __forceinline__ RowStats scaled_to(const RowStats& s, float m, float c) {
+  const float base = base_of(m, c), a = exponent(ordinary(base) ? base_of(s.m, c) - base : (s.m - m) * c), f = exp2_fast(a);
+  return s.m == -INFINITY ? RowStats{m, s.S, s.P} : RowStats{m, f * s.S, f * (s.P + s.S * a)};
+}
+// Those of a warp's lanes together.
+__device__ __forceinline__ RowStats join_lanes(RowStats s, float c) {
+  const float m = warp_max(s.m);
+  s = scaled_to(s, m, c);
+  return {m, warp_sum(s.S), warp_sum(s.P)};
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
@@ -53,198 +52,415 @@ __device__ __forceinline__ uint32_t in_first_block(const void* p) {
   return a;
 }
 
-// A row by a cluster of blocks, each a run of batches, each thread every THREADS-th of them.  One pass over the scores:
-//   Sums: a thread keeps the running maximum of its scores and the sums relative to it; where a group of batches has a larger score the sums are
-//   scaled (rare after the first few).  They are joined over warp, block and cluster.
-//   Best k: nothing is kept but the batch in which each thread's maximum came first.  With (score, index) ordered so that the lowest index comes first
-//   among equals, a thread's order is at least that of all its scores, and the k-th largest of the 32 largest orders of groups of threads is a
-//   bound that k scores reach.  Only the few threads whose order reaches it can hold more of them: a warp reads each such thread's batches again
-//   (k / THREADS of the row about), collects the scores that reach the bound, and a score's place is the number of those before it.  Where the bound
-//   lets too many pass (a row made for it) or too few (NaN), the block finds its best one after the other.
-template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS)
-logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, int parts,
-                 LogprobsOut out) {
-  constexpr int E = RowBatches<T>::E, WARPS = THREADS / 32, CAP = THREADS < 64 ? 256 : 512;
-  __shared__ RowStats warp_stats[WARPS], part_stats[LOGP_MAX_PARTS];
-  __shared__ uint64_t room64[32], found[CAP], part_best[LOGP_MAX_PARTS * MTS_LOGPROBS_MAX_TOP], best[MTS_LOGPROBS_MAX_TOP];
-  __shared__ int count;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-  const int64_t n = blockIdx.x / parts;
-  const int part = blockIdx.x % parts;
-  if (parts > 1) cluster_arrive();                                      // the first block has begun before others write to it
+// A batch added to the sums.
+template <typename T, bool ORDINARY>
+__device__ __forceinline__ void add_batch(const uint4& w, float m, float base, float c, Pair& S, Pair& P) {
+  constexpr int E = RowBatches<T>::E;
+  float v[E];
+  RowBatches<T>::unpack(w, v);
+  const Pair minus(-base, -base), c2(c, c);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    const float2 f = ORDINARY ? fma2(Pair(v[e], v[e + 1]), c2, minus).get() : make_float2((v[e] - m) * c, (v[e + 1] - m) * c);
+    const float d0 = exponent(f.x), d1 = exponent(f.y);
+    const Pair p(exp2_fast(d0), exp2_fast(d1));
+    S = S + p;
+    P = fma2(p, Pair(d0, d1), P);
+  }
+}
+
+// Working memory of a row.
+template <int WARPS>
+struct RowRoom {
+  alignas(16) uint4 listed[LOGP_LISTED];
+  alignas(16) float top[WARPS][32];
+  uint64_t found[LOGP_FOUND], best[MTS_LOGPROBS_MAX_TOP], bound;
+  int32_t listed_at[LOGP_LISTED];
+  RowStats stats[WARPS];
+  float bound_score, m, log_s, nothing;
+  int listed_count, found_count;
+};
+
+// The k-th largest of the maxima of 32 R groups of threads (X: float or uint64_t), by one warp; `of_thread` is used up.  Equal ones count one by one.
+template <int R, typename X>
+__device__ __forceinline__ X kth_largest(X (*of_thread)[32], int warps, int k, X least, X most) {
+  constexpr int PER = 16 / (int)sizeof(X);
+  const int lane = lane_id();
+  X mine[R];
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    mine[q] = least;
+    for (int w = q; w < warps; w += R) mine[q] = max(mine[q], of_thread[w][lane]);
+  }
+  __syncwarp();
+  X* flat = &of_thread[0][0];
+#pragma unroll
+  for (int q = 0; q < R; ++q) flat[q * 32 + lane] = mine[q];
+  __syncwarp();
+  int before[R] = {};
+#pragma unroll 4
+  for (int i = 0; i < 32 * R; i += PER) {
+    X o[PER];
+    *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(flat + i);
+#pragma unroll
+    for (int q = 0; q < R; ++q)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) before[q] += o[e] > mine[q];
+  }
+  // the smallest of those with fewer than k before them
+  X bound = before[0] < k ? mine[0] : most;
+#pragma unroll
+  for (int q = 1; q < R; ++q)
+    if (before[q] < k && mine[q] < bound) bound = mine[q];
+  if constexpr (sizeof(X) == 4) return warp_min(bound);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) bound = min(bound, __shfl_xor_sync(0xFFFFFFFFu, bound, o));
+  return bound;
+}
+template <typename X>
+__device__ __forceinline__ X kth_of_groups(X (*of_thread)[32], int warps, int k, X least, X most) {
+  return k <= 16 || warps < 2 ? kth_largest<1>(of_thread, warps, k, least, most) : kth_largest<2>(of_thread, warps, k, least, most);
+}
+
+// The best k of batches [b0, b1) into room.best where the bound by score alone lets too many pass or too few: rows with many equal scores (ruled out
+// altogether, say), and rows with NaN.  The threads find where their maximum came first and the bound is made of (score, index); where that does not
+// settle it either, the best are found one after the other.
+template <typename T, int WARPS>
+__device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, int32_t b1, int k, float m, RowRoom<WARPS>& room) {
+  constexpr int E = RowBatches<T>::E;
+  const int lane = lane_id(), warp = WARPS == 1 ? 0 : threadIdx.x / 32, tid = WARPS == 1 ? lane : threadIdx.x;
+  const int threads = WARPS == 1 ? 32 : blockDim.x, warps = threads / 32;
+  const auto sync = [] { if (WARPS == 1) __syncwarp(); else __syncthreads(); };
+  const int32_t b = b0 + tid;
+  uint64_t order = 0;
+  for (int32_t at = b; at < b1 && !order; at += threads)
+    if (max_value<T>(max_bits<T>(r.raw(at))) == m) order = score_order(m, max(r.first(at), 0));
+  sync();                                                               // what was found before has been looked at
+  uint64_t(*orders)[32] = reinterpret_cast<uint64_t(*)[32]>(room.found);
+  orders[warp][lane] = order;
+  sync();
+  if (warp == 0) {
+    // the score itself lies up to E - 1 places behind its batch's first
+    const uint64_t kth = kth_of_groups<uint64_t>(orders, warps, k, 0, ~0ull);
+    if (lane == 0) {
+      room.bound = kth > E ? kth - (E - 1) : 0;
+      room.found_count = 0;
+    }
+  }
+  sync();
+  const uint64_t bound = room.bound;
+  if (order >= bound) {
+    for (int32_t at = b; at < b1 && *const_cast<volatile int*>(&room.found_count) <= LOGP_FOUND; at += threads) {
+      float v[E];
+      RowBatches<T>::unpack(r.raw(at), v);
+      const int32_t i = r.first(at);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint64_t o = score_order(v[e], i + e);
+        if (o >= bound && i + e >= 0 && i + e < r.V) {
+          const int place = atomicAdd(&room.found_count, 1);
+          if (place < LOGP_FOUND) room.found[place] = o;
+        }
+      }
+    }
+  }
+  if (tid < k) room.best[tid] = 0;
+  sync();
+  const int have = room.found_count;
+  if (have <= LOGP_FOUND && (have >= k || bound == 0)) {
+    for (int i = tid; i < have; i += threads) {
+      const uint64_t o = room.found[i];
+      int place = 0;
+      for (int j = 0; j < have; ++j) place += room.found[j] > o;
+      if (place < k) room.best[place] = o;
+    }
+  } else {
+    uint64_t last = ~0ull;
+    for (int q = 0; q < k; ++q) {
+      uint64_t most = 0;
+      for (int32_t at = b; at < b1; at += threads) {
+        float v[E];
+        RowBatches<T>::unpack(r.raw(at), v);
+        const int32_t i = r.first(at);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const uint64_t o = score_order(v[e], i + e);
+          if (i + e >= 0 && i + e < r.V && o < last && o > most) most = o;
+        }
+      }
+      for (int o = 16; o; o >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+      sync();
+      if (lane == 0) room.found[warp] = most;
+      sync();
+      for (int x = 0; x < warps; ++x) most = max(most, room.found[x]);
+      last = most;
+      if (tid == 0) room.best[q] = most;
+    }
+  }
+  sync();
+}
+
+// A row (or a part of it, by a cluster of blocks) by the warps of a block, each thread every T-th batch of it; short rows by one warp.
+//   HELD: a thread's batches are all loaded at once and stay in registers: the largest score first, then the sums.
+//   else: a thread keeps the running maximum of its scores and sums relative to it, which are scaled where a group of batches has a larger
+//         one (rare after the first few).
+// The best k cost the pass nothing but each thread's maximum: the k-th largest of the maxima of 32 or 64 groups of threads is a bound that at least k
+// scores reach, and few others.  Threads whose maximum reaches it (else a warp, which reads such a thread's batches again) list those of
+// their batches that do, the block looks through the list, and a score's place is the number of those found before it, where (score, index) are
+// ordered so that the lowest index comes first among equals.
+template <typename T, bool HELD, bool ONE_WARP>
+__global__ void __launch_bounds__(ONE_WARP ? LOGP_ROWS * 32 : LOGP_WARPS * 32, ONE_WARP ? 8 : 2)
+logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, int log_parts,
+                 int32_t share, LogprobsOut out) {
+  constexpr int E = RowBatches<T>::E, WARPS = ONE_WARP ? 1 : LOGP_WARPS, U = HELD ? LOGP_HELD : LOGP_UNROLL;
+  __shared__ RowRoom<WARPS> rooms[ONE_WARP ? LOGP_ROWS : 1];
+  __shared__ RowStats part_stats[ONE_WARP ? 1 : LOGP_MAX_PARTS];
+  __shared__ uint64_t part_best[ONE_WARP ? 1 : LOGP_MAX_PARTS * MTS_LOGPROBS_MAX_TOP];
+  const int lane = lane_id(), warp = ONE_WARP ? 0 : threadIdx.x / 32, tid = ONE_WARP ? lane : threadIdx.x;
+  const int threads = ONE_WARP ? 32 : blockDim.x, warps = threads / 32;
+  RowRoom<WARPS>& room = rooms[ONE_WARP ? threadIdx.x / 32 : 0];
+  const int parts = ONE_WARP ? 1 : 1 << log_parts, part = ONE_WARP ? 0 : blockIdx.x & (parts - 1);
+  const int64_t n = ONE_WARP ? (int64_t)blockIdx.x * LOGP_ROWS + threadIdx.x / 32 : blockIdx.x >> log_parts;
+  if (ONE_WARP && n >= N) return;
+  const auto sync = [] { if (ONE_WARP) __syncwarp(); else __syncthreads(); };
+  if (!ONE_WARP && parts > 1) cluster_arrive();                         // the first block has begun before others write to it
   const RowBatches<T> r(logits + n * row_stride, V);
-  const int32_t b0 = (int32_t)((int64_t)r.count * part / parts), b1 = (int32_t)((int64_t)r.count * (part + 1) / parts);
+  const int32_t b0 = min(r.count, part * share), b1 = min(r.count, b0 + share);
   const float c = scale * LOG2E;
+  const int k = top_k;
   int64_t target = -1;
   float target_score = 0.f;
   if (part == 0 && tid == 0 && out.logp) {
     target = targets[n];
     if (target >= 0 && target < V) target_score = to_f32(r.row[target]);
   }
-  if (tid == 0) count = 0;
+  if (tid == 0) room.listed_count = room.found_count = 0;
 
-  float m = -INFINITY, base = 0.f;
+  const int32_t b = b0 + tid;
+  const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
+  uint4 w[U];
+  float m = -INFINITY;
   Pair S(0.f, 0.f), P(0.f, 0.f);
-  const Pair c2(c, c);
-  int32_t best_batch = b0 + tid;
-  for (int32_t g = b0; g < b1; g += THREADS * LOGP_UNROLL) {
-    uint4 w[LOGP_UNROLL];
-    const int32_t b = g + tid;
-    if (g > 0 && g + THREADS * LOGP_UNROLL < r.count && g + THREADS * LOGP_UNROLL <= b1) {
+  RowStats st;
+  if constexpr (HELD) {
+    const bool all = r.template all_whole<U>(b0, b1, tid, threads);
+    r.load_held(b0, b1, tid, threads, all, w);
+    if (!all) {
 #pragma unroll
-      for (int u = 0; u < LOGP_UNROLL; ++u) w[u] = __ldg(reinterpret_cast<const uint4*>(r.row + r.first(b + u * THREADS)));
+      for (int u = 0; u < U; ++u)
+        if (b + u * threads >= b1) w[u] = nothing_there;
+    }
+    uint32_t most = max_bits<T>(w[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u) most = max_bits<T>(most, w[u]);
+    m = max_value<T>(most);
+    st.m = warp_max(m);
+    if (k > 0) room.top[warp][lane] = m;
+    if (!ONE_WARP && lane == 0) room.stats[warp].m = st.m;
+    sync();
+    if (k > 0 && warp == 0) {
+      const float kth = kth_of_groups<float>(room.top, warps, k, -INFINITY, INFINITY);
+      if (lane == 0) room.bound_score = kth;
+    }
+    if (!ONE_WARP) st.m = warp_max(lane < warps ? room.stats[lane].m : -INFINITY);
+    const float base = base_of(st.m, c);
+    if (ordinary(base)) {
+      if (all) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], st.m, base, c, S, P);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (b + u * threads < b1) add_batch<T, true>(w[u], st.m, base, c, S, P);
+      }
     } else {
-#pragma unroll
-      for (int u = 0; u < LOGP_UNROLL; ++u) w[u] = r.raw(b + u * THREADS < b1 ? b + u * THREADS : r.count);
+#pragma unroll 1
+      for (int32_t at = b; at < b1; at += threads) add_batch<T, false>(r.raw(at), st.m, base, c, S, P);
     }
-    float top[LOGP_UNROLL];
-#pragma unroll
-    for (int u = 0; u < LOGP_UNROLL; ++u) top[u] = max_of<T>(w[u]);
-    float most = top[0];
-#pragma unroll
-    for (int u = 1; u < LOGP_UNROLL; ++u) most = fmaxf(most, top[u]);
-    if (most > m) {
-      const float a = exponent((m - most) * c), f = exp2_fast(a);
-      P = (P + S * Pair(a, a)) * Pair(f, f);
-      S = S * Pair(f, f);
-#pragma unroll
-      for (int u = LOGP_UNROLL - 1; u >= 0; --u)
-        if (top[u] == most) best_batch = b + u * THREADS;
-      m = base = most;
+    st.S = warp_sum(S.sum());
+    st.P = warp_sum(P.sum());
+    if (!ONE_WARP && lane == 0) room.stats[warp] = st;
+    sync();
+    if (!ONE_WARP && warp == 0) {
+      st.S = warp_sum(lane < warps ? room.stats[lane].S : 0.f);
+      st.P = warp_sum(lane < warps ? room.stats[lane].P : 0.f);
     }
-    const Pair minus(-base, -base);
+  } else {
+    float base = 0.f;
+    for (int32_t g = b0; g < b1; g += threads * U) {
+      const int32_t bg = g + tid;
+      const bool all = r.template all_whole<U>(g, b1, tid, threads);
+      r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
+      if (!all) {
 #pragma unroll
-    for (int u = 0; u < LOGP_UNROLL; ++u) {
-      float v[E];
-      RowBatches<T>::unpack(w[u], v);
+        for (int u = 0; u < U; ++u)
+          if (bg + u * threads >= b1) w[u] = nothing_there;
+      }
+      uint32_t most_bits = max_bits<T>(w[0]);
 #pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 d = ((Pair(v[e], v[e + 1]) + minus) * c2).get();
-        const float d0 = exponent(d.x), d1 = exponent(d.y);
-        const Pair p(exp2_fast(d0), exp2_fast(d1));
-        S = S + p;
-        P = fma2(p, Pair(d0, d1), P);
+      for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
+      const float most = max_value<T>(most_bits);
+      if (most > m) {
+        const RowStats s = scaled_to({m, S.sum(), P.sum()}, most, c);
+        S = Pair(s.S, 0.f);
+        P = Pair(s.P, 0.f);
+        m = most;
+        base = base_of(m, c);
+      }
+      if (ordinary(base)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], m, base, c, S, P);
+      } else {
+#pragma unroll 1
+        for (int32_t at = bg; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), m, base, c, S, P);
       }
     }
+    st = join_lanes({m, S.sum(), P.sum()}, c);
+    if (k > 0) room.top[warp][lane] = m;
+    if (lane == 0) room.stats[warp] = st;
+    sync();
+    const RowStats nobody = {-INFINITY, 0.f, 0.f};
+    if (warp == 0) {
+      if (k > 0) {
+        const float kth = kth_of_groups<float>(room.top, warps, k, -INFINITY, INFINITY);
+        if (lane == 0) room.bound_score = kth;
+      }
+      st = join_lanes(lane < warps ? room.stats[lane] : nobody, c);
+    }
+    if (k > 0) sync();
   }
-  RowStats st = {m, S.get().x + S.get().y, P.get().x + P.get().y};
-  st = join_lanes<32>(st, c);
-  // the thread's order, and the largest of its group of THREADS / 32 threads
-  uint64_t order = 0;
-  if (b0 + tid < b1) order = score_order(m, max(r.first(best_batch), 0));
-  uint64_t group = order;
-#pragma unroll
-  for (int o = THREADS / 64; o; o >>= 1) group = max(group, __shfl_xor_sync(0xFFFFFFFFu, group, o));
-  if (lane % (THREADS / 32) == 0) room64[tid / (THREADS / 32)] = group;
-  if (lane == 0) warp_stats[warp] = st;
-  __syncthreads();
+  // the first warp alone has the block's sums
 
-  const int k = min((int64_t)top_k, (int64_t)V);
   if (k > 0) {
-    // the k-th largest of the 32
-    const uint64_t mine = room64[lane];
-    int before = 0;
+    if (ONE_WARP) sync();
+    const float bound = room.bound_score;
+    const bool few = bound == -INFINITY;                                // fewer than k of the groups have a score: those of a short row, or ruled out
+    if (!few) {
+      const auto list = [&](const uint4& batch, int32_t i) {
+        const int at = atomicAdd(&room.listed_count, 1);
+        if (at < LOGP_LISTED) {
+          room.listed[at] = batch;
+          room.listed_at[at] = i;
+        }
+      };
+      if constexpr (HELD) {
+        if (m >= bound) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const uint64_t o = room64[i];
-      before += o > mine || (o == mine && i < lane);
-    }
-    const unsigned kth = __ballot_sync(0xFFFFFFFFu, before == k - 1);
-    uint64_t bound = __shfl_sync(0xFFFFFFFFu, mine, __ffs(kth) - 1);
-    bound = bound > E ? bound - (E - 1) : 0;                            // the score itself lies up to E - 1 places behind its batch's first
-    unsigned winners = __ballot_sync(0xFFFFFFFFu, order >= bound && b0 + tid < b1);
-    while (winners) {
-      const int w = __ffs(winners) - 1;
-      winners &= winners - 1;
-      for (int32_t b = b0 + warp * 32 + w + lane * THREADS; b < b1; b += 32 * THREADS) {
-        float v[E];
-        RowBatches<T>::unpack(r.raw(b), v);
-        const int32_t i = r.first(b);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint64_t o = score_order(v[e], i + e);
-          if (o >= bound && i + e >= 0 && i + e < V) {
-            const int at = atomicAdd(&count, 1);
-            if (at < CAP) found[at] = o;
+          for (int u = 0; u < U; ++u)
+            if (max_value<T>(max_bits<T>(w[u])) >= bound && b + u * threads < b1) list(w[u], r.first(b + u * threads));
+        }
+      } else {
+        unsigned winners = __ballot_sync(0xFFFFFFFFu, m >= bound);
+#pragma unroll 1
+        while (winners) {
+          const int x = __ffs(winners) - 1;
+          winners &= winners - 1;
+          const int y = winners ? __ffs(winners) - 1 : x;               // two threads' batches at a time
+          winners &= winners - 1;
+#pragma unroll 1
+          for (int64_t q = (int64_t)lane * threads; q < b1 - b0; q += 32 * threads) {
+            const int32_t bx = b0 + warp * 32 + x + (int32_t)q, by = b0 + warp * 32 + y + (int32_t)q;
+            const uint4 wx = r.raw(bx < b1 ? bx : r.count), wy = r.raw(y != x && by < b1 ? by : r.count);
+            if (max_value<T>(max_bits<T>(wx)) >= bound) list(wx, r.first(bx));
+            if (max_value<T>(max_bits<T>(wy)) >= bound) list(wy, r.first(by));
           }
         }
       }
     }
-    __syncthreads();
-    const int have = count;
-    if (have <= CAP && (have >= k || bound == 0)) {
-      if (tid < k) best[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < have; i += THREADS) {
-        const uint64_t o = found[i];
-        int place = 0;
-        for (int j = 0; j < have; ++j) place += found[j] > o;
-        if (place < k) best[place] = o;
-      }
-    } else {
-      uint64_t last = ~0ull;
-      for (int q = 0; q < k; ++q) {
-        uint64_t top = 0;
-        for (int32_t b = b0 + tid; b < b1; b += THREADS) {
-          float v[E];
-          RowBatches<T>::unpack(r.raw(b), v);
-          const int32_t i = r.first(b);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint64_t o = score_order(v[e], i + e);
-            if (i + e >= 0 && i + e < V && o < last && o > top) top = o;
-          }
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        __syncthreads();
-        if (lane == 0) room64[warp] = top;
-        __syncthreads();
-        for (int w = 0; w < WARPS; ++w) top = max(top, room64[w]);
-        last = top;
-        if (tid == 0) best[q] = top;
-      }
-    }
-    __syncthreads();
   }
-  const RowStats nobody = {-INFINITY, 0.f, 0.f};
-  st = join_lanes<WARPS>(lane < WARPS ? warp_stats[lane] : nobody, c);
+  if (warp == 0 && (ONE_WARP || parts == 1)) {
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, base = base_of(st.m, c);
+    const float off = ordinary(base) ? fmaf(m0, c, -base) * LN2 : 0.f;  // what the sums' logarithm has too much by the rounding of the base
+    const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
+    const float nothing = st.S == 0.f ? -INFINITY : 0.f;
+    if (lane == 0) {
+      room.m = m0;
+      room.log_s = log_s;
+      room.nothing = nothing;
+      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - m0) * scale - log_s + nothing;
+      if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_sum - st.P / st.S * LN2;
+      if (out.stats) {
+        out.stats[2 * n] = m0;
+        out.stats[2 * n + 1] = log_s;
+      }
+    }
+  }
+  if (k == 0 && (ONE_WARP || parts == 1)) return;
 
-  if (parts > 1) {
-    // to the first block, which joins them
+  const auto write = [&](int place, uint64_t o) {
+    if (out.top_index) out.top_index[n * k + place] = order_index(o);
+    if (out.top_logp) out.top_logp[n * k + place] = (order_score(o) - room.m) * scale - room.log_s + room.nothing;
+  };
+  if (k > 0) {
+    sync();
+    const int listed = room.listed_count;
+    const float bound = room.bound_score;
+    bool settled = bound != -INFINITY && listed <= LOGP_LISTED;
+    if (settled) {
+      for (int i = tid; i < listed * E; i += threads) {
+        const float v = to_f32(reinterpret_cast<const T*>(room.listed)[i]);
+        const int32_t at = room.listed_at[i / E] + i % E;
+        if (v >= bound && at >= 0 && at < V) {
+          const int place = atomicAdd(&room.found_count, 1);
+          if (place < LOGP_FOUND) room.found[place] = score_order(v, at);
+        }
+      }
+      if (!ONE_WARP && parts > 1 && tid < k) room.best[tid] = 0;
+      sync();
+      const int have = room.found_count;
+      for (int i = tid; i < have; i += threads) {
+        const uint64_t o = room.found[i];
+        int place = 0;
+        for (int j = 0; j < have; ++j) place += room.found[j] > o;
+        if (place < k) {
+          if (ONE_WARP || parts == 1) write(place, o);
+          else room.best[place] = o;
+        }
+      }
+      if (ONE_WARP || parts == 1) return;
+      sync();
+    } else {
+      best_of_equals<T, WARPS>(r, b0, b1, k, m, room);
+      if (ONE_WARP || parts == 1) {
+        if (tid < k) write(tid, room.best[tid]);
+        return;
+      }
+    }
+  }
+
+  if constexpr (!ONE_WARP) {
+    // to the first block of the cluster, which joins the parts
     cluster_wait();
     const uint32_t to = in_first_block(&part_stats[part]);
     if (tid == 0)
       asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;" :: "r"(to), "f"(st.m), "f"(st.S), "f"(st.P) : "memory");
-    if (tid < k) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(in_first_block(&part_best[part * k + tid])), "l"(best[tid]) : "memory");
+    if (tid < k) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(in_first_block(&part_best[part * k + tid])), "l"(room.best[tid]) : "memory");
     cluster_arrive();
     cluster_wait();
     if (part != 0) return;
-    st = join_lanes<LOGP_MAX_PARTS>(lane < parts ? part_stats[lane] : nobody, c);
-    for (int i = tid; i < parts * k; i += THREADS) {
+    const RowStats nobody = {-INFINITY, 0.f, 0.f};
+    st = join_lanes(lane < parts ? part_stats[lane] : nobody, c);
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, base = base_of(st.m, c);
+    const float off = ordinary(base) ? fmaf(m0, c, -base) * LN2 : 0.f;
+    const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
+    const float nothing = st.S == 0.f ? -INFINITY : 0.f;
+    if (tid == 0) {
+      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - m0) * scale - log_s + nothing;
+      if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_sum - st.P / st.S * LN2;
+      if (out.stats) {
+        out.stats[2 * n] = m0;
+        out.stats[2 * n + 1] = log_s;
+      }
+    }
+    for (int i = tid; i < parts * k; i += threads) {
       const uint64_t o = part_best[i];
       int place = 0;
       for (int j = 0; j < parts * k; ++j) place += part_best[j] > o;
-      if (place < k && o != 0) best[place] = o;
+      if (place < k && o != 0) {
+        if (out.top_index) out.top_index[n * k + place] = order_index(o);
+        if (out.top_logp) out.top_logp[n * k + place] = (order_score(o) - m0) * scale - log_s + nothing;
+      }
     }
-    __syncthreads();
-  }
-  base = st.m == -INFINITY ? 0.f : st.m;
-  const float log_s = st.S > 0.f ? logf(st.S) : st.S == 0.f ? 0.f : NAN;
-  const float nothing = st.S == 0.f ? -INFINITY : 0.f;
-  if (tid == 0) {
-    if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - base) * scale - log_s + nothing;
-    if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_s - st.P / st.S * LN2;
-    if (out.stats) {
-      out.stats[2 * n] = base;
-      out.stats[2 * n + 1] = log_s;
-    }
-  }
-  if (tid < k) {
-    const uint64_t o = best[tid];
-    if (out.top_index) out.top_index[n * top_k + tid] = order_index(o);
-    if (out.top_logp) out.top_logp[n * top_k + tid] = (order_score(o) - base) * scale - log_s + nothing;
   }
 }
 
@@ -284,21 +500,31 @@ int check_logits(const char* what, const void* logits, int64_t row_stride, int32
   return check_rows(what, "logits", logits, dtype, N, V, row_stride);
 }
 
-template <typename T, int THREADS>
-int launch_forward(const char* what, const T* logits, int64_t row_stride, int64_t N, int64_t V, float scale, const int64_t* targets, int top_k, int parts,
-                   const LogprobsOut& out, cudaStream_t s) {
+struct ForwardCall {
+  int64_t row_stride, N;
+  int32_t V;
+  float scale;
+  const int64_t* targets;
+  int top_k;
+  LogprobsOut out;
+  cudaStream_t stream;
+};
+
+template <typename T, bool HELD, bool ONE_WARP>
+int launch_forward(const char* what, const T* logits, const ForwardCall& a, int warps, int log_parts, int32_t share) {
+  const int parts = 1 << log_parts;
   cudaLaunchAttribute cluster;
   cluster.id = cudaLaunchAttributeClusterDimension;
   cluster.val.clusterDim.x = (unsigned)parts;
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3((unsigned)(N * parts));
-  config.blockDim = dim3(THREADS);
-  config.stream = s;
+  config.gridDim = dim3((unsigned)(ONE_WARP ? ceil_div(a.N, LOGP_ROWS) : a.N * parts));
+  config.blockDim = dim3(32 * (ONE_WARP ? LOGP_ROWS : warps));
+  config.stream = a.stream;
   config.attrs = &cluster;
   config.numAttrs = parts > 1 ? 1 : 0;
-  LaunchScope scope(K_LOGPROBS_FWD, s);
-  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, THREADS>, logits, row_stride, (int32_t)V, scale, targets, top_k, parts, out), what);
+  LaunchScope scope(K_LOGPROBS_FWD, a.stream);
+  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, HELD, ONE_WARP>, logits, a.row_stride, a.N, a.V, a.scale, a.targets, a.top_k, log_parts, share, a.out), what);
 }
 
 }  // namespace
@@ -319,18 +545,20 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
   const LogprobsOut out = {logp, entropy, stats, top_index, top_logp};
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    const int64_t batches = ceil_div(V, RowBatches<T>::E);
-    int threads = 32, parts = 1;
-    while (threads < 512 && batches >= 8 * threads) threads *= 2;
-    while (parts < LOGP_MAX_PARTS && N * parts < 296 && batches >= 1024 * parts) parts *= 2;
     const T* x = static_cast<const T*>(logits);
-    switch (threads) {
-      case 32: return launch_forward<T, 32>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
-      case 64: return launch_forward<T, 64>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
-      case 128: return launch_forward<T, 128>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
-      case 256: return launch_forward<T, 256>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
-      default: return launch_forward<T, 512>(what, x, row_stride, N, V, scale, targets, top_k, parts, out, s);
-    }
+    const ForwardCall a = {row_stride, N, (int32_t)V, scale, targets, top_k, out, s};
+    const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
+    int log_parts = 0;
+    const char* fp = getenv("LOGP_PARTS");
+    if (fp) log_parts = atoi(fp);
+    else while (1 << log_parts < LOGP_MAX_PARTS && N << log_parts < 296 && batches >= 1024 << log_parts) ++log_parts;
+    const int64_t share = ceil_div(batches, 1 << log_parts) ;
+    const char* fw = getenv("LOGP_BPT");
+    const int bpt = fw ? atoi(fw) : 8;
+    if (log_parts == 0 && share <= 32 * LOGP_HELD) return launch_forward<T, true, true>(what, x, a, 1, 0, (int32_t)share);
+    int warps = (int)(ceil_div(share, 32 * bpt) < LOGP_WARPS ? ceil_div(share, 32 * bpt) : LOGP_WARPS);
+    if (share <= (int64_t)warps * 32 * LOGP_HELD) return launch_forward<T, true, false>(what, x, a, warps, log_parts, (int32_t)share);
+    return launch_forward<T, false, false>(what, x, a, warps, log_parts, (int32_t)share);
   });
 }
 

@@ -49,12 +49,45 @@ struct RowBatches {
       for (int e = 0; e < E; ++e) v[e] = i + e >= 0 && i + e < V ? to_f32(row[i + e]) : -INFINITY;
     }
   }
+  static constexpr uint32_t LOW = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __half) ? 0xFC00FC00u : 0xFF80FF80u);     // -infinity
+  // Whether all batches begin + (the warp's first thread ... + 31) + u threads, u < U, are whole and before `end`.
+  template <int U>
+  __device__ __forceinline__ bool all_whole(int32_t begin, int32_t end, int tid, int threads) const {
+    const int32_t first_of_warp = begin + (tid & ~31);
+    return first_of_warp >= (shift != 0) && (int64_t)first_of_warp + 31 + (U - 1) * threads < min(end, (V + shift) / E);
+  }
+  // Batches begin + tid + u threads before `end` into w[u]; those behind it are left as they are.
+  template <int U>
+  __device__ __forceinline__ void load_held(int32_t begin, int32_t end, int tid, int threads, bool all, uint4 (&w)[U]) const {
+    const T* p = row + first(begin + tid);
+    if (all) {
+#pragma unroll
+      for (int u = 0; u < U; ++u, p += threads * E) w[u] = __ldg(reinterpret_cast<const uint4*>(p));
+    } else {
+      const int32_t w0 = shift != 0, span = min(end, (V + shift) / E) - w0, b = begin + tid;      // whole batches: [w0, w0 + span)
+#pragma unroll
+      for (int u = 0; u < U; ++u, p += threads * E)
+        if ((uint32_t)(b + u * threads - w0) < (uint32_t)max(span, 0)) w[u] = __ldg(reinterpret_cast<const uint4*>(p));
+      fill_ends(begin, end, tid, threads, w);
+    }
+  }
+  // The row's first and last batch where they are not whole, into those that a thread holds: batch begin + tid + u threads in w[u], up to `end`.
+  template <int U>
+  __device__ __forceinline__ void fill_ends(int32_t begin, int32_t end, int tid, int threads, uint4 (&w)[U]) const {
+    if (begin == 0 && tid == 0 && !whole(0)) w[0] = raw(0);
+    const int32_t last = count - 1, behind = last - begin - tid;          // of the thread's first batch
+    if (last > 0 && last < end && !whole(last) && behind >= 0) {
+      const uint4 edge = raw(last);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (behind == u * threads) w[u] = edge;
+    }
+  }
   // The batch as it is stored, -infinity outside the row.
   __device__ __forceinline__ uint4 raw(int32_t b) const {
     const int32_t i = first(b);
     if (i >= 0 && i <= V - E) return __ldg(reinterpret_cast<const uint4*>(row + i));
-    const uint32_t low = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __half) ? 0xFC00FC00u : 0xFF80FF80u);
-    uint4 w = make_uint4(low, low, low, low);
+    uint4 w = make_uint4(LOW, LOW, LOW, LOW);
     if (i > -E && i < V) {
       T* const e = reinterpret_cast<T*>(&w);
 #pragma unroll
@@ -93,6 +126,23 @@ __device__ __forceinline__ float order_score(uint64_t o) {
   return k == 0u ? NAN : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
+// Largest of a warp's numbers (NaN counts as -infinity).
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(fmaxf(x, -INFINITY)));
+  return y;
+}
+__device__ __forceinline__ float warp_min(float x) {
+  float y;
+  asm volatile("redux.sync.min.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  return x;
+}
+
 // Pairs of fp32 numbers in one instruction.
 struct Pair {
   unsigned long long bits;
@@ -103,15 +153,11 @@ struct Pair {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(bits));
     return f;
   }
+  __device__ __forceinline__ float sum() const { const float2 f = get(); return f.x + f.y; }
 };
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) {
   Pair r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-  return r;
-}
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-  Pair r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
   return r;
 }
 __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
@@ -120,20 +166,39 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
   return r;
 }
 
-// Largest of the elements of 16 bytes (numbers only: NaN counts as -infinity).
+// Largest of the elements of 16 bytes (numbers only: NaN counts as -infinity): first as a pair of 16-bit elements or an fp32 number, which can
+// be compared on, then as fp32.
 template <typename T>
-__device__ __forceinline__ float max_of(const uint4& w) {
-  if constexpr (sizeof(T) == 4) {
-    return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
-  } else {
-    uint32_t m;
-    if constexpr (sizeof(T) == 2 && !__is_same(T, __half))
-      asm("{\n\t.reg .b32 a, b;\n\tmax.bf16x2 a, %1, %2;\n\tmax.bf16x2 b, %3, %4;\n\tmax.bf16x2 %0, a, b;\n\t}" : "=r"(m) : "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w));
-    else
-      asm("{\n\t.reg .b32 a, b;\n\tmax.f16x2 a, %1, %2;\n\tmax.f16x2 b, %3, %4;\n\tmax.f16x2 %0, a, b;\n\t}" : "=r"(m) : "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w));
-    const float2 f = unpack2<T>(m);
-    return fmaxf(fmaxf(f.x, f.y), -INFINITY);
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) {
+  uint32_t m;
+  if constexpr (sizeof(T) == 4) asm("max.f32 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+  else if constexpr (__is_same(T, __half)) asm("max.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+  else asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, const uint4& w) {
+  if constexpr (sizeof(T) == 4) {                                         // three operands in one instruction
+    asm("max.f32 %0, %0, %1, %2;" : "+r"(a) : "r"(w.x), "r"(w.y));
+    asm("max.f32 %0, %0, %1, %2;" : "+r"(a) : "r"(w.z), "r"(w.w));
+    return a;
   }
+  return max_bits<T>(max_bits<T>(max_bits<T>(w.x, w.y), max_bits<T>(w.z, w.w)), a);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t max_bits(const uint4& w) {
+  if constexpr (sizeof(T) == 4) {
+    uint32_t a;
+    asm("max.f32 %0, %1, %2, %3;" : "=r"(a) : "r"(w.x), "r"(w.y), "r"(w.z));
+    return max_bits<T>(a, w.w);
+  }
+  return max_bits<T>(max_bits<T>(w.x, w.y), max_bits<T>(w.z, w.w));
+}
+template <typename T>
+__device__ __forceinline__ float max_value(uint32_t m) {
+  if constexpr (sizeof(T) == 4) return fmaxf(__uint_as_float(m), -INFINITY);
+  const float2 f = unpack2<T>(m);
+  return fmaxf(fmaxf(f.x, f.y), -INFINITY);
 }
 
 // Sum and maximum over a block of THREADS in a fixed order; every thread gets the result.  `room`: shared, [THREADS / 32]; free again at the
