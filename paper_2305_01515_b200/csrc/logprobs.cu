@@ -3,18 +3,16 @@
 //   z = scale x,  m = max x,  S = sum_v exp(scale (x_v - m)),  log p_v = scale (x_v - m) - log S
 //   entropy = -sum_v p_v log p_v = log S - (sum_v exp(scale (x_v - m)) scale (x_v - m)) / S
 //   dx_v = scale (g_logp ([v = target] - p_v) - g_entropy p_v (log p_v + entropy))
-#include <stdlib.h>
 #include "rows.cuh"
 
 namespace mts {
 
-constexpr int LOGP_THREADS = 256;
 constexpr int LOGP_WARPS = 16;                 // of a block that works on a row
 constexpr int LOGP_ROWS = 4;                   // rows of a block whose warps have one each
 constexpr int LOGP_MAX_PARTS = 8;              // blocks of a cluster that share a row
-constexpr int LOGP_HELD = 8;                   // batches that a thread holds of a row that is held in registers
-constexpr int LOGP_UNROLL = 8;                 // batches on their way for a thread otherwise
-constexpr int LOGP_LISTED = 64;                // batches that can hold a score which reaches the bound
+constexpr int LOGP_UNROLL = 8;                 // batches on their way for a thread: a group
+constexpr int LOGP_UNITS = 8;                  // runs of a thread's groups whose maxima are kept
+constexpr int LOGP_HITS = 128;                 // of them that can hold a score which reaches the bound
 constexpr int LOGP_FOUND = 512;                // scores that can reach it
 
 struct LogprobsOut {
@@ -69,28 +67,28 @@ __device__ __forceinline__ void add_batch(const uint4& w, float m, float base, f
   }
 }
 
-// Working memory of a row.
-template <int WARPS>
+// Working memory of a row, behind which lie, for W warps: float top[2 W][32], each thread's maxima of its even and of its odd units, and float
+// unit[LOGP_UNITS][32 W].
 struct RowRoom {
-  alignas(16) uint4 listed[LOGP_LISTED];
-  alignas(16) float top[WARPS][32];
   uint64_t found[LOGP_FOUND], best[MTS_LOGPROBS_MAX_TOP], bound;
-  int32_t listed_at[LOGP_LISTED];
-  RowStats stats[WARPS];
+  int32_t hits[LOGP_HITS];
+  RowStats stats[LOGP_WARPS];
   float bound_score, m, log_s, nothing;
-  int listed_count, found_count;
+  int hit_count, found_count;
 };
+constexpr int LOGP_ROOM = (sizeof(RowRoom) + 15) / 16 * 16;
+__host__ __device__ constexpr int room_bytes(int warps) { return LOGP_ROOM + (2 + LOGP_UNITS) * 32 * 4 * warps; }
 
 // The k-th largest of the maxima of 32 R groups of threads (X: float or uint64_t), by one warp; `of_thread` is used up.  Equal ones count one by one.
 template <int R, typename X>
-__device__ __forceinline__ X kth_largest(X (*of_thread)[32], int warps, int k, X least, X most) {
+__device__ __forceinline__ X kth_largest(X (*of_thread)[32], int rows, int k, X least, X most) {
   constexpr int PER = 16 / (int)sizeof(X);
   const int lane = lane_id();
   X mine[R];
 #pragma unroll
   for (int q = 0; q < R; ++q) {
     mine[q] = least;
-    for (int w = q; w < warps; w += R) mine[q] = max(mine[q], of_thread[w][lane]);
+    for (int w = q; w < rows; w += R) mine[q] = max(mine[q], of_thread[w][lane]);
   }
   __syncwarp();
   X* flat = &of_thread[0][0];
@@ -118,19 +116,19 @@ __device__ __forceinline__ X kth_largest(X (*of_thread)[32], int warps, int k, X
   return bound;
 }
 template <typename X>
-__device__ __forceinline__ X kth_of_groups(X (*of_thread)[32], int warps, int k, X least, X most) {
-  return k <= 16 || warps < 2 ? kth_largest<1>(of_thread, warps, k, least, most) : kth_largest<2>(of_thread, warps, k, least, most);
+__device__ __forceinline__ X kth_of_groups(X (*of_thread)[32], int rows, int k, X least, X most) {
+  return k <= 16 || rows < 2 ? kth_largest<1>(of_thread, rows, k, least, most) : kth_largest<2>(of_thread, rows, k, least, most);
 }
 
 // The best k of batches [b0, b1) into room.best where the bound by score alone lets too many pass or too few: rows with many equal scores (ruled out
 // altogether, say), and rows with NaN.  The threads find where their maximum came first and the bound is made of (score, index); where that does not
 // settle it either, the best are found one after the other.
-template <typename T, int WARPS>
-__device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, int32_t b1, int k, float m, RowRoom<WARPS>& room) {
+template <typename T, bool ONE_WARP>
+__device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, int32_t b1, int k, float m, RowRoom& room) {
   constexpr int E = RowBatches<T>::E;
-  const int lane = lane_id(), warp = WARPS == 1 ? 0 : threadIdx.x / 32, tid = WARPS == 1 ? lane : threadIdx.x;
-  const int threads = WARPS == 1 ? 32 : blockDim.x, warps = threads / 32;
-  const auto sync = [] { if (WARPS == 1) __syncwarp(); else __syncthreads(); };
+  const int lane = lane_id(), warp = ONE_WARP ? 0 : threadIdx.x / 32, tid = ONE_WARP ? lane : threadIdx.x;
+  const int threads = ONE_WARP ? 32 : blockDim.x, warps = threads / 32;
+  const auto sync = [] { if (ONE_WARP) __syncwarp(); else __syncthreads(); };
   const int32_t b = b0 + tid;
   uint64_t order = 0;
   for (int32_t at = b; at < b1 && !order; at += threads)
@@ -200,25 +198,26 @@ __device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, i
   sync();
 }
 
-// A row (or a part of it, by a cluster of blocks) by the warps of a block, each thread every T-th batch of it; short rows by one warp.
-//   HELD: a thread's batches are all loaded at once and stay in registers: the largest score first, then the sums.
-//   else: a thread keeps the running maximum of its scores and sums relative to it, which are scaled where a group of batches has a larger
-//         one (rare after the first few).
-// The best k cost the pass nothing but each thread's maximum: the k-th largest of the maxima of 32 or 64 groups of threads is a bound that at least k
-// scores reach, and few others.  Threads whose maximum reaches it (else a warp, which reads such a thread's batches again) list those of
-// their batches that do, the block looks through the list, and a score's place is the number of those found before it, where (score, index) are
-// ordered so that the lowest index comes first among equals.
-template <typename T, bool HELD, bool ONE_WARP>
+// A row (or a part of it, by a cluster of blocks) by the warps of a block, each thread every T-th batch of it; where there are rows enough a warp has
+// one for itself.  A thread keeps the running maximum of its scores and sums relative to it, which are scaled where a group of its batches has a
+// larger one (rare after the first few).
+// The best k cost the pass nothing but the maxima of each thread's groups, or of up to LOGP_UNITS runs of them: the k-th largest of the
+// maxima of 32 or 64 groups of threads is a bound that at least k scores reach, and few others.  The units whose maxima reach it are read again, and a
+// score's place is the number of those found before it, where (score, index) are ordered so that the lowest index comes first among equals.
+template <typename T, bool ONE_WARP>
 __global__ void __launch_bounds__(ONE_WARP ? LOGP_ROWS * 32 : LOGP_WARPS * 32, ONE_WARP ? 8 : 2)
 logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, int log_parts,
-                 int32_t share, LogprobsOut out) {
-  constexpr int E = RowBatches<T>::E, WARPS = ONE_WARP ? 1 : LOGP_WARPS, U = HELD ? LOGP_HELD : LOGP_UNROLL;
-  __shared__ RowRoom<WARPS> rooms[ONE_WARP ? LOGP_ROWS : 1];
+                 int32_t share, int log_unit, LogprobsOut out) {
+  constexpr int E = RowBatches<T>::E, U = LOGP_UNROLL;
+  extern __shared__ __align__(16) unsigned char rooms[];
   __shared__ RowStats part_stats[ONE_WARP ? 1 : LOGP_MAX_PARTS];
   __shared__ uint64_t part_best[ONE_WARP ? 1 : LOGP_MAX_PARTS * MTS_LOGPROBS_MAX_TOP];
   const int lane = lane_id(), warp = ONE_WARP ? 0 : threadIdx.x / 32, tid = ONE_WARP ? lane : threadIdx.x;
   const int threads = ONE_WARP ? 32 : blockDim.x, warps = threads / 32;
-  RowRoom<WARPS>& room = rooms[ONE_WARP ? threadIdx.x / 32 : 0];
+  unsigned char* const mine = rooms + (ONE_WARP ? threadIdx.x / 32 * room_bytes(1) : 0);
+  RowRoom& room = *reinterpret_cast<RowRoom*>(mine);
+  float(*const top)[32] = reinterpret_cast<float(*)[32]>(mine + LOGP_ROOM);
+  float* const unit_top = &top[2 * warps][0];
   const int parts = ONE_WARP ? 1 : 1 << log_parts, part = ONE_WARP ? 0 : blockIdx.x & (parts - 1);
   const int64_t n = ONE_WARP ? (int64_t)blockIdx.x * LOGP_ROWS + threadIdx.x / 32 : blockIdx.x >> log_parts;
   if (ONE_WARP && n >= N) return;
@@ -234,143 +233,82 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     target = targets[n];
     if (target >= 0 && target < V) target_score = to_f32(r.row[target]);
   }
-  if (tid == 0) room.listed_count = room.found_count = 0;
+  if (tid == 0) room.hit_count = room.found_count = 0;
 
-  const int32_t b = b0 + tid;
   const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
-  uint4 w[U];
-  float m = -INFINITY;
+  float m = -INFINITY, base = 0.f, of_unit = -INFINITY, of_units[2] = {-INFINITY, -INFINITY};
   Pair S(0.f, 0.f), P(0.f, 0.f);
-  RowStats st;
-  if constexpr (HELD) {
-    const bool all = r.template all_whole<U>(b0, b1, tid, threads);
-    r.load_held(b0, b1, tid, threads, all, w);
+  int group = 0;
+  for (int32_t g = b0; g < b1; g += threads * U, ++group) {
+    const int32_t b = g + tid;
+    const bool all = r.template all_whole<U>(g, b1, tid, threads);
+    uint4 w[U];
+    r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
     if (!all) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (b + u * threads >= b1) w[u] = nothing_there;
     }
-    uint32_t most = max_bits<T>(w[0]);
+    uint32_t most_bits = max_bits<T>(w[0]);
 #pragma unroll
-    for (int u = 1; u < U; ++u) most = max_bits<T>(most, w[u]);
-    m = max_value<T>(most);
-    st.m = warp_max(m);
-    if (k > 0) room.top[warp][lane] = m;
-    if (!ONE_WARP && lane == 0) room.stats[warp].m = st.m;
-    sync();
-    if (k > 0 && warp == 0) {
-      const float kth = kth_of_groups<float>(room.top, warps, k, -INFINITY, INFINITY);
+    for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
+    const float most = max_value<T>(most_bits);
+    if (k > 0) {
+      const int unit = group >> log_unit;
+      of_unit = unit << log_unit == group ? most : fmaxf(of_unit, most);
+      unit_top[unit * threads + tid] = of_unit;
+      of_units[unit & 1] = fmaxf(of_units[unit & 1], most);
+    }
+    if (most > m) {
+      const RowStats s = scaled_to({m, S.sum(), P.sum()}, most, c);
+      S = Pair(s.S, 0.f);
+      P = Pair(s.P, 0.f);
+      m = most;
+      base = base_of(m, c);
+    }
+    if (!ordinary(base)) {
+#pragma unroll 1
+      for (int32_t at = b; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), m, base, c, S, P);
+    } else if (all) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], m, base, c, S, P);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (b + u * threads < b1) add_batch<T, true>(w[u], m, base, c, S, P);
+    }
+  }
+  RowStats st = join_lanes({m, S.sum(), P.sum()}, c);
+  if (k > 0) {
+    top[2 * warp][lane] = of_units[0];
+    top[2 * warp + 1][lane] = of_units[1];
+  }
+  if (!ONE_WARP && lane == 0) room.stats[warp] = st;
+  if (!ONE_WARP || k > 0) sync();
+  const RowStats nobody = {-INFINITY, 0.f, 0.f};
+  if (warp == 0) {
+    if (k > 0) {
+      const float kth = kth_of_groups<float>(top, 2 * warps, k, -INFINITY, INFINITY);
       if (lane == 0) room.bound_score = kth;
     }
-    if (!ONE_WARP) st.m = warp_max(lane < warps ? room.stats[lane].m : -INFINITY);
-    const float base = base_of(st.m, c);
-    if (ordinary(base)) {
-      if (all) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], st.m, base, c, S, P);
-      } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (b + u * threads < b1) add_batch<T, true>(w[u], st.m, base, c, S, P);
-      }
-    } else {
-#pragma unroll 1
-      for (int32_t at = b; at < b1; at += threads) add_batch<T, false>(r.raw(at), st.m, base, c, S, P);
-    }
-    st.S = warp_sum(S.sum());
-    st.P = warp_sum(P.sum());
-    if (!ONE_WARP && lane == 0) room.stats[warp] = st;
-    sync();
-    if (!ONE_WARP && warp == 0) {
-      st.S = warp_sum(lane < warps ? room.stats[lane].S : 0.f);
-      st.P = warp_sum(lane < warps ? room.stats[lane].P : 0.f);
-    }
-  } else {
-    float base = 0.f;
-    for (int32_t g = b0; g < b1; g += threads * U) {
-      const int32_t bg = g + tid;
-      const bool all = r.template all_whole<U>(g, b1, tid, threads);
-      r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
-      if (!all) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (bg + u * threads >= b1) w[u] = nothing_there;
-      }
-      uint32_t most_bits = max_bits<T>(w[0]);
-#pragma unroll
-      for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
-      const float most = max_value<T>(most_bits);
-      if (most > m) {
-        const RowStats s = scaled_to({m, S.sum(), P.sum()}, most, c);
-        S = Pair(s.S, 0.f);
-        P = Pair(s.P, 0.f);
-        m = most;
-        base = base_of(m, c);
-      }
-      if (ordinary(base)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], m, base, c, S, P);
-      } else {
-#pragma unroll 1
-        for (int32_t at = bg; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), m, base, c, S, P);
-      }
-    }
-    st = join_lanes({m, S.sum(), P.sum()}, c);
-    if (k > 0) room.top[warp][lane] = m;
-    if (lane == 0) room.stats[warp] = st;
-    sync();
-    const RowStats nobody = {-INFINITY, 0.f, 0.f};
-    if (warp == 0) {
-      if (k > 0) {
-        const float kth = kth_of_groups<float>(room.top, warps, k, -INFINITY, INFINITY);
-        if (lane == 0) room.bound_score = kth;
-      }
-      st = join_lanes(lane < warps ? room.stats[lane] : nobody, c);
-    }
-    if (k > 0) sync();
+    if (!ONE_WARP) st = join_lanes(lane < warps ? room.stats[lane] : nobody, c);     // which this warp alone has
   }
-  // the first warp alone has the block's sums
-
   if (k > 0) {
-    if (ONE_WARP) sync();
+    sync();
     const float bound = room.bound_score;
-    const bool few = bound == -INFINITY;                                // fewer than k of the groups have a score: those of a short row, or ruled out
-    if (!few) {
-      const auto list = [&](const uint4& batch, int32_t i) {
-        const int at = atomicAdd(&room.listed_count, 1);
-        if (at < LOGP_LISTED) {
-          room.listed[at] = batch;
-          room.listed_at[at] = i;
-        }
-      };
-      if constexpr (HELD) {
-        if (m >= bound) {
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (max_value<T>(max_bits<T>(w[u])) >= bound && b + u * threads < b1) list(w[u], r.first(b + u * threads));
-        }
-      } else {
-        unsigned winners = __ballot_sync(0xFFFFFFFFu, m >= bound);
-#pragma unroll 1
-        while (winners) {
-          const int x = __ffs(winners) - 1;
-          winners &= winners - 1;
-          const int y = winners ? __ffs(winners) - 1 : x;               // two threads' batches at a time
-          winners &= winners - 1;
-#pragma unroll 1
-          for (int64_t q = (int64_t)lane * threads; q < b1 - b0; q += 32 * threads) {
-            const int32_t bx = b0 + warp * 32 + x + (int32_t)q, by = b0 + warp * 32 + y + (int32_t)q;
-            const uint4 wx = r.raw(bx < b1 ? bx : r.count), wy = r.raw(y != x && by < b1 ? by : r.count);
-            if (max_value<T>(max_bits<T>(wx)) >= bound) list(wx, r.first(bx));
-            if (max_value<T>(max_bits<T>(wy)) >= bound) list(wy, r.first(by));
-          }
+    // (-infinity: fewer than k of the groups have a score, those of a short row, or ruled out)
+    if (m >= bound && bound != -INFINITY) {
+      for (int unit = 0; unit << log_unit < group; ++unit) {
+        if (unit_top[unit * threads + tid] >= bound) {
+          const int at = atomicAdd(&room.hit_count, 1);
+          if (at < LOGP_HITS) room.hits[at] = unit << 16 | tid;
         }
       }
     }
   }
   if (warp == 0 && (ONE_WARP || parts == 1)) {
-    const float m0 = st.m == -INFINITY ? 0.f : st.m, base = base_of(st.m, c);
-    const float off = ordinary(base) ? fmaf(m0, c, -base) * LN2 : 0.f;  // what the sums' logarithm has too much by the rounding of the base
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, rounded = base_of(st.m, c);
+    const float off = ordinary(rounded) ? fmaf(m0, c, -rounded) * LN2 : 0.f;         // what the sums' logarithm has too much by the rounding of the base
     const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
     const float nothing = st.S == 0.f ? -INFINITY : 0.f;
     if (lane == 0) {
@@ -393,34 +331,50 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   };
   if (k > 0) {
     sync();
-    const int listed = room.listed_count;
+    const int hits = room.hit_count;
     const float bound = room.bound_score;
-    bool settled = bound != -INFINITY && listed <= LOGP_LISTED;
+    bool settled = bound != -INFINITY && hits <= LOGP_HITS;
     if (settled) {
-      for (int i = tid; i < listed * E; i += threads) {
-        const float v = to_f32(reinterpret_cast<const T*>(room.listed)[i]);
-        const int32_t at = room.listed_at[i / E] + i % E;
-        if (v >= bound && at >= 0 && at < V) {
+      const int log_per = 3 + log_unit;                                 // a unit's batches
+      static_assert(U == 8, "a group of 2^3 batches");
+      for (int i = tid; i < hits << log_per; i += threads) {
+        const int which = room.hits[i >> log_per];
+        const int64_t at = b0 + (which & 0xFFFF) + (((int64_t)(which >> 16) << log_per) + (i & ((1 << log_per) - 1))) * threads;
+        if (at >= b1) continue;
+        const uint4 batch = r.raw((int32_t)at);
+        float v[E];
+        RowBatches<T>::unpack(batch, v);
+        unsigned reach = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) reach |= (v[e] >= bound) << e;      // -infinity outside the row
+#pragma unroll 1
+        for (; reach; reach &= reach - 1) {
+          const int32_t j = r.first((int32_t)at) + __ffs(reach) - 1;
           const int place = atomicAdd(&room.found_count, 1);
-          if (place < LOGP_FOUND) room.found[place] = score_order(v, at);
+          if (place < LOGP_FOUND) room.found[place] = score_order(to_f32(r.row[j]), j);
         }
       }
       if (!ONE_WARP && parts > 1 && tid < k) room.best[tid] = 0;
       sync();
       const int have = room.found_count;
-      for (int i = tid; i < have; i += threads) {
-        const uint64_t o = room.found[i];
-        int place = 0;
-        for (int j = 0; j < have; ++j) place += room.found[j] > o;
-        if (place < k) {
-          if (ONE_WARP || parts == 1) write(place, o);
-          else room.best[place] = o;
+      settled = have <= LOGP_FOUND;
+      if (settled) {
+        for (int i = tid; i < have; i += threads) {
+          const uint64_t o = room.found[i];
+          int place = 0;
+#pragma unroll 8
+          for (int j = 0; j < have; ++j) place += room.found[j] > o;
+          if (place < k) {
+            if (ONE_WARP || parts == 1) write(place, o);
+            else room.best[place] = o;
+          }
         }
+        if (ONE_WARP || parts == 1) return;
+        sync();
       }
-      if (ONE_WARP || parts == 1) return;
-      sync();
-    } else {
-      best_of_equals<T, WARPS>(r, b0, b1, k, m, room);
+    }
+    if (!settled) {
+      best_of_equals<T, ONE_WARP>(r, b0, b1, k, m, room);
       if (ONE_WARP || parts == 1) {
         if (tid < k) write(tid, room.best[tid]);
         return;
@@ -438,10 +392,9 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     cluster_arrive();
     cluster_wait();
     if (part != 0) return;
-    const RowStats nobody = {-INFINITY, 0.f, 0.f};
     st = join_lanes(lane < parts ? part_stats[lane] : nobody, c);
-    const float m0 = st.m == -INFINITY ? 0.f : st.m, base = base_of(st.m, c);
-    const float off = ordinary(base) ? fmaf(m0, c, -base) * LN2 : 0.f;
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, rounded = base_of(st.m, c);
+    const float off = ordinary(rounded) ? fmaf(m0, c, -rounded) * LN2 : 0.f;
     const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
     const float nothing = st.S == 0.f ? -INFINITY : 0.f;
     if (tid == 0) {
@@ -455,6 +408,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     for (int i = tid; i < parts * k; i += threads) {
       const uint64_t o = part_best[i];
       int place = 0;
+#pragma unroll 8
       for (int j = 0; j < parts * k; ++j) place += part_best[j] > o;
       if (place < k && o != 0) {
         if (out.top_index) out.top_index[n * k + place] = order_index(o);
@@ -464,25 +418,53 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   }
 }
 
+// Gradient: a thread takes BACK_UNROLL batches of the gradient's row (16 bytes that start on a 16-byte boundary of it) and reads the scores that lie under them.
+constexpr int BACK_THREADS = 256, BACK_UNROLL = 4;
+
 template <typename T>
-__global__ void __launch_bounds__(LOGP_THREADS)
+__global__ void __launch_bounds__(BACK_THREADS)
 logprobs_backward(const T* logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ targets, const float* __restrict__ stats,
                   const float* __restrict__ entropy, const float* __restrict__ grad_logp, const float* __restrict__ grad_entropy, T* grad_logits,
-                  int64_t grad_stride) {
-  const int64_t n = blockIdx.x;
+                  int64_t grad_stride, int32_t pieces) {
+  constexpr int E = RowBatches<T>::E, U = BACK_UNROLL;
+  const int64_t n = blockIdx.x / pieces;
+  const int32_t piece = blockIdx.x - (int32_t)(n * pieces);
+  const RowBatches<T> r(grad_logits + n * grad_stride, V);
+  const RowUnder<T> under(logits + n * row_stride, r);
   const float c = scale * LOG2E, m = stats[2 * n], log_s = stats[2 * n + 1];
   const int64_t t = targets ? targets[n] : -1;
   const float gl = !grad_logp || t < 0 ? 0.f : t >= V ? NAN : grad_logp[n], gh = grad_entropy ? grad_entropy[n] : 0.f;
-  // dx = p (alpha + beta d) + [v = target] scale gl, with d = log2 of exp(scale (x - m))
+  // dx = p (alpha + beta d) + [v = target] scale gl, with d = log2 of exp(scale (x - m)) and p = 2^(d - bias)
   const float alpha = -scale * (gl + (gh != 0.f ? gh * (entropy[n] - log_s) : 0.f)), beta = -scale * gh * LN2, bias = log_s * LOG2E;
-  for (int j = threadIdx.x; j < V; j += LOGP_THREADS) {
-    float g = 0.f;
-    if (gl != 0.f || gh != 0.f) {
-      const float x = to_f32(logits[n * row_stride + j]);
-      const float d = exponent((x - m) * c), p = exp2_fast(d - bias);
-      g = p * (alpha + beta * d) + (j == t ? scale * gl : 0.f);
+  const bool any = gl != 0.f || gh != 0.f;
+  const int32_t b = piece * (int)(blockDim.x * U) + threadIdx.x;
+  uint4 w[U];
+  if (any) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = under.raw(b + u * (int)blockDim.x);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int32_t at = b + u * (int)blockDim.x, i = r.first(at);
+    if (at >= r.count) break;
+    float v[E];
+    if (any) {
+      RowBatches<T>::unpack(w[u], v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = exponent((v[e] - m) * c);
+        v[e] = exp2_fast(d - bias) * fmaf(beta, d, alpha);
+      }
+      if (t >= i && t < i + E) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (t == i + e) v[e] += scale * gl;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = 0.f;
     }
-    grad_logits[n * grad_stride + j] = from_f32<T>(g);
+    r.store(at, v);
   }
 }
 
@@ -510,8 +492,10 @@ struct ForwardCall {
   cudaStream_t stream;
 };
 
-template <typename T, bool HELD, bool ONE_WARP>
+template <typename T, bool ONE_WARP>
 int launch_forward(const char* what, const T* logits, const ForwardCall& a, int warps, int log_parts, int32_t share) {
+  int log_unit = 0;
+  while (ceil_div(share, (int64_t)warps * 32 * LOGP_UNROLL << log_unit) > LOGP_UNITS) ++log_unit;
   const int parts = 1 << log_parts;
   cudaLaunchAttribute cluster;
   cluster.id = cudaLaunchAttributeClusterDimension;
@@ -523,8 +507,9 @@ int launch_forward(const char* what, const T* logits, const ForwardCall& a, int 
   config.stream = a.stream;
   config.attrs = &cluster;
   config.numAttrs = parts > 1 ? 1 : 0;
+  config.dynamicSmemBytes = ONE_WARP ? LOGP_ROWS * room_bytes(1) : room_bytes(warps);
   LaunchScope scope(K_LOGPROBS_FWD, a.stream);
-  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, HELD, ONE_WARP>, logits, a.row_stride, a.N, a.V, a.scale, a.targets, a.top_k, log_parts, share, a.out), what);
+  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, ONE_WARP>, logits, a.row_stride, a.N, a.V, a.scale, a.targets, a.top_k, log_parts, share, log_unit, a.out), what);
 }
 
 }  // namespace
@@ -548,17 +533,18 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
     const T* x = static_cast<const T*>(logits);
     const ForwardCall a = {row_stride, N, (int32_t)V, scale, targets, top_k, out, s};
     const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
+    // Few rows: each by a cluster, while the GPU has an SM for every block and a part 1,024 batches (one row of 5,000 fp32 batches by 1, 2, 4 and 8
+    // blocks: 6.0, 6.4, 5.8 and 6.0 us; 100 rows of 2,500: 5.9 us by single blocks, 7.1 by pairs).
     int log_parts = 0;
-    const char* fp = getenv("LOGP_PARTS");
-    if (fp) log_parts = atoi(fp);
-    else while (1 << log_parts < LOGP_MAX_PARTS && N << log_parts < 296 && batches >= 1024 << log_parts) ++log_parts;
-    const int64_t share = ceil_div(batches, 1 << log_parts) ;
-    const char* fw = getenv("LOGP_BPT");
-    const int bpt = fw ? atoi(fw) : 8;
-    if (log_parts == 0 && share <= 32 * LOGP_HELD) return launch_forward<T, true, true>(what, x, a, 1, 0, (int32_t)share);
-    int warps = (int)(ceil_div(share, 32 * bpt) < LOGP_WARPS ? ceil_div(share, 32 * bpt) : LOGP_WARPS);
-    if (share <= (int64_t)warps * 32 * LOGP_HELD) return launch_forward<T, true, false>(what, x, a, warps, log_parts, (int32_t)share);
-    return launch_forward<T, false, false>(what, x, a, warps, log_parts, (int32_t)share);
+    while (2 << log_parts <= LOGP_MAX_PARTS && N << log_parts <= 74 && batches >= 2048 << log_parts) ++log_parts;
+    const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
+    // Warps of a row: what a warp does for a row apart from its scores costs as much as a dozen batches a lane, so as few as keep the row short: us
+    // with 1, 2, 4, 8 for 50,000 rows of 500 batches 172, 183, 265, 462; 25,000 of 1,000 148, 131, 144, 249; 6,250 of 4,000 153, 98, 95, 102; 2,048 of
+    // 16,384 243, 125, 111, 101 (16: 111).  Where that leaves SMs idle more, while a thread has a few batches (300 rows of 1,250: 19.0, 11.8, 9.4, 8.6).
+    int warps = share <= 700 ? 1 : share <= 3000 ? 2 : share <= 8000 ? 4 : 8;
+    while (warps < LOGP_WARPS && (N << log_parts) * warps < 148 * 16 && share >= (warps < 8 ? 64 : 256) * warps) warps *= 2;
+    if (warps == 1 && log_parts == 0) return launch_forward<T, true>(what, x, a, 1, 0, share);
+    return launch_forward<T, false>(what, x, a, warps, log_parts, share);
   });
 }
 
@@ -578,9 +564,14 @@ extern "C" int mts_logprobs_backward(const void* logits, int64_t row_stride, int
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
+    const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
+    int threads = 32;
+    while (threads < BACK_THREADS && batches > threads * BACK_UNROLL) threads *= 2;
+    const int64_t pieces = ceil_div(batches, threads * BACK_UNROLL);
+    if (N * pieces > INT32_MAX) return set_error(MTS_ERR_UNSUPPORTED, "%s: %lld rows of %lld", what, (long long)N, (long long)V);
     LaunchScope scope(K_LOGPROBS_BWD, s);
-    logprobs_backward<T><<<(unsigned)N, LOGP_THREADS, 0, s>>>(static_cast<const T*>(logits), row_stride, (int32_t)V, scale, targets, stats, entropy,
-                                                              grad_logp, grad_entropy, static_cast<T*>(grad_logits), grad_stride);
+    logprobs_backward<T><<<(unsigned)(N * pieces), threads, 0, s>>>(static_cast<const T*>(logits), row_stride, (int32_t)V, scale, targets, stats, entropy,
+                                                                    grad_logp, grad_entropy, static_cast<T*>(grad_logits), grad_stride, (int32_t)pieces);
     return check_launch(what);
   });
 }

@@ -38,17 +38,6 @@ struct RowBatches {
   }
   __device__ __forceinline__ int32_t first(int32_t b) const { return b * E - shift; }      // may be negative; at most V + E
   __device__ __forceinline__ bool whole(int32_t b) const { const int32_t i = first(b); return i >= 0 && i <= V - E; }
-  // The batch as fp32, -infinity outside the row.
-  __device__ __forceinline__ void load(int32_t b, float (&v)[E]) const {
-    const int32_t i = first(b);
-    if (i >= 0 && i <= V - E) {
-      const uint4 w = *reinterpret_cast<const uint4*>(row + i);
-      unpack(w, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = i + e >= 0 && i + e < V ? to_f32(row[i + e]) : -INFINITY;
-    }
-  }
   static constexpr uint32_t LOW = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __half) ? 0xFC00FC00u : 0xFF80FF80u);     // -infinity
   // Whether all batches begin + (the warp's first thread ... + 31) + u threads, u < U, are whole and before `end`.
   template <int U>
@@ -96,6 +85,19 @@ struct RowBatches {
     }
     return w;
   }
+  // Writes the batch's elements that lie in the row.
+  __device__ __forceinline__ void store(int32_t b, const float (&v)[E]) const {
+    const int32_t i = first(b);
+    T* const to = const_cast<T*>(row) + i;
+    if (i >= 0 && i <= V - E) {
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+      else *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (i + e >= 0 && i + e < V) to[e] = from_f32<T>(v[e]);
+    }
+  }
   static __device__ __forceinline__ void unpack(const uint4& w, float (&v)[E]) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -108,6 +110,56 @@ struct RowBatches {
         v[2 * k + 1] = f.y;
       }
     }
+  }
+};
+
+// The elements of another row under the batches of `RowBatches` r (a row of scores under the row of their gradient), which need not start on boundaries: two
+// aligned accesses and a shift where they do not.
+template <typename T>
+struct RowUnder {
+  static constexpr int E = RowBatches<T>::E;
+  const T* row;
+  const RowBatches<T>& r;
+  int32_t ahead;                 // elements from a boundary to a batch's first
+  __device__ __forceinline__ RowUnder(const T* row_, const RowBatches<T>& r_) : row(row_), r(r_) {
+    ahead = (int32_t)((reinterpret_cast<uintptr_t>(row_) / sizeof(T) + E - r_.shift) % E);
+  }
+  // Whether the accesses for batch b lie within the row.
+  __device__ __forceinline__ bool within(int32_t b) const {
+    const int32_t i = r.first(b) - ahead;
+    return i >= 0 && i <= r.V - (ahead ? 2 * E : E);
+  }
+  __device__ __forceinline__ uint4 shifted(const uint4& lo, const uint4& hi) const {
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const int words = ahead * (int)sizeof(T) / 4;
+    uint32_t s[5];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      uint32_t x = w[k];
+      if (words == 1) x = w[k + 1];
+      if (words == 2) x = w[k + 2];
+      if (words == 3 && k + 3 < 8) x = w[k + 3 < 8 ? k + 3 : 7];
+      s[k] = x;
+    }
+    const int bits = ahead * (int)sizeof(T) * 8 % 32;
+    return make_uint4(__funnelshift_r(s[0], s[1], bits), __funnelshift_r(s[1], s[2], bits), __funnelshift_r(s[2], s[3], bits), __funnelshift_r(s[3], s[4], bits));
+  }
+  // The batch as it is stored, -infinity outside the row.  Not through the read-only path: the gradient may take the scores' place.
+  __device__ __forceinline__ uint4 raw(int32_t b) const {
+    const int32_t i = r.first(b);
+    if (within(b)) {
+      const uint4* p = reinterpret_cast<const uint4*>(row + (i - ahead));
+      const uint4 lo = p[0];
+      return ahead ? shifted(lo, p[1]) : lo;
+    }
+    uint4 w = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
+    if (i > -E && i < r.V) {
+      T* const e = reinterpret_cast<T*>(&w);
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (i + k >= 0 && i + k < r.V) e[k] = row[i + k];
+    }
+    return w;
   }
 };
 
