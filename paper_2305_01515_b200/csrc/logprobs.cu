@@ -204,7 +204,8 @@ __device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, i
 // The best k cost the pass nothing but the maxima of each thread's groups, or of up to LOGP_UNITS runs of them: the k-th largest of the
 // maxima of 32 or 64 groups of threads is a bound that at least k scores reach, and few others.  The units whose maxima reach it are read again, and a
 // score's place is the number of those found before it, where (score, index) are ordered so that the lowest index comes first among equals.
-template <typename T, bool ONE_WARP>
+// SHORT: rows of one group of a warp, which list the batches themselves instead of units.
+template <typename T, bool ONE_WARP, bool SHORT>
 __global__ void __launch_bounds__(ONE_WARP ? LOGP_ROWS * 32 : LOGP_WARPS * 32, ONE_WARP ? 8 : 2)
 logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, int32_t V, float scale, const int64_t* __restrict__ targets, int top_k, int log_parts,
                  int32_t share, int log_unit, LogprobsOut out) {
@@ -239,10 +240,10 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   float m = -INFINITY, base = 0.f, of_unit = -INFINITY, of_units[2] = {-INFINITY, -INFINITY};
   Pair S(0.f, 0.f), P(0.f, 0.f);
   int group = 0;
+  uint4 w[U];
   for (int32_t g = b0; g < b1; g += threads * U, ++group) {
     const int32_t b = g + tid;
     const bool all = r.template all_whole<U>(g, b1, tid, threads);
-    uint4 w[U];
     r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
     if (!all) {
 #pragma unroll
@@ -253,7 +254,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
 #pragma unroll
     for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
     const float most = max_value<T>(most_bits);
-    if (k > 0) {
+    if (k > 0 && !SHORT) {
       const int unit = group >> log_unit;
       of_unit = unit << log_unit == group ? most : fmaxf(of_unit, most);
       unit_top[unit * threads + tid] = of_unit;
@@ -277,7 +278,9 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
       for (int u = 0; u < U; ++u)
         if (b + u * threads < b1) add_batch<T, true>(w[u], m, base, c, S, P);
     }
+    if (SHORT) break;
   }
+  if (SHORT) of_units[0] = m;
   RowStats st = join_lanes({m, S.sum(), P.sum()}, c);
   if (k > 0) {
     top[2 * warp][lane] = of_units[0];
@@ -298,11 +301,17 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     const float bound = room.bound_score;
     // (-infinity: fewer than k of the groups have a score, those of a short row, or ruled out)
     if (m >= bound && bound != -INFINITY) {
-      for (int unit = 0; unit << log_unit < group; ++unit) {
-        if (unit_top[unit * threads + tid] >= bound) {
-          const int at = atomicAdd(&room.hit_count, 1);
-          if (at < LOGP_HITS) room.hits[at] = unit << 16 | tid;
-        }
+      const auto hit = [&](int unit) {
+        const int at = atomicAdd(&room.hit_count, 1);
+        if (at < LOGP_HITS) room.hits[at] = unit << 16 | tid;
+      };
+      if constexpr (SHORT) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (max_value<T>(max_bits<T>(w[u])) >= bound) hit(u);
+      } else {
+        for (int unit = 0; unit << log_unit < group; ++unit)
+          if (unit_top[unit * threads + tid] >= bound) hit(unit);
       }
     }
   }
@@ -335,7 +344,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     const float bound = room.bound_score;
     bool settled = bound != -INFINITY && hits <= LOGP_HITS;
     if (settled) {
-      const int log_per = 3 + log_unit;                                 // a unit's batches
+      const int log_per = SHORT ? 0 : 3 + log_unit;                                 // a unit's batches
       static_assert(U == 8, "a group of 2^3 batches");
       for (int i = tid; i < hits << log_per; i += threads) {
         const int which = room.hits[i >> log_per];
@@ -492,7 +501,7 @@ struct ForwardCall {
   cudaStream_t stream;
 };
 
-template <typename T, bool ONE_WARP>
+template <typename T, bool ONE_WARP, bool SHORT>
 int launch_forward(const char* what, const T* logits, const ForwardCall& a, int warps, int log_parts, int32_t share) {
   int log_unit = 0;
   while (ceil_div(share, (int64_t)warps * 32 * LOGP_UNROLL << log_unit) > LOGP_UNITS) ++log_unit;
@@ -509,7 +518,7 @@ int launch_forward(const char* what, const T* logits, const ForwardCall& a, int 
   config.numAttrs = parts > 1 ? 1 : 0;
   config.dynamicSmemBytes = ONE_WARP ? LOGP_ROWS * room_bytes(1) : room_bytes(warps);
   LaunchScope scope(K_LOGPROBS_FWD, a.stream);
-  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, ONE_WARP>, logits, a.row_stride, a.N, a.V, a.scale, a.targets, a.top_k, log_parts, share, log_unit, a.out), what);
+  return check_cuda(cudaLaunchKernelEx(&config, logprobs_forward<T, ONE_WARP, SHORT>, logits, a.row_stride, a.N, a.V, a.scale, a.targets, a.top_k, log_parts, share, log_unit, a.out), what);
 }
 
 }  // namespace
@@ -543,8 +552,9 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
     // 16,384 243, 125, 111, 101 (16: 111).  Where that leaves SMs idle more, while a thread has a few batches (300 rows of 1,250: 19.0, 11.8, 9.4, 8.6).
     int warps = share <= 700 ? 1 : share <= 3000 ? 2 : share <= 8000 ? 4 : 8;
     while (warps < LOGP_WARPS && (N << log_parts) * warps < 148 * 16 && share >= (warps < 8 ? 64 : 256) * warps) warps *= 2;
-    if (warps == 1 && log_parts == 0) return launch_forward<T, true>(what, x, a, 1, 0, share);
-    return launch_forward<T, false>(what, x, a, warps, log_parts, share);
+    if (warps == 1 && log_parts == 0)
+      return share <= 32 * LOGP_UNROLL ? launch_forward<T, true, true>(what, x, a, 1, 0, share) : launch_forward<T, true, false>(what, x, a, 1, 0, share);
+    return launch_forward<T, false, false>(what, x, a, warps, log_parts, share);
   });
 }
 
