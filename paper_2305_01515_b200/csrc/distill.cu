@@ -3,85 +3,281 @@
 //   q = softmax of scale teacher_k over the listed items (and exp(rest) for all others together),  p = softmax(scale x)
 //   loss = sum_k q_k (log q_k - log p_{i_k}) + q_rest (log q_rest - log p_rest),   p_rest = what p gives to the items not listed
 //   dx_v = weight scale (p_v - q_v) for a listed item, weight scale p_v (1 - q_rest / p_rest) for another
+#include <stdlib.h>
 #include "rows.cuh"
 
 namespace mts {
 
-constexpr int DISTILL_THREADS = 256;
+constexpr int DISTILL_WARPS = 16;
 constexpr int DISTILL_MAX_K = MTS_DISTILL_MAX_K;
+constexpr int DISTILL_UNROLL = 8, DISTILL_GRAD_UNROLL = 4;     // batches on their way for a thread
+constexpr int LISTED_SLOTS = 2 * DISTILL_MAX_K;                // of the table of batches that hold a listed item
 
-template <typename T, typename Q>
-__global__ void __launch_bounds__(DISTILL_THREADS)
-distill_loss(const T* logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ index, const Q* __restrict__ teacher, int K,
-             const float* __restrict__ rest, const float* __restrict__ weights, float* __restrict__ loss, T* grad, int64_t grad_stride) {
-  __shared__ float room[DISTILL_THREADS / 32];
-  __shared__ float q_of[DISTILL_MAX_K];
-  __shared__ int32_t at[DISTILL_MAX_K];
-  const int64_t n = blockIdx.x;
-  const T* row = logits + n * row_stride;
-  const float c = scale * LOG2E;
-  // the teacher's distribution
-  const int k = threadIdx.x;
-  const int64_t i = k < K ? index[n * K + k] : -1;
-  const bool listed = i >= 0, wrong = i >= V;
-  const float t = listed ? to_f32(teacher[n * K + k]) * scale : -INFINITY, t_rest = rest ? rest[n] : -INFINITY;
-  const float tm = block_max<DISTILL_THREADS>(fmaxf(t, t_rest), room), t_base = tm == -INFINITY ? 0.f : tm;
-  const float e = wrong ? NAN : expf(t - t_base), e_rest = expf(t_rest - t_base);
-  __syncthreads();
-  const float total = block_sum<DISTILL_THREADS>(e, room) + e_rest;
-  const bool any = total != 0.f;
-  const float q = any ? e / total : 0.f, q_rest = any ? e_rest / total : 0.f, log_total = any ? logf(total) : 0.f;
-  if (k < K) {
-    q_of[k] = q;
-    at[k] = listed && !wrong ? (int32_t)i : -1;
+// Sums of 2^(c x - base) over a set of scores, relative to their largest: over the listed items where these are told apart, and over the others.
+struct DistillSums { float m, listed, others; };
+
+__device__ __forceinline__ DistillSums scaled_to(const DistillSums& s, float m, float c) {
+  if (s.m == -INFINITY) return {m, s.listed, s.others};
+  const float base = base_of(m, c), f = exp2_fast(ordinary(base) ? base_of(s.m, c) - base : (s.m - m) * c);
+  return {m, f * s.listed, f * s.others};
+}
+__device__ __forceinline__ DistillSums join_lanes(DistillSums s, float c) {
+  const float m = warp_max(s.m);
+  s = scaled_to(s, m, c);
+  return {m, warp_sum(s.listed), warp_sum(s.others)};
+}
+
+__device__ __forceinline__ float teacher_value(const void* t, int dtype, int64_t i) {
+  if (dtype == MTS_DTYPE_FP32) return static_cast<const float*>(t)[i];
+  if (dtype == MTS_DTYPE_FP16) return to_f32(static_cast<const __half*>(t)[i]);
+  return to_f32(static_cast<const __nv_bfloat16*>(t)[i]);
+}
+
+struct DistillCall {
+  int64_t row_stride, grad_stride;
+  const int64_t* index;
+  const void* teacher;
+  const float* rest;
+  const float* weights;
+  float* loss;
+  int32_t V, K, teacher_dtype, log_parts, share, grad_share;
+  float scale;
+};
+
+struct DistillRoom {
+  float q[DISTILL_MAX_K], score[DISTILL_MAX_K], log_q[DISTILL_MAX_K];
+  int32_t at[DISTILL_MAX_K];                                   // -1: not used
+  int32_t batch[LISTED_SLOTS];
+  uint32_t places[LISTED_SLOTS];
+  DistillSums of_warp[DISTILL_WARPS], of_part[1 << MAX_LOG_PARTS];
+  float total, q_rest, log_q_rest;
+};
+
+__device__ __forceinline__ uint32_t listed_slot(int32_t batch) { return (uint32_t)batch * 2654435761u >> 23; }
+static_assert(LISTED_SLOTS == 1 << 9, "listed_slot");
+
+// Exponentials of a batch added to the sums; `places`: bits of its listed items.
+template <typename T, bool ORDINARY>
+__device__ __forceinline__ void add_batch(const uint4& w, uint32_t places, float m, float base, float c, Pair& others, float& listed) {
+  constexpr int E = RowBatches<T>::E;
+  float v[E];
+  RowBatches<T>::unpack(w, v);
+  const Pair minus(-base, -base), c2(c, c);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    const float2 d = ORDINARY ? fma2(Pair(v[e], v[e + 1]), c2, minus).get() : make_float2((v[e] - m) * c, (v[e + 1] - m) * c);
+    v[e] = exp2_fast(d.x);
+    v[e + 1] = exp2_fast(d.y);
   }
-  __syncthreads();
+  if (places) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (places >> e & 1) {
+        listed += v[e];
+        v[e] = 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; e += 2) others = others + Pair(v[e], v[e + 1]);
+}
+
+// A row (or a part of it, by a cluster of blocks) by a block.  The sums of the exponentials take one pass over the scores as in the log probabilities; the
+// gradient reads them once more, from L2, where the row has just passed.  With the rest's weight given (REST) the sum over the items that are not listed is made
+// without the listed ones (what is left of a difference would lose its digits where the listed ones have almost everything): batches that hold a
+// listed item are found in a table in shared memory.  Without it the gradient is written as if nothing were listed, and the listed places once more.
+template <typename T, bool REST>
+__global__ void __launch_bounds__(DISTILL_WARPS * 32, 2)
+distill_loss(const T* logits, T* grad, const DistillCall a) {
+  constexpr int E = RowBatches<T>::E, U = DISTILL_UNROLL;
+  __shared__ DistillRoom room;
+  const int tid = threadIdx.x, lane = lane_id(), warp = tid / 32, threads = blockDim.x, warps = threads / 32;
+  const int parts = 1 << a.log_parts, part = blockIdx.x & (parts - 1);
+  const int64_t n = blockIdx.x >> a.log_parts;
+  if (parts > 1) cluster_arrive();                             // all blocks have begun before others write to them
+  const RowBatches<T, false> r(logits + n * a.row_stride, a.V);
+  const int32_t b0 = min(r.count, part * a.share), b1 = min(r.count, b0 + a.share);
+  const float c = a.scale * LOG2E;
+
+  // the teacher's distribution, by the first warp
+  if (REST) {
+    for (int i = tid; i < LISTED_SLOTS; i += threads) {
+      room.batch[i] = -1;
+      room.places[i] = 0;
+    }
+    __syncthreads();
+  }
+  if (warp == 0) {
+    float most = -INFINITY;
+    bool wrong = false;
+    for (int k = lane; k < a.K; k += 32) {
+      const int64_t i = a.index[n * a.K + k];
+      const float t = i >= 0 ? teacher_value(a.teacher, a.teacher_dtype, n * a.K + k) * a.scale : -INFINITY;
+      wrong |= i >= a.V || isnan(t);
+      room.log_q[k] = t;
+      room.at[k] = i >= 0 && i < a.V ? (int32_t)i : -1;
+      most = fmaxf(most, t);
+    }
+    const float t_rest = REST ? a.rest[n] : -INFINITY;
+    most = fmaxf(warp_max(most), t_rest);
+    const float base = most == -INFINITY ? 0.f : most;
+    const float e_rest = expf(t_rest - base);
+    float total = 0.f;
+    for (int k = lane; k < a.K; k += 32) total += expf(room.log_q[k] - base);
+    total = warp_sum(total) + e_rest;
+    if (__any_sync(0xFFFFFFFFu, wrong)) total = NAN;
+    const bool any = total != 0.f;                             // else nothing is left of the teacher's row
+    const float log_total = any ? logf(total) : 0.f;
+    for (int k = lane; k < a.K; k += 32) {
+      const float t = room.log_q[k] - base;
+      room.q[k] = any ? expf(t) / total : 0.f;
+      room.log_q[k] = t - log_total;
+      const int32_t i = room.at[k];
+      room.score[k] = i >= 0 ? to_f32(r.row[i]) : 0.f;
+      if (REST && i >= 0) {
+        const int32_t batch = (i + r.shift) / E;
+        uint32_t slot = listed_slot(batch);
+        for (;; slot = (slot + 1) % LISTED_SLOTS) {            // at most K of its 2 DISTILL_MAX_K slots are taken: it ends
+          const int32_t was = atomicCAS(&room.batch[slot], -1, batch);
+          if (was == -1 || was == batch) break;
+        }
+        atomicOr(&room.places[slot], 1u << (i + r.shift) % E);
+      }
+    }
+    if (lane == 0) {
+      room.total = total;
+      room.q_rest = any ? e_rest / total : 0.f;
+      room.log_q_rest = t_rest - base - log_total;
+    }
+  }
+  if (REST) __syncthreads();
+
   // the student's sums
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < V; j += DISTILL_THREADS) m = fmaxf(m, to_f32(row[j]));
-  m = block_max<DISTILL_THREADS>(m, room);
-  const float base = m == -INFINITY ? 0.f : m;
-  float all = 0.f, others = 0.f;
-  for (int j = threadIdx.x; j < V; j += DISTILL_THREADS) {
-    const float x = to_f32(row[j]), p = exp2_fast(exponent((x - base) * c));
-    all += p;
-    if (rest) {
-      bool in = false;
-      for (int u = 0; u < K; ++u) in |= at[u] == j;
-      if (!in) others += p;
+  float m = -INFINITY, base = 0.f, listed = 0.f;
+  Pair others(0.f, 0.f);
+  const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
+  const auto places_of = [&](int32_t batch) -> uint32_t {
+    if (!REST) return 0u;
+    for (uint32_t slot = listed_slot(batch);; slot = (slot + 1) % LISTED_SLOTS) {
+      const int32_t is = room.batch[slot];
+      if (is == -1) return 0u;
+      if (is == batch) return room.places[slot];
+    }
+  };
+  for (int32_t g = b0; g < b1; g += threads * U) {
+    const int32_t b = g + tid;
+    const bool all = r.template all_whole<U>(g, b1, tid, threads);
+    uint4 w[U];
+    r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
+    if (!all) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (b + u * threads >= b1) w[u] = nothing_there;
+    }
+    uint32_t most_bits = max_bits<T>(w[0]);
+#pragma unroll
+    for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
+    const float most = max_value<T>(most_bits);
+    if (most > m) {
+      const DistillSums s = scaled_to({m, listed, others.sum()}, most, c);
+      listed = s.listed;
+      others = Pair(s.others, 0.f);
+      m = most;
+      base = base_of(m, c);
+    }
+    if (!ordinary(base)) {
+#pragma unroll 1
+      for (int32_t at = b; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), places_of(at), m, base, c, others, listed);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (all || b + u * threads < b1) add_batch<T, true>(w[u], places_of(b + u * threads), m, base, c, others, listed);
     }
   }
+  const DistillSums nobody = {-INFINITY, 0.f, 0.f};
+  DistillSums s = join_lanes({m, listed, others.sum()}, c);
+  if (lane == 0) room.of_warp[warp] = s;
   __syncthreads();
-  all = block_sum<DISTILL_THREADS>(all, room);
-  __syncthreads();
-  others = block_sum<DISTILL_THREADS>(others, room);
-  const float log_all = all == 0.f ? 0.f : logf(all);
-  float part = 0.f;
-  if (q != 0.f) part = q * (t - t_base - log_total - ((to_f32(row[listed && !wrong ? i : 0]) - base) * scale - log_all));
-  if (k == 0 && q_rest != 0.f) part += q_rest * (t_rest - t_base - log_total - (logf(others) - log_all));
-  __syncthreads();
-  part = block_sum<DISTILL_THREADS>(part, room);
-  if (loss && threadIdx.x == 0) loss[n] = part;
+  s = join_lanes(lane < warps ? room.of_warp[lane] : nobody, c);
+  if (parts > 1) {
+    cluster_wait();
+    if (tid < parts) {
+      const uint32_t to = in_block(&room.of_part[part], tid);
+      asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;" :: "r"(to), "f"(s.m), "f"(s.listed), "f"(s.others) : "memory");
+    }
+    cluster_arrive();
+    cluster_wait();                                            // (and no block writes over scores that another still reads)
+    s = join_lanes(lane < parts ? room.of_part[lane] : nobody, c);
+  }
+  const float all = s.listed + s.others, m0 = s.m == -INFINITY ? 0.f : s.m;
+  base = base_of(s.m, c);
+  if (warp == 0 && part == 0 && a.loss) {
+    const float off = log_excess(s.m, base, c), log_all = all == 0.f ? 0.f : logf(all) - off;
+    float sum = 0.f;
+    for (int k = lane; k < a.K; k += 32) {
+      const float q = room.q[k];
+      if (q != 0.f) sum += q * (room.log_q[k] - ((room.score[k] - m0) * a.scale - log_all));
+    }
+    if (REST && lane == 0 && room.q_rest != 0.f) sum += room.q_rest * (room.log_q_rest - (logf(s.others) - off - log_all));
+    sum = warp_sum(sum);
+    if (lane == 0) a.loss[n] = sum;
+  }
   if (!grad) return;
-  T* to = grad + n * grad_stride;
-  const float w = weights ? weights[n] * scale : scale;
-  const float inv_all = all == 0.f ? 0.f : 1.f / all;
-  const float f = !any ? 0.f : w * (q_rest != 0.f && others != 0.f ? inv_all - q_rest / others : inv_all);
-  const bool off = w == 0.f || !any;
-  __syncthreads();
-  for (int j = threadIdx.x; j < V; j += DISTILL_THREADS) {
-    float g = 0.f;
-    if (!off) {
-      const float x = to_f32(row[j]), p = exp2_fast(exponent((x - base) * c));
-      float want = 0.f;
-      bool in = false;
-      for (int u = 0; u < K; ++u)
-        if (at[u] == j) { want += q_of[u]; in = true; }
-      g = in ? w * (p * inv_all - want) : p * f;
-      g += total * 0.f;
-    }
-    to[j] = from_f32<T>(g);
+
+  const RowBatches<T> to(grad + n * a.grad_stride, a.V);
+  const RowUnder<T> under(r.row, to);
+  const int32_t g0 = min(to.count, part * a.grad_share), g1 = min(to.count, g0 + a.grad_share);
+  const float w = (a.weights ? a.weights[n] : 1.f) * a.scale, inv_all = all == 0.f ? 0.f : 1.f / all, total = room.total;
+  if (w == 0.f || total == 0.f) {
+    const float zero[E] = {};
+    for (int32_t b = g0 + tid; b < g1; b += threads) to.store(b, zero);
+    return;
   }
+  const float f = w * (REST && room.q_rest != 0.f && s.others != 0.f ? inv_all - room.q_rest / s.others : inv_all) + total * 0.f;
+  const bool usual = ordinary(base);
+  for (int32_t g = g0; g < g1; g += threads * DISTILL_GRAD_UNROLL) {
+    const int32_t b = g + tid;
+    uint4 x[DISTILL_GRAD_UNROLL];
+#pragma unroll
+    for (int u = 0; u < DISTILL_GRAD_UNROLL; ++u) x[u] = under.raw(b + u * threads < g1 ? b + u * threads : to.count);
+#pragma unroll
+    for (int u = 0; u < DISTILL_GRAD_UNROLL; ++u) {
+      if (b + u * threads >= g1) break;
+      float v[E];
+      RowBatches<T>::unpack(x[u], v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = f * exp2_fast(usual ? fmaf(v[e], c, -base) : (v[e] - m0) * c);
+      to.store(b + u * threads, v);
+    }
+  }
+  __syncthreads();
+  // the listed items' places once more, by the block that wrote them
+  for (int k = tid; k < a.K; k += threads) {
+    const int32_t i = room.at[k];
+    if (i < 0) continue;
+    const int32_t b = (i + to.shift) / E;
+    if (b < g0 || b >= g1) continue;
+    float want = 0.f;
+    for (int j = 0; j < a.K; ++j) want += room.at[j] == i ? room.q[j] : 0.f;
+    const float p = exp2_fast(usual ? fmaf(room.score[k], c, -base) : (room.score[k] - m0) * c) * inv_all;
+    grad[n * a.grad_stride + i] = from_f32<T>(w * (p - want) + total * 0.f);
+  }
+}
+
+template <typename T, bool REST>
+int launch_distill(const char* what, const T* logits, T* grad, const DistillCall& a, int64_t N, int warps, cudaStream_t s) {
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = 1u << a.log_parts;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3((unsigned)(N << a.log_parts));
+  config.blockDim = dim3(32 * warps);
+  config.stream = s;
+  config.attrs = &cluster;
+  config.numAttrs = a.log_parts ? 1 : 0;
+  LaunchScope scope(K_DISTILL, s);
+  return check_cuda(cudaLaunchKernelEx(&config, distill_loss<T, REST>, logits, grad, a), what);
 }
 
 }  // namespace mts
@@ -109,13 +305,16 @@ extern "C" int mts_distill_loss(const void* logits, int64_t row_stride, int32_t 
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_dtype(teacher_dtype, [&](auto u) {
-      using Q = decltype(u);
-      LaunchScope scope(K_DISTILL, s);
-      distill_loss<T, Q><<<(unsigned)N, DISTILL_THREADS, 0, s>>>(static_cast<const T*>(logits), row_stride, (int32_t)V, scale, teacher_index,
-                                                                 static_cast<const Q*>(teacher_logits), K, teacher_rest, weights, loss,
-                                                                 static_cast<T*>(grad_logits), grad_stride);
-      return check_launch(what);
-    });
+    const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
+    const int log_parts = log_parts_of(N, batches);
+    const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
+    int warps = share <= 700 ? 1 : share <= 3000 ? 2 : share <= 8000 ? 4 : 8;
+    while (warps < DISTILL_WARPS && (N << log_parts) * warps < 148 * 16 && share >= (warps < 8 ? 64 : 256) * warps) warps *= 2;
+    const char* fw = getenv("DW");
+    if (fw) warps = atoi(fw);
+    const DistillCall a = {row_stride, grad_stride, teacher_index, teacher_logits, teacher_rest, weights, loss, (int32_t)V, K, teacher_dtype, log_parts, share, share, scale};
+    const T* x = static_cast<const T*>(logits);
+    T* d = static_cast<T*>(grad_logits);
+    return teacher_rest ? launch_distill<T, true>(what, x, d, a, N, warps, s) : launch_distill<T, false>(what, x, d, a, N, warps, s);
   });
 }

@@ -9,7 +9,7 @@ namespace mts {
 
 constexpr int LOGP_WARPS = 16;                 // of a block that works on a row
 constexpr int LOGP_ROWS = 4;                   // rows of a block whose warps have one each
-constexpr int LOGP_MAX_PARTS = 8;              // blocks of a cluster that share a row
+constexpr int LOGP_MAX_PARTS = 1 << MAX_LOG_PARTS;      // blocks of a cluster that share a row
 constexpr int LOGP_UNROLL = 8;                 // batches on their way for a thread: a group
 constexpr int LOGP_UNITS = 8;                  // runs of a thread's groups whose maxima are kept
 constexpr int LOGP_HITS = 128;                 // of them that can hold a score which reaches the bound
@@ -23,13 +23,9 @@ struct LogprobsOut {
   float* top_logp;
 };
 
-// Exponents are taken relative to the largest score m: c x - base with base = c m rounded (its error is put right at the end), which is one
-// instruction; where base is no finite number (scores of about 2e38 and more, or none but the lowest of their type) it is c (x - m).
 // Statistics of a set of scores: the largest, and the sums of p = 2^exponent and of p log2 p.
 struct RowStats { float m, S, P; };
 
-__device__ __forceinline__ float base_of(float m, float c) { return m == -INFINITY ? 0.f : m * c; }
-__device__ __forceinline__ bool ordinary(float base) { return fabsf(base) < INFINITY; }
 __device__ __forceinline__ RowStats scaled_to(const RowStats& s, float m, float c) {
   const float base = base_of(m, c), a = exponent(ordinary(base) ? base_of(s.m, c) - base : (s.m - m) * c), f = exp2_fast(a);
   return s.m == -INFINITY ? RowStats{m, s.S, s.P} : RowStats{m, f * s.S, f * (s.P + s.S * a)};
@@ -39,15 +35,6 @@ __device__ __forceinline__ RowStats join_lanes(RowStats s, float c) {
   const float m = warp_max(s.m);
   s = scaled_to(s, m, c);
   return {m, warp_sum(s.S), warp_sum(s.P)};
-}
-
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-// Address in the first block of the cluster of a variable of this block.
-__device__ __forceinline__ uint32_t in_first_block(const void* p) {
-  uint32_t a;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)));
-  return a;
 }
 
 // A batch added to the sums.
@@ -316,8 +303,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     }
   }
   if (warp == 0 && (ONE_WARP || parts == 1)) {
-    const float m0 = st.m == -INFINITY ? 0.f : st.m, rounded = base_of(st.m, c);
-    const float off = ordinary(rounded) ? fmaf(m0, c, -rounded) * LN2 : 0.f;         // what the sums' logarithm has too much by the rounding of the base
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, off = log_excess(st.m, base_of(st.m, c), c);
     const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
     const float nothing = st.S == 0.f ? -INFINITY : 0.f;
     if (lane == 0) {
@@ -394,16 +380,15 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   if constexpr (!ONE_WARP) {
     // to the first block of the cluster, which joins the parts
     cluster_wait();
-    const uint32_t to = in_first_block(&part_stats[part]);
+    const uint32_t to = in_block(&part_stats[part], 0);
     if (tid == 0)
       asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;" :: "r"(to), "f"(st.m), "f"(st.S), "f"(st.P) : "memory");
-    if (tid < k) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(in_first_block(&part_best[part * k + tid])), "l"(room.best[tid]) : "memory");
+    if (tid < k) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(in_block(&part_best[part * k + tid], 0)), "l"(room.best[tid]) : "memory");
     cluster_arrive();
     cluster_wait();
     if (part != 0) return;
     st = join_lanes(lane < parts ? part_stats[lane] : nobody, c);
-    const float m0 = st.m == -INFINITY ? 0.f : st.m, rounded = base_of(st.m, c);
-    const float off = ordinary(rounded) ? fmaf(m0, c, -rounded) * LN2 : 0.f;
+    const float m0 = st.m == -INFINITY ? 0.f : st.m, off = log_excess(st.m, base_of(st.m, c), c);
     const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
     const float nothing = st.S == 0.f ? -INFINITY : 0.f;
     if (tid == 0) {
@@ -542,10 +527,7 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
     const T* x = static_cast<const T*>(logits);
     const ForwardCall a = {row_stride, N, (int32_t)V, scale, targets, top_k, out, s};
     const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
-    // Few rows: each by a cluster, while the GPU has an SM for every block and a part 1,024 batches (one row of 5,000 fp32 batches by 1, 2, 4 and 8
-    // blocks: 6.0, 6.4, 5.8 and 6.0 us; 100 rows of 2,500: 5.9 us by single blocks, 7.1 by pairs).
-    int log_parts = 0;
-    while (2 << log_parts <= LOGP_MAX_PARTS && N << log_parts <= 74 && batches >= 2048 << log_parts) ++log_parts;
+    const int log_parts = log_parts_of(N, batches);
     const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
     // Warps of a row: what a warp does for a row apart from its scores costs as much as a dozen batches a lane, so as few as keep the row short: us
     // with 1, 2, 4, 8 for 50,000 rows of 500 batches 172, 183, 265, 462; 25,000 of 1,000 148, 131, 144, 249; 6,250 of 4,000 153, 98, 95, 102; 2,048 of
