@@ -3,7 +3,6 @@
 //   q = softmax of scale teacher_k over the listed items (and exp(rest) for all others together),  p = softmax(scale x)
 //   loss = sum_k q_k (log q_k - log p_{i_k}) + q_rest (log q_rest - log p_rest),   p_rest = what p gives to the items not listed
 //   dx_v = weight scale (p_v - q_v) for a listed item, weight scale p_v (1 - q_rest / p_rest) for another
-#include <stdlib.h>
 #include "rows.cuh"
 
 namespace mts {
@@ -11,7 +10,7 @@ namespace mts {
 constexpr int DISTILL_WARPS = 16;
 constexpr int DISTILL_MAX_K = MTS_DISTILL_MAX_K;
 constexpr int DISTILL_UNROLL = 8, DISTILL_GRAD_UNROLL = 4;     // batches on their way for a thread
-constexpr int LISTED_SLOTS = 2 * DISTILL_MAX_K;                // of the table of batches that hold a listed item
+constexpr int LISTED_BYTES = 32768;                            // of the bits that say which batches of a part hold a listed item
 
 // Sums of 2^(c x - base) over a set of scores, relative to their largest: over the listed items where these are told apart, and over the others.
 struct DistillSums { float m, listed, others; };
@@ -40,27 +39,21 @@ struct DistillCall {
   const float* rest;
   const float* weights;
   float* loss;
-  int32_t V, K, teacher_dtype, log_parts, share, grad_share;
+  int32_t V, K, teacher_dtype, log_parts, share;
   float scale;
 };
 
 struct DistillRoom {
   float q[DISTILL_MAX_K], score[DISTILL_MAX_K], log_q[DISTILL_MAX_K];
   int32_t at[DISTILL_MAX_K];                                   // -1: not used
-  int32_t batch[LISTED_SLOTS];
-  uint32_t places[LISTED_SLOTS];
   DistillSums of_warp[DISTILL_WARPS], of_part[1 << MAX_LOG_PARTS];
   float total, q_rest, log_q_rest;
 };
 
-__device__ __forceinline__ uint32_t listed_slot(int32_t batch) { return (uint32_t)batch * 2654435761u >> 23; }
-static_assert(LISTED_SLOTS == 1 << 9, "listed_slot");
-
-// Exponentials of a batch added to the sums; `places`: bits of its listed items.
+// Exponentials of a batch.
 template <typename T, bool ORDINARY>
-__device__ __forceinline__ void add_batch(const uint4& w, uint32_t places, float m, float base, float c, Pair& others, float& listed) {
+__device__ __forceinline__ void exponentials(const uint4& w, float m, float base, float c, float (&v)[RowBatches<T>::E]) {
   constexpr int E = RowBatches<T>::E;
-  float v[E];
   RowBatches<T>::unpack(w, v);
   const Pair minus(-base, -base), c2(c, c);
 #pragma unroll
@@ -69,28 +62,26 @@ __device__ __forceinline__ void add_batch(const uint4& w, uint32_t places, float
     v[e] = exp2_fast(d.x);
     v[e + 1] = exp2_fast(d.y);
   }
-  if (places) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (places >> e & 1) {
-        listed += v[e];
-        v[e] = 0.f;
-      }
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < E; e += 2) others = others + Pair(v[e], v[e + 1]);
+}
+template <typename T>
+__device__ __forceinline__ Pair sum_of(const float (&v)[RowBatches<T>::E]) {
+  Pair s = Pair(v[0], v[1]) + Pair(v[2], v[3]);
+  if constexpr (RowBatches<T>::E == 8) s = s + (Pair(v[4], v[5]) + Pair(v[6], v[7]));
+  return s;
 }
 
 // A row (or a part of it, by a cluster of blocks) by a block.  The sums of the exponentials take one pass over the scores as in the log probabilities; the
-// gradient reads them once more, from L2, where the row has just passed.  With the rest's weight given (REST) the sum over the items that are not listed is made
-// without the listed ones (what is left of a difference would lose its digits where the listed ones have almost everything): batches that hold a
-// listed item are found in a table in shared memory.  Without it the gradient is written as if nothing were listed, and the listed places once more.
+// gradient reads them once more, from L2, where the row has just passed.
+// With the rest's weight given (REST) the sum over the items that are not listed is made without the listed ones: what is left of a difference would lose its
+// digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
+// leaves these out, and they are added afterwards item by item.
+// The gradient is written as if nothing were listed, and the listed places once more.
 template <typename T, bool REST>
 __global__ void __launch_bounds__(DISTILL_WARPS * 32, 2)
 distill_loss(const T* logits, T* grad, const DistillCall a) {
   constexpr int E = RowBatches<T>::E, U = DISTILL_UNROLL;
   __shared__ DistillRoom room;
+  extern __shared__ __align__(16) uint8_t left_out[];
   const int tid = threadIdx.x, lane = lane_id(), warp = tid / 32, threads = blockDim.x, warps = threads / 32;
   const int parts = 1 << a.log_parts, part = blockIdx.x & (parts - 1);
   const int64_t n = blockIdx.x >> a.log_parts;
@@ -99,14 +90,20 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   const int32_t b0 = min(r.count, part * a.share), b1 = min(r.count, b0 + a.share);
   const float c = a.scale * LOG2E;
 
-  // the teacher's distribution, by the first warp
+  // the bits of the batches that are left out: byte of a thread's group, bit of the batch in it
   if (REST) {
-    for (int i = tid; i < LISTED_SLOTS; i += threads) {
-      room.batch[i] = -1;
-      room.places[i] = 0;
-    }
+    const int bytes = min(LISTED_BYTES, (b1 - b0 + threads * U - 1) / (threads * U) * threads);
+    for (int i = tid; i < bytes / 4; i += threads) reinterpret_cast<uint32_t*>(left_out)[i] = 0;
     __syncthreads();
+    for (int k = tid; k < a.K; k += threads) {
+      const int64_t i = a.index[n * a.K + k];
+      if (i < 0 || i >= a.V) continue;
+      const int32_t b = (int32_t)(i + r.shift) / E - b0, group = b / (threads * U), in = b - group * threads * U;
+      const int64_t byte = (int64_t)group * threads + in % threads;
+      if (b >= 0 && b < b1 - b0 && byte < LISTED_BYTES) atomicOr(reinterpret_cast<uint32_t*>(left_out) + byte / 4, 1u << (in / threads + byte % 4 * 8));
+    }
   }
+  // the teacher's distribution, by the first warp
   if (warp == 0) {
     float most = -INFINITY;
     bool wrong = false;
@@ -134,15 +131,6 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       room.log_q[k] = t - log_total;
       const int32_t i = room.at[k];
       room.score[k] = i >= 0 ? to_f32(r.row[i]) : 0.f;
-      if (REST && i >= 0) {
-        const int32_t batch = (i + r.shift) / E;
-        uint32_t slot = listed_slot(batch);
-        for (;; slot = (slot + 1) % LISTED_SLOTS) {            // at most K of its 2 DISTILL_MAX_K slots are taken: it ends
-          const int32_t was = atomicCAS(&room.batch[slot], -1, batch);
-          if (was == -1 || was == batch) break;
-        }
-        atomicOr(&room.places[slot], 1u << (i + r.shift) % E);
-      }
     }
     if (lane == 0) {
       room.total = total;
@@ -156,14 +144,20 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   float m = -INFINITY, base = 0.f, listed = 0.f;
   Pair others(0.f, 0.f);
   const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
-  const auto places_of = [&](int32_t batch) -> uint32_t {
-    if (!REST) return 0u;
-    for (uint32_t slot = listed_slot(batch);; slot = (slot + 1) % LISTED_SLOTS) {
-      const int32_t is = room.batch[slot];
-      if (is == -1) return 0u;
-      if (is == batch) return room.places[slot];
-    }
+  // whether batch b holds a listed item, where the bits do not reach
+  const auto holds_listed = [&](int32_t b) {
+    for (int k = 0; k < a.K; ++k)
+      if (room.at[k] >= 0 && (room.at[k] + r.shift) / E == b) return true;
+    return false;
   };
+  const auto rescale = [&](float most) {
+    const DistillSums s = scaled_to({m, listed, others.sum()}, most, c);
+    listed = s.listed;
+    others = Pair(s.others, 0.f);
+    m = most;
+    base = base_of(m, c);
+  };
+  int32_t byte = tid;
   for (int32_t g = b0; g < b1; g += threads * U) {
     const int32_t b = g + tid;
     const bool all = r.template all_whole<U>(g, b1, tid, threads);
@@ -178,20 +172,61 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
 #pragma unroll
     for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
     const float most = max_value<T>(most_bits);
-    if (most > m) {
-      const DistillSums s = scaled_to({m, listed, others.sum()}, most, c);
-      listed = s.listed;
-      others = Pair(s.others, 0.f);
-      m = most;
-      base = base_of(m, c);
+    if (most > m) rescale(most);
+    unsigned out = 0;
+    if (REST) {
+      if (byte < LISTED_BYTES) {
+        out = left_out[byte];
+      } else {
+        for (int u = 0; u < U; ++u) out |= holds_listed(b + u * threads) << u;
+      }
+      byte += threads;
     }
     if (!ordinary(base)) {
 #pragma unroll 1
-      for (int32_t at = b; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), places_of(at), m, base, c, others, listed);
+      for (int u = 0; u < U; ++u) {
+        if (b + u * threads >= b1 || out >> u & 1) continue;
+        float v[E];
+        exponentials<T, false>(r.raw(b + u * threads), m, base, c, v);
+        others = others + sum_of<T>(v);
+      }
     } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (all || b + u * threads < b1) add_batch<T, true>(w[u], places_of(b + u * threads), m, base, c, others, listed);
+      for (int u = 0; u < U; ++u) {
+        if (!all && b + u * threads >= b1) continue;
+        float v[E];
+        exponentials<T, true>(w[u], m, base, c, v);
+        const Pair s = sum_of<T>(v);
+        if (!REST || !(out >> u & 1)) others = others + s;
+      }
+    }
+  }
+  if (REST) {
+    // the batches left out, each by the thread of the first place in it
+    for (int k = tid; k < a.K; k += threads) {
+      const int32_t b = (room.at[k] + r.shift) / E;
+      if (room.at[k] < 0 || b < b0 || b >= b1) continue;
+      unsigned places = 0;
+      bool first = true;
+      for (int j = 0; j < a.K; ++j) {
+        const int32_t i = room.at[j] + r.shift;
+        if (room.at[j] >= 0 && i / E == b) {
+          places |= 1u << i % E;
+          first &= j >= k;
+        }
+      }
+      if (!first) continue;
+      const uint4 batch = r.raw(b);
+      const float most = max_value<T>(max_bits<T>(batch));
+      if (most > m) rescale(most);
+      float v[E];
+      if (ordinary(base)) exponentials<T, true>(batch, m, base, c, v);
+      else exponentials<T, false>(batch, m, base, c, v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (places >> e & 1) listed += v[e];
+        else others = others + Pair(v[e], 0.f);
+      }
     }
   }
   const DistillSums nobody = {-INFINITY, 0.f, 0.f};
@@ -226,7 +261,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
 
   const RowBatches<T> to(grad + n * a.grad_stride, a.V);
   const RowUnder<T> under(r.row, to);
-  const int32_t g0 = min(to.count, part * a.grad_share), g1 = min(to.count, g0 + a.grad_share);
+  const int32_t g0 = min(to.count, part * a.share), g1 = min(to.count, g0 + a.share);
   const float w = (a.weights ? a.weights[n] : 1.f) * a.scale, inv_all = all == 0.f ? 0.f : 1.f / all, total = room.total;
   if (w == 0.f || total == 0.f) {
     const float zero[E] = {};
@@ -235,19 +270,49 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   }
   const float f = w * (REST && room.q_rest != 0.f && s.others != 0.f ? inv_all - room.q_rest / s.others : inv_all) + total * 0.f;
   const bool usual = ordinary(base);
-  for (int32_t g = g0; g < g1; g += threads * DISTILL_GRAD_UNROLL) {
+  const auto gradient = [&](const uint4& x, float (&v)[E]) {
+    RowBatches<T>::unpack(x, v);
+    const Pair minus(-base, -base), c2(c, c), f2(f, f);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 d = usual ? fma2(Pair(v[e], v[e + 1]), c2, minus).get() : make_float2((v[e] - m0) * c, (v[e + 1] - m0) * c);
+      const float2 g = (Pair(exp2_fast(d.x), exp2_fast(d.y)) * f2).get();
+      v[e] = g.x;
+      v[e + 1] = g.y;
+    }
+  };
+  constexpr int GU = DISTILL_GRAD_UNROLL;
+  int32_t in0, in1;
+  under.inner(&in0, &in1);
+  in1 = min(in1, g1);
+  for (int32_t g = g0; g < g1; g += threads * GU) {
     const int32_t b = g + tid;
-    uint4 x[DISTILL_GRAD_UNROLL];
+    float v[E];
+    if (usual && g >= in0 && g + threads * GU <= in1) {        // nothing to test
+      const T* from = r.row + (to.first(b) - under.ahead);
+      T* at = grad + n * a.grad_stride + to.first(b);
+      uint4 x[GU];
 #pragma unroll
-    for (int u = 0; u < DISTILL_GRAD_UNROLL; ++u) x[u] = under.raw(b + u * threads < g1 ? b + u * threads : to.count);
+      for (int u = 0; u < GU; ++u, from += threads * E) x[u] = under.inside(from);
 #pragma unroll
-    for (int u = 0; u < DISTILL_GRAD_UNROLL; ++u) {
-      if (b + u * threads >= g1) break;
-      float v[E];
-      RowBatches<T>::unpack(x[u], v);
+      for (int u = 0; u < GU; ++u, at += threads * E) {
+        RowBatches<T>::unpack(x[u], v);
+        const Pair minus(-base, -base), c2(c, c), f2(f, f);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = f * exp2_fast(usual ? fmaf(v[e], c, -base) : (v[e] - m0) * c);
-      to.store(b + u * threads, v);
+        for (int e = 0; e < E; e += 2) {
+          const float2 d = fma2(Pair(v[e], v[e + 1]), c2, minus).get();
+          const float2 y = (Pair(exp2_fast(d.x), exp2_fast(d.y)) * f2).get();
+          v[e] = y.x;
+          v[e + 1] = y.y;
+        }
+        RowBatches<T>::store16(at, v);
+      }
+    } else {
+#pragma unroll 1
+      for (int32_t q = b; q < min(g1, g + threads * GU); q += threads) {
+        gradient(under.raw(q), v);
+        to.store(q, v);
+      }
     }
   }
   __syncthreads();
@@ -273,6 +338,8 @@ int launch_distill(const char* what, const T* logits, T* grad, const DistillCall
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3((unsigned)(N << a.log_parts));
   config.blockDim = dim3(32 * warps);
+  const int64_t groups = ceil_div(a.share, 32 * warps * DISTILL_UNROLL);
+  config.dynamicSmemBytes = !REST ? 0 : (size_t)(groups * 32 * warps < LISTED_BYTES ? groups * 32 * warps : LISTED_BYTES);
   config.stream = s;
   config.attrs = &cluster;
   config.numAttrs = a.log_parts ? 1 : 0;
@@ -310,9 +377,7 @@ extern "C" int mts_distill_loss(const void* logits, int64_t row_stride, int32_t 
     const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
     int warps = share <= 700 ? 1 : share <= 3000 ? 2 : share <= 8000 ? 4 : 8;
     while (warps < DISTILL_WARPS && (N << log_parts) * warps < 148 * 16 && share >= (warps < 8 ? 64 : 256) * warps) warps *= 2;
-    const char* fw = getenv("DW");
-    if (fw) warps = atoi(fw);
-    const DistillCall a = {row_stride, grad_stride, teacher_index, teacher_logits, teacher_rest, weights, loss, (int32_t)V, K, teacher_dtype, log_parts, share, share, scale};
+    const DistillCall a = {row_stride, grad_stride, teacher_index, teacher_logits, teacher_rest, weights, loss, (int32_t)V, K, teacher_dtype, log_parts, share, scale};
     const T* x = static_cast<const T*>(logits);
     T* d = static_cast<T*>(grad_logits);
     return teacher_rest ? launch_distill<T, true>(what, x, d, a, N, warps, s) : launch_distill<T, false>(what, x, d, a, N, warps, s);

@@ -89,13 +89,17 @@ struct RowBatches {
     }
     return w;
   }
+  // A whole batch, not to be read again soon.
+  static __device__ __forceinline__ void store16(T* to, const float (&v)[E]) {
+    if constexpr (sizeof(T) == 4) __stcs(reinterpret_cast<float4*>(to), make_float4(v[0], v[1], v[2], v[3]));
+    else __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])));
+  }
   // Writes the batch's elements that lie in the row.
   __device__ __forceinline__ void store(int32_t b, const float (&v)[E]) const {
     const int32_t i = first(b);
     T* const to = const_cast<T*>(row) + i;
     if (i >= 0 && i <= V - E) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-      else *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+      store16(to, v);
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
@@ -148,14 +152,21 @@ struct RowUnder {
     const int bits = ahead * (int)sizeof(T) * 8 % 32;
     return make_uint4(__funnelshift_r(s[0], s[1], bits), __funnelshift_r(s[1], s[2], bits), __funnelshift_r(s[2], s[3], bits), __funnelshift_r(s[3], s[4], bits));
   }
+  // Batches [*from, *to) are whole and their accesses within the row.
+  __device__ __forceinline__ void inner(int32_t* from, int32_t* to) const {
+    *from = (r.shift + ahead + E - 1) / E;
+    *to = (int32_t)(((int64_t)r.V - (ahead ? 2 * E : E) + ahead + r.shift) / E) + 1;
+    if (r.V < (ahead ? 2 * E : E)) *to = *from;
+  }
+  __device__ __forceinline__ uint4 inside(const T* p) const {               // p: the batch's first element's access
+    const uint4* const q = reinterpret_cast<const uint4*>(p);
+    const uint4 lo = __ldcs(q);
+    return ahead ? shifted(lo, __ldcs(q + 1)) : lo;
+  }
   // The batch as it is stored, -infinity outside the row.  Not through the read-only path: the gradient may take the scores' place.
   __device__ __forceinline__ uint4 raw(int32_t b) const {
     const int32_t i = r.first(b);
-    if (within(b)) {
-      const uint4* p = reinterpret_cast<const uint4*>(row + (i - ahead));
-      const uint4 lo = p[0];
-      return ahead ? shifted(lo, p[1]) : lo;
-    }
+    if (within(b)) return inside(row + (i - ahead));
     uint4 w = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
     if (i > -E && i < r.V) {
       T* const e = reinterpret_cast<T*>(&w);
@@ -214,6 +225,11 @@ struct Pair {
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) {
   Pair r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+  return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
   return r;
 }
 __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
