@@ -17,14 +17,15 @@ constexpr int NORM_CHUNKS = 4;                           // chunks that a warp h
 constexpr int NORM_WARPS = MTS_RMS_NORM_MAX_D / (NORM_CHUNK * NORM_CHUNKS);
 
 // A row's part that a warp holds: I chunks of 256 columns, `step` chunks apart.  VECTOR: a lane has eight neighbouring columns (rows on 16-byte
-// boundaries); else every 32nd column, which any row can be read by in whole sectors.  Columns behind the row's end hold 0.
-template <typename T, bool VECTOR, int I>
+// boundaries); else every 32nd column, which any row can be read by in whole sectors.  Columns behind the row's end hold 0.  LANES: lanes of a row,
+// fewer than 32 where rows are short and on boundaries.
+template <typename T, bool VECTOR, int I, int LANES = 32>
 struct Tile {
   static constexpr int Q = VECTOR ? (int)sizeof(T) / 2 : 1;
   uint4 q[VECTOR ? I : 1][Q];
   T s[VECTOR ? 1 : I][8];
 
-  static __device__ __forceinline__ int column(int chunk, int e) { return chunk * NORM_CHUNK + (VECTOR ? lane_id() * 8 + e : lane_id() + 32 * e); }
+  static __device__ __forceinline__ int column(int chunk, int e) { return chunk * NORM_CHUNK + (VECTOR ? lane_id() % LANES * 8 + e : lane_id() + 32 * e); }
   __device__ __forceinline__ void load(const T* row, int D, int chunk, int step) {
 #pragma unroll
     for (int i = 0; i < I; ++i, chunk += step) {
@@ -71,9 +72,9 @@ struct Tile {
 };
 
 // Eight values of a lane, written to their columns of a row.
-template <typename T, bool VECTOR>
+template <typename T, bool VECTOR, int LANES>
 __device__ __forceinline__ void store8(T* row, int D, int chunk, const float (&v)[8]) {
-  using Columns = Tile<T, VECTOR, 1>;
+  using Columns = Tile<T, VECTOR, 1, LANES>;
   if constexpr (VECTOR) {
     T* const to = row + Columns::column(chunk, 0);
     if (Columns::column(chunk, 8) <= D) {
@@ -97,9 +98,9 @@ struct Weight {
 };
 
 // A lane's eight weights, 0 behind the row's end.
-template <bool VECTOR>
+template <bool VECTOR, int LANES>
 __device__ __forceinline__ void weights8(const Weight& w, int D, int chunk, float (&v)[8]) {
-  const int at = Tile<float, VECTOR, 1>::column(chunk, 0);
+  const int at = Tile<float, VECTOR, 1, LANES>::column(chunk, 0);
   if (VECTOR && w.aligned && at + 8 <= D) {
     if (w.dtype == MTS_DTYPE_FP32) {
       const float4 a = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w.w) + at)), b = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w.w) + at) + 1);
@@ -118,26 +119,35 @@ __device__ __forceinline__ void weights8(const Weight& w, int D, int chunk, floa
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int j = Tile<float, VECTOR, 1>::column(chunk, e);
+    const int j = Tile<float, VECTOR, 1, LANES>::column(chunk, e);
     v[e] = 0.f;
     if (j < D) v[e] = w.dtype == MTS_DTYPE_FP32 ? __ldg(static_cast<const float*>(w.w) + j)
                     : w.dtype == MTS_DTYPE_FP16 ? to_f32(__ldg(static_cast<const __half*>(w.w) + j)) : to_f32(__ldg(static_cast<const __nv_bfloat16*>(w.w) + j));
   }
 }
 
-// Sum and maximum over the warps of a row, in a fixed order; `room`: shared, of this use alone.
+// Sum and maximum over the lanes, or the warps, of a row, in a fixed order; `room`: shared, of this row and use alone.
+__device__ __forceinline__ void row_barrier(int warps) { __barrier_sync_count(threadIdx.y + 1, 32 * warps); }
+template <int LANES>
 __device__ __forceinline__ float row_sum(float x, float* room, int warp, int warps) {
-  x = warp_sum(x);
-  if (warps == 1) return x;
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  if (LANES < 32 || warps == 1) return x;
   if (lane_id() == 0) room[warp] = x;
-  __syncthreads();
+  row_barrier(warps);
   return warp_sum(lane_id() < warps ? room[lane_id()] : 0.f);
 }
+template <int LANES>
 __device__ __forceinline__ float row_max(float x, float* room, int warp, int warps) {
-  x = warp_max(x);
-  if (warps == 1) return x;
+  if constexpr (LANES == 32) {
+    x = warp_max(x);
+  } else {
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  }
+  if (LANES < 32 || warps == 1) return x;
   if (lane_id() == 0) room[warp] = x;
-  __syncthreads();
+  row_barrier(warps);
   return warp_max(lane_id() < warps ? room[lane_id()] : 0.f);
 }
 
@@ -157,9 +167,9 @@ struct NormForward {
 };
 
 // Eight codes of a lane.
-template <bool VECTOR>
+template <bool VECTOR, int LANES>
 __device__ __forceinline__ void store_codes(uint8_t* row, int D, int chunk, const float (&y)[8]) {
-  using Columns = Tile<float, VECTOR, 1>;
+  using Columns = Tile<float, VECTOR, 1, LANES>;
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k)
@@ -175,136 +185,174 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int D, int chunk, cons
     if (Columns::column(chunk, e) < D) row[Columns::column(chunk, e)] = (uint8_t)(w[e / 4] >> 8 * (e % 4));
 }
 
-// A row by blockDim.x / 32 warps, up to 1,024 columns by each, and blockDim.y rows a block (of one warp each); everything of a row is in registers
-// between its one reading and its one writing.
-template <typename T, bool VECTOR, int I, int THREADS, bool CODES>
-__global__ void __launch_bounds__(THREADS)
+// A row by blockDim.x / 32 warps, up to 1,024 columns by each, or R rows by a warp (times 32 / LANES), so that a warp has four chunks on their way
+// whatever the width; blockDim.y such sets a block.  Everything of a row is in registers between its one reading and its one writing.
+template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS, bool CODES>
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VECTOR && sizeof(T) == 2) || R * I <= 2 ? 4 : 2)
 rms_norm_forward(const NormForward<T> a) {
+  using Columns = Tile<T, VECTOR, 1, LANES>;
   __shared__ float room[2][NORM_WARPS];
   const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
-  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  if (row >= a.N) return;                                // a warp as a whole; blocks of several warps a row have one row
-  float v[I][8];
+  const int64_t first = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * (R * (32 / LANES)) + lane_id() / LANES;
+  if (first - lane_id() / LANES >= a.N) return;          // a warp as a whole; blocks of several warps a row have one row
+  float v[R][I][8], c[R];
+  int64_t row[R];
+  int D[R];                                              // no columns where there is no row
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    row[r] = first + r * (32 / LANES);
+    D[r] = row[r] < a.N ? a.D : 0;
+    if (row[r] >= a.N) row[r] = a.N - 1;
+  }
   {
-    Tile<T, VECTOR, I> x, r;
-    x.load(a.x + row * a.x_stride, a.D, warp, warps);
-    if (a.residual) r.load(a.residual + row * a.residual_stride, a.D, warp, warps);
+    Tile<T, VECTOR, I, LANES> x[R], other[R];
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      x.get(i, v[i]);
-      if (a.residual) {
-        float other[8];
-        r.get(i, other);
+    for (int r = 0; r < R; ++r) {
+      x[r].load(a.x + row[r] * a.x_stride, D[r], warp, warps);
+      if (a.residual) other[r].load(a.residual + row[r] * a.residual_stride, D[r], warp, warps);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = to_f32(from_f32<T>(v[i][e] + other[e]));       // the stream as it is stored
-        store8<T, VECTOR>(a.sum + row * a.sum_stride, a.D, warp + i * warps, v[i]);
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        x[r].get(i, v[r][i]);
+        if (a.residual) {
+          float o[8];
+          other[r].get(i, o);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[r][i][e] = to_f32(from_f32<T>(v[r][i][e] + o[e]));     // the stream as it is stored
+          store8<T, VECTOR, LANES>(a.sum + row[r] * a.sum_stride, D[r], warp + i * warps, v[r][i]);
+        }
       }
     }
   }
-  float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < I; ++i)
+  for (int r = 0; r < R; ++r) {
+    float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(v[i][e], v[i][e], s);
-  const float c = 1.f / sqrtf(row_sum(s, room[0], warp, warps) / a.D + a.eps);
-  if (a.inv_rms && warp == 0 && lane_id() == 0) a.inv_rms[row] = c;
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(v[r][i][e], v[r][i][e], s);
+    c[r] = 1.f / sqrtf(row_sum<LANES>(s, room[0], warp, R == 1 ? warps : 1) / a.D + a.eps);
+    if (a.inv_rms && warp == 0 && lane_id() % LANES == 0 && D[r]) a.inv_rms[row[r]] = c[r];
+  }
 #pragma unroll
   for (int i = 0; i < I; ++i) {
     float w[8];
-    weights8<VECTOR>(a.weight, a.D, warp + i * warps, w);
+    weights8<VECTOR, LANES>(a.weight, a.D, warp + i * warps, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * c * w[e];
-    if (!CODES) store8<T, VECTOR>(a.out + row * a.out_stride, a.D, warp + i * warps, v[i]);
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[r][i][e] = v[r][i][e] * c[r] * w[e];
+      if (!CODES) store8<T, VECTOR, LANES>(a.out + row[r] * a.out_stride, D[r], warp + i * warps, v[r][i]);
+    }
   }
   if constexpr (CODES) {
-    const int log_part = __ffs(a.group) - 6;             // a group is 32 << log_part columns
-    float all = 0.f;
-    if (a.group == 0) {
 #pragma unroll
-      for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) all = fmaxf(all, fabsf(v[i][e]));
-      all = fmaxf(row_max(all, room[1], warp, warps), LEAST_MAX);
-      if (warp == 0 && lane_id() == 0) a.scales[row] = all / TOP_CODE;
-    }
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const int chunk = warp + i * warps;
-      if (chunk * NORM_CHUNK >= a.D) continue;
-      float m[8];                                        // of the group of element e
+    for (int r = 0; r < R; ++r) {
+      float inverse = 0.f;
       if (a.group == 0) {
+        float all = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = all;
-      } else if (VECTOR) {                               // a group is group / 8 neighbouring lanes
-        float most = LEAST_MAX;
+        for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
-        for (int o = 1; o < a.group / 8; o *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+          for (int e = 0; e < 8; ++e) all = fmaxf(all, fabsf(v[r][i][e]));
+        all = fmaxf(row_max<LANES>(all, room[1], warp, R == 1 ? warps : 1), LEAST_MAX);
+        if (warp == 0 && lane_id() % LANES == 0 && D[r]) a.scales[row[r]] = all / TOP_CODE;
+        inverse = TOP_CODE / all;
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = most;
-        const int at = Tile<T, VECTOR, 1>::column(chunk, 0), g = at >> (log_part + 5);
-        if ((at & (a.group - 1)) == 0 && g < a.groups) a.scales[row * a.groups + g] = most / TOP_CODE;
-      } else {                                           // a group is all lanes of group / 32 elements
-        float most = 0.f;
+      for (int i = 0; i < I; ++i) {
+        const int chunk = warp + i * warps;
+        if (chunk * NORM_CHUNK >= a.D) continue;
+        float(&y)[8] = v[r][i];
+        if (a.group == 0 || VECTOR) {
+          if (a.group) {                                 // a group is group / 8 neighbouring lanes
+            float most = LEAST_MAX;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = fmaxf(warp_max(fabsf(v[i][e])), LEAST_MAX);
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(y[e]));
+            for (int o = 1; o < min(a.group / 8, LANES); o *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+            inverse = TOP_CODE / most;
+            const int at = Columns::column(chunk, 0), g = at >> (__ffs(a.group) - 1);
+            if ((at & (a.group - 1)) == 0 && at < D[r]) a.scales[row[r] * a.groups + g] = most / TOP_CODE;
+          }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          most = 0.f;
+          for (int e = 0; e < 8; ++e) y[e] *= inverse;
+        } else {                                         // a group is all lanes of group / 32 elements
+          const auto groups_of = [&](auto part) {
+            constexpr int PART = decltype(part)::value;
 #pragma unroll
-          for (int f = 0; f < 8; ++f)
-            if (f >> log_part == e >> log_part) most = fmaxf(most, m[f]);
-          const int g = (chunk * 8 + e) >> log_part;
-          if (lane_id() == 0 && (e & ((1 << log_part) - 1)) == 0 && g < a.groups) a.scales[row * a.groups + g] = most / TOP_CODE;
-          v[i][e] *= TOP_CODE / most;
+            for (int p = 0; p < 8; p += PART) {
+              float most = 0.f;
+#pragma unroll
+              for (int e = 0; e < PART; ++e) most = fmaxf(most, fabsf(y[p + e]));
+              most = fmaxf(warp_max(most), LEAST_MAX);
+              const float inverse_of_group = TOP_CODE / most;
+#pragma unroll
+              for (int e = 0; e < PART; ++e) y[p + e] *= inverse_of_group;
+              const int g = (chunk * 8 + p) / PART;
+              if (lane_id() == 0 && g < a.groups && D[r]) a.scales[row[r] * a.groups + g] = most / TOP_CODE;
+            }
+          };
+          if (a.group == 32) groups_of(std::integral_constant<int, 1>());
+          else if (a.group == 64) groups_of(std::integral_constant<int, 2>());
+          else if (a.group == 128) groups_of(std::integral_constant<int, 4>());
+          else groups_of(std::integral_constant<int, 8>());
         }
+        store_codes<VECTOR, LANES>(a.codes + row[r] * a.out_stride, D[r], chunk, y);
       }
-      if (VECTOR || a.group == 0) {
-        const float inverse = TOP_CODE / m[0];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] *= inverse;
-      }
-      store_codes<VECTOR>(a.codes + row * a.out_stride, a.D, chunk, v[i]);
     }
   }
 }
 
-// Eight codes a thread where rows and codes lie on boundaries of eight, else one.
-template <typename T, bool VECTOR>
+// Pieces of eight codes where rows and codes lie on boundaries of eight, else single ones: 1 << log_threads threads a row, U pieces on their way for each.
+template <typename T, bool VECTOR, int U>
 __global__ void __launch_bounds__(256)
 rows_from_8bit(const uint8_t* __restrict__ codes, int64_t codes_stride, const float* __restrict__ scales, int group, int groups, int D, T* __restrict__ out,
-               int64_t out_stride, int64_t N, int pieces) {
+               int64_t out_stride, int64_t N, int log_threads) {
   constexpr int E = VECTOR ? 8 : 1;
-  // threads lie along the columns, then along the rows
-  const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = item <= UINT32_MAX ? (uint32_t)item / (uint32_t)pieces : item / pieces;
-  const int j = (int)(item - row * pieces) * E;
+  const int64_t row = ((int64_t)blockIdx.x << (8 - log_threads)) + (threadIdx.x >> log_threads);
   if (row >= N) return;
-  const float scale = scales[group ? row * groups + j / group : row];
-  const uint8_t* from = codes + row * codes_stride + j;
-  T* to = out + row * out_stride + j;
-  if (VECTOR && j + 8 <= D) {
-    const uint2 w = __ldcs(reinterpret_cast<const uint2*>(from));
-    float v[8];
+  const uint8_t* from = codes + row * codes_stride;
+  T* to = out + row * out_stride;
+  const int shift = group ? __ffs(group) - 1 : 31;       // 0: all columns are of group 0
+  const float* scale = scales + row * groups;
+  for (int j0 = (threadIdx.x & ((1 << log_threads) - 1)) * E; j0 < D; j0 += (U * E) << log_threads) {
+    uint2 w[U];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((k < 2 ? w.x : w.y) >> 16 * (k % 2)), __NV_E4M3);
-      const float2 f = __half22float2(__half2(h));
-      v[2 * k] = f.x * scale;
-      v[2 * k + 1] = f.y * scale;
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + (u << log_threads) * E;
+      if (VECTOR && j + 8 <= D) w[u] = __ldcs(reinterpret_cast<const uint2*>(from + j));
+      else if (j < D) w[u].x = from[j];
     }
-    if constexpr (sizeof(T) == 4) {
-      __stcs(reinterpret_cast<float4*>(to), make_float4(v[0], v[1], v[2], v[3]));
-      __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(v[4], v[5], v[6], v[7]));
-    } else {
-      __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + (u << log_threads) * E;
+      if (j >= D) break;
+      const float s = __ldg(scale + (j >> shift));
+      if (VECTOR && j + 8 <= D) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((k < 2 ? w[u].x : w[u].y) >> 16 * (k % 2)), __NV_E4M3);
+          const float2 f = __half22float2(__half2(h));
+          v[2 * k] = f.x * s;
+          v[2 * k + 1] = f.y * s;
+        }
+        if constexpr (sizeof(T) == 4) {
+          __stcs(reinterpret_cast<float4*>(to + j), make_float4(v[0], v[1], v[2], v[3]));
+          __stcs(reinterpret_cast<float4*>(to + j) + 1, make_float4(v[4], v[5], v[6], v[7]));
+        } else {
+          __stcs(reinterpret_cast<uint4*>(to + j), make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])));
+        }
+      } else {
+        for (int e = 0; e < E && j + e < D; ++e)
+          to[j + e] = from_f32<T>(__half2float(__half(__nv_cvt_fp8_to_halfraw(e ? from[j + e] : (uint8_t)w[u].x, __NV_E4M3))) * s);
+      }
     }
-    return;
   }
-  for (int e = 0; e < E && j + e < D; ++e) to[e] = from_f32<T>(__half2float(__half(__nv_cvt_fp8_to_halfraw(from[e], __NV_E4M3))) * scale);
 }
 
-constexpr int NORM_BACK_ROWS = 8;                        // of a block whose rows are one warp's
 constexpr int NORM_BACK_BLOCKS = 592;                    // at most: each leaves a row of partial sums of the weight's gradient
 
 template <typename T>
@@ -320,72 +368,102 @@ struct NormBackward {
   int32_t D;
 };
 
-// As many blocks as the GPU holds walk over the rows; each thread keeps the sums of its columns of the weight's gradient in registers.
-template <typename T, bool VECTOR, int I, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+// As many blocks as the GPU holds walk over the rows (shaped as in the forward, with two chunks a warp while there are warps enough: three arrays are in
+// registers); each thread keeps the sums of its columns of the weight's gradient.
+template <typename T>
+__host__ __device__ constexpr int back_blocks(bool vector) { return vector && sizeof(T) == 2 ? 3 : 2; }       // of 256 threads on an SM
+template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? back_blocks<T>(VECTOR) : 1)
 rms_norm_backward(const NormBackward<T> a) {
+  using Columns = Tile<T, VECTOR, 1, LANES>;
   __shared__ float room[2][NORM_WARPS];
-  __shared__ float columns[NORM_BACK_ROWS][NORM_CHUNK];
+  __shared__ float columns[8][NORM_CHUNK];               // of 8 warps
   const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
   float acc[I][8] = {};
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < a.N; row += (int64_t)gridDim.x * blockDim.y, turn ^= 1) {
-    Tile<T, VECTOR, I> x, g, t;
-    x.load(a.x + row * a.x_stride, a.D, warp, warps);
-    g.load(a.grad_out + row * a.out_stride, a.D, warp, warps);
-    if (a.grad_sum) t.load(a.grad_sum + row * a.sum_stride, a.D, warp, warps);
-    const float c = a.inv_rms[row];
-    float s = 0.f;
+  constexpr int SET = R * (32 / LANES);                  // rows of a warp
+  const int64_t step = (int64_t)gridDim.x * blockDim.y * SET;
+  for (int64_t set = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * SET; set < a.N; set += step, turn ^= 1) {
+    Tile<T, VECTOR, I, LANES> x[R], g[R], t[R];
+    float c[R], m[R];
+    int64_t row[R];
+    int D[R];
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      float r[8], dy[8], w[8];
-      x.get(i, r);
-      g.get(i, dy);
-      weights8<VECTOR>(a.weight, a.D, warp + i * warps, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(dy[e] * w[e], r[e], s);
+    for (int r = 0; r < R; ++r) {
+      row[r] = set + r * (32 / LANES) + lane_id() / LANES;
+      D[r] = row[r] < a.N ? a.D : 0;
+      if (row[r] >= a.N) row[r] = a.N - 1;
+      x[r].load(a.x + row[r] * a.x_stride, D[r], warp, warps);
+      g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp, warps);
+      if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp, warps);
+      c[r] = a.inv_rms[row[r]];
+      m[r] = 0.f;
     }
-    const float m = row_sum(s, room[turn], warp, warps) / a.D * (c * c);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      float r[8], dy[8], w[8], d[8];
-      x.get(i, r);
-      g.get(i, dy);
-      weights8<VECTOR>(a.weight, a.D, warp + i * warps, w);
+      float w[8];
+      weights8<VECTOR, LANES>(a.weight, a.D, warp + i * warps, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        d[e] = c * (dy[e] * w[e] - r[e] * m);
-        acc[i][e] = fmaf(dy[e], r[e] * c, acc[i][e]);
-      }
-      if (a.grad_sum) {
-        float other[8];
-        t.get(i, other);
+      for (int r = 0; r < R; ++r) {
+        float y[8], dy[8];
+        x[r].get(i, y);
+        g[r].get(i, dy);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] += other[e];
+        for (int e = 0; e < 8; ++e) m[r] = fmaf(dy[e] * w[e], y[e], m[r]);
       }
-      store8<T, VECTOR>(a.grad_x + row * a.gx_stride, a.D, warp + i * warps, d);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) m[r] = row_sum<LANES>(m[r], room[turn] + threadIdx.y * warps, warp, R == 1 ? warps : 1) / a.D * (c[r] * c[r]);
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      float w[8];
+      weights8<VECTOR, LANES>(a.weight, a.D, warp + i * warps, w);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float y[8], dy[8], d[8];
+        x[r].get(i, y);
+        g[r].get(i, dy);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          d[e] = c[r] * (dy[e] * w[e] - y[e] * m[r]);
+          acc[i][e] = fmaf(dy[e], y[e] * c[r], acc[i][e]);
+        }
+        if (a.grad_sum) {
+          float o[8];
+          t[r].get(i, o);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[e] += o[e];
+        }
+        store8<T, VECTOR, LANES>(a.grad_x + row[r] * a.gx_stride, D[r], warp + i * warps, d);
+      }
     }
   }
   if (!a.partial) return;
   float* const to = a.partial + (int64_t)blockIdx.x * a.D;
 #pragma unroll
   for (int i = 0; i < I; ++i) {
-    const int chunk = warp + i * warps;
+    if (LANES < 32) {
+#pragma unroll
+      for (int o = LANES; o < 32; o *= 2)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[i][e] += __shfl_xor_sync(0xFFFFFFFFu, acc[i][e], o);
+    }
     if (blockDim.y == 1) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (Tile<T, VECTOR, 1>::column(chunk, e) < a.D) to[Tile<T, VECTOR, 1>::column(chunk, e)] = acc[i][e];
+        if (Columns::column(warp + i * warps, e) < a.D) to[Columns::column(warp + i * warps, e)] = acc[i][e];
       continue;
     }
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) columns[threadIdx.y][Tile<T, VECTOR, 1>::column(0, e)] = acc[i][e];
+    for (int e = 0; e < 8; ++e) columns[threadIdx.y * warps + warp][Columns::column(0, e)] = acc[i][e];
     __syncthreads();
-    const int j = threadIdx.y * 32 + lane_id();          // 256 threads, a column each
-    float sum = 0.f;
-#pragma unroll
-    for (int y = 0; y < NORM_BACK_ROWS; ++y) sum += columns[y][j];
-    if (chunk * NORM_CHUNK + j < a.D) to[chunk * NORM_CHUNK + j] = sum;
+    for (int j = threadIdx.y * blockDim.x + threadIdx.x; j < warps * NORM_CHUNK; j += blockDim.x * blockDim.y) {
+      const int chunk = j / NORM_CHUNK, at = (chunk + i * warps) * NORM_CHUNK + j % NORM_CHUNK;
+      float sum = 0.f;
+      for (int y = 0; y < (int)blockDim.y; ++y) sum += columns[y * warps + chunk][j % NORM_CHUNK];
+      if (j % NORM_CHUNK < LANES * 8 && at < a.D) to[at] = sum;
+    }
   }
 }
 
@@ -433,28 +511,55 @@ Weight weight_of(const void* w, int32_t dtype) { return {w, dtype, ((uintptr_t)w
 // Bits of the places where rows start.
 uintptr_t rows_bits(const void* p, int64_t stride, int32_t dtype) { return (uintptr_t)p | (uintptr_t)(stride * dtype_bytes(dtype)); }
 
-// Warps of a row, chunks of each (1, 2 or 4), and rows of a block.
-struct RowShape { int warps, chunks, rows; };
-RowShape shape_of(int64_t N, int32_t D, int rows) {
+// Warps of a row, chunks of each, lanes of a row, and sets (rows, or what a warp has of them) of a block.
+struct RowShape { int warps, chunks, lanes, sets; };
+RowShape shape_of(int32_t D, bool vector, int most_chunks) {
   const int chunks = (D + NORM_CHUNK - 1) / NORM_CHUNK;
-  if (chunks <= NORM_CHUNKS) return {1, chunks <= 2 ? chunks : 4, rows};
-  return {(chunks + NORM_CHUNKS - 1) / NORM_CHUNKS, 4, 1};
+  if (chunks <= most_chunks) return {1, chunks <= 2 ? chunks : 4, vector && D <= 32 ? 4 : vector && D <= 64 ? 8 : vector && D <= 128 ? 16 : 32, 8};
+  if ((chunks + most_chunks - 1) / most_chunks > NORM_WARPS) most_chunks = NORM_CHUNKS;
+  const int warps = (chunks + most_chunks - 1) / most_chunks;
+  return {warps, most_chunks, 32, most_chunks == 2 && warps <= 4 ? 8 / warps : 1};
 }
 
-// Calls fn(whether rows are on vector boundaries, chunks of a warp, threads of a block at most) with constants.
-template <typename Fn>
-void with_shape(bool vector, const RowShape& shape, Fn&& fn) {
+// Calls fn(whether rows are on vector boundaries, rows of a warp, chunks of a row, lanes of a row, threads of a block at most) with constants.  MOST: chunks
+// that a warp has on their way; `several`: several short rows for them, where T is kept in 16 bits and by vectors (else they take too many registers: 54 and 68 us
+// for 100,003 x 332 in fp32 with one row and two) and there are rows for all warps (192 rows of 128 take 2 us less with one).
+template <int MOST, typename T, typename Fn>
+void with_shape(bool vector, bool several, const RowShape& shape, Fn&& fn) {
   using std::integral_constant;
-  const auto with_chunks = [&](auto v) {
-    if (shape.chunks == 1) fn(v, integral_constant<int, 1>(), integral_constant<int, 256>());
-    else if (shape.chunks == 2) fn(v, integral_constant<int, 2>(), integral_constant<int, 256>());
-    else if (shape.warps <= 8) fn(v, integral_constant<int, 4>(), integral_constant<int, 256>());
-    else if (shape.warps <= 16) fn(v, integral_constant<int, 4>(), integral_constant<int, 512>());
-    else fn(v, integral_constant<int, 4>(), integral_constant<int, 1024>());
+  using One = integral_constant<int, 1>;
+  using Full = integral_constant<int, 32>;
+  using Small = integral_constant<int, 256>;
+  using Large = integral_constant<int, 1024>;
+  const bool small = shape.warps * shape.sets <= 8;
+  const auto with_rows = [&](auto v, auto chunks, auto lanes) {
+    if constexpr (decltype(v)::value && sizeof(T) == 2 && decltype(chunks)::value < MOST) {
+      if (several) return fn(v, integral_constant<int, MOST / decltype(chunks)::value>(), chunks, lanes, Small());
+    }
+    return fn(v, One(), chunks, lanes, Small());
   };
-  if (vector) with_chunks(std::true_type());
+  const auto with_chunks = [&](auto v) {
+    if (shape.chunks == 1) return with_rows(v, One(), Full());
+    if (shape.chunks == 2 && small) return with_rows(v, integral_constant<int, 2>(), Full());
+    if constexpr (MOST == 4) {
+      if (small) return fn(v, One(), integral_constant<int, 4>(), Full(), Small());
+    } else {
+      if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Large());
+    }
+    return fn(v, One(), integral_constant<int, 4>(), Full(), Large());
+  };
+  if (shape.lanes == 4) with_rows(std::true_type(), One(), integral_constant<int, 4>());
+  else if (shape.lanes == 8) with_rows(std::true_type(), One(), integral_constant<int, 8>());
+  else if (shape.lanes == 16) with_rows(std::true_type(), One(), integral_constant<int, 16>());
+  else if (vector) with_chunks(std::true_type());
   else with_chunks(std::false_type());
 }
+
+// Whether a warp has several rows, and the rows of a block.
+bool several_rows(const RowShape& shape, bool vector, int32_t dtype, int64_t N, int most) {
+  return vector && dtype_bytes(dtype) == 2 && shape.warps == 1 && shape.chunks < most && N >= 148ll * 32 * most * (32 / shape.lanes);
+}
+int rows_of(const RowShape& shape, bool several, int most) { return shape.sets * (several ? most / shape.chunks : 1) * (32 / shape.lanes); }
 
 int norm_forward(const char* what, const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
                  int32_t weight_dtype, int32_t dtype, int64_t N, int32_t D, float eps, void* sum_out, int64_t sum_stride, void* out, uint8_t* codes,
@@ -476,15 +581,17 @@ int norm_forward(const char* what, const void* x, int64_t x_stride, const void* 
                               x_stride, residual_stride, sum_stride, out_stride, N, weight_of(weight, weight_dtype), D, group, groups, eps};
     const uintptr_t bits = rows_bits(x, x_stride, dtype) | (residual ? rows_bits(residual, residual_stride, dtype) | rows_bits(sum_out, sum_stride, dtype) : 0) |
                            (codes ? 0 : rows_bits(out, out_stride, dtype));
-    const RowShape shape = shape_of(N, D, 8);
-    const dim3 block(32 * shape.warps, shape.rows);
-    const unsigned grid = (unsigned)ceil_div(N, shape.rows);
+    const bool vector = bits % 16 == 0;
+    const RowShape shape = shape_of(D, vector, NORM_CHUNKS);
+    const dim3 block(32 * shape.warps, shape.sets);
+    const bool several = several_rows(shape, vector, dtype, N, NORM_CHUNKS);
+    const unsigned grid = (unsigned)ceil_div(N, rows_of(shape, several, NORM_CHUNKS));
     LaunchScope scope(K_NORM_FWD, s);
-    with_shape(bits % 16 == 0, shape, [&](auto vector, auto chunks, auto threads) {
-      constexpr bool V = decltype(vector)::value;
-      constexpr int I = decltype(chunks)::value, TH = decltype(threads)::value;
-      if (codes) rms_norm_forward<T, V, I, TH, true><<<grid, block, 0, s>>>(a);
-      else rms_norm_forward<T, V, I, TH, false><<<grid, block, 0, s>>>(a);
+    with_shape<NORM_CHUNKS, T>(vector, several, shape, [&](auto v, auto rows, auto chunks, auto lanes, auto threads) {
+      constexpr bool V = decltype(v)::value;
+      constexpr int R = decltype(rows)::value, I = decltype(chunks)::value, L = decltype(lanes)::value, TH = decltype(threads)::value;
+      if (codes) rms_norm_forward<T, V, R, I, L, TH, true><<<grid, block, 0, s>>>(a);
+      else rms_norm_forward<T, V, R, I, L, TH, false><<<grid, block, 0, s>>>(a);
     });
     return check_launch(what);
   });
@@ -530,11 +637,13 @@ extern "C" int mts_rows_from_8bit(const uint8_t* codes, int64_t codes_stride, co
     using T = decltype(t);
     const bool vector = (rows_bits(out, out_stride, out_dtype) % 16 | (uintptr_t)codes % 8 | (uintptr_t)codes_stride % 8) == 0;
     const int groups = group ? (D + group - 1) / group : 1, pieces = vector ? (D + 7) / 8 : D;
-    const int64_t blocks = ceil_div(N * pieces, 256);
-    if (blocks > INT32_MAX) return set_error(MTS_ERR_UNSUPPORTED, "%s: N %lld, D %d", what, (long long)N, D);
+    int log_threads = 0;
+    while (log_threads < 8 && 1 << log_threads < pieces) ++log_threads;
+    const int64_t blocks = ceil_div(N, 256 >> log_threads);
     LaunchScope scope(K_NORM_FWD, s);
-    if (vector) rows_from_8bit<T, true><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, pieces);
-    else rows_from_8bit<T, false><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, pieces);
+    if (vector && pieces <= 256) rows_from_8bit<T, true, 1><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);
+    else if (vector) rows_from_8bit<T, true, 4><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);
+    else rows_from_8bit<T, false, 4><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);
     return check_launch(what);
   });
 }
@@ -571,13 +680,18 @@ extern "C" int mts_rms_norm_backward(const void* x, int64_t x_stride, const void
                                x_stride, grad_out_stride, grad_sum_stride, grad_x_stride, N, weight_of(weight, weight_dtype), D};
     const uintptr_t bits = rows_bits(x, x_stride, dtype) | rows_bits(grad_out, grad_out_stride, dtype) | (grad_sum ? rows_bits(grad_sum, grad_sum_stride, dtype) : 0) |
                            rows_bits(grad_x, grad_x_stride, dtype);
-    const RowShape shape = shape_of(N, D, NORM_BACK_ROWS);
-    const int64_t wanted = ceil_div(N, shape.rows), most = shape.warps == 1 ? 296 : shape.warps <= 4 ? 592 : shape.warps <= 8 ? 296 : 148;
+    const bool vector = bits % 16 == 0;
+    const RowShape shape = shape_of(D, vector, 2);
+    // blocks that the GPU holds at once
+    const bool several = several_rows(shape, vector, dtype, N, 2);
+    const int64_t wanted = ceil_div(N, rows_of(shape, several, 2)), threads = shape.warps * shape.sets * 32;
+    const int64_t most = threads <= 256 ? 148 * back_blocks<T>(vector) : threads <= 512 ? 296 : 148;
     const int blocks = (int)(wanted < most ? wanted : most);
     {
       LaunchScope scope(K_NORM_BWD, s);
-      with_shape(bits % 16 == 0, shape, [&](auto vector, auto chunks, auto threads) {
-        rms_norm_backward<T, decltype(vector)::value, decltype(chunks)::value, decltype(threads)::value><<<blocks, dim3(32 * shape.warps, shape.rows), 0, s>>>(a);
+      with_shape<2, T>(vector, several, shape, [&](auto v, auto rows, auto chunks, auto lanes, auto th) {
+        rms_norm_backward<T, decltype(v)::value, decltype(rows)::value, decltype(chunks)::value, decltype(lanes)::value, decltype(th)::value>
+            <<<blocks, dim3(32 * shape.warps, shape.sets), 0, s>>>(a);
       });
     }
     int e = check_launch(what);
