@@ -749,7 +749,7 @@ int mts_rms_norm_backward(const void* x, int64_t x_stride, const void* weight, i
                           int64_t grad_sum_stride, void* grad_x, int64_t grad_x_stride, float* grad_weight, void* workspace,
                           size_t workspace_bytes, void* stream);
 
-/* Log probabilities under p = softmax(scale * logits[n, :]), scale > 0 (the inverse of a temperature).  All outputs are nullable:
+/* Log probabilities under p = softmax(scale * logits[n, :]), 0 < scale <= 1e30 (the inverse of a temperature).  All outputs are nullable:
  *   logp      : fp32 [N], log p of targets[n] (int64 [N]); 0 where the target is negative (no event: padding), NaN where it is >= V.
  *   entropy   : fp32 [N], -sum_v p_v log p_v.
  *   top_index : int64 [N, top_k], the top_k <= MTS_LOGPROBS_MAX_TOP largest scores, the lowest index first among equals;
@@ -758,7 +758,7 @@ int mts_rms_norm_backward(const void* x, int64_t x_stride, const void* weight, i
  * A score of -infinity rules an item out: p = 0, log p = -infinity, nothing in the entropy.  A row in which every item is ruled out has p = 0
  * everywhere, log p = -infinity, entropy 0 (its stats are {0, 0}).  A row with a NaN or +infinity has NaN for logp, entropy and top_logp;
  * its alternatives are picked among its numbers, NaN coming last.
- * Errors: INVALID_ARG (top_k > V, scale not positive and finite too), UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V,
+ * Errors: INVALID_ARG (top_k > V, scale out of range too), UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V,
  * top_k > MTS_LOGPROBS_MAX_TOP), ALIGNMENT, CUDA. */
 #define MTS_SCORES_MAX_N 100000000
 #define MTS_SCORES_MAX_V 1000000000
@@ -787,7 +787,7 @@ int mts_logprobs_backward(const void* logits, int64_t row_stride, int32_t dtype,
  * score of -infinity is an item that the student rules out: infinite loss where the teacher gives it any weight, the gradient stays
  * finite (p = 0; everywhere in a row in which every item is ruled out).  A row of weight 0 has gradient 0 whatever it holds.  No factor
  * 1 / scale^2 is put in.  grad_logits may be the memory of logits (same stride).
- * Errors: INVALID_ARG, UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V, K > MTS_DISTILL_MAX_K), ALIGNMENT, CUDA. */
+ * Errors: INVALID_ARG (scale as above), UNSUPPORTED (N > MTS_SCORES_MAX_N, V > MTS_SCORES_MAX_V, K > MTS_DISTILL_MAX_K), ALIGNMENT, CUDA. */
 #define MTS_DISTILL_MAX_K 256
 int mts_distill_loss(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale,
                      const int64_t* teacher_index, const void* teacher_logits, int32_t teacher_dtype, int32_t K,

@@ -359,7 +359,7 @@ extern "C" int mts_distill_loss(const void* logits, int64_t row_stride, int32_t 
   if (N < 0 || V < 1 || K < 1) return set_error(MTS_ERR_INVALID_ARG, "%s: N %lld, V %lld, K %d", what, (long long)N, (long long)V, K);
   if (N > MTS_SCORES_MAX_N || V > MTS_SCORES_MAX_V || K > MTS_DISTILL_MAX_K)
     return set_error(MTS_ERR_UNSUPPORTED, "%s: N %lld, V %lld, K %d", what, (long long)N, (long long)V, K);
-  if (!(scale > 0.f && scale <= 3.4e38f)) return set_error(MTS_ERR_INVALID_ARG, "%s: scale %g", what, scale);
+  if (!(scale > 0.f && scale <= 1e30f)) return set_error(MTS_ERR_INVALID_ARG, "%s: scale %g", what, scale);
   int rc = check_rows(what, "logits", logits, dtype, N, V, row_stride);
   if (rc == MTS_OK && grad_logits) rc = check_rows(what, "grad_logits", grad_logits, dtype, N, V, grad_stride);
   if (rc != MTS_OK) return rc;

@@ -472,7 +472,7 @@ int check_logits(const char* what, const void* logits, int64_t row_stride, int32
   if (!known_dtype(dtype)) return set_error(MTS_ERR_INVALID_ARG, "%s: dtype %d", what, dtype);
   if (N < 0 || V < 1) return set_error(MTS_ERR_INVALID_ARG, "%s: N %lld, V %lld", what, (long long)N, (long long)V);
   if (N > MTS_SCORES_MAX_N || V > MTS_SCORES_MAX_V) return set_error(MTS_ERR_UNSUPPORTED, "%s: N %lld, V %lld", what, (long long)N, (long long)V);
-  if (!(scale > 0.f && scale <= 3.4e38f)) return set_error(MTS_ERR_INVALID_ARG, "%s: scale %g", what, scale);
+  if (!(scale > 0.f && scale <= 1e30f)) return set_error(MTS_ERR_INVALID_ARG, "%s: scale %g", what, scale);
   return check_rows(what, "logits", logits, dtype, N, V, row_stride);
 }
 

@@ -353,7 +353,7 @@ rows_from_8bit(const uint8_t* __restrict__ codes, int64_t codes_stride, const fl
   }
 }
 
-constexpr int NORM_BACK_BLOCKS = 592;                    // at most: each leaves a row of partial sums of the weight's gradient
+constexpr int NORM_BACK_BLOCKS = 444;                    // at most: each leaves a row of partial sums of the weight's gradient
 
 template <typename T>
 struct NormBackward {

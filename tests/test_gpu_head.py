@@ -1,5 +1,7 @@
 """The head of the tower inside torch's autograd, its functions together as a tower uses them, on other streams and in captured graphs."""
 import math
+import os
+import sys
 
 import pytest
 import torch
@@ -11,6 +13,8 @@ from paper_2305_01515_b200 import sequence as sq
 pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
 
 
 def rms64(x, w, res=None, eps=1e-6):
@@ -310,3 +314,34 @@ def test_results_are_the_same_in_every_run():
         now = [r.logp, r.entropy, r.top_index, r.top_logp, y, loss] + list(torch.autograd.grad(r.logp.sum() + r.entropy.sum() + loss.sum() + y.float().square().sum(), (x, w)))
         first = first or now
         assert all(torch.equal(a, b) for a, b in zip(first, now))
+
+
+def test_the_example_scores_a_catalogue():
+    """The example's step on next items: its gradients against the same tower with torch's own norm and softmax, and that it runs, trains a table and serves."""
+    import history_tower
+
+    tower = history_tower.HistoryTower(rows=2000, S=12, L=24, seed=3, items=701)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    indices, item = torch.randint(2000, (12 * 24,), generator=g, device=DEV), torch.randint(-1, 701, (12,), generator=g, device=DEV)
+    teacher = (torch.rand(12, 701, generator=g, device=DEV).topk(9)[1], torch.randn(12, 9, generator=g, device=DEV), torch.randn(12, generator=g, device=DEV))
+    with torch.no_grad():
+        tower.p["bias"].copy_(torch.randn(tower.p["bias"].shape, generator=g, device=DEV))
+    events = tower.table.forward(indices, tower.bag, 12 * 24).requires_grad_()
+    leaves = [events, *tower.p.values()]
+    got = torch.autograd.grad(tower.next_loss(events, item, teacher).sum(), leaves)
+    read, state = tower.read(events)
+    r = read + state
+    scores = (r / (r.square().mean(1, keepdim=True) + 1e-6).sqrt() * tower.p["norm"]) @ tower.p["items"]
+    logp = torch.where(item < 0, 0.0, torch.log_softmax(scores, 1).gather(1, item.clamp(min=0).unsqueeze(1))[:, 0])
+    half = torch.log_softmax(scores * 0.5, 1)
+    q = torch.softmax(torch.cat([teacher[1] * 0.5, teacher[2].unsqueeze(1)], 1), 1)
+    others = torch.logsumexp(half.scatter(1, teacher[0], -math.inf), 1, keepdim=True)
+    want = torch.autograd.grad((-logp + (q * (q.log() - torch.cat([half.gather(1, teacher[0]), others], 1))).sum(1)).sum(), leaves)
+    for x, y in zip(got, want):                              # both in fp32, sums of up to 701 terms and products on the way
+        assert float((x - y).norm()) <= 1e-4 * float(y.norm())
+    before = tower.table.weights_numpy()
+    assert all(math.isfinite(float(tower.next_step(indices, item, teacher))) for _ in range(3))
+    assert (before != tower.table.weights_numpy()).any()
+    best, logp = tower.recommend(indices, 5)
+    assert best.shape == (12, 5) and bool((logp[:, :-1] >= logp[:, 1:]).all()) and bool(((best >= 0) & (best < 701)).all())
+    tower.close()

@@ -68,7 +68,7 @@ def test_logprobs():
         mb.logprobs_forward(x, st, dt, N, V, scale, t, k, lp, en, stt, ti, tl)
 
     each(mb.ERR_INVALID_ARG, call, dict(x=None), dict(st=99), dict(dt=3), dict(N=-1), dict(V=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan),
-         dict(scale=math.inf), dict(t=None), dict(k=-1), dict(k=6, V=5))
+         dict(scale=math.inf), dict(scale=2e30), dict(t=None), dict(k=-1), dict(k=6, V=5))
     each(mb.ERR_UNSUPPORTED, call, dict(N=100_000_001), dict(V=1_000_000_001, st=1 << 40), dict(k=mb.LOGPROBS_MAX_TOP + 1))
     each(mb.ERR_ALIGNMENT, call, dict(x=P + 2), dict(t=P + 4), dict(ti=P + 4), dict(lp=P + 2), dict(en=P + 1), dict(stt=P + 2), dict(tl=P + 2))
 
@@ -86,7 +86,7 @@ def test_distill_loss():
         mb.distill_loss(x, st, dt, N, V, scale, i, t, td, K, r, w, loss, dx, ds)
 
     each(mb.ERR_INVALID_ARG, call, dict(x=None), dict(i=None), dict(t=None), dict(loss=None, dx=None), dict(dt=3), dict(td=5), dict(N=-1), dict(V=0), dict(K=0),
-         dict(K=-1), dict(scale=0.0), dict(scale=math.nan), dict(st=99), dict(ds=99))
+         dict(K=-1), dict(scale=0.0), dict(scale=math.nan), dict(scale=2e30), dict(st=99), dict(ds=99))
     each(mb.ERR_UNSUPPORTED, call, dict(K=mb.DISTILL_MAX_K + 1), dict(N=100_000_001), dict(V=1_000_000_001, st=1 << 40, ds=1 << 40))
     each(mb.ERR_ALIGNMENT, call, dict(x=P + 2), dict(dx=P + 2), dict(i=P + 4), dict(t=P + 1), dict(t=P + 2), dict(r=P + 2), dict(w=P + 1), dict(loss=P + 2))
 
