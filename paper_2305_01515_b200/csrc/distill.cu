@@ -10,7 +10,7 @@ namespace mts {
 constexpr int DISTILL_WARPS = 16;
 constexpr int DISTILL_MAX_K = MTS_DISTILL_MAX_K;
 constexpr int DISTILL_UNROLL = 8, DISTILL_GRAD_UNROLL = 4;     // batches on their way for a thread
-constexpr int LISTED_BYTES = 32768;                            // of the bits that say which batches of a part hold a listed item
+constexpr int LISTED_BYTES = 24576;                            // of the bits that say which batches of a part hold a listed item
 
 // Sums of 2^(c x - base) over a set of scores, relative to their largest: over the listed items where these are told apart, and over the others.
 struct DistillSums { float m, listed, others; };
@@ -39,16 +39,17 @@ struct DistillCall {
   const float* rest;
   const float* weights;
   float* loss;
-  int32_t V, K, teacher_dtype, log_parts, share;
+  int32_t V, K, teacher_dtype, log_parts, share, warps, log_slots;      // warps: those that take part in the sums
   float scale;
 };
 
 struct DistillRoom {
-  float q[DISTILL_MAX_K], score[DISTILL_MAX_K], log_q[DISTILL_MAX_K];
-  int32_t at[DISTILL_MAX_K];                                   // -1: not used
-  DistillSums of_warp[DISTILL_WARPS], of_part[1 << MAX_LOG_PARTS];
+  DistillSums of_warp[DISTILL_WARPS + 1], of_part[1 << MAX_LOG_PARTS];
   float total, q_rest, log_q_rest;
 };
+// Behind it: float q[K], score[K], log_q[K], int32_t place[K], and with the rest's weight the table of the batches that hold a listed item (int32_t batch[],
+// uint32_t places[], first[], of 1 << log_slots places, four times K at least), int32_t slot[K] and the bits of the batches that the pass leaves out.
+__host__ __device__ constexpr int rounded16(int bytes) { return (bytes + 15) / 16 * 16; }
 
 // Exponentials of a batch.
 template <typename T, bool ORDINARY>
@@ -70,19 +71,34 @@ __device__ __forceinline__ Pair sum_of(const float (&v)[RowBatches<T>::E]) {
   return s;
 }
 
+// A barrier of the whole block, met by the teacher's warp and the others at different places.
+__device__ __forceinline__ void bits_ready() { asm volatile("bar.sync 1;" ::: "memory"); }
+
 // A row (or a part of it, by a cluster of blocks) by a block.  The sums of the exponentials take one pass over the scores as in the log probabilities; the
-// gradient reads them once more, from L2, where the row has just passed.
+// gradient reads them once more, from L2, where the row has just passed.  One warp gathers the teacher's row and the scores of the listed items (indices, then what
+// they point to: two latencies in a row); where a row has four warps or more it is one of its own, while the others sum.
 // With the rest's weight given (REST) the sum over the items that are not listed is made without the listed ones: what is left of a difference would lose its
 // digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
 // leaves these out, and they are added afterwards item by item.
 // The gradient is written as if nothing were listed, and the listed places once more.
 template <typename T, bool REST>
-__global__ void __launch_bounds__(DISTILL_WARPS * 32, 2)
+__global__ void __maxnreg__(64)                                // of (DISTILL_WARPS + 1) * 32 threads at most: 32 warps an SM
 distill_loss(const T* logits, T* grad, const DistillCall a) {
-  constexpr int E = RowBatches<T>::E, U = DISTILL_UNROLL;
+  constexpr int E = RowBatches<T>::E, LOG_E = E == 8 ? 3 : 2, U = DISTILL_UNROLL;
   __shared__ DistillRoom room;
-  extern __shared__ __align__(16) uint8_t left_out[];
-  const int tid = threadIdx.x, lane = lane_id(), warp = tid / 32, threads = blockDim.x, warps = threads / 32;
+  extern __shared__ __align__(16) uint8_t behind[];
+  float* const q = reinterpret_cast<float*>(behind);
+  float* const score = q + a.K;
+  float* const log_q = score + a.K;
+  int32_t* const place = reinterpret_cast<int32_t*>(log_q + a.K);
+  const int slots = 1 << a.log_slots;
+  int32_t* const in_slot = reinterpret_cast<int32_t*>(behind + rounded16(16 * a.K));
+  uint32_t* const places_of = reinterpret_cast<uint32_t*>(in_slot + slots);
+  uint32_t* const first_of = places_of + slots;
+  int32_t* const slot_of_place = reinterpret_cast<int32_t*>(first_of + slots);
+  uint8_t* const left_out = reinterpret_cast<uint8_t*>(slot_of_place + a.K);
+  const int tid = threadIdx.x, lane = lane_id(), warp = tid / 32, everyone = blockDim.x, warps = a.warps, threads = 32 * warps;
+  const bool own_warp = everyone > threads;                    // of the teacher's row
   const int parts = 1 << a.log_parts, part = blockIdx.x & (parts - 1);
   const int64_t n = blockIdx.x >> a.log_parts;
   if (parts > 1) cluster_arrive();                             // all blocks have begun before others write to them
@@ -90,66 +106,9 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   const int32_t b0 = min(r.count, part * a.share), b1 = min(r.count, b0 + a.share);
   const float c = a.scale * LOG2E;
 
-  // the bits of the batches that are left out: byte of a thread's group, bit of the batch in it
-  if (REST) {
-    const int bytes = min(LISTED_BYTES, (b1 - b0 + threads * U - 1) / (threads * U) * threads);
-    for (int i = tid; i < bytes / 4; i += threads) reinterpret_cast<uint32_t*>(left_out)[i] = 0;
-    __syncthreads();
-    for (int k = tid; k < a.K; k += threads) {
-      const int64_t i = a.index[n * a.K + k];
-      if (i < 0 || i >= a.V) continue;
-      const int32_t b = (int32_t)(i + r.shift) / E - b0, group = b / (threads * U), in = b - group * threads * U;
-      const int64_t byte = (int64_t)group * threads + in % threads;
-      if (b >= 0 && b < b1 - b0 && byte < LISTED_BYTES) atomicOr(reinterpret_cast<uint32_t*>(left_out) + byte / 4, 1u << (in / threads + byte % 4 * 8));
-    }
-  }
-  // the teacher's distribution, by the first warp
-  if (warp == 0) {
-    float most = -INFINITY;
-    bool wrong = false;
-    for (int k = lane; k < a.K; k += 32) {
-      const int64_t i = a.index[n * a.K + k];
-      const float t = i >= 0 ? teacher_value(a.teacher, a.teacher_dtype, n * a.K + k) * a.scale : -INFINITY;
-      wrong |= i >= a.V || isnan(t);
-      room.log_q[k] = t;
-      room.at[k] = i >= 0 && i < a.V ? (int32_t)i : -1;
-      most = fmaxf(most, t);
-    }
-    const float t_rest = REST ? a.rest[n] : -INFINITY;
-    most = fmaxf(warp_max(most), t_rest);
-    const float base = most == -INFINITY ? 0.f : most;
-    const float e_rest = expf(t_rest - base);
-    float total = 0.f;
-    for (int k = lane; k < a.K; k += 32) total += expf(room.log_q[k] - base);
-    total = warp_sum(total) + e_rest;
-    if (__any_sync(0xFFFFFFFFu, wrong)) total = NAN;
-    const bool any = total != 0.f;                             // else nothing is left of the teacher's row
-    const float log_total = any ? logf(total) : 0.f;
-    for (int k = lane; k < a.K; k += 32) {
-      const float t = room.log_q[k] - base;
-      room.q[k] = any ? expf(t) / total : 0.f;
-      room.log_q[k] = t - log_total;
-      const int32_t i = room.at[k];
-      room.score[k] = i >= 0 ? to_f32(r.row[i]) : 0.f;
-    }
-    if (lane == 0) {
-      room.total = total;
-      room.q_rest = any ? e_rest / total : 0.f;
-      room.log_q_rest = t_rest - base - log_total;
-    }
-  }
-  if (REST) __syncthreads();
-
-  // the student's sums
+  // the student's sums of this thread
   float m = -INFINITY, base = 0.f, listed = 0.f;
   Pair others(0.f, 0.f);
-  const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
-  // whether batch b holds a listed item, where the bits do not reach
-  const auto holds_listed = [&](int32_t b) {
-    for (int k = 0; k < a.K; ++k)
-      if (room.at[k] >= 0 && (room.at[k] + r.shift) / E == b) return true;
-    return false;
-  };
   const auto rescale = [&](float most) {
     const DistillSums s = scaled_to({m, listed, others.sum()}, most, c);
     listed = s.listed;
@@ -157,75 +116,150 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     m = most;
     base = base_of(m, c);
   };
-  int32_t byte = tid;
-  for (int32_t g = b0; g < b1; g += threads * U) {
-    const int32_t b = g + tid;
-    const bool all = r.template all_whole<U>(g, b1, tid, threads);
-    uint4 w[U];
-    r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
-    if (!all) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (b + u * threads >= b1) w[u] = nothing_there;
-    }
-    uint32_t most_bits = max_bits<T>(w[0]);
-#pragma unroll
-    for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
-    const float most = max_value<T>(most_bits);
-    if (most > m) rescale(most);
-    unsigned out = 0;
+
+  if (warp == (own_warp ? warps : 0)) {
+    // the teacher's row.  `place`: an item's number of elements from the first batch's begin, so that its batch is place / E; -1: not used
     if (REST) {
-      if (byte < LISTED_BYTES) {
-        out = left_out[byte];
-      } else {
-        for (int u = 0; u < U; ++u) out |= holds_listed(b + u * threads) << u;
-      }
-      byte += threads;
+      const int bytes = min(LISTED_BYTES, (b1 - b0 + threads * U - 1) / (threads * U) * threads);
+      for (int i = lane; i < bytes / 4; i += 32) reinterpret_cast<uint32_t*>(left_out)[i] = 0;
     }
-    if (!ordinary(base)) {
-#pragma unroll 1
-      for (int u = 0; u < U; ++u) {
-        if (b + u * threads >= b1 || out >> u & 1) continue;
-        float v[E];
-        exponentials<T, false>(r.raw(b + u * threads), m, base, c, v);
-        others = others + sum_of<T>(v);
+    __syncwarp();
+    float most = -INFINITY;
+    bool wrong = false;
+    for (int k = lane; k < a.K; k += 32) {
+      const int64_t i = a.index[n * a.K + k];
+      const float t = i >= 0 ? teacher_value(a.teacher, a.teacher_dtype, n * a.K + k) * a.scale : -INFINITY;
+      wrong |= i >= a.V || isnan(t);
+      log_q[k] = t;
+      place[k] = i >= 0 && i < a.V ? (int32_t)i + r.shift : -1;
+      most = fmaxf(most, t);
+      if (REST && i >= 0 && i < a.V) {
+        const int32_t b = (((int32_t)i + r.shift) >> LOG_E) - b0, group = b / (threads * U), in = b - group * threads * U;
+        const int64_t byte = (int64_t)group * threads + in % threads;
+        if (b >= 0 && b < b1 - b0 && byte < LISTED_BYTES) atomicOr(reinterpret_cast<uint32_t*>(left_out) + byte / 4, 1u << (in / threads + byte % 4 * 8));
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!all && b + u * threads >= b1) continue;
+    }
+    if (REST) bits_ready();                                    // the others may look at the bits and places
+    const float t_rest = REST ? a.rest[n] : -INFINITY;
+    for (int k = lane; k < a.K; k += 32) score[k] = place[k] >= 0 ? to_f32(r.row[place[k] - r.shift]) : 0.f;
+    most = fmaxf(warp_max(most), t_rest);
+    const float t_base = most == -INFINITY ? 0.f : most;
+    const float e_rest = expf(t_rest - t_base);
+    float total = 0.f;
+    for (int k = lane; k < a.K; k += 32) total += expf(log_q[k] - t_base);
+    total = warp_sum(total) + e_rest;
+    if (__any_sync(0xFFFFFFFFu, wrong)) total = NAN;
+    const bool any = total != 0.f;                             // else nothing is left of the teacher's row
+    const float log_total = any ? logf(total) : 0.f;
+    for (int k = lane; k < a.K; k += 32) {
+      const float t = log_q[k] - t_base;
+      q[k] = any ? expf(t) / total : 0.f;
+      log_q[k] = t - log_total;
+    }
+    if (lane == 0) {
+      room.total = total;
+      room.q_rest = any ? e_rest / total : 0.f;
+      room.log_q_rest = t_rest - t_base - log_total;
+    }
+    if (REST) {
+      // the batches that are left out, each for its first place, item by item: a table has the places of a batch's listed items and their first
+      for (int i = lane; i < slots / 4; i += 32) {
+        reinterpret_cast<int4*>(in_slot)[i] = make_int4(-1, -1, -1, -1);
+        reinterpret_cast<uint4*>(places_of)[i] = make_uint4(0u, 0u, 0u, 0u);
+        reinterpret_cast<uint4*>(first_of)[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+      }
+      __syncwarp();
+      const auto slot_of = [&](int32_t b) {
+        uint32_t slot = (uint32_t)b * 2654435761u >> (32 - a.log_slots);
+        for (;; slot = (slot + 1) & (slots - 1)) {             // at most a quarter of the slots are taken: it ends
+          const int32_t was = atomicCAS(&in_slot[slot], -1, b);
+          if (was == -1 || was == b) return slot;
+        }
+      };
+      for (int k = lane; k < a.K; k += 32) {
+        const int32_t b = place[k] >> LOG_E;
+        if (b < b0 || b >= b1) continue;                       // -1 too
+        const uint32_t slot = slot_of(b);
+        slot_of_place[k] = (int32_t)slot;
+        atomicOr(&places_of[slot], 1u << (place[k] & (E - 1)));
+        atomicMin(&first_of[slot], (uint32_t)k);
+      }
+      __syncwarp();
+      for (int k = lane; k < a.K; k += 32) {
+        const int32_t b = place[k] >> LOG_E;
+        if (b < b0 || b >= b1) continue;
+        const uint32_t slot = slot_of_place[k], places = places_of[slot];
+        if (first_of[slot] != k) continue;
+        const uint4 batch = r.raw(b);
+        const float top = max_value<T>(max_bits<T>(batch));
+        if (top > m) rescale(top);
         float v[E];
-        exponentials<T, true>(w[u], m, base, c, v);
-        const Pair s = sum_of<T>(v);
-        if (!REST || !(out >> u & 1)) others = others + s;
+        if (ordinary(base)) exponentials<T, true>(batch, m, base, c, v);
+        else exponentials<T, false>(batch, m, base, c, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (places >> e & 1) listed += v[e];
+          else others = others + Pair(v[e], 0.f);
+        }
       }
     }
   }
-  if (REST) {
-    // the batches left out, each by the thread of the first place in it
-    for (int k = tid; k < a.K; k += threads) {
-      const int32_t b = (room.at[k] + r.shift) / E;
-      if (room.at[k] < 0 || b < b0 || b >= b1) continue;
-      unsigned places = 0;
-      bool first = true;
-      for (int j = 0; j < a.K; ++j) {
-        const int32_t i = room.at[j] + r.shift;
-        if (room.at[j] >= 0 && i / E == b) {
-          places |= 1u << i % E;
-          first &= j >= k;
-        }
-      }
-      if (!first) continue;
-      const uint4 batch = r.raw(b);
-      const float most = max_value<T>(max_bits<T>(batch));
-      if (most > m) rescale(most);
-      float v[E];
-      if (ordinary(base)) exponentials<T, true>(batch, m, base, c, v);
-      else exponentials<T, false>(batch, m, base, c, v);
+  if (warp < warps) {
+    const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
+    // whether batch b holds a listed item, where the bits do not reach
+    const auto holds_listed = [&](int32_t b) {
+      for (int k = 0; k < a.K; ++k)
+        if (place[k] >> LOG_E == b) return true;          // -1 >> LOG_E is -1
+      return false;
+    };
+    uint4 w[U];
+    bool all = false;
+    const auto load = [&](int32_t g) {
+      all = r.template all_whole<U>(g, b1, tid, threads);
+      r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
+    };
+    if (b0 < b1) load(b0);
+    if (REST && (own_warp || warp != 0)) bits_ready();
+    int32_t byte = tid;
+    for (int32_t g = b0; g < b1; g += threads * U) {
+      const int32_t b = g + tid;
+      if (g > b0) load(g);
+      if (!all) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (places >> e & 1) listed += v[e];
-        else others = others + Pair(v[e], 0.f);
+        for (int u = 0; u < U; ++u)
+          if (b + u * threads >= b1) w[u] = nothing_there;
+      }
+      uint32_t most_bits = max_bits<T>(w[0]);
+#pragma unroll
+      for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
+      const float most = max_value<T>(most_bits);
+      if (most > m) rescale(most);
+      unsigned out = 0;
+      if (REST) {
+        if (byte < LISTED_BYTES) {
+          out = left_out[byte];
+        } else {
+          for (int u = 0; u < U; ++u) out |= holds_listed(b + u * threads) << u;
+        }
+        byte += threads;
+      }
+      if (!ordinary(base)) {
+#pragma unroll 1
+        for (int u = 0; u < U; ++u) {
+          if (b + u * threads >= b1 || out >> u & 1) continue;
+          float v[E];
+          exponentials<T, false>(r.raw(b + u * threads), m, base, c, v);
+          others = others + sum_of<T>(v);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (!all && b + u * threads >= b1) continue;
+          float v[E];
+          exponentials<T, true>(w[u], m, base, c, v);
+          const Pair s = sum_of<T>(v);
+          if (!REST || !(out >> u & 1)) others = others + s;
+        }
       }
     }
   }
@@ -233,7 +267,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   DistillSums s = join_lanes({m, listed, others.sum()}, c);
   if (lane == 0) room.of_warp[warp] = s;
   __syncthreads();
-  s = join_lanes(lane < warps ? room.of_warp[lane] : nobody, c);
+  s = join_lanes(lane < everyone / 32 ? room.of_warp[lane] : nobody, c);
   if (parts > 1) {
     cluster_wait();
     if (tid < parts) {
@@ -250,8 +284,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     const float off = log_excess(s.m, base, c), log_all = all == 0.f ? 0.f : logf(all) - off;
     float sum = 0.f;
     for (int k = lane; k < a.K; k += 32) {
-      const float q = room.q[k];
-      if (q != 0.f) sum += q * (room.log_q[k] - ((room.score[k] - m0) * a.scale - log_all));
+      if (q[k] != 0.f) sum += q[k] * (log_q[k] - ((score[k] - m0) * a.scale - log_all));
     }
     if (REST && lane == 0 && room.q_rest != 0.f) sum += room.q_rest * (room.log_q_rest - (logf(s.others) - off - log_all));
     sum = warp_sum(sum);
@@ -265,7 +298,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   const float w = (a.weights ? a.weights[n] : 1.f) * a.scale, inv_all = all == 0.f ? 0.f : 1.f / all, total = room.total;
   if (w == 0.f || total == 0.f) {
     const float zero[E] = {};
-    for (int32_t b = g0 + tid; b < g1; b += threads) to.store(b, zero);
+    for (int32_t b = g0 + tid; b < g1; b += everyone) to.store(b, zero);
     return;
   }
   const float f = w * (REST && room.q_rest != 0.f && s.others != 0.f ? inv_all - room.q_rest / s.others : inv_all) + total * 0.f;
@@ -285,17 +318,17 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   int32_t in0, in1;
   under.inner(&in0, &in1);
   in1 = min(in1, g1);
-  for (int32_t g = g0; g < g1; g += threads * GU) {
+  for (int32_t g = g0; g < g1; g += everyone * GU) {
     const int32_t b = g + tid;
     float v[E];
-    if (usual && g >= in0 && g + threads * GU <= in1) {        // nothing to test
+    if (usual && g >= in0 && g + everyone * GU <= in1) {        // nothing to test
       const T* from = r.row + (to.first(b) - under.ahead);
       T* at = grad + n * a.grad_stride + to.first(b);
       uint4 x[GU];
 #pragma unroll
-      for (int u = 0; u < GU; ++u, from += threads * E) x[u] = under.inside(from);
+      for (int u = 0; u < GU; ++u, from += everyone * E) x[u] = under.inside(from);
 #pragma unroll
-      for (int u = 0; u < GU; ++u, at += threads * E) {
+      for (int u = 0; u < GU; ++u, at += everyone * E) {
         RowBatches<T>::unpack(x[u], v);
         const Pair minus(-base, -base), c2(c, c), f2(f, f);
 #pragma unroll
@@ -309,7 +342,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       }
     } else {
 #pragma unroll 1
-      for (int32_t q = b; q < min(g1, g + threads * GU); q += threads) {
+      for (int32_t q = b; q < min(g1, g + everyone * GU); q += everyone) {
         gradient(under.raw(q), v);
         to.store(q, v);
       }
@@ -317,14 +350,14 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   }
   __syncthreads();
   // the listed items' places once more, by the block that wrote them
-  for (int k = tid; k < a.K; k += threads) {
-    const int32_t i = room.at[k];
-    if (i < 0) continue;
-    const int32_t b = (i + to.shift) / E;
+  for (int k = tid; k < a.K; k += everyone) {
+    if (place[k] < 0) continue;
+    const int32_t i = place[k] - r.shift, b = (i + to.shift) >> LOG_E;
     if (b < g0 || b >= g1) continue;
     float want = 0.f;
-    for (int j = 0; j < a.K; ++j) want += room.at[j] == i ? room.q[j] : 0.f;
-    const float p = exp2_fast(usual ? fmaf(room.score[k], c, -base) : (room.score[k] - m0) * c) * inv_all;
+#pragma unroll 4
+    for (int j = 0; j < a.K; ++j) want += place[j] == place[k] ? q[j] : 0.f;
+    const float p = exp2_fast(usual ? fmaf(score[k], c, -base) : (score[k] - m0) * c) * inv_all;
     grad[n * a.grad_stride + i] = from_f32<T>(w * (p - want) + total * 0.f);
   }
 }
@@ -337,9 +370,9 @@ int launch_distill(const char* what, const T* logits, T* grad, const DistillCall
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3((unsigned)(N << a.log_parts));
-  config.blockDim = dim3(32 * warps);
-  const int64_t groups = ceil_div(a.share, 32 * warps * DISTILL_UNROLL);
-  config.dynamicSmemBytes = !REST ? 0 : (size_t)(groups * 32 * warps < LISTED_BYTES ? groups * 32 * warps : LISTED_BYTES);
+  config.blockDim = dim3(32 * (warps + (warps >= 4)));
+  const int64_t bits = ceil_div(a.share, 32 * warps * DISTILL_UNROLL) * 32 * warps;
+  config.dynamicSmemBytes = (size_t)rounded16(16 * a.K) + (REST ? (size_t)(12 << a.log_slots) + 4 * a.K + (size_t)(bits < LISTED_BYTES ? bits : LISTED_BYTES) : 0);
   config.stream = s;
   config.attrs = &cluster;
   config.numAttrs = a.log_parts ? 1 : 0;
@@ -375,9 +408,13 @@ extern "C" int mts_distill_loss(const void* logits, int64_t row_stride, int32_t 
     const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
     const int log_parts = log_parts_of(N, batches);
     const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
-    int warps = share <= 700 ? 1 : share <= 3000 ? 2 : share <= 8000 ? 4 : 8;
+    // Warps that sum a row, with its gradient, us with 1, 4, 8 and 16: 20,000 rows of 625 batches 107, 144, 244, 630; 10,000 of 1,250 105, 114, 139, 349; 5,000 of
+    // 2,000 102, 73, 89, 191; 4,000 of 5,000 183, 144, 148, 261; 4,096 of 8,192 289, 246, 220, 316; 1,000 of 25,000 330, 257, 212, 181.  More where SMs idle.
+    int warps = share <= 1500 ? 1 : share <= 6000 ? 4 : share <= 20000 ? 8 : 16;
     while (warps < DISTILL_WARPS && (N << log_parts) * warps < 148 * 16 && share >= (warps < 8 ? 64 : 256) * warps) warps *= 2;
-    const DistillCall a = {row_stride, grad_stride, teacher_index, teacher_logits, teacher_rest, weights, loss, (int32_t)V, K, teacher_dtype, log_parts, share, scale};
+    int log_slots = 5;
+    while (1 << log_slots < 4 * K) ++log_slots;
+    const DistillCall a = {row_stride, grad_stride, teacher_index, teacher_logits, teacher_rest, weights, loss, (int32_t)V, K, teacher_dtype, log_parts, share, warps, log_slots, scale};
     const T* x = static_cast<const T*>(logits);
     T* d = static_cast<T*>(grad_logits);
     return teacher_rest ? launch_distill<T, true>(what, x, d, a, N, warps, s) : launch_distill<T, false>(what, x, d, a, N, warps, s);
