@@ -30,17 +30,19 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < I; ++i, chunk += step) {
       if constexpr (VECTOR) {
-        const int at = column(chunk, 0);
-        if (at + 8 <= D) {
+        constexpr int P = 8 / Q;                         // elements of 16 bytes
 #pragma unroll
-          for (int k = 0; k < Q; ++k) q[i][k] = reinterpret_cast<const uint4*>(row + at)[k];
-        } else {
+        for (int k = 0; k < Q; ++k) {
+          const int at = column(chunk, k * P);
+          if (at + P <= D) {
+            q[i][k] = *reinterpret_cast<const uint4*>(row + at);
+          } else {
+            q[i][k] = make_uint4(0u, 0u, 0u, 0u);
+            T* const e = reinterpret_cast<T*>(&q[i][k]);
 #pragma unroll
-          for (int k = 0; k < Q; ++k) q[i][k] = make_uint4(0u, 0u, 0u, 0u);
-          T* const e = reinterpret_cast<T*>(q[i]);
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (at + k < D) e[k] = row[at + k];
+            for (int p = 0; p < P; ++p)
+              if (at + p < D) e[p] = row[at + p];
+          }
         }
       } else {
 #pragma unroll
@@ -76,16 +78,20 @@ template <typename T, bool VECTOR, int LANES>
 __device__ __forceinline__ void store8(T* row, int D, int chunk, const float (&v)[8]) {
   using Columns = Tile<T, VECTOR, 1, LANES>;
   if constexpr (VECTOR) {
-    T* const to = row + Columns::column(chunk, 0);
-    if (Columns::column(chunk, 8) <= D) {
-      if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    constexpr int Q = (int)sizeof(T) / 2, P = 8 / Q;
+#pragma unroll
+    for (int k = 0; k < Q; ++k) {
+      const int at = Columns::column(chunk, k * P);
+      if (at + P <= D) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(row + at) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        else *reinterpret_cast<uint4*>(row + at) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
       } else {
-        *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          if (at + p < D) row[at + p] = from_f32<T>(v[k * P + p]);
       }
-      return;
     }
+    return;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e)
@@ -96,6 +102,11 @@ struct Weight {
   const void* w;
   int32_t dtype, aligned;                                // aligned: on a 16-byte boundary
 };
+
+__device__ __forceinline__ float weight_at(const Weight& w, int j) {
+  if (w.dtype == MTS_DTYPE_FP32) return __ldg(static_cast<const float*>(w.w) + j);
+  return w.dtype == MTS_DTYPE_FP16 ? to_f32(__ldg(static_cast<const __half*>(w.w) + j)) : to_f32(__ldg(static_cast<const __nv_bfloat16*>(w.w) + j));
+}
 
 // A lane's eight weights, 0 behind the row's end.
 template <bool VECTOR, int LANES>
@@ -120,9 +131,7 @@ __device__ __forceinline__ void weights8(const Weight& w, int D, int chunk, floa
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int j = Tile<float, VECTOR, 1, LANES>::column(chunk, e);
-    v[e] = 0.f;
-    if (j < D) v[e] = w.dtype == MTS_DTYPE_FP32 ? __ldg(static_cast<const float*>(w.w) + j)
-                    : w.dtype == MTS_DTYPE_FP16 ? to_f32(__ldg(static_cast<const __half*>(w.w) + j)) : to_f32(__ldg(static_cast<const __nv_bfloat16*>(w.w) + j));
+    v[e] = j < D ? weight_at(w, j) : 0.f;
   }
 }
 
