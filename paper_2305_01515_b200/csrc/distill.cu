@@ -8,7 +8,6 @@
 namespace mts {
 
 constexpr int DISTILL_WARPS = 16;
-constexpr int DISTILL_MAX_K = MTS_DISTILL_MAX_K;
 constexpr int DISTILL_UNROLL = 8, DISTILL_GRAD_UNROLL = 4;     // batches on their way for a thread
 constexpr int LISTED_BYTES = 24576;                            // of the bits that say which batches of a part hold a listed item
 

@@ -1,4 +1,4 @@
-// Rows of a [N, V] tensor read by aligned vectors wherever they start, and reductions over a block.  Internal to the library.
+// Rows of a [N, V] tensor read by aligned vectors wherever they start, and what softmaxes over them share.  Internal to the library.
 #pragma once
 
 #include <math.h>
@@ -271,37 +271,6 @@ __device__ __forceinline__ float max_value(uint32_t m) {
   if constexpr (sizeof(T) == 4) return fmaxf(__uint_as_float(m), -INFINITY);
   const float2 f = unpack2<T>(m);
   return fmaxf(fmaxf(f.x, f.y), -INFINITY);
-}
-
-// Sum and maximum over a block of THREADS in a fixed order; every thread gets the result.  `room`: shared, [THREADS / 32]; free again at the
-// next barrier of the block.
-template <int THREADS>
-__device__ __forceinline__ float block_sum(float x, float* room) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-  if constexpr (THREADS > 32) {
-    __syncthreads();
-    if (lane_id() == 0) room[threadIdx.x / 32] = x;
-    __syncthreads();
-    x = 0.f;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) x += room[w];
-  }
-  return x;
-}
-template <int THREADS>
-__device__ __forceinline__ float block_max(float x, float* room) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-  if constexpr (THREADS > 32) {
-    __syncthreads();
-    if (lane_id() == 0) room[threadIdx.x / 32] = x;
-    __syncthreads();
-    x = room[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 32; ++w) x = fmaxf(x, room[w]);
-  }
-  return x;
 }
 
 // Exponents of a softmax are taken relative to the largest score m: c x - base with base = c m rounded (its error is put right at the end), which is one

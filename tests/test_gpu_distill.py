@@ -224,3 +224,27 @@ def test_no_rows_and_rows_far_apart():
     _, dx = check(x, index, teacher, torch.zeros(N, device=DEV))
     call(x, index, teacher, torch.zeros(N, device=DEV), to=x)
     assert torch.equal(x, dx)
+
+
+@pytest.mark.parametrize("V,dtype", [(900001, torch.float32), (1700003, torch.bfloat16)])
+def test_rows_longer_than_the_bits_of_their_batches(V, dtype):
+    """Too many rows for a cluster each, and listed items at a row's end, behind the batches that have a bit each."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x, _ = placed(torch.randn(75, V, generator=g, device=DEV), dtype, 0, 1)
+    index = torch.randint(V, (75, 30), generator=g, device=DEV)
+    index[:, 0] = V - 1 - torch.arange(75, device=DEV)
+    index[:, 1] = V - 1
+    index[:40, 2] = V - 2
+    check(x, index, torch.randn(75, 30, generator=g, device=DEV), torch.randn(75, generator=g, device=DEV))
+
+
+@pytest.mark.parametrize("N,V", [(600, 3001), (3, 60001)])
+def test_results_are_the_same_in_every_run(N, V):
+    """Listed items many to a batch and the same ones twice: the order in which threads find them does not matter."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(N, V, generator=g, device=DEV).bfloat16()
+    index = torch.randint(64, (N, 200), generator=g, device=DEV) * torch.randint(1, V // 64, (N, 1), generator=g, device=DEV)
+    teacher, rest = torch.randn(N, 200, generator=g, device=DEV), torch.randn(N, generator=g, device=DEV)
+    first = call(x, index, teacher, rest)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, call(x, index, teacher, rest)))

@@ -259,3 +259,17 @@ def test_offsets_past_32_bits():
     want, bound = gradient64(x, t, gl, None, 1.0)
     backward(x, t, stats, ent, gl, None, 1.0, x)
     close(x, want, bound + want.abs() * 2.0 ** -8 + 1e-37)
+
+
+@pytest.mark.parametrize("N,V,k,dtype", [(80, 300001, 32, torch.float32), (76, 1200007, 20, torch.bfloat16), (151, 150001, 5, torch.float32)])
+@pytest.mark.parametrize("kind", ["spread", "up", "few"])
+def test_best_of_long_rows_by_single_blocks(N, V, k, dtype, kind):
+    """Rows of more groups than a thread keeps maxima of, too many for a cluster each."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(N, V, generator=g, device=DEV)
+    if kind == "up":
+        x = x * 0.001 + torch.arange(V, device=DEV) / V * 8
+    if kind == "few":
+        x.masked_fill_(torch.rand(N, V, generator=g, device=DEV) < 1 - 40 / V, -INF)
+    x, _ = placed(x, dtype, 0, 3)
+    check(x, torch.randint(-1, V, (N,), generator=g, device=DEV), k, 1.0)
