@@ -111,15 +111,19 @@ __device__ __forceinline__ X kth_of_groups(X (*of_thread)[32], int rows, int k, 
 // altogether, say), and rows with NaN.  The threads find where their maximum came first and the bound is made of (score, index); where that does not
 // settle it either, the best are found one after the other.
 template <typename T, bool ONE_WARP>
-__device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, int32_t b1, int k, float m, RowRoom& room) {
+__device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, int32_t b1, int k, RowRoom& room) {
   constexpr int E = RowBatches<T>::E;
   const int lane = lane_id(), warp = ONE_WARP ? 0 : threadIdx.x / 32, tid = ONE_WARP ? lane : threadIdx.x;
   const int threads = ONE_WARP ? 32 : blockDim.x, warps = threads / 32;
   const auto sync = [] { if (ONE_WARP) __syncwarp(); else __syncthreads(); };
   const int32_t b = b0 + tid;
   uint64_t order = 0;
-  for (int32_t at = b; at < b1 && !order; at += threads)
-    if (max_value<T>(max_bits<T>(r.raw(at))) == m) order = score_order(m, max(r.first(at), 0));
+  float m = -INFINITY;
+  for (int32_t at = b; at < b1; at += threads) {
+    const float most = max_value<T>(max_bits<T>(r.raw(at)));
+    if (most > m || !order) order = score_order(most, max(r.first(at), 0));
+    m = fmaxf(m, most);
+  }
   sync();                                                               // what was found before has been looked at
   uint64_t(*orders)[32] = reinterpret_cast<uint64_t(*)[32]>(room.found);
   orders[warp][lane] = order;
@@ -212,9 +216,15 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   const auto sync = [] { if (ONE_WARP) __syncwarp(); else __syncthreads(); };
   if (!ONE_WARP && parts > 1) cluster_arrive();                         // the first block has begun before others write to it
   const RowBatches<T> r(logits + n * row_stride, V);
-  const int32_t b0 = min(r.count, part * share), b1 = min(r.count, b0 + share);
+  const int32_t b0 = min(r.whole_end, r.whole_begin + part * share), b1 = min(r.whole_end, b0 + share);
   const float c = scale * LOG2E;
   const int k = top_k;
+  // an element of the row's ends, for some lanes of the first warp
+  float edge = -INFINITY;
+  if (warp == 0 && lane < 2 * E) {
+    const int32_t i = r.edge(lane);
+    if (i >= 0 && (lane < E ? part == 0 : part == parts - 1)) edge = to_f32(r.row[i]);
+  }
   int64_t target = -1;
   float target_score = 0.f;
   if (part == 0 && tid == 0 && out.logp) {
@@ -226,16 +236,27 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   const uint4 nothing_there = make_uint4(RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW, RowBatches<T>::LOW);
   float m = -INFINITY, base = 0.f, of_unit = -INFINITY, of_units[2] = {-INFINITY, -INFINITY};
   Pair S(0.f, 0.f), P(0.f, 0.f);
+  const auto rescale = [&](float most) {
+    const RowStats s = scaled_to({m, S.sum(), P.sum()}, most, c);
+    S = Pair(s.S, 0.f);
+    P = Pair(s.P, 0.f);
+    m = most;
+    base = base_of(m, c);
+  };
   int group = 0;
   uint4 w[U];
   for (int32_t g = b0; g < b1; g += threads * U, ++group) {
-    const int32_t b = g + tid;
-    const bool all = r.template all_whole<U>(g, b1, tid, threads);
-    r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
-    if (!all) {
+    const int32_t b = g + tid, left = b1 - (b - lane);                  // of the warp's first batch
+    const T* p = r.row + r.first(b);
+    if (left > (U - 1) * threads + 31) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (b + u * threads >= b1) w[u] = nothing_there;
+      for (int u = 0; u < U; ++u, p += threads * E) w[u] = r.load16(p);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u, p += threads * E) {
+        w[u] = nothing_there;
+        if (b + u * threads < b1) w[u] = r.load16(p);
+      }
     }
     uint32_t most_bits = max_bits<T>(w[0]);
 #pragma unroll
@@ -247,25 +268,25 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
       unit_top[unit * threads + tid] = of_unit;
       of_units[unit & 1] = fmaxf(of_units[unit & 1], most);
     }
-    if (most > m) {
-      const RowStats s = scaled_to({m, S.sum(), P.sum()}, most, c);
-      S = Pair(s.S, 0.f);
-      P = Pair(s.P, 0.f);
-      m = most;
-      base = base_of(m, c);
-    }
-    if (!ordinary(base)) {
+    if (most > m) rescale(most);
+    if (ordinary(base)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u * threads >= left) break;
+        add_batch<T, true>(w[u], m, base, c, S, P);
+      }
+    } else {
 #pragma unroll 1
       for (int32_t at = b; at < min(b1, g + threads * U); at += threads) add_batch<T, false>(r.raw(at), m, base, c, S, P);
-    } else if (all) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) add_batch<T, true>(w[u], m, base, c, S, P);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (b + u * threads < b1) add_batch<T, true>(w[u], m, base, c, S, P);
     }
     if (SHORT) break;
+  }
+  if (edge != -INFINITY) {
+    if (edge > m) rescale(edge);
+    const float d = exponent(ordinary(base) ? fmaf(edge, c, -base) : (edge - m) * c), p = exp2_fast(d);
+    S = S + Pair(p, 0.f);
+    P = P + Pair(p * d, 0.f);
+    of_units[0] = fmaxf(of_units[0], edge);
   }
   if (SHORT) of_units[0] = m;
   RowStats st = join_lanes({m, S.sum(), P.sum()}, c);
@@ -288,6 +309,10 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     const float bound = room.bound_score;
     // (-infinity: fewer than k of the groups have a score, those of a short row, or ruled out)
     if (m >= bound && bound != -INFINITY) {
+      if (edge >= bound) {
+        const int at = atomicAdd(&room.found_count, 1);
+        if (at < LOGP_FOUND) room.found[at] = score_order(edge, r.edge(lane));
+      }
       const auto hit = [&](int unit) {
         const int at = atomicAdd(&room.hit_count, 1);
         if (at < LOGP_HITS) room.hits[at] = unit << 16 | tid;
@@ -336,12 +361,12 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
         const int which = room.hits[i >> log_per];
         const int64_t at = b0 + (which & 0xFFFF) + (((int64_t)(which >> 16) << log_per) + (i & ((1 << log_per) - 1))) * threads;
         if (at >= b1) continue;
-        const uint4 batch = r.raw((int32_t)at);
+        const uint4 batch = r.load16(r.row + r.first((int32_t)at));
         float v[E];
         RowBatches<T>::unpack(batch, v);
         unsigned reach = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) reach |= (v[e] >= bound) << e;      // -infinity outside the row
+        for (int e = 0; e < E; ++e) reach |= (v[e] >= bound) << e;
 #pragma unroll 1
         for (; reach; reach &= reach - 1) {
           const int32_t j = r.first((int32_t)at) + __ffs(reach) - 1;
@@ -369,7 +394,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
       }
     }
     if (!settled) {
-      best_of_equals<T, ONE_WARP>(r, b0, b1, k, m, room);
+      best_of_equals<T, ONE_WARP>(r, part == 0 ? 0 : b0, part == parts - 1 ? r.count : b1, k, room);
       if (ONE_WARP || parts == 1) {
         if (tid < k) write(tid, room.best[tid]);
         return;
@@ -528,7 +553,7 @@ extern "C" int mts_logprobs_forward(const void* logits, int64_t row_stride, int3
     const ForwardCall a = {row_stride, N, (int32_t)V, scale, targets, top_k, out, s};
     const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
     const int log_parts = log_parts_of(N, batches);
-    const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
+    const int32_t share = (int32_t)ceil_div(V / RowBatches<T>::E, 1 << log_parts);
     // Warps of a row: what a warp does for a row apart from its scores costs as much as a dozen batches a lane, so as few as keep the row short: us
     // with 1, 2, 4, 8 for 50,000 rows of 500 batches 172, 183, 265, 462; 25,000 of 1,000 148, 131, 144, 249; 6,250 of 4,000 153, 98, 95, 102; 2,048 of
     // 16,384 243, 125, 111, 101 (16: 111).  Where that leaves SMs idle more, while a thread has a few batches (300 rows of 1,250: 19.0, 11.8, 9.4, 8.6).

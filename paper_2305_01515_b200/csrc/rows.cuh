@@ -35,10 +35,17 @@ struct RowBatches {
     return READ_ONLY ? __ldg(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
   }
   const T* row;
-  int32_t V, shift, count;
+  int32_t V, shift, count, whole_begin, whole_end;       // batches [whole_begin, whole_end) are whole
   __device__ __forceinline__ RowBatches(const T* row_, int32_t V_) : row(row_), V(V_) {
     shift = (int32_t)((reinterpret_cast<uintptr_t>(row_) & 15) / sizeof(T));
     count = (int32_t)(((int64_t)V + shift + E - 1) / E);
+    whole_begin = shift != 0;
+    whole_end = max((V + shift) / E, whole_begin);
+  }
+  // Of the elements before the whole batches each of E lanes has one at most, of those behind them the next E lanes; -1: none.
+  __device__ __forceinline__ int32_t edge(int lane) const {
+    const int32_t i = lane < E ? lane : first(whole_end) + lane - E;
+    return i < (lane < E ? min(V, first(whole_begin)) : V) ? i : -1;
   }
   __device__ __forceinline__ int32_t first(int32_t b) const { return b * E - shift; }      // may be negative; at most V + E
   __device__ __forceinline__ bool whole(int32_t b) const { const int32_t i = first(b); return i >= 0 && i <= V - E; }
