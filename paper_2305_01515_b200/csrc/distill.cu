@@ -45,6 +45,7 @@ struct DistillCall {
 struct DistillRoom {
   DistillSums of_warp[DISTILL_WARPS + 1], of_part[1 << MAX_LOG_PARTS];
   float total, q_rest, log_q_rest;
+  uint32_t edges_listed;                                       // of the elements before and behind the whole batches, a bit for the lane that has it
 };
 // Behind it: float q[K], score[K], log_q[K], int32_t place[K], and with the rest's weight the table of the batches that hold a listed item (int32_t batch[],
 // uint32_t places[], first[], of 1 << log_slots places, four times K at least), int32_t slot[K] and the bits of the batches that the pass leaves out.
@@ -102,7 +103,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   const int64_t n = blockIdx.x >> a.log_parts;
   if (parts > 1) cluster_arrive();                             // all blocks have begun before others write to them
   const RowBatches<T, false> r(logits + n * a.row_stride, a.V);
-  const int32_t b0 = min(r.count, part * a.share), b1 = min(r.count, b0 + a.share);
+  const int32_t b0 = min(r.whole_end, r.whole_begin + part * a.share), b1 = min(r.whole_end, b0 + a.share);
   const float c = a.scale * LOG2E;
 
   // the student's sums of this thread
@@ -121,6 +122,12 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     if (REST) {
       const int bytes = min(LISTED_BYTES, (b1 - b0 + threads * U - 1) / (threads * U) * threads);
       for (int i = lane; i < bytes / 4; i += 32) reinterpret_cast<uint32_t*>(left_out)[i] = 0;
+      if (lane == 0) room.edges_listed = 0;
+    }
+    float edge = -INFINITY;
+    if (lane < 2 * E) {
+      const int32_t i = r.edge(lane);
+      if (i >= 0 && (lane < E ? part == 0 : part == parts - 1)) edge = to_f32(r.row[i]);
     }
     __syncwarp();
     float most = -INFINITY;
@@ -135,7 +142,9 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       if (REST && i >= 0 && i < a.V) {
         const int32_t b = (((int32_t)i + r.shift) >> LOG_E) - b0, group = b / (threads * U), in = b - group * threads * U;
         const int64_t byte = (int64_t)group * threads + in % threads;
-        if (b >= 0 && b < b1 - b0 && byte < LISTED_BYTES) atomicOr(reinterpret_cast<uint32_t*>(left_out) + byte / 4, 1u << (in / threads + byte % 4 * 8));
+        if (i < r.first(r.whole_begin)) atomicOr(&room.edges_listed, 1u << i);
+        else if (i >= r.first(r.whole_end)) atomicOr(&room.edges_listed, 1u << (E + i - r.first(r.whole_end)));
+        else if (b >= 0 && b < b1 - b0 && byte < LISTED_BYTES) atomicOr(reinterpret_cast<uint32_t*>(left_out) + byte / 4, 1u << (in / threads + byte % 4 * 8));
       }
     }
     if (REST) bits_ready();                                    // the others may look at the bits and places
@@ -159,6 +168,12 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       room.total = total;
       room.q_rest = any ? e_rest / total : 0.f;
       room.log_q_rest = t_rest - t_base - log_total;
+    }
+    if (edge != -INFINITY) {
+      if (edge > m) rescale(edge);
+      const float p = exp2_fast(ordinary(base) ? fmaf(edge, c, -base) : (edge - m) * c);
+      if (REST && room.edges_listed >> lane & 1) listed += p;
+      else others = others + Pair(p, 0.f);
     }
     if (REST) {
       // the batches that are left out, each for its first place, item by item: a table has the places of a batch's listed items and their first
@@ -212,10 +227,19 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       return false;
     };
     uint4 w[U];
-    bool all = false;
     const auto load = [&](int32_t g) {
-      all = r.template all_whole<U>(g, b1, tid, threads);
-      r.load_held(g, min(b1, g + threads * U), tid, threads, all, w);
+      const int32_t b = g + tid;
+      const T* p = r.row + r.first(b);
+      if (b1 - (b - lane) > (U - 1) * threads + 31) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, p += threads * E) w[u] = r.load16(p);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u, p += threads * E) {
+          w[u] = nothing_there;
+          if (b + u * threads < b1) w[u] = r.load16(p);
+        }
+      }
     };
     if (b0 < b1) load(b0);
     if (REST && (own_warp || warp != 0)) bits_ready();
@@ -223,11 +247,6 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     for (int32_t g = b0; g < b1; g += threads * U) {
       const int32_t b = g + tid;
       if (g > b0) load(g);
-      if (!all) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (b + u * threads >= b1) w[u] = nothing_there;
-      }
       uint32_t most_bits = max_bits<T>(w[0]);
 #pragma unroll
       for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
@@ -253,7 +272,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       } else {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (!all && b + u * threads >= b1) continue;
+          if (u * threads >= b1 - (b - lane)) break;
           float v[E];
           exponentials<T, true>(w[u], m, base, c, v);
           const Pair s = sum_of<T>(v);
@@ -293,7 +312,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
 
   const RowBatches<T> to(grad + n * a.grad_stride, a.V);
   const RowUnder<T> under(r.row, to);
-  const int32_t g0 = min(to.count, part * a.share), g1 = min(to.count, g0 + a.share);
+  const int32_t g0 = part * a.share, g1 = part == parts - 1 ? to.count : g0 + a.share;
   const float w = (a.weights ? a.weights[n] : 1.f) * a.scale, inv_all = all == 0.f ? 0.f : 1.f / all, total = room.total;
   if (w == 0.f || total == 0.f) {
     const float zero[E] = {};
@@ -406,7 +425,7 @@ extern "C" int mts_distill_loss(const void* logits, int64_t row_stride, int32_t 
     using T = decltype(t);
     const int64_t batches = ceil_div(V, RowBatches<T>::E) + 1;          // wherever rows start
     const int log_parts = log_parts_of(N, batches);
-    const int32_t share = (int32_t)ceil_div(batches, 1 << log_parts);
+    const int32_t share = (int32_t)ceil_div(V / RowBatches<T>::E, 1 << log_parts);
     // Warps that sum a row, with its gradient, us with 1, 4, 8 and 16: 20,000 rows of 625 batches 107, 144, 244, 630; 10,000 of 1,250 105, 114, 139, 349; 5,000 of
     // 2,000 102, 73, 89, 191; 4,000 of 5,000 183, 144, 148, 261; 4,096 of 8,192 289, 246, 220, 316; 1,000 of 25,000 330, 257, 212, 181.  More where SMs idle.
     int warps = share <= 1500 ? 1 : share <= 6000 ? 4 : share <= 20000 ? 8 : 16;

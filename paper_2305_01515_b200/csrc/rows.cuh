@@ -48,41 +48,7 @@ struct RowBatches {
     return i < (lane < E ? min(V, first(whole_begin)) : V) ? i : -1;
   }
   __device__ __forceinline__ int32_t first(int32_t b) const { return b * E - shift; }      // may be negative; at most V + E
-  __device__ __forceinline__ bool whole(int32_t b) const { const int32_t i = first(b); return i >= 0 && i <= V - E; }
   static constexpr uint32_t LOW = sizeof(T) == 4 ? 0xFF800000u : (__is_same(T, __half) ? 0xFC00FC00u : 0xFF80FF80u);     // -infinity
-  // Whether all batches begin + (the warp's first thread ... + 31) + u threads, u < U, are whole and before `end`.
-  template <int U>
-  __device__ __forceinline__ bool all_whole(int32_t begin, int32_t end, int tid, int threads) const {
-    const int32_t first_of_warp = begin + (tid & ~31);
-    return first_of_warp >= (shift != 0) && (int64_t)first_of_warp + 31 + (U - 1) * threads < min(end, (V + shift) / E);
-  }
-  // Batches begin + tid + u threads before `end` into w[u]; those behind it are left as they are.
-  template <int U>
-  __device__ __forceinline__ void load_held(int32_t begin, int32_t end, int tid, int threads, bool all, uint4 (&w)[U]) const {
-    const T* p = row + first(begin + tid);
-    if (all) {
-#pragma unroll
-      for (int u = 0; u < U; ++u, p += threads * E) w[u] = load16(p);
-    } else {
-      const int32_t w0 = shift != 0, span = min(end, (V + shift) / E) - w0, b = begin + tid;      // whole batches: [w0, w0 + span)
-#pragma unroll
-      for (int u = 0; u < U; ++u, p += threads * E)
-        if ((uint32_t)(b + u * threads - w0) < (uint32_t)max(span, 0)) w[u] = load16(p);
-      fill_ends(begin, end, tid, threads, w);
-    }
-  }
-  // The row's first and last batch where they are not whole, into those that a thread holds: batch begin + tid + u threads in w[u], up to `end`.
-  template <int U>
-  __device__ __forceinline__ void fill_ends(int32_t begin, int32_t end, int tid, int threads, uint4 (&w)[U]) const {
-    if (begin == 0 && tid == 0 && !whole(0)) w[0] = raw(0);
-    const int32_t last = count - 1, behind = last - begin - tid;          // of the thread's first batch
-    if (last > 0 && last < end && !whole(last) && behind >= 0) {
-      const uint4 edge = raw(last);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (behind == u * threads) w[u] = edge;
-    }
-  }
   // The batch as it is stored, -infinity outside the row.
   __device__ __forceinline__ uint4 raw(int32_t b) const {
     const int32_t i = first(b);
