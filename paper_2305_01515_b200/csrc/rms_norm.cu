@@ -45,8 +45,10 @@ struct Tile {
           }
         }
       } else {
+        const T* const p = row + column(chunk, 0);
+        const int left = D - column(chunk, 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[i][e] = column(chunk, e) < D ? row[column(chunk, e)] : from_f32<T>(0.f);
+        for (int e = 0; e < 8; ++e) s[i][e] = left > 32 * e ? p[32 * e] : from_f32<T>(0.f);
       }
     }
   }
@@ -93,20 +95,17 @@ __device__ __forceinline__ void store8(T* row, int D, int chunk, const float (&v
     }
     return;
   }
+  T* const p = row + Columns::column(chunk, 0);
+  const int left = D - Columns::column(chunk, 0);
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (Columns::column(chunk, e) < D) row[Columns::column(chunk, e)] = from_f32<T>(v[e]);
+    if (left > 32 * e) p[32 * e] = from_f32<T>(v[e]);
 }
 
 struct Weight {
   const void* w;
   int32_t dtype, aligned;                                // aligned: on a 16-byte boundary
 };
-
-__device__ __forceinline__ float weight_at(const Weight& w, int j) {
-  if (w.dtype == MTS_DTYPE_FP32) return __ldg(static_cast<const float*>(w.w) + j);
-  return w.dtype == MTS_DTYPE_FP16 ? to_f32(__ldg(static_cast<const __half*>(w.w) + j)) : to_f32(__ldg(static_cast<const __nv_bfloat16*>(w.w) + j));
-}
 
 // A lane's eight weights, 0 behind the row's end.
 template <bool VECTOR, int LANES>
@@ -128,11 +127,15 @@ __device__ __forceinline__ void weights8(const Weight& w, int D, int chunk, floa
     }
     return;
   }
+  constexpr int STEP = VECTOR ? 1 : 32;
+  const auto one_by_one = [&](auto* p) {
+    p += at;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int j = Tile<float, VECTOR, 1, LANES>::column(chunk, e);
-    v[e] = j < D ? weight_at(w, j) : 0.f;
-  }
+    for (int e = 0; e < 8; ++e) v[e] = D - at > STEP * e ? to_f32(__ldg(p + STEP * e)) : 0.f;
+  };
+  if (w.dtype == MTS_DTYPE_FP32) one_by_one(static_cast<const float*>(w.w));
+  else if (w.dtype == MTS_DTYPE_FP16) one_by_one(static_cast<const __half*>(w.w));
+  else one_by_one(static_cast<const __nv_bfloat16*>(w.w));
 }
 
 // Sum and maximum over the lanes, or the warps, of a row, in a fixed order; `room`: shared, of this row and use alone.
