@@ -2,6 +2,10 @@
 //
 //   r = round(x + residual),  c = 1 / sqrt(mean_j r_j^2 + eps),  y_j = r_j c w_j
 //   dx_j = dr_j + c (dy_j w_j - r_j a),  a = c^2 mean_j(dy_j w_j r_j),   dw_j = sum over rows of dy_j r_j c
+//
+// Memory bounds it: six operations an element forward, a dozen backward.  So a row is read once, held in registers until its sum is known, and written
+// once; the sum of squares, of dw and everything between is fp32 (dw's parts of blocks are added in fp64), and each output is rounded to its type once.  r is rounded before it is
+// normalised because that is the stream which the next layer and the backward see.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -199,6 +203,9 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int D, int chunk, cons
 
 // A row by blockDim.x / 32 warps, up to 1,024 columns by each, or R rows by a warp (times 32 / LANES), so that a warp has four chunks on their way
 // whatever the width; blockDim.y such sets a block.  Everything of a row is in registers between its one reading and its one writing.
+// us, with a residual: 131,072 x 1,024 bf16 162 (6.63 TB/s, the copy rate); 8,192 x 8,192 to 8 bits, groups of 128, 95 (4.8 TB/s: issue slots 71% busy with the
+// codes and their maxima); 120,007 x 256 to 8 bits 44 (4.9 TB/s); 2,000 x 32,768 106 (one block of 1,024 threads an SM, 5.0 TB/s).  100,003 x 333 fp32 without, off
+// boundaries, 52 (5.1 TB/s): single elements, and the last chunk's 179 places that hold none.
 template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS, bool CODES>
 __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VECTOR && sizeof(T) == 2) || R * I <= 2 ? 4 : 2)
 rms_norm_forward(const NormForward<T> a) {
@@ -318,6 +325,7 @@ rms_norm_forward(const NormForward<T> a) {
 }
 
 // Pieces of eight codes where rows and codes lie on boundaries of eight, else single ones: 1 << log_threads threads a row, U pieces on their way for each.
+// 120,007 x 256 codes to bf16: 21 us (4.4 TB/s); 20,011 x 5,000: 58 (5.2).
 template <typename T, bool VECTOR, int U>
 __global__ void __launch_bounds__(256)
 rows_from_8bit(const uint8_t* __restrict__ codes, int64_t codes_stride, const float* __restrict__ scales, int group, int groups, int D, T* __restrict__ out,
@@ -381,9 +389,17 @@ struct NormBackward {
 };
 
 // As many blocks as the GPU holds walk over the rows (shaped as in the forward, with two chunks a warp while there are warps enough: three arrays are in
-// registers); each thread keeps the sums of its columns of the weight's gradient.
+// registers); each thread keeps the sums of its columns of the weight's gradient, and the blocks' sums are added by the kernel below: no atomics, so that
+// results are the same in every run.  131,072 x 1,024 bf16 with the stream's gradient: 200-207 us (5.2-5.4 TB/s of what moves); 100,003 x 333 fp32 88 (4.6).
+// Four chunks a warp and a third fewer warps took 272 us there, one chunk a warp 200 for 332 fp32 columns (112 with two).
+// Where rows are wider than 8,192 columns in fp32 or off boundaries, or than 16,384, the arrays of four chunks do not fit: they are read again for the second part, from L1 or L2 where the
+// row has just passed (3,000 x 32,768 bf16: 391 us with everything held and spilled, 260 so; 5,000 x 10,001 fp32 364 and 271).
 template <typename T>
 __host__ __device__ constexpr int back_blocks(bool vector) { return vector && sizeof(T) == 2 ? 3 : 2; }       // of 256 threads on an SM
+// Warps of a row at most while they hold it: 128 registers a thread where it comes in fp32 or single elements (8,000 x 4,099 fp32: 262 us with 64 and twice the warps, 145
+// so), 64 where it comes in vectors of 16-bit elements (10,000 x 5,000: 168 us with 128, 146 so).
+template <typename T>
+__host__ __device__ constexpr int back_warps(bool vector) { return vector && sizeof(T) == 2 ? NORM_WARPS : 16; }
 template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? back_blocks<T>(VECTOR) : 1)
 rms_norm_backward(const NormBackward<T> a) {
@@ -394,9 +410,10 @@ rms_norm_backward(const NormBackward<T> a) {
   float acc[I][8] = {};
   int turn = 0;
   constexpr int SET = R * (32 / LANES);                  // rows of a warp
+  constexpr bool HELD = I <= 2;                          // in registers between the two parts
   const int64_t step = (int64_t)gridDim.x * blockDim.y * SET;
   for (int64_t set = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * SET; set < a.N; set += step, turn ^= 1) {
-    Tile<T, VECTOR, I, LANES> x[R], g[R], t[R];
+    Tile<T, VECTOR, HELD ? I : 1, LANES> x[R], g[R], t[R];
     float c[R], m[R];
     int64_t row[R];
     int D[R];
@@ -405,9 +422,11 @@ rms_norm_backward(const NormBackward<T> a) {
       row[r] = set + r * (32 / LANES) + lane_id() / LANES;
       D[r] = row[r] < a.N ? a.D : 0;
       if (row[r] >= a.N) row[r] = a.N - 1;
-      x[r].load(a.x + row[r] * a.x_stride, D[r], warp, warps);
-      g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp, warps);
-      if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp, warps);
+      if (HELD) {
+        x[r].load(a.x + row[r] * a.x_stride, D[r], warp, warps);
+        g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp, warps);
+        if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp, warps);
+      }
       c[r] = a.inv_rms[row[r]];
       m[r] = 0.f;
     }
@@ -418,8 +437,12 @@ rms_norm_backward(const NormBackward<T> a) {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[8], dy[8];
-        x[r].get(i, y);
-        g[r].get(i, dy);
+        if (!HELD) {
+          x[r].load(a.x + row[r] * a.x_stride, D[r], warp + i * warps, warps);
+          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp + i * warps, warps);
+        }
+        x[r].get(HELD ? i : 0, y);
+        g[r].get(HELD ? i : 0, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[r] = fmaf(dy[e] * w[e], y[e], m[r]);
       }
@@ -433,8 +456,13 @@ rms_norm_backward(const NormBackward<T> a) {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[8], dy[8], d[8];
-        x[r].get(i, y);
-        g[r].get(i, dy);
+        if (!HELD) {
+          x[r].load(a.x + row[r] * a.x_stride, D[r], warp + i * warps, warps);
+          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp + i * warps, warps);
+          if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp + i * warps, warps);
+        }
+        x[r].get(HELD ? i : 0, y);
+        g[r].get(HELD ? i : 0, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           d[e] = c[r] * (dy[e] * w[e] - y[e] * m[r]);
@@ -442,7 +470,7 @@ rms_norm_backward(const NormBackward<T> a) {
         }
         if (a.grad_sum) {
           float o[8];
-          t[r].get(i, o);
+          t[r].get(HELD ? i : 0, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e) d[e] += o[e];
         }
@@ -479,7 +507,7 @@ rms_norm_backward(const NormBackward<T> a) {
   }
 }
 
-// The blocks' sums, 32 columns a block, in 64 bits.
+// The blocks' sums, 32 columns a block, in 64 bits (6 us).
 __global__ void __launch_bounds__(1024)
 rms_norm_weight_gradient(const float* __restrict__ partial, int blocks, int D, float* __restrict__ grad_weight) {
   __shared__ double room[32][33];
@@ -523,12 +551,13 @@ Weight weight_of(const void* w, int32_t dtype) { return {w, dtype, ((uintptr_t)w
 // Bits of the places where rows start.
 uintptr_t rows_bits(const void* p, int64_t stride, int32_t dtype) { return (uintptr_t)p | (uintptr_t)(stride * dtype_bytes(dtype)); }
 
-// Warps of a row, chunks of each, lanes of a row, and sets (rows, or what a warp has of them) of a block.
+// Warps of a row, chunks of each, lanes of a row, and sets (rows, or what a warp has of them) of a block.  Chunks of a warp: most_chunks, or all four where
+// that takes more than most_warps.
 struct RowShape { int warps, chunks, lanes, sets; };
-RowShape shape_of(int32_t D, bool vector, int most_chunks) {
+RowShape shape_of(int32_t D, bool vector, int most_chunks, int most_warps) {
   const int chunks = (D + NORM_CHUNK - 1) / NORM_CHUNK;
   if (chunks <= most_chunks) return {1, chunks <= 2 ? chunks : 4, vector && D <= 32 ? 4 : vector && D <= 64 ? 8 : vector && D <= 128 ? 16 : 32, 8};
-  if ((chunks + most_chunks - 1) / most_chunks > NORM_WARPS) most_chunks = NORM_CHUNKS;
+  if ((chunks + most_chunks - 1) / most_chunks > most_warps) most_chunks = NORM_CHUNKS;
   const int warps = (chunks + most_chunks - 1) / most_chunks;
   return {warps, most_chunks, 32, most_chunks == 2 && warps <= 4 ? 8 / warps : 1};
 }
@@ -542,6 +571,7 @@ void with_shape(bool vector, bool several, const RowShape& shape, Fn&& fn) {
   using One = integral_constant<int, 1>;
   using Full = integral_constant<int, 32>;
   using Small = integral_constant<int, 256>;
+  using Middle = integral_constant<int, 512>;
   using Large = integral_constant<int, 1024>;
   const bool small = shape.warps * shape.sets <= 8;
   const auto with_rows = [&](auto v, auto chunks, auto lanes) {
@@ -556,7 +586,12 @@ void with_shape(bool vector, bool several, const RowShape& shape, Fn&& fn) {
     if constexpr (MOST == 4) {
       if (small) return fn(v, One(), integral_constant<int, 4>(), Full(), Small());
     } else {
-      if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Large());
+      if constexpr (back_warps<T>(decltype(v)::value) == 16) {
+        if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Middle());
+        if (shape.warps <= 16) return fn(v, One(), integral_constant<int, 4>(), Full(), Middle());
+      } else {
+        if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Large());
+      }
     }
     return fn(v, One(), integral_constant<int, 4>(), Full(), Large());
   };
@@ -594,7 +629,7 @@ int norm_forward(const char* what, const void* x, int64_t x_stride, const void* 
     const uintptr_t bits = rows_bits(x, x_stride, dtype) | (residual ? rows_bits(residual, residual_stride, dtype) | rows_bits(sum_out, sum_stride, dtype) : 0) |
                            (codes ? 0 : rows_bits(out, out_stride, dtype));
     const bool vector = bits % 16 == 0;
-    const RowShape shape = shape_of(D, vector, NORM_CHUNKS);
+    const RowShape shape = shape_of(D, vector, NORM_CHUNKS, NORM_WARPS);
     const dim3 block(32 * shape.warps, shape.sets);
     const bool several = several_rows(shape, vector, dtype, N, NORM_CHUNKS);
     const unsigned grid = (unsigned)ceil_div(N, rows_of(shape, several, NORM_CHUNKS));
@@ -693,11 +728,11 @@ extern "C" int mts_rms_norm_backward(const void* x, int64_t x_stride, const void
     const uintptr_t bits = rows_bits(x, x_stride, dtype) | rows_bits(grad_out, grad_out_stride, dtype) | (grad_sum ? rows_bits(grad_sum, grad_sum_stride, dtype) : 0) |
                            rows_bits(grad_x, grad_x_stride, dtype);
     const bool vector = bits % 16 == 0;
-    const RowShape shape = shape_of(D, vector, 2);
+    const RowShape shape = shape_of(D, vector, 2, back_warps<T>(vector));
     // blocks that the GPU holds at once
     const bool several = several_rows(shape, vector, dtype, N, 2);
     const int64_t wanted = ceil_div(N, rows_of(shape, several, 2)), threads = shape.warps * shape.sets * 32;
-    const int64_t most = threads <= 256 ? 148 * back_blocks<T>(vector) : threads <= 512 ? 296 : 148;
+    const int64_t most = threads <= 256 ? 148 * back_blocks<T>(vector) : threads <= 512 && back_warps<T>(vector) == NORM_WARPS ? 296 : 148;
     const int blocks = (int)(wanted < most ? wanted : most);
     {
       LaunchScope scope(K_NORM_BWD, s);
