@@ -3,6 +3,9 @@
 //   q = softmax of scale teacher_k over the listed items (and exp(rest) for all others together),  p = softmax(scale x)
 //   loss = sum_k q_k (log q_k - log p_{i_k}) + q_rest (log q_rest - log p_rest),   p_rest = what p gives to the items not listed
 //   dx_v = weight scale (p_v - q_v) for a listed item, weight scale p_v (1 - q_rest / p_rest) for another
+//
+// The loss reads the scores once; with the gradient they are read again and it is written, all in one launch, so that the second reading comes from L2.  Sums and the
+// teacher's distribution are fp32, the gradient is rounded to its type once.
 #include "rows.cuh"
 
 namespace mts {
@@ -81,6 +84,9 @@ __device__ __forceinline__ void bits_ready() { asm volatile("bar.sync 1;" ::: "m
 // digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
 // leaves these out, and they are added afterwards item by item.
 // The gradient is written as if nothing were listed, and the listed places once more.
+// us: 4,096 x 65,536 bf16, 50 items, with gradient 215 (5.0 TB/s of its floor's bytes; 7% more reads than that, issue slots 47% busy: a block's warps sum, wait for each other and write in
+// turn); 2,047 x 32,003 fp16, 64 items and the rest, 75, loss alone 40; 20,000 x 5,001 fp32, 20 and the rest, 186; 64 x 20,000 fp32, loss alone, 6-8: latency.  Rows kept in shared
+// memory between the passes took longer (fewer blocks an SM), and so did clusters for many rows.
 template <typename T, bool REST>
 __global__ void __maxnreg__(64)                                // of (DISTILL_WARPS + 1) * 32 threads at most: 32 warps an SM
 distill_loss(const T* logits, T* grad, const DistillCall a) {

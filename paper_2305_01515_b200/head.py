@@ -1,6 +1,8 @@
 """Torch plumbing for the head of the sequence tower: the norm of the residual stream, log probabilities of given items under a softmax over
 the catalogue, and the loss against a larger tower's best items.  As in `sequence`, nothing here computes anything on its own: every step is a
-call into libmtrains_b200.so on torch's current stream of the tensors' device.  First derivatives only (torch raises where others are asked for)."""
+call into libmtrains_b200.so on torch's current stream of the tensors' device.  First derivatives only (torch raises where others are asked for).
+Calls may be captured into CUDA graphs; a backward pass is captured while no autograd graph of an eager pass over the same leaves is alive, as torch
+wants it."""
 from __future__ import annotations
 
 from typing import NamedTuple, Optional

@@ -235,3 +235,27 @@ def test_offsets_past_32_bits():
     torch.cuda.synchronize()
     want, c = norm64(x.double(), w.double())
     close(out, want, want.abs() * (2.0 ** -11 + 100 * U) + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("N,D", [(330, 2500), (500, 4104), (350, 8201), (310, 16384), (301, 16389), (200, 20008)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_backward_of_wide_rows_many_to_a_block(N, D, dtype):
+    """Rows that a block's warps share, several to a block one after the other; the gradient in the place of either input of it too."""
+    g = torch.Generator(device=DEV).manual_seed(N + D)
+    x, dy, ds = (torch.randn(N, D, generator=g, device=DEV).to(dtype) for _ in range(3))
+    w = 1 + 0.3 * torch.randn(D, generator=g, device=DEV)
+    inv = norm64(x.double(), w.double())[1][:, 0].float()
+    ws = torch.full((mb.rms_norm_workspace_bytes(N, D),), 255, dtype=torch.uint8, device=DEV)
+
+    def run(dy, ds, dx):
+        dw = torch.full((D,), -5.0, device=DEV)
+        mb.rms_norm_backward(x, D, w, 0, KIND[dtype], N, D, inv, dy, D, ds, D, dx, D, dw, ws, ws.numel())
+        torch.cuda.synchronize()
+        return dx, dw
+
+    dx, dw = run(dy, ds, torch.empty_like(x))
+    want, size, dw64, dw_size, _ = backward64(x.double(), w.double(), dy.double(), ds.double())
+    close(dx, want, want.abs() * half(dtype) + size * (SUM + 10 * U) + 2.0 ** -25 * (dtype == torch.float16))
+    close(dw, dw64, dw_size * (N + 6) * U)
+    a, b = dy.clone(), ds.clone()
+    assert all(torch.equal(p, q) for p, q in zip(run(a, ds, a), (dx, dw))) and all(torch.equal(p, q) for p, q in zip(run(dy, b, b), (dx, dw)))
