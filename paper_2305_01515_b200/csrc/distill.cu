@@ -84,7 +84,7 @@ __device__ __forceinline__ void bits_ready() { asm volatile("bar.sync 1;" ::: "m
 // digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
 // leaves these out, and they are added afterwards item by item.
 // The gradient is written as if nothing were listed, and the listed places once more.
-// us: 4,096 x 65,536 bf16, 50 items, with gradient 215 (5.0 TB/s of its floor's bytes; 7% more reads than that, issue slots 47% busy: a block's warps sum, wait for each other and write in
+// us: 4,096 x 65,536 bf16, 50 items, with gradient 215 (5.0 TB/s of its floor's bytes; 6% more reads than the scores, issue slots 47% busy: a block's warps sum, wait for each other and write in
 // turn); 2,047 x 32,003 fp16, 64 items and the rest, 75, loss alone 40; 20,000 x 5,001 fp32, 20 and the rest, 186; 64 x 20,000 fp32, loss alone, 6-8: latency.  Rows kept in shared
 // memory between the passes took longer (fewer blocks an SM), and so did clusters for many rows.
 template <typename T, bool REST>

@@ -444,7 +444,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   }
 }
 
-// Gradient, dx = p (alpha + beta d) + [v = target] scale g_logp: 4,099 x 50,001 bf16, rows of gradients and of scores at different places, 131-142 us (5.8-6.3 TB/s, 89-96% of
+// Gradient, dx = p (alpha + beta d) + [v = target] scale g_logp: 4,099 x 50,001 bf16, rows of gradients and of scores at different places, 131-147 us (5.6-6.3 TB/s, 85-96% of
 // the copy rate); issue slots 80% busy with the shifts.  A thread takes BACK_UNROLL batches of the gradient's row (16 bytes that start on a 16-byte boundary of it) and reads the scores that lie under them.
 constexpr int BACK_THREADS = 256, BACK_UNROLL = 4;
 
