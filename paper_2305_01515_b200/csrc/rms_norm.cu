@@ -373,6 +373,8 @@ rows_from_8bit(const uint8_t* __restrict__ codes, int64_t codes_stride, const fl
   }
 }
 
+constexpr int NORM_BACK_WARPS = 16;                      // of a row at most
+static_assert(NORM_BACK_WARPS * NORM_CHUNK * 8 >= MTS_RMS_NORM_MAX_D, "eight chunks a warp hold the widest row");
 constexpr int NORM_BACK_BLOCKS = 444;                    // at most: each leaves a row of partial sums of the weight's gradient
 
 template <typename T>
@@ -392,16 +394,17 @@ struct NormBackward {
 // registers); each thread keeps the sums of its columns of the weight's gradient, and the blocks' sums are added by the kernel below: no atomics, so that
 // results are the same in every run.  131,072 x 1,024 bf16 with the stream's gradient: 200-207 us (5.2-5.4 TB/s of what moves); 100,003 x 333 fp32 88 (4.6).
 // Four chunks a warp and a third fewer warps took 272 us there, one chunk a warp 200 for 332 fp32 columns (112 with two).
-// Where rows are wider than 8,192 columns in fp32 or off boundaries, or than 16,384, the arrays of four chunks do not fit: they are read again for the second part, from L1 or L2 where the
-// row has just passed (3,000 x 32,768 bf16: 391 us with everything held and spilled, 260 so; 5,000 x 10,001 fp32 364 and 271).
+// A thread has 80 registers where rows come in vectors of 16-bit elements and a warp has two chunks, 128 else, and spills none: no instance has a stack.  A row has 16 warps at
+// most; where two chunks for each do not hold it they have four or eight.  Where the arrays of these do not fit (HELD false) they are read again for the second part,
+// from L1 or L2 where the row has just passed.  us: 10,000 x 5,000 bf16 117 (3 arrays, 2.6 TB/s), 6,000 x 16,384 242 (with the stream's gradient, 3.3), 3,000 x 32,768 264 and 332
+// (2.2 and 2.4); fp32 8,000 x 4,099 135 (2.9), 6,000 x 8,192 141 (4.2), 5,000 x 10,001 195 (3.1); 5,000 x 10,001 fp16 188 (1.6).
 template <typename T>
-__host__ __device__ constexpr int back_blocks(bool vector) { return vector && sizeof(T) == 2 ? 3 : 2; }       // of 256 threads on an SM
-// Warps of a row at most while they hold it: 128 registers a thread where it comes in fp32 or single elements (8,000 x 4,099 fp32: 262 us with 64 and twice the warps, 145
-// so), 64 where it comes in vectors of 16-bit elements (10,000 x 5,000: 168 us with 128, 146 so).
+__host__ __device__ constexpr int back_blocks(bool vector) { return vector && sizeof(T) == 2 ? 3 : 2; }       // of 256 threads on an SM, two chunks a warp
+// Warps of a row at most while they have two chunks each.
 template <typename T>
-__host__ __device__ constexpr int back_warps(bool vector) { return vector && sizeof(T) == 2 ? NORM_WARPS : 16; }
+__host__ __device__ constexpr int back_warps(bool vector) { return vector && sizeof(T) == 2 ? 12 : NORM_BACK_WARPS; }
 template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? back_blocks<T>(VECTOR) : 1)
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? back_blocks<T>(VECTOR) : THREADS == 384 ? 2 : 1)
 rms_norm_backward(const NormBackward<T> a) {
   using Columns = Tile<T, VECTOR, 1, LANES>;
   __shared__ float room[2][NORM_WARPS];
@@ -409,11 +412,19 @@ rms_norm_backward(const NormBackward<T> a) {
   const int warp = threadIdx.x / 32, warps = blockDim.x / 32;
   float acc[I][8] = {};
   int turn = 0;
+  // A warp's i-th chunk; eight of them would have their addresses kept from row to row, for which there are no registers.
+  const auto chunk_of = [&](int i) {
+    int chunk = warp + i * warps;
+    if (I == 8) asm volatile("" : "+r"(chunk));
+    return chunk;
+  };
   constexpr int SET = R * (32 / LANES);                  // rows of a warp
-  constexpr bool HELD = I <= 2;                          // in registers between the two parts
+  constexpr bool HELD = I <= (VECTOR && sizeof(T) == 2 ? 4 : 2);      // in registers between the two parts
+  constexpr bool LATE = HELD && I == 4;                  // but for the stream's gradient, which the second part reads
   const int64_t step = (int64_t)gridDim.x * blockDim.y * SET;
   for (int64_t set = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * SET; set < a.N; set += step, turn ^= 1) {
-    Tile<T, VECTOR, HELD ? I : 1, LANES> x[R], g[R], t[R];
+    Tile<T, VECTOR, HELD ? I : 1, LANES> x[R], g[R];
+    Tile<T, VECTOR, HELD && !LATE ? I : 1, LANES> t[R];
     float c[R], m[R];
     int64_t row[R];
     int D[R];
@@ -425,21 +436,22 @@ rms_norm_backward(const NormBackward<T> a) {
       if (HELD) {
         x[r].load(a.x + row[r] * a.x_stride, D[r], warp, warps);
         g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp, warps);
-        if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp, warps);
+        if (a.grad_sum && !LATE) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp, warps);
       }
       c[r] = a.inv_rms[row[r]];
       m[r] = 0.f;
     }
 #pragma unroll
     for (int i = 0; i < I; ++i) {
+      const int chunk = chunk_of(i);
       float w[8];
-      weights8<VECTOR, LANES>(a.weight, a.D, warp + i * warps, w);
+      weights8<VECTOR, LANES>(a.weight, a.D, chunk, w);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[8], dy[8];
         if (!HELD) {
-          x[r].load(a.x + row[r] * a.x_stride, D[r], warp + i * warps, warps);
-          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp + i * warps, warps);
+          x[r].load(a.x + row[r] * a.x_stride, D[r], chunk, warps);
+          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], chunk, warps);
         }
         x[r].get(HELD ? i : 0, y);
         g[r].get(HELD ? i : 0, dy);
@@ -451,15 +463,15 @@ rms_norm_backward(const NormBackward<T> a) {
     for (int r = 0; r < R; ++r) m[r] = row_sum<LANES>(m[r], room[turn] + threadIdx.y * warps, warp, R == 1 ? warps : 1) / a.D * (c[r] * c[r]);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
+      const int chunk = chunk_of(i);
       float w[8];
-      weights8<VECTOR, LANES>(a.weight, a.D, warp + i * warps, w);
+      weights8<VECTOR, LANES>(a.weight, a.D, chunk, w);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float y[8], dy[8], d[8];
         if (!HELD) {
-          x[r].load(a.x + row[r] * a.x_stride, D[r], warp + i * warps, warps);
-          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], warp + i * warps, warps);
-          if (a.grad_sum) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], warp + i * warps, warps);
+          x[r].load(a.x + row[r] * a.x_stride, D[r], chunk, warps);
+          g[r].load(a.grad_out + row[r] * a.out_stride, D[r], chunk, warps);
         }
         x[r].get(HELD ? i : 0, y);
         g[r].get(HELD ? i : 0, dy);
@@ -469,12 +481,14 @@ rms_norm_backward(const NormBackward<T> a) {
           acc[i][e] = fmaf(dy[e], y[e] * c[r], acc[i][e]);
         }
         if (a.grad_sum) {
+          if (I == 8 && !VECTOR) asm volatile("" ::: "memory");      // not before x and dy have been used
           float o[8];
-          t[r].get(HELD ? i : 0, o);
+          if (!HELD || LATE) t[r].load(a.grad_sum + row[r] * a.sum_stride, D[r], chunk, warps);
+          t[r].get(HELD && !LATE ? i : 0, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e) d[e] += o[e];
         }
-        store8<T, VECTOR, LANES>(a.grad_x + row[r] * a.gx_stride, D[r], warp + i * warps, d);
+        store8<T, VECTOR, LANES>(a.grad_x + row[r] * a.gx_stride, D[r], chunk, d);
       }
     }
   }
@@ -551,13 +565,13 @@ Weight weight_of(const void* w, int32_t dtype) { return {w, dtype, ((uintptr_t)w
 // Bits of the places where rows start.
 uintptr_t rows_bits(const void* p, int64_t stride, int32_t dtype) { return (uintptr_t)p | (uintptr_t)(stride * dtype_bytes(dtype)); }
 
-// Warps of a row, chunks of each, lanes of a row, and sets (rows, or what a warp has of them) of a block.  Chunks of a warp: most_chunks, or all four where
-// that takes more than most_warps.
+// Warps of a row, chunks of each, lanes of a row, and sets (rows, or what a warp has of them) of a block.  Chunks of a warp: most_chunks, or twice and four times as
+// many where that takes more than most_warps (in the backward alone, and then NORM_BACK_WARPS).
 struct RowShape { int warps, chunks, lanes, sets; };
 RowShape shape_of(int32_t D, bool vector, int most_chunks, int most_warps) {
   const int chunks = (D + NORM_CHUNK - 1) / NORM_CHUNK;
   if (chunks <= most_chunks) return {1, chunks <= 2 ? chunks : 4, vector && D <= 32 ? 4 : vector && D <= 64 ? 8 : vector && D <= 128 ? 16 : 32, 8};
-  if ((chunks + most_chunks - 1) / most_chunks > most_warps) most_chunks = NORM_CHUNKS;
+  for (; (chunks + most_chunks - 1) / most_chunks > most_warps; most_warps = NORM_BACK_WARPS) most_chunks *= 2;
   const int warps = (chunks + most_chunks - 1) / most_chunks;
   return {warps, most_chunks, 32, most_chunks == 2 && warps <= 4 ? 8 / warps : 1};
 }
@@ -585,15 +599,12 @@ void with_shape(bool vector, bool several, const RowShape& shape, Fn&& fn) {
     if (shape.chunks == 2 && small) return with_rows(v, integral_constant<int, 2>(), Full());
     if constexpr (MOST == 4) {
       if (small) return fn(v, One(), integral_constant<int, 4>(), Full(), Small());
+      return fn(v, One(), integral_constant<int, 4>(), Full(), Large());
     } else {
-      if constexpr (back_warps<T>(decltype(v)::value) == 16) {
-        if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Middle());
-        if (shape.warps <= 16) return fn(v, One(), integral_constant<int, 4>(), Full(), Middle());
-      } else {
-        if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), Large());
-      }
+      if (shape.chunks == 2) return fn(v, One(), integral_constant<int, 2>(), Full(), integral_constant<int, back_warps<T>(decltype(v)::value) * 32>());
+      if (shape.chunks == 4) return fn(v, One(), integral_constant<int, 4>(), Full(), Middle());
+      return fn(v, One(), integral_constant<int, 8>(), Full(), Middle());
     }
-    return fn(v, One(), integral_constant<int, 4>(), Full(), Large());
   };
   if (shape.lanes == 4) with_rows(std::true_type(), One(), integral_constant<int, 4>());
   else if (shape.lanes == 8) with_rows(std::true_type(), One(), integral_constant<int, 8>());
@@ -732,7 +743,7 @@ extern "C" int mts_rms_norm_backward(const void* x, int64_t x_stride, const void
     // blocks that the GPU holds at once
     const bool several = several_rows(shape, vector, dtype, N, 2);
     const int64_t wanted = ceil_div(N, rows_of(shape, several, 2)), threads = shape.warps * shape.sets * 32;
-    const int64_t most = threads <= 256 ? 148 * back_blocks<T>(vector) : threads <= 512 && back_warps<T>(vector) == NORM_WARPS ? 296 : 148;
+    const int64_t most = 148 * (threads <= 256 ? (shape.chunks <= 2 ? back_blocks<T>(vector) : 2) : threads <= 384 && shape.chunks == 2 && back_warps<T>(vector) == 12 ? 2 : 1);
     const int blocks = (int)(wanted < most ? wanted : most);
     {
       LaunchScope scope(K_NORM_BWD, s);

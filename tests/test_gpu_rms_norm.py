@@ -259,3 +259,25 @@ def test_backward_of_wide_rows_many_to_a_block(N, D, dtype):
     close(dw, dw64, dw_size * (N + 6) * U)
     a, b = dy.clone(), ds.clone()
     assert all(torch.equal(p, q) for p, q in zip(run(a, ds, a), (dx, dw))) and all(torch.equal(p, q) for p, q in zip(run(dy, b, b), (dx, dw)))
+
+
+@pytest.mark.parametrize("N,D", [(301, 4097), (297, 6144), (299, 6152), (149, 8192), (150, 8200), (298, 12296), (151, 16384), (149, 16392), (150, 24577), (149, 32767),
+                                 (297, 32768)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("with_sum", [False, True])
+def test_backward_of_widths_where_the_rows_shape_changes(N, D, dtype, with_sum):
+    """The widths at which a warp takes two, four and eight chunks, by vectors and (odd ones) by elements, with more rows than blocks."""
+    g = torch.Generator(device=DEV).manual_seed(N + D)
+    x, dy, ds = (torch.randn(N, D, generator=g, device=DEV).to(dtype) for _ in range(3))
+    ds = ds if with_sum else None
+    w = (1 + 0.3 * torch.randn(D, generator=g, device=DEV)).to(dtype)
+    inv = norm64(x.double(), w.double())[1][:, 0].float()
+    dx, room = placed(torch.zeros(N, D), dtype, 0, 0)
+    ws = torch.full((mb.rms_norm_workspace_bytes(N, D),), 255, dtype=torch.uint8, device=DEV)
+    dw = torch.full((D,), -5.0, device=DEV)
+    mb.rms_norm_backward(x, D, w, KIND[dtype], KIND[dtype], N, D, inv, dy, D, ds, D, dx, D, dw, ws, ws.numel())
+    torch.cuda.synchronize()
+    want, size, dw64, dw_size, _ = backward64(x.double(), w.double(), dy.double(), None if ds is None else ds.double())
+    close(dx, want, want.abs() * half(dtype) + size * (SUM + 10 * U) + 2.0 ** -25 * (dtype == torch.float16))
+    close(dw, dw64, dw_size * (N + 6) * U)
+    assert untouched(dx, room)
