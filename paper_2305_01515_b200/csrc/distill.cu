@@ -19,7 +19,7 @@ struct DistillSums { float m, listed, others; };
 
 __device__ __forceinline__ DistillSums scaled_to(const DistillSums& s, float m, float c) {
   if (s.m == -INFINITY) return {m, s.listed, s.others};
-  const float base = base_of(m, c), f = exp2_fast(ordinary(base) ? base_of(s.m, c) - base : (s.m - m) * c);
+  const float f = exp2_fast(change_of_base(s.m, m, c));
   return {m, f * s.listed, f * s.others};
 }
 __device__ __forceinline__ DistillSums join_lanes(DistillSums s, float c) {

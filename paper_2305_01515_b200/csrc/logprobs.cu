@@ -31,7 +31,7 @@ struct LogprobsOut {
 struct RowStats { float m, S, P; };
 
 __device__ __forceinline__ RowStats scaled_to(const RowStats& s, float m, float c) {
-  const float base = base_of(m, c), a = exponent(ordinary(base) ? base_of(s.m, c) - base : (s.m - m) * c), f = exp2_fast(a);
+  const float a = exponent(change_of_base(s.m, m, c)), f = exp2_fast(a);
   return s.m == -INFINITY ? RowStats{m, s.S, s.P} : RowStats{m, f * s.S, f * (s.P + s.S * a)};
 }
 // Those of a warp's lanes together.

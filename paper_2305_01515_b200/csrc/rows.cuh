@@ -246,12 +246,20 @@ __device__ __forceinline__ float max_value(uint32_t m) {
   return fmaxf(fmaxf(f.x, f.y), -INFINITY);
 }
 
-// Exponents of a softmax are taken relative to the largest score m: c x - base with base = c m rounded (its error is put right at the end), which is one
-// instruction; where base is no finite number (scores of about 2e38 and more, or none but the lowest of their type) it is c (x - m).
+// Exponents of a softmax are taken relative to the largest score m: c x - base with base = c m rounded, which is one instruction and leaves out no more of c m than
+// half a unit of base's last place; that is put right at the end.  Below 2^23 it is less than one half, so that terms are at most 2^0.5.  From there on (large scales, or
+// nothing but a mask's lowest value seen so far) it could be anything, and the exponent is c (x - m).
 __device__ __forceinline__ float base_of(float m, float c) { return m == -INFINITY ? 0.f : __fmul_rn(m, c); }      // never joined with a sum into one rounding
-__device__ __forceinline__ bool ordinary(float base) { return fabsf(base) < INFINITY; }
+__device__ __forceinline__ bool ordinary(float base) { return fabsf(base) < 8388608.f; }
 // What the logarithm of a sum of 2^(c x - base) has too much by the rounding of the base.
 __device__ __forceinline__ float log_excess(float m, float base, float c) { return ordinary(base) && m != -INFINITY ? fmaf(m, c, -base) * LN2 : 0.f; }
+
+// Exponent of the factor that takes sums relative to `from`, in the form that goes with it, to sums relative to `to`, which is not smaller.
+__device__ __forceinline__ float change_of_base(float from, float to, float c) {
+  const float a = base_of(from, c), b = base_of(to, c);
+  if (ordinary(b)) return ordinary(a) ? a - b : fmaf(from, c, -b);
+  return ordinary(a) ? -fmaf(to, c, -a) : (from - to) * c;
+}
 
 // Clusters: blocks that share a row.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }

@@ -248,3 +248,32 @@ def test_results_are_the_same_in_every_run(N, V):
     first = call(x, index, teacher, rest)
     for _ in range(5):
         assert all(torch.equal(a, b) for a, b in zip(first, call(x, index, teacher, rest)))
+
+
+@pytest.mark.parametrize("mask", [-1e10, -1e30, "lowest"])
+@pytest.mark.parametrize("scale", [0.25, 0.5, 1.0, 1e4, 1e10, 1e30])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [100, 3000, 70001])
+def test_masks_of_large_finite_values_at_every_scale(mask, scale, dtype, V):
+    """scale * score far beyond what fp32 has digits for, in some places, in whole threads' places and in whole rows; scores at scales up to the largest."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    low = torch.finfo(dtype).min
+    low = low if mask == "lowest" else max(mask, low)
+    x = 10 * torch.randn(6, V, generator=g, device=DEV)
+    x[0].masked_fill_(torch.rand(V, generator=g, device=DEV) < 0.5, low)
+    x[1, :V * 3 // 4] = low
+    x[2] = low
+    x[2, V // 3] = 7.0
+    x[3] = low
+    x[4, V // 2:] = low
+    x = x.to(dtype)
+    index = places(6, V, 8, g)
+    index[2, 0] = V // 3
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    teacher = torch.randn(6, 8, generator=g, device=DEV) / scale
+    weights = torch.full((6,), 1.0 / scale, device=DEV)
+    loss, dx = call(x, index, teacher, None, weights, scale)
+    want, bound, d, d_bound = formula(x, index, teacher, None, weights, scale)
+    want = torch.where(want > torch.finfo(torch.float32).max, INF, want)     # weights of about 1/8 times up to 3.4e68: fp32 has no number for them
+    close(loss, want, bound)
+    close(dx, d, d_bound + d.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -25 * (dtype == torch.float16) + 1e-37)

@@ -273,3 +273,36 @@ def test_best_of_long_rows_by_single_blocks(N, V, k, dtype, kind):
         x.masked_fill_(torch.rand(N, V, generator=g, device=DEV) < 1 - 40 / V, -INF)
     x, _ = placed(x, dtype, 0, 3)
     check(x, torch.randint(-1, V, (N,), generator=g, device=DEV), k, 1.0)
+
+
+MASKS = [-1e10, -1e30, "lowest"]
+
+
+def masked_rows(V, dtype, mask):
+    """Rows with masks of large finite values: half of the places, long runs of them, all places but one, all of them, and none."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    low = torch.finfo(dtype).min
+    x = 10 * torch.randn(6, V, generator=g, device=DEV)
+    x[0].masked_fill_(torch.rand(V, generator=g, device=DEV) < 0.5, max(mask, low) if mask != "lowest" else low)
+    x[1, :V * 3 // 4] = max(mask, low) if mask != "lowest" else low
+    x[2] = max(mask, low) if mask != "lowest" else low
+    x[2, V // 3] = 7.0
+    x[3] = max(mask, low) if mask != "lowest" else low
+    x[4, V // 2:] = max(mask, low) if mask != "lowest" else low
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("scale", [0.25, 0.5, 1.0, 1e4, 1e10, 1e30])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [100, 3000, 70001])
+def test_masks_of_large_finite_values_at_every_scale(mask, scale, dtype, V):
+    """scale * score far beyond what fp32 has digits for, in some places, in whole threads' places and in whole rows; scores at scales up to the largest."""
+    x = masked_rows(V, dtype, mask)
+    t = torch.tensor([1, V - 1, V // 3, 5, 3, 2], device=DEV)
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    check(x, t, 4, scale)
+    _, ent, stats, _, _ = forward(x, t, 0, scale)
+    gl, gh = torch.ones(6, device=DEV) / scale, torch.full((6,), 0.5, device=DEV) / scale
+    want, bound = gradient64(x, t, gl, gh, scale)
+    close(backward(x, t, stats, ent, gl, gh, scale), want, bound + want.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -25 * (dtype == torch.float16) + 1e-37)
