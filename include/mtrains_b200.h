@@ -783,7 +783,8 @@ int mts_logprobs_backward(const void* logits, int64_t row_stride, int32_t dtype,
  * loss fp32 [N] (not weighted); grad_logits [N, V] of the scores' type, nullable (loss alone); weights fp32 [N], NULL = 1: the gradient of the
  * loss that is made of these rows.  teacher_index int64 [N, K], teacher_logits [N, K] of a type of their own, both contiguous.
  * A negative index leaves its place out (rows with fewer than K); an index >= V makes the row's loss and gradient NaN; an index given
- * more than once has the sum of its places' q, its item counting once in p_rest.  Where nothing is left of the teacher's row, loss and gradient are 0.  A
+ * more than once has the sum of its places' q, its item counting once in p_rest.  p_rest is summed relative to the best of its items, so that what listed items far above
+ * them leave is not lost; from 2^-16384 on it counts as 0 (all others ruled out).  Where nothing is left of the teacher's row, loss and gradient are 0.  A
  * score of -infinity is an item that the student rules out: infinite loss where the teacher gives it any weight, the gradient stays
  * finite (p = 0; everywhere in a row in which every item is ruled out).  A row of weight 0 has gradient 0 whatever it holds.  No factor
  * 1 / scale^2 is put in.  grad_logits may be the memory of logits (same stride).

@@ -14,19 +14,23 @@ constexpr int DISTILL_WARPS = 16;
 constexpr int DISTILL_UNROLL = 8, DISTILL_GRAD_UNROLL = 4;     // batches on their way for a thread
 constexpr int LISTED_BYTES = 24576;                            // of the bits that say which batches of a part hold a listed item
 
-// Sums of 2^(c x - base) over a set of scores, relative to their largest: over the listed items where these are told apart, and over the others.
-struct DistillSums { float m, listed, others; };
+// Sums of 2^(c x - base) over a set of scores, each relative to the largest of its own: of all items (the listed ones empty), or of the items that are not listed and
+// of those that are.  What one set has can be hundreds of powers of two below the other.
+struct DistillSums { float m, sum, m_listed, listed; };
 
-__device__ __forceinline__ DistillSums scaled_to(const DistillSums& s, float m, float c) {
-  if (s.m == -INFINITY) return {m, s.listed, s.others};
-  const float f = exp2_fast(change_of_base(s.m, m, c));
-  return {m, f * s.listed, f * s.others};
+__device__ __forceinline__ float scaled_to(float sum, float from, float to, float c) { return from == -INFINITY ? sum : exp2_fast(change_of_base(from, to, c)) * sum; }
+template <bool REST>
+__device__ __forceinline__ DistillSums join_lanes(const DistillSums& s, float c) {
+  DistillSums j = {warp_max(s.m), 0.f, -INFINITY, 0.f};
+  j.sum = warp_sum(scaled_to(s.sum, s.m, j.m, c));
+  if (REST) {
+    j.m_listed = warp_max(s.m_listed);
+    j.listed = warp_sum(scaled_to(s.listed, s.m_listed, j.m_listed, c));
+  }
+  return j;
 }
-__device__ __forceinline__ DistillSums join_lanes(DistillSums s, float c) {
-  const float m = warp_max(s.m);
-  s = scaled_to(s, m, c);
-  return {m, warp_sum(s.listed), warp_sum(s.others)};
-}
+// 2^(c x - base) of one score.
+__device__ __forceinline__ float power(float x, float m, float base, float c) { return exp2_fast(ordinary(base) ? fmaf(x, c, -base) : (x - m) * c); }
 
 __device__ __forceinline__ float teacher_value(const void* t, int dtype, int64_t i) {
   if (dtype == MTS_DTYPE_FP32) return static_cast<const float*>(t)[i];
@@ -54,11 +58,9 @@ struct DistillRoom {
 // uint32_t places[], first[], of 1 << log_slots places, four times K at least), int32_t slot[K] and the bits of the batches that the pass leaves out.
 __host__ __device__ constexpr int rounded16(int bytes) { return (bytes + 15) / 16 * 16; }
 
-// Exponentials of a batch.
-template <typename T, bool ORDINARY>
-__device__ __forceinline__ void exponentials(const uint4& w, float m, float base, float c, float (&v)[RowBatches<T>::E]) {
-  constexpr int E = RowBatches<T>::E;
-  RowBatches<T>::unpack(w, v);
+// Exponentials of a batch's scores.
+template <bool ORDINARY, int E>
+__device__ __forceinline__ void exponentials(float (&v)[E], float m, float base, float c) {
   const Pair minus(-base, -base), c2(c, c);
 #pragma unroll
   for (int e = 0; e < E; e += 2) {
@@ -80,8 +82,8 @@ __device__ __forceinline__ void bits_ready() { asm volatile("bar.sync 1;" ::: "m
 // A row (or a part of it, by a cluster of blocks) by a block.  The sums of the exponentials take one pass over the scores as in the log probabilities; the
 // gradient reads them once more, from L2, where the row has just passed.  One warp gathers the teacher's row and the scores of the listed items (indices, then what
 // they point to: two latencies in a row); where a row has four warps or more it is one of its own, while the others sum.
-// With the rest's weight given (REST) the sum over the items that are not listed is made without the listed ones: what is left of a difference would lose its
-// digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
+// With the rest's weight given (REST) the sum over the items that are not listed is made without the listed ones and relative to their own largest: what is left of a
+// difference, or relative to the row's largest, would lose its digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
 // leaves these out, and they are added afterwards item by item.
 // The gradient is written as if nothing were listed, and the listed places once more.
 // us: 4,096 x 65,536 bf16, 50 items, with gradient 215 (5.0 TB/s of its floor's bytes; 6% more reads than the scores, issue slots 47% busy: a block's warps sum, wait for each other and write in
@@ -113,14 +115,19 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
   const float c = a.scale * LOG2E;
 
   // the student's sums of this thread
-  float m = -INFINITY, base = 0.f, listed = 0.f;
+  float m = -INFINITY, base = 0.f, m_listed = -INFINITY, listed = 0.f;
   Pair others(0.f, 0.f);
   const auto rescale = [&](float most) {
-    const DistillSums s = scaled_to({m, listed, others.sum()}, most, c);
-    listed = s.listed;
-    others = Pair(s.others, 0.f);
+    others = Pair(scaled_to(others.sum(), m, most, c), 0.f);
     m = most;
     base = base_of(m, c);
+  };
+  const auto add_listed = [&](float x) {
+    if (x > m_listed) {
+      listed = scaled_to(listed, m_listed, x, c);
+      m_listed = x;
+    }
+    listed += power(x, m_listed, base_of(m_listed, c), c);
   };
 
   if (warp == (own_warp ? warps : 0)) {
@@ -176,10 +183,12 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       room.log_q_rest = t_rest - t_base - log_total;
     }
     if (edge != -INFINITY) {
-      if (edge > m) rescale(edge);
-      const float p = exp2_fast(ordinary(base) ? fmaf(edge, c, -base) : (edge - m) * c);
-      if (REST && room.edges_listed >> lane & 1) listed += p;
-      else others = others + Pair(p, 0.f);
+      if (REST && room.edges_listed >> lane & 1) {
+        add_listed(edge);
+      } else {
+        if (edge > m) rescale(edge);
+        others = others + Pair(power(edge, m, base, c), 0.f);
+      }
     }
     if (REST) {
       // the batches that are left out, each for its first place, item by item: a table has the places of a batch's listed items and their first
@@ -210,17 +219,20 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
         if (b < b0 || b >= b1) continue;
         const uint32_t slot = slot_of_place[k], places = places_of[slot];
         if (first_of[slot] != k) continue;
-        const uint4 batch = r.raw(b);
-        const float top = max_value<T>(max_bits<T>(batch));
-        if (top > m) rescale(top);
-        float v[E];
-        if (ordinary(base)) exponentials<T, true>(batch, m, base, c, v);
-        else exponentials<T, false>(batch, m, base, c, v);
+        float v[E], top = -INFINITY;
+        RowBatches<T>::unpack(r.raw(b), v);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          if (places >> e & 1) listed += v[e];
-          else others = others + Pair(v[e], 0.f);
+          if (places >> e & 1) {
+            add_listed(v[e]);
+            v[e] = -INFINITY;
+          }
+          top = fmaxf(top, v[e]);
         }
+        if (top > m) rescale(top);
+        if (ordinary(base)) exponentials<true>(v, m, base, c);
+        else exponentials<false>(v, m, base, c);
+        others = others + sum_of<T>(v);
       }
     }
   }
@@ -253,11 +265,6 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     for (int32_t g = b0; g < b1; g += threads * U) {
       const int32_t b = g + tid;
       if (g > b0) load(g);
-      uint32_t most_bits = max_bits<T>(w[0]);
-#pragma unroll
-      for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
-      const float most = max_value<T>(most_bits);
-      if (most > m) rescale(most);
       unsigned out = 0;
       if (REST) {
         if (byte < LISTED_BYTES) {
@@ -266,13 +273,24 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
           for (int u = 0; u < U; ++u) out |= holds_listed(b + u * threads) << u;
         }
         byte += threads;
+        if (out) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (out >> u & 1) w[u] = nothing_there;
+        }
       }
+      uint32_t most_bits = max_bits<T>(w[0]);
+#pragma unroll
+      for (int u = 1; u < U; ++u) most_bits = max_bits<T>(most_bits, w[u]);
+      const float most = max_value<T>(most_bits);
+      if (most > m) rescale(most);
       if (!ordinary(base)) {
 #pragma unroll 1
         for (int u = 0; u < U; ++u) {
           if (b + u * threads >= b1 || out >> u & 1) continue;
           float v[E];
-          exponentials<T, false>(r.raw(b + u * threads), m, base, c, v);
+          RowBatches<T>::unpack(r.raw(b + u * threads), v);
+          exponentials<false>(v, m, base, c);
           others = others + sum_of<T>(v);
         }
       } else {
@@ -280,39 +298,47 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
         for (int u = 0; u < U; ++u) {
           if (u * threads >= b1 - (b - lane)) break;
           float v[E];
-          exponentials<T, true>(w[u], m, base, c, v);
-          const Pair s = sum_of<T>(v);
-          if (!REST || !(out >> u & 1)) others = others + s;
+          RowBatches<T>::unpack(w[u], v);
+          exponentials<true>(v, m, base, c);
+          others = others + sum_of<T>(v);
         }
       }
     }
   }
-  const DistillSums nobody = {-INFINITY, 0.f, 0.f};
-  DistillSums s = join_lanes({m, listed, others.sum()}, c);
+  const DistillSums nobody = {-INFINITY, 0.f, -INFINITY, 0.f};
+  DistillSums s = join_lanes<REST>({m, others.sum(), m_listed, listed}, c);
   if (lane == 0) room.of_warp[warp] = s;
   __syncthreads();
-  s = join_lanes(lane < everyone / 32 ? room.of_warp[lane] : nobody, c);
+  s = join_lanes<REST>(lane < everyone / 32 ? room.of_warp[lane] : nobody, c);
   if (parts > 1) {
     cluster_wait();
     if (tid < parts) {
       const uint32_t to = in_block(&room.of_part[part], tid);
-      asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;" :: "r"(to), "f"(s.m), "f"(s.listed), "f"(s.others) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\tst.shared::cluster.f32 [%0 + 8], %3;\n\tst.shared::cluster.f32 [%0 + 12], %4;"
+                   :: "r"(to), "f"(s.m), "f"(s.sum), "f"(s.m_listed), "f"(s.listed) : "memory");
     }
     cluster_arrive();
     cluster_wait();                                            // (and no block writes over scores that another still reads)
-    s = join_lanes(lane < parts ? room.of_part[lane] : nobody, c);
+    s = join_lanes<REST>(lane < parts ? room.of_part[lane] : nobody, c);
   }
-  const float all = s.listed + s.others, m0 = s.m == -INFINITY ? 0.f : s.m;
-  base = base_of(s.m, c);
+  // of all items, and what of it the ones that are not listed have (all, where they are not told apart)
+  m = REST ? fmaxf(s.m, s.m_listed) : s.m;
+  base = base_of(m, c);
+  if (REST && change_of_base(s.m, m, c) <= LEAST_EXP) s.sum *= 0.f;      // ruled out; NaN stays
+  const float sum = REST ? scaled_to(s.sum, s.m, m, c) : s.sum, all = REST ? sum + scaled_to(s.listed, s.m_listed, m, c) : sum, m0 = m == -INFINITY ? 0.f : m;
+  const float base_rest = REST ? base_of(s.m, c) : base, m0_rest = REST ? (s.m == -INFINITY ? 0.f : s.m) : m0;
   if (warp == 0 && part == 0 && a.loss) {
-    const float off = log_excess(s.m, base, c), log_all = all == 0.f ? 0.f : logf(all) - off;
-    float sum = 0.f;
+    const float log_all = all == 0.f ? 0.f : logf(all) - log_excess(m, base, c);
+    float loss = 0.f;
     for (int k = lane; k < a.K; k += 32) {
-      if (q[k] != 0.f) sum += q[k] * (log_q[k] - ((score[k] - m0) * a.scale - log_all));
+      if (q[k] != 0.f) loss += q[k] * (log_q[k] - ((score[k] - m0) * a.scale - log_all));
     }
-    if (REST && lane == 0 && room.q_rest != 0.f) sum += room.q_rest * (room.log_q_rest - (logf(s.others) - off - log_all));
-    sum = warp_sum(sum);
-    if (lane == 0) a.loss[n] = sum;
+    if (REST && lane == 0 && room.q_rest != 0.f) {
+      const float log_p = logf(s.sum) - log_excess(s.m, base_rest, c) + (s.m == -INFINITY ? 0.f : (s.m - m0) * a.scale) - log_all;
+      loss += room.q_rest * (room.log_q_rest - log_p);
+    }
+    loss = warp_sum(loss);
+    if (lane == 0) a.loss[n] = loss;
   }
   if (!grad) return;
 
@@ -325,14 +351,15 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     for (int32_t b = g0 + tid; b < g1; b += everyone) to.store(b, zero);
     return;
   }
-  const float f = w * (REST && room.q_rest != 0.f && s.others != 0.f ? inv_all - room.q_rest / s.others : inv_all) + total * 0.f;
-  const bool usual = ordinary(base);
+  // of an item that is not listed: p - q_rest p / p_rest = (p_rest - q_rest) 2^(c x - base_rest) / (their sum)
+  const float f = (!REST ? w * inv_all : s.sum == 0.f ? 0.f : w * (sum * inv_all - room.q_rest) / s.sum) + total * 0.f;
+  const bool usual = ordinary(base_rest);
   const auto gradient = [&](const uint4& x, float (&v)[E]) {
     RowBatches<T>::unpack(x, v);
-    const Pair minus(-base, -base), c2(c, c), f2(f, f);
+    const Pair minus(-base_rest, -base_rest), c2(c, c), f2(f, f);
 #pragma unroll
     for (int e = 0; e < E; e += 2) {
-      const float2 d = usual ? fma2(Pair(v[e], v[e + 1]), c2, minus).get() : make_float2((v[e] - m0) * c, (v[e + 1] - m0) * c);
+      const float2 d = usual ? fma2(Pair(v[e], v[e + 1]), c2, minus).get() : make_float2((v[e] - m0_rest) * c, (v[e + 1] - m0_rest) * c);
       const float2 g = (Pair(exp2_fast(d.x), exp2_fast(d.y)) * f2).get();
       v[e] = g.x;
       v[e + 1] = g.y;
@@ -354,7 +381,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
 #pragma unroll
       for (int u = 0; u < GU; ++u, at += everyone * E) {
         RowBatches<T>::unpack(x[u], v);
-        const Pair minus(-base, -base), c2(c, c), f2(f, f);
+        const Pair minus(-base_rest, -base_rest), c2(c, c), f2(f, f);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
           const float2 d = fma2(Pair(v[e], v[e + 1]), c2, minus).get();
@@ -381,7 +408,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     float want = 0.f;
 #pragma unroll 4
     for (int j = 0; j < a.K; ++j) want += place[j] == place[k] ? q[j] : 0.f;
-    const float p = exp2_fast(usual ? fmaf(score[k], c, -base) : (score[k] - m0) * c) * inv_all;
+    const float p = power(score[k], m0, base, c) * inv_all;
     grad[n * a.grad_stride + i] = from_f32<T>(w * (p - want) + total * 0.f);
   }
 }

@@ -277,3 +277,60 @@ def test_masks_of_large_finite_values_at_every_scale(mask, scale, dtype, V):
     want = torch.where(want > torch.finfo(torch.float32).max, INF, want)     # weights of about 1/8 times up to 3.4e68: fp32 has no number for them
     close(loss, want, bound)
     close(dx, d, d_bound + d.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -25 * (dtype == torch.float16) + 1e-37)
+
+
+def formula_of_far_items(x, index, teacher, rest, scale):
+    """(loss, its bound, gradient, its bound) in 64 bits through logarithms, for listed items any distance above the others (all different, rest given).  The bounds are
+    `formula`'s: the two logarithms of sums off by off_o and off_a, the teacher's by off_q, differences of logarithms rounded a few times."""
+    V = x.shape[1]
+    z = x.double() * scale
+    listed = torch.zeros(x.shape, dtype=torch.bool, device=DEV).scatter_(1, index, True)
+    others = z.masked_fill(listed, -INF)
+    lse, lse_o = torch.logsumexp(z, 1, keepdim=True), torch.logsumexp(others, 1, keepdim=True)
+    t = torch.cat([teacher.double() * scale, rest.double().unsqueeze(1)], 1)
+    log_q = torch.log_softmax(t, 1)
+    q = log_q.exp()
+    log_p = torch.cat([z.gather(1, index), lse_o], 1) - lse
+    loss = (q * (log_q - log_p)).sum(1)
+    p, share = (z - lse).exp(), (others - lse_o).exp() * q[:, -1:]
+    g = scale * (p - torch.where(listed, torch.zeros_like(p).scatter_(1, index, q[:, :-1]), share))
+    mean = lambda w, top: (w * torch.where(w > 0, top - z, 0.0)).sum(1, keepdim=True)  # noqa: E731
+    top, top_o = z.amax(1, keepdim=True), others.amax(1, keepdim=True)
+    off_a = (170 + V / 256 + 2 * mean(p, top)) * U
+    off_o = (170 + V / 256 + 2 * mean((others - lse_o).exp(), top_o)) * U
+    far = t.amax(1, keepdim=True) - t
+    off_q = (300 + 4 * far + 2 * (q * far).sum(1, keepdim=True)) * U
+    loss_bound = (q * (2 * off_q * (1 + log_q.abs() + log_p.abs()) + off_a + off_o + 8 * U * (log_q.abs() + log_p.abs()))).sum(1)
+    off_e = (12 + 4 * (torch.where(listed, top, top_o) - z)) * U
+    p_rest = log_p[:, -1:].exp()
+    part = torch.where(listed, 0.0, (others - lse_o).exp())        # of an other: (p_rest - q_rest) times this
+    bound = scale * torch.where(listed, p * (off_a + off_e + (12 + 4 * (top - z)) * U) + q.new_zeros(p.shape).scatter_(1, index, (q * (off_q + 4 * U))[:, :-1]),
+                                part * (p_rest * (off_a + off_o + (12 + 4 * (top - top_o)) * U) + q[:, -1:] * 2 * off_q[:, -1:] + (p_rest + q[:, -1:]) * (off_o + off_e)))
+    return loss, loss_bound, g, bound + 4 * U * g.abs()
+
+
+@pytest.mark.parametrize("above", [-40.0, 0.0, 60.0, 85.0, 100.0, 1000.0])
+@pytest.mark.parametrize("scale", [0.5, 1.0, 8.0])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,K", [(5, 100, 3), (7, 3001, 50), (3, 70003, 20), (600, 9000, 33)])
+def test_listed_items_far_above_the_others(above, scale, dtype, N, V, K):
+    """The rest's place keeps its loss and the others their gradients however little the student gives them: the loss is infinite only where the student rules out all."""
+    g = torch.Generator(device=DEV).manual_seed(V + K)
+    x = torch.randn(N, V, generator=g, device=DEV)
+    index = places(N, V, K, g)
+    index[0] = torch.arange(K, device=DEV) + V - K               # at the row's end
+    x.scatter_add_(1, index, torch.full((N, K), above / scale, device=DEV))
+    x, _ = placed(x, dtype, 1, 3)
+    teacher, rest = 2 * torch.randn(N, K, generator=g, device=DEV), scale + torch.randn(N, generator=g, device=DEV)
+    loss, dx = call(x, index, teacher, rest, None, scale)
+    want, bound, d, d_bound = formula_of_far_items(x, index, teacher, rest, scale)
+    close(loss, want, bound)
+    close(dx, d, d_bound + d.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -25 * (dtype == torch.float16) + 1e-37)
+
+
+def test_formula_of_far_items_against_the_plain_one():
+    g = torch.Generator(device=DEV).manual_seed(9)
+    x = torch.randn(4, 60, generator=g, device=DEV)
+    index, teacher, rest = places(4, 60, 5, g), torch.randn(4, 5, generator=g, device=DEV), torch.randn(4, generator=g, device=DEV)
+    a, b = formula(x, index, teacher, rest, None, 0.8), formula_of_far_items(x, index, teacher, rest, 0.8)
+    assert float((a[0] - b[0]).abs().max()) < 1e-12 and float((a[2] - b[2]).abs().max()) < 1e-12
