@@ -147,7 +147,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     bool wrong = false;
     for (int k = lane; k < a.K; k += 32) {
       const int64_t i = a.index[n * a.K + k];
-      const float t = i >= 0 ? teacher_value(a.teacher, a.teacher_dtype, n * a.K + k) * a.scale : -INFINITY;
+      const float t = i >= 0 ? teacher_value(a.teacher, a.teacher_dtype, n * a.K + k) : -INFINITY;
       wrong |= i >= a.V || isnan(t);
       log_q[k] = t;
       place[k] = i >= 0 && i < a.V ? (int32_t)i + r.shift : -1;
@@ -163,24 +163,33 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     if (REST) bits_ready();                                    // the others may look at the bits and places
     const float t_rest = REST ? a.rest[n] : -INFINITY;
     for (int k = lane; k < a.K; k += 32) score[k] = place[k] >= 0 ? to_f32(r.row[place[k] - r.shift]) : 0.f;
-    most = fmaxf(warp_max(most), t_rest);
-    const float t_base = most == -INFINITY ? 0.f : most;
-    const float e_rest = expf(t_rest - t_base);
+    most = warp_max(most);
+    // Exponents relative to the best listed one, whose product with the scale need not be a number of fp32 (nor lose digits); where the rest has more, relative to that.
+    const float top = most == -INFINITY ? 0.f : most;
+    float d_rest = REST ? fmaf(-top, a.scale, t_rest) : -INFINITY, shift = 0.f;
+    if (REST && t_rest > -INFINITY && (d_rest > 0.f || most == -INFINITY)) {
+      shift = d_rest;
+      d_rest = t_rest - t_rest;                                // 0, or NaN where the rest is infinite
+    }
+    const float e_rest = expf(d_rest);
     float total = 0.f;
-    for (int k = lane; k < a.K; k += 32) total += expf(log_q[k] - t_base);
+    for (int k = lane; k < a.K; k += 32) {
+      log_q[k] = (log_q[k] - top) * a.scale - shift;
+      total += expf(log_q[k]);
+    }
     total = warp_sum(total) + e_rest;
     if (__any_sync(0xFFFFFFFFu, wrong)) total = NAN;
     const bool any = total != 0.f;                             // else nothing is left of the teacher's row
     const float log_total = any ? logf(total) : 0.f;
     for (int k = lane; k < a.K; k += 32) {
-      const float t = log_q[k] - t_base;
-      q[k] = any ? expf(t) / total : 0.f;
-      log_q[k] = t - log_total;
+      const float d = log_q[k];
+      q[k] = any ? expf(d) / total : 0.f;
+      log_q[k] = d - log_total;
     }
     if (lane == 0) {
       room.total = total;
       room.q_rest = any ? e_rest / total : 0.f;
-      room.log_q_rest = t_rest - t_base - log_total;
+      room.log_q_rest = d_rest - log_total;
     }
     if (edge != -INFINITY) {
       if (REST && room.edges_listed >> lane & 1) {

@@ -334,3 +334,21 @@ def test_formula_of_far_items_against_the_plain_one():
     index, teacher, rest = places(4, 60, 5, g), torch.randn(4, 5, generator=g, device=DEV), torch.randn(4, generator=g, device=DEV)
     a, b = formula(x, index, teacher, rest, None, 0.8), formula_of_far_items(x, index, teacher, rest, 0.8)
     assert float((a[0] - b[0]).abs().max()) < 1e-12 and float((a[2] - b[2]).abs().max()) < 1e-12
+
+
+@pytest.mark.parametrize("with_rest", [False, True])
+@pytest.mark.parametrize("scale,size,apart", [(1.3e6, 10.0, 2.0 ** -20), (1000.0, 10.0, 1e-3), (1e-3, 1e4, 700.0), (1e30, 1e9, 100.0), (1e30, -1e9, 100.0), (1.0, -3e38, 2e31), (1e30, 0.0, 1e-30)])
+def test_teachers_scores_at_large_scales(with_rest, scale, size, apart):
+    """A teacher's scores whose product with the scale has no digits for their differences, or is no number of fp32: only differences count; the rest beside, above and
+    below them."""
+    g = torch.Generator(device=DEV).manual_seed(int(abs(size)) % 1000)
+    N, V, K = 7, 900, 12
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    x = torch.randn(N, V, generator=g, device=DEV) / max(scale, 1.0)
+    index = places(N, V, K, g)
+    teacher = (size + apart * torch.randint(-4, 5, (N, K), generator=g, device=DEV).double()).float()
+    rest = None
+    if with_rest:
+        rest = (teacher.double().amax(1) * scale + torch.tensor([0.0, 1.0, -1.0, 30.0, -30.0, 3e38, -3e38], device=DEV).double()).clamp(-3.4e38, 3.4e38).float()
+    weights = torch.full((N,), 1.0 / max(scale, 1.0), device=DEV)
+    check(x, index, teacher, rest, weights, scale)
