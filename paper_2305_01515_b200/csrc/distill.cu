@@ -174,7 +174,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     const float e_rest = expf(d_rest);
     float total = 0.f;
     for (int k = lane; k < a.K; k += 32) {
-      log_q[k] = (log_q[k] - top) * a.scale - shift;
+      log_q[k] = scaled_difference(log_q[k], top, a.scale) - shift;
       total += expf(log_q[k]);
     }
     total = warp_sum(total) + e_rest;
@@ -340,10 +340,10 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     const float log_all = all == 0.f ? 0.f : logf(all) - log_excess(m, base, c);
     float loss = 0.f;
     for (int k = lane; k < a.K; k += 32) {
-      if (q[k] != 0.f) loss += q[k] * (log_q[k] - ((score[k] - m0) * a.scale - log_all));
+      if (q[k] != 0.f) loss += q[k] * (log_q[k] - (scaled_difference(score[k], m0, a.scale) - log_all));
     }
     if (REST && lane == 0 && room.q_rest != 0.f) {
-      const float log_p = logf(s.sum) - log_excess(s.m, base_rest, c) + (s.m == -INFINITY ? 0.f : (s.m - m0) * a.scale) - log_all;
+      const float log_p = logf(s.sum) - log_excess(s.m, base_rest, c) + (s.m == -INFINITY ? 0.f : scaled_difference(s.m, m0, a.scale)) - log_all;
       loss += room.q_rest * (room.log_q_rest - log_p);
     }
     loss = warp_sum(loss);

@@ -342,7 +342,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
       room.m = m0;
       room.log_s = log_s;
       room.nothing = nothing;
-      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - m0) * scale - log_s + nothing;
+      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : scaled_difference(target_score, m0, scale) - log_s + nothing;
       if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_sum - st.P / st.S * LN2;
       if (out.stats) {
         out.stats[2 * n] = m0;
@@ -354,7 +354,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
 
   const auto write = [&](int place, uint64_t o) {
     if (out.top_index) out.top_index[n * k + place] = order_index(o);
-    if (out.top_logp) out.top_logp[n * k + place] = (order_score(o) - room.m) * scale - room.log_s + room.nothing;
+    if (out.top_logp) out.top_logp[n * k + place] = scaled_difference(order_score(o), room.m, scale) - room.log_s + room.nothing;
   };
   if (k > 0) {
     sync();
@@ -424,7 +424,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
     const float log_sum = logf(st.S), log_s = st.S > 0.f ? log_sum - off : st.S == 0.f ? 0.f : NAN;
     const float nothing = st.S == 0.f ? -INFINITY : 0.f;
     if (tid == 0) {
-      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : (target_score - m0) * scale - log_s + nothing;
+      if (out.logp) out.logp[n] = target < 0 ? 0.f : target >= V ? NAN : scaled_difference(target_score, m0, scale) - log_s + nothing;
       if (out.entropy) out.entropy[n] = st.S == 0.f ? 0.f : log_sum - st.P / st.S * LN2;
       if (out.stats) {
         out.stats[2 * n] = m0;
@@ -438,7 +438,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
       for (int j = 0; j < parts * k; ++j) place += part_best[j] > o;
       if (place < k && o != 0) {
         if (out.top_index) out.top_index[n * k + place] = order_index(o);
-        if (out.top_logp) out.top_logp[n * k + place] = (order_score(o) - m0) * scale - log_s + nothing;
+        if (out.top_logp) out.top_logp[n * k + place] = scaled_difference(order_score(o), m0, scale) - log_s + nothing;
       }
     }
   }
@@ -449,7 +449,7 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
 constexpr int BACK_THREADS = 256, BACK_UNROLL = 4;
 
 template <typename T>
-__global__ void __launch_bounds__(BACK_THREADS)
+__global__ void __launch_bounds__(BACK_THREADS, 8)
 logprobs_backward(const T* logits, int64_t row_stride, int32_t V, float scale, const int64_t* __restrict__ targets, const float* __restrict__ stats,
                   const float* __restrict__ entropy, const float* __restrict__ grad_logp, const float* __restrict__ grad_entropy, T* grad_logits,
                   int64_t grad_stride, int32_t pieces) {
@@ -464,6 +464,7 @@ logprobs_backward(const T* logits, int64_t row_stride, int32_t V, float scale, c
   // dx = p (alpha + beta d) + [v = target] scale gl, with d = log2 of exp(scale (x - m)) and p = 2^(d - bias)
   const float alpha = -scale * (gl + (gh != 0.f ? gh * (entropy[n] - log_s) : 0.f)), beta = -scale * gh * LN2, bias = log_s * LOG2E;
   const bool any = gl != 0.f || gh != 0.f;
+  const Pair minus(-0.5f * m, -0.5f * m), c2(2.f * c, 2.f * c);
   const int32_t b = piece * (int)(blockDim.x * U) + threadIdx.x;
   uint4 w[U];
   if (any) {
@@ -478,9 +479,12 @@ logprobs_backward(const T* logits, int64_t row_stride, int32_t V, float scale, c
     if (any) {
       RowBatches<T>::unpack(w[u], v);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float d = exponent((v[e] - m) * c);
-        v[e] = exp2_fast(d - bias) * fmaf(beta, d, alpha);
+      for (int e = 0; e < E; e += 2) {
+        const float2 x = (fma2(Pair(v[e], v[e + 1]), Pair(0.5f, 0.5f), minus) * c2).get();      // as in scaled_difference
+        const Pair d(exponent(x.x), exponent(x.y));
+        const float2 f = (d + Pair(-bias, -bias)).get(), y = (Pair(exp2_fast(f.x), exp2_fast(f.y)) * fma2(Pair(beta, beta), d, Pair(alpha, alpha))).get();
+        v[e] = y.x;
+        v[e + 1] = y.y;
       }
       if (t >= i && t < i + E) {
 #pragma unroll

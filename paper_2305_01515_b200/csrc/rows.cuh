@@ -254,6 +254,8 @@ __device__ __forceinline__ bool ordinary(float base) { return fabsf(base) < 8388
 // What the logarithm of a sum of 2^(c x - base) has too much by the rounding of the base.
 __device__ __forceinline__ float log_excess(float m, float base, float c) { return ordinary(base) && m != -INFINITY ? fmaf(m, c, -base) * LN2 : 0.f; }
 
+// scale (x - y), where x - y itself need not be a number of fp32 (scores of either sign around 2e38 and more, under a small scale).
+__device__ __forceinline__ float scaled_difference(float x, float y, float scale) { return fmaf(0.5f, x, -0.5f * y) * (2.f * scale); }
 // Exponent of the factor that takes sums relative to `from`, in the form that goes with it, to sums relative to `to`, which is not smaller.
 __device__ __forceinline__ float change_of_base(float from, float to, float c) {
   const float a = base_of(from, c), b = base_of(to, c);

@@ -352,3 +352,19 @@ def test_teachers_scores_at_large_scales(with_rest, scale, size, apart):
         rest = (teacher.double().amax(1) * scale + torch.tensor([0.0, 1.0, -1.0, 30.0, -30.0, 3e38, -3e38], device=DEV).double()).clamp(-3.4e38, 3.4e38).float()
     weights = torch.full((N,), 1.0 / max(scale, 1.0), device=DEV)
     check(x, index, teacher, rest, weights, scale)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -124, 1e-30, 0.25])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("with_rest", [False, True])
+def test_scores_whose_difference_is_no_number(scale, dtype, with_rest):
+    """Scores of both signs up to the type's largest, the student's and the teacher's: their difference overflows, its product with a small scale does not."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    x = ((torch.rand(4, 3001, generator=g, device=DEV) * 2 - 1) * 3.3e38).to(dtype)
+    index = places(4, 3001, 9, g)
+    index[0, 0], index[1, 0] = x[0].argmin(), x[1].argmax()
+    teacher = ((torch.rand(4, 9, generator=g, device=DEV) * 2 - 1) * 3.3e38).to(dtype)
+    rest = torch.zeros(4, device=DEV) if with_rest else None
+    weights = torch.full((4,), 1.0 / scale, device=DEV)
+    check(x, index, teacher, rest, weights, scale)

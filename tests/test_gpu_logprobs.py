@@ -306,3 +306,20 @@ def test_masks_of_large_finite_values_at_every_scale(mask, scale, dtype, V):
     gl, gh = torch.ones(6, device=DEV) / scale, torch.full((6,), 0.5, device=DEV) / scale
     want, bound = gradient64(x, t, gl, gh, scale)
     close(backward(x, t, stats, ent, gl, gh, scale), want, bound + want.abs() * torch.finfo(dtype).eps / 2 + 2.0 ** -25 * (dtype == torch.float16) + 1e-37)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -124, 1e-30, 0.25])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [60, 5000, 70001])
+def test_scores_whose_difference_is_no_number(scale, dtype, V):
+    """Scores of both signs up to the type's largest: their difference overflows, its product with a small scale does not."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    x = ((torch.rand(4, V, generator=g, device=DEV) * 2 - 1) * 3.3e38).to(dtype)
+    t = torch.stack([x[0].argmin(), x[1].argmax(), torch.tensor(7, device=DEV), torch.tensor(-1, device=DEV)])
+    check(x, t, 5, scale)
+    check(x, t, min(V, 32), scale)
+    _, ent, stats, _, _ = forward(x, t, 0, scale)
+    gl, gh = torch.ones(4, device=DEV) / scale, torch.ones(4, device=DEV) / scale
+    want, bound = gradient64(x, t, gl, gh, scale)
+    close(backward(x, t, stats, ent, gl, gh, scale), want, bound + want.abs() * torch.finfo(dtype).eps / 2 + 1e-37)
