@@ -460,7 +460,7 @@ logprobs_backward(const T* logits, int64_t row_stride, int32_t V, float scale, c
   const RowUnder<T> under(logits + n * row_stride, r);
   const float c = scale * LOG2E, m = stats[2 * n], log_s = stats[2 * n + 1];
   const int64_t t = targets ? targets[n] : -1;
-  const float gl = !grad_logp || t < 0 ? 0.f : t >= V ? NAN : grad_logp[n], gh = grad_entropy ? grad_entropy[n] : 0.f;
+  const float g = grad_logp ? grad_logp[n] : 0.f, gl = t < 0 || g == 0.f ? 0.f : t >= V ? NAN : g, gh = grad_entropy ? grad_entropy[n] : 0.f;
   // dx = p (alpha + beta d) + [v = target] scale gl, with d = log2 of exp(scale (x - m)) and p = 2^(d - bias)
   const float alpha = -scale * (gl + (gh != 0.f ? gh * (entropy[n] - log_s) : 0.f)), beta = -scale * gh * LN2, bias = log_s * LOG2E;
   const bool any = gl != 0.f || gh != 0.f;

@@ -323,3 +323,15 @@ def test_scores_whose_difference_is_no_number(scale, dtype, V):
     gl, gh = torch.ones(4, device=DEV) / scale, torch.ones(4, device=DEV) / scale
     want, bound = gradient64(x, t, gl, gh, scale)
     close(backward(x, t, stats, ent, gl, gh, scale), want, bound + want.abs() * torch.finfo(dtype).eps / 2 + 1e-37)
+
+
+def test_a_target_that_is_not_there_and_whose_gradient_is_zero():
+    """A loss that leaves a row out by a gradient of 0 leaves it out altogether, and the entropy's gradient does not see its target."""
+    x = torch.randn(3, 500, device=DEV)
+    t = torch.tensor([500, 1 << 40, 500], device=DEV)
+    _, ent, stats, _, _ = forward(x, t)
+    gl, gh = torch.tensor([0.0, -0.0, 1.0], device=DEV), torch.tensor([0.0, 2.0, 0.0], device=DEV)
+    d = backward(x, t, stats, ent, gl, gh, 1.0)
+    want, bound = gradient64(x, torch.full_like(t, -1), gl, gh, 1.0)
+    assert bool((d[0] == 0).all()) and bool(d[2].isnan().all())
+    close(d[1], want[1], bound[1])
