@@ -727,7 +727,8 @@ int mts_rms_norm_forward(const void* x, int64_t x_stride, const void* residual, 
                          int32_t weight_dtype, int32_t dtype, int64_t N, int32_t D, float eps, void* sum_out, int64_t sum_stride,
                          void* out, int64_t out_stride, float* inv_rms, void* stream);
 /* The same with out in 8 bits: groups of `group` columns (32, 64, 128 or 256, counted from column 0, the last may be shorter; 0: the whole
- * row) share a scale = max(max_j |y_j|, 2^-100) / 448, codes_j = e4m3(y_j * (448 / max)), rounded to nearest even (NaN stays NaN).
+ * row) share a scale = max(c max_j |u_j|, 2^-100) / 448 with u = r weight rounded to fp32, and codes_j = e4m3(u_j * (448 / max_j |u_j|)), rounded to nearest even (NaN stays
+ * NaN): c is in the scales alone, codes are whole functions of r and weight.  Where c max_j |u_j| is below 2^-100, codes_j = e4m3(c u_j (448 * 2^100)), c counting as 590,000 at most.
  * codes: uint8 [N, D] (the bits of e4m3 numbers); scales: fp32 [N, ceil(D / group)] contiguous ([N] where group is 0).  Forward only: for serving,
  * or with a backward that takes the rounding as the identity.  Errors as above. */
 int mts_rms_norm_forward_8bit(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,

@@ -182,6 +182,13 @@ struct NormForward {
   float eps;
 };
 
+// A group's scale, and what its values are multiplied with for their codes; `most`: the largest of them, without the factor c.
+__device__ __forceinline__ float scale_of(float most, float c) { return fmaxf(most * c, LEAST_MAX) / TOP_CODE; }
+__device__ __forceinline__ float inverse_of(float most, float c) {
+  constexpr float MOST_C = 5.9e5f;                       // with more the product has no number (infinite and NaN as they are)
+  return most * c >= LEAST_MAX ? TOP_CODE / most : TOP_CODE / LEAST_MAX * (c > MOST_C && c < INFINITY ? MOST_C : c);
+}
+
 // Eight codes of a lane.
 template <bool VECTOR, int LANES>
 __device__ __forceinline__ void store_codes(uint8_t* row, int D, int chunk, const float (&y)[8]) {
@@ -255,6 +262,7 @@ rms_norm_forward(const NormForward<T> a) {
     c[r] = 1.f / sqrtf(row_sum<LANES>(s, room[0], warp, R == 1 ? warps : 1) / a.D + a.eps);
     if (a.inv_rms && warp == 0 && lane_id() % LANES == 0 && D[r]) a.inv_rms[row[r]] = c[r];
   }
+  // In 8 bits c cancels out of the codes and goes to the scales alone: which code a value between two has depends on x and weight, not on the last bit of a sum over the row.
 #pragma unroll
   for (int i = 0; i < I; ++i) {
     float w[8];
@@ -262,7 +270,7 @@ rms_norm_forward(const NormForward<T> a) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[r][i][e] = v[r][i][e] * c[r] * w[e];
+      for (int e = 0; e < 8; ++e) if (CODES) v[r][i][e] *= w[e]; else v[r][i][e] = v[r][i][e] * c[r] * w[e];
       if (!CODES) store8<T, VECTOR, LANES>(a.out + row[r] * a.out_stride, D[r], warp + i * warps, v[r][i]);
     }
   }
@@ -276,9 +284,9 @@ rms_norm_forward(const NormForward<T> a) {
         for (int i = 0; i < I; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) all = fmaxf(all, fabsf(v[r][i][e]));
-        all = fmaxf(row_max<LANES>(all, room[1], warp, R == 1 ? warps : 1), LEAST_MAX);
-        if (warp == 0 && lane_id() % LANES == 0 && D[r]) a.scales[row[r]] = all / TOP_CODE;
-        inverse = TOP_CODE / all;
+        all = row_max<LANES>(all, room[1], warp, R == 1 ? warps : 1);
+        if (warp == 0 && lane_id() % LANES == 0 && D[r]) a.scales[row[r]] = scale_of(all, c[r]);
+        inverse = inverse_of(all, c[r]);
       }
 #pragma unroll
       for (int i = 0; i < I; ++i) {
@@ -287,13 +295,13 @@ rms_norm_forward(const NormForward<T> a) {
         float(&y)[8] = v[r][i];
         if (a.group == 0 || VECTOR) {
           if (a.group) {                                 // a group is group / 8 neighbouring lanes
-            float most = LEAST_MAX;
+            float most = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(y[e]));
             for (int o = 1; o < min(a.group / 8, LANES); o *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-            inverse = TOP_CODE / most;
+            inverse = inverse_of(most, c[r]);
             const int at = Columns::column(chunk, 0), g = at >> (__ffs(a.group) - 1);
-            if ((at & (a.group - 1)) == 0 && at < D[r]) a.scales[row[r] * a.groups + g] = most / TOP_CODE;
+            if ((at & (a.group - 1)) == 0 && at < D[r]) a.scales[row[r] * a.groups + g] = scale_of(most, c[r]);
           }
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] *= inverse;
@@ -305,12 +313,12 @@ rms_norm_forward(const NormForward<T> a) {
               float most = 0.f;
 #pragma unroll
               for (int e = 0; e < PART; ++e) most = fmaxf(most, fabsf(y[p + e]));
-              most = fmaxf(warp_max(most), LEAST_MAX);
-              const float inverse_of_group = TOP_CODE / most;
+              most = warp_max(most);
+              const float inverse_of_group = inverse_of(most, c[r]);
 #pragma unroll
               for (int e = 0; e < PART; ++e) y[p + e] *= inverse_of_group;
               const int g = (chunk * 8 + p) / PART;
-              if (lane_id() == 0 && g < a.groups && D[r]) a.scales[row[r] * a.groups + g] = most / TOP_CODE;
+              if (lane_id() == 0 && g < a.groups && D[r]) a.scales[row[r] * a.groups + g] = scale_of(most, c[r]);
             }
           };
           if (a.group == 32) groups_of(std::integral_constant<int, 1>());

@@ -281,3 +281,47 @@ def test_backward_of_widths_where_the_rows_shape_changes(N, D, dtype, with_sum):
     close(dx, want, want.abs() * half(dtype) + size * (SUM + 10 * U) + 2.0 ** -25 * (dtype == torch.float16))
     close(dw, dw64, dw_size * (N + 6) * U)
     assert untouched(dx, room)
+
+
+@pytest.mark.parametrize("N,D,pad,shift", [(3, 7, 0, 1), (300, 256, 0, 0), (301, 264, 0, 8), (120, 1024, 0, 0), (90, 1000, 24, 0), (50, 333, 3, 2), (40, 4104, 0, 0), (9, 20001, 1, 3),
+                                           (12, 32768, 0, 0), (40000, 256, 0, 0), (152000, 24, 0, 0)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [0, 32, 64, 128, 256])
+@pytest.mark.parametrize("wide_weight", [False, True])
+def test_8bit_codes_are_those_of_x_and_weight_alone(N, D, pad, shift, dtype, group, wide_weight):
+    """Every code, those between two numbers too, is e4m3(u (448 / max |u|)) with u = r weight in fp32: torch's own product, quotient, product and conversion give the same."""
+    g = torch.Generator(device=DEV).manual_seed(N + D + group)
+    x, _ = placed(torch.randn(N, D, generator=g, device=DEV), dtype, pad, shift)
+    w = (1 + 0.3 * torch.randn(D, generator=g, device=DEV)).to(torch.float32 if wide_weight else dtype)
+    n = group or D
+    G = -(-D // n)
+    codes, scales = torch.empty(N, D, dtype=torch.uint8, device=DEV), torch.empty(N, G, device=DEV)
+    mb.rms_norm_forward_8bit(x, D + pad, None, 0, w, KIND[w.dtype], KIND[dtype], N, D, EPS, None, 0, codes, D, scales, group, None)
+    torch.cuda.synchronize()
+    u = torch.nn.functional.pad(x.float() * w.float(), (0, G * n - D)).view(N, G, n)
+    top = u.abs().amax(2, keepdim=True)
+    want = (u * (torch.full_like(top, 448.0) / top)).view(N, G * n)[:, :D].to(torch.float8_e4m3fn)
+    assert torch.equal(codes, want.contiguous().view(torch.uint8)), int((codes != want.contiguous().view(torch.uint8)).sum())
+    most = top[:, :, 0].double() * norm64(x.double(), w.double())[1]
+    close(scales, most / 448.0, most / 448.0 * (C + 6 * U))
+
+
+@pytest.mark.parametrize("group", [0, 32, 256])
+@pytest.mark.parametrize("D", [512, 515])
+def test_8bit_values_below_the_least_maximum(group, D):
+    """Groups whose largest value is below 2^-100 have its scale: codes of 448 2^100 y, small ones of the type among them."""
+    g = torch.Generator(device=DEV).manual_seed(D)
+    x = torch.randn(20, D, generator=g, device=DEV)
+    w = torch.exp2(torch.arange(D, device=DEV) // 32 * -1.0 - 96)
+    G = -(-D // (group or D))
+    codes, scales, inv = torch.empty(20, D, dtype=torch.uint8, device=DEV), torch.empty(20, G, device=DEV), torch.empty(20, device=DEV)
+    mb.rms_norm_forward_8bit(x, D, None, 0, w, 0, 0, 20, D, EPS, None, 0, codes, D, scales, group, inv)
+    torch.cuda.synchronize()
+    n = group or D
+    y = torch.nn.functional.pad(norm64(x.double(), w.double())[0], (0, G * n - D)).view(20, G, n)
+    most = y.abs().amax(2).clamp(min=2.0 ** -100)
+    close(scales, most / 448.0, most / 448.0 * (C + 6 * U))
+    held = codes.view(torch.float8_e4m3fn).double()
+    v = (y * (448.0 / most).unsqueeze(2)).view(20, G * n)[:, :D]
+    close(held, v, v.abs() * (2.0 ** -4 + 2 * C + 16 * U) + 2.0 ** -10 * (1 + 1e-4))
+    assert not group or bool((scales == 2.0 ** -100 / 448).any()) and bool((held == 0).any())
