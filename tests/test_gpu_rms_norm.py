@@ -325,3 +325,68 @@ def test_8bit_values_below_the_least_maximum(group, D):
     v = (y * (448.0 / most).unsqueeze(2)).view(20, G * n)[:, :D]
     close(held, v, v.abs() * (2.0 ** -4 + 2 * C + 16 * U) + 2.0 ** -10 * (1 + 1e-4))
     assert not group or bool((scales == 2.0 ** -100 / 448).any()) and bool((held == 0).any())
+
+
+# short rows in such numbers that a warp has several (16 bits, on boundaries), the last of them with some to spare
+MANY = [(151553, 16), (151559, 32), (75777, 40), (75781, 64), (37889, 128), (37893, 104), (18945, 256), (18947, 200), (18945, 512), (18949, 264)]
+
+
+@pytest.mark.parametrize("N,D", MANY)
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("residual", [False, True])
+def test_many_short_rows(N, D, dtype, residual):
+    """Forward in the type and in 8 bits, and backward, of rows of which a warp takes two to thirty-two."""
+    g = torch.Generator(device=DEV).manual_seed(N + D)
+    x, dy, ds = (torch.randn(N, D, generator=g, device=DEV).to(dtype) for _ in range(3))
+    res = torch.randn(N, D, generator=g, device=DEV).to(dtype) if residual else None
+    w = (1 + 0.3 * torch.randn(D, generator=g, device=DEV)).to(dtype)
+    total = torch.empty_like(x) if residual else None
+    out, room = placed(torch.zeros(N, D), dtype, 0, 0)
+    inv = torch.full((N + 1,), -1.0, device=DEV)
+    mb.rms_norm_forward(x, D, res, D, w, KIND[dtype], KIND[dtype], N, D, EPS, total, D, out, D, inv)
+    torch.cuda.synchronize()
+    r = x if res is None else total
+    assert res is None or torch.equal(total, (x.float() + res.float()).to(dtype))
+    want, c = norm64(r.double(), w.double())
+    close(inv[:N], c[:, 0], C * c[:, 0])
+    close(out, want, want.abs() * (half(dtype) + C + 4 * U) + 2.0 ** -25 * (dtype == torch.float16))
+    assert untouched(out, room) and float(inv[N]) == -1.0
+    for group in (0, 32, 128):
+        n = group or D
+        G = -(-D // n)
+        codes, scales = torch.full((N + 1, D), 99, dtype=torch.uint8, device=DEV), torch.full((N + 1, G), -3.0, device=DEV)
+        total8 = torch.empty_like(x) if residual else None
+        mb.rms_norm_forward_8bit(x, D, res, D, w, KIND[dtype], KIND[dtype], N, D, EPS, total8, D, codes, D, scales, group, None)
+        torch.cuda.synchronize()
+        top = torch.nn.functional.pad(want.abs(), (0, G * n - D)).view(N, G, n).amax(2).clamp(min=2.0 ** -100)
+        close(scales[:N], top / 448.0, top / 448.0 * (C + 6 * U))
+        held = codes[:N].view(torch.float8_e4m3fn).double() * scales[:N].double().repeat_interleave(n, 1)[:, :D]
+        close(held, want, want.abs() * (2.0 ** -4 + 2 * C + 16 * U) + (top / 448.0).repeat_interleave(n, 1)[:, :D] * 2.0 ** -10 * (1 + 1e-4))
+        assert bool((codes[N] == 99).all()) and bool((scales[N] == -3.0).all()) and (res is None or torch.equal(total8, total))
+    dx, room = placed(torch.zeros(N, D), dtype, 0, 0)
+    dw, ws = torch.full((D,), -5.0, device=DEV), torch.full((mb.rms_norm_workspace_bytes(N, D),), 255, dtype=torch.uint8, device=DEV)
+    mb.rms_norm_backward(r, D, w, KIND[dtype], KIND[dtype], N, D, inv, dy, D, ds, D, dx, D, dw, ws, ws.numel())
+    torch.cuda.synchronize()
+    want, size, dw64, dw_size, _ = backward64(r.double(), w.double(), dy.double(), ds.double())
+    close(dx, want, want.abs() * half(dtype) + size * (SUM + C + 10 * U) + 2.0 ** -25 * (dtype == torch.float16))
+    close(dw, dw64, dw_size * (600 + 90 + 6) * U)            # at most 600 rows one after the other, the root of the forward
+    assert untouched(dx, room)
+
+
+@pytest.mark.parametrize("N,D,stride,group", [(5, 64, 64, 0), (9, 264, 264, 32), (300, 2048, 2048, 64), (7, 2051, 2056, 128), (11, 4096, 4096, 0), (6, 4099, 4104, 256), (3, 20005, 20008, 32),
+                                              (2, 32768, 32768, 0), (4, 4099, 4104, 0)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_from_8_bits_by_vectors(N, D, stride, group, dtype):
+    """Codes and values on boundaries of eight, narrow and wide, with ends that fill no piece; the places behind them are left as they were."""
+    g = torch.Generator(device=DEV).manual_seed(N + D)
+    G = -(-D // group) if group else 1
+    codes = torch.randint(256, (N, stride), generator=g, device=DEV, dtype=torch.uint8)
+    codes[(codes & 127) == 127] = 5                          # no NaN
+    scales = torch.rand(N, G, generator=g, device=DEV) + 0.01
+    out, room = placed(torch.zeros(N, D), dtype, stride - D, 0)
+    assert out.data_ptr() % 16 == 0 and codes.data_ptr() % 8 == 0
+    mb.rows_from_8bit(codes, stride, scales, group, N, D, out, KIND[dtype], stride)
+    torch.cuda.synchronize()
+    want = codes[:, :D].contiguous().view(torch.float8_e4m3fn).double() * scales.double().repeat_interleave(group or D, 1)[:, :D]
+    close(out, want, want.abs() * (half(dtype) + U) + 2.0 ** -25 * (dtype == torch.float16))
+    assert untouched(out, room)
