@@ -368,3 +368,22 @@ def test_scores_whose_difference_is_no_number(scale, dtype, with_rest):
     rest = torch.zeros(4, device=DEV) if with_rest else None
     weights = torch.full((4,), 1.0 / scale, device=DEV)
     check(x, index, teacher, rest, weights, scale)
+
+
+@pytest.mark.parametrize("N,V,K", [(2401, 900, 5), (2399, 5001, 33), (1203, 3002, 64), (1203, 8001, 200), (700, 20003, 12), (40, 100003, 256), (300, 30, 30)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("with_rest", [False, True])
+def test_rows_by_one_two_four_and_more_warps(N, V, K, dtype, with_rest):
+    """As many rows as keep the GPU busy with few warps a row, and fewer; the same items more than once, places out of use, rows off boundaries."""
+    g = torch.Generator(device=DEV).manual_seed(N + V)
+    x, _ = placed(2 * torch.randn(N, V, generator=g, device=DEV), dtype, 1, 1)
+    index = torch.randint(-1, V, (N, K), generator=g, device=DEV)
+    index[::3] = torch.where(index[::3] < 0, -1, index[::3] % 17 % V)         # many to a batch
+    index[1::3] = torch.where(index[1::3] < 0, -1, V - 1 - index[1::3] % 11 % V)
+    teacher = torch.randn(N, K, generator=g, device=DEV).to(dtype)
+    rest = None
+    if with_rest:
+        rest = torch.randn(N, generator=g, device=DEV)
+        listed = torch.zeros(N, V + 1, dtype=torch.bool, device=DEV).scatter_(1, torch.where(index >= 0, index, V), True)[:, :V]
+        rest[listed.all(1)] = -INF
+    check(x, index, teacher, rest, torch.randn(N, generator=g, device=DEV), 0.8)

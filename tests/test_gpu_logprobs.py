@@ -335,3 +335,34 @@ def test_a_target_that_is_not_there_and_whose_gradient_is_zero():
     want, bound = gradient64(x, torch.full_like(t, -1), gl, gh, 1.0)
     assert bool((d[0] == 0).all()) and bool(d[2].isnan().all())
     close(d[1], want[1], bound[1])
+
+
+@pytest.mark.parametrize("N,V,k", [(2401, 700, 9), (2403, 2050, 32), (2399, 2801, 10), (1203, 6001, 17), (700, 20003, 5), (310, 50001, 32), (40, 100003, 3), (2400, 33, 33 - 1)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["spread", "masked", "ties", "nan"])
+def test_rows_by_one_two_four_and_more_warps(N, V, k, dtype, kind):
+    """As many rows as keep the GPU busy with few warps a row, and fewer, off boundaries."""
+    g = torch.Generator(device=DEV).manual_seed(N + V)
+    x = 3 * torch.randn(N, V, generator=g, device=DEV)
+    if kind == "masked":
+        x.masked_fill_(torch.rand(N, V, generator=g, device=DEV) < torch.rand(N, 1, generator=g, device=DEV), -INF)
+        x[::5] = -INF
+        x[::5, V // 2:V // 2 + 3] = 1.5
+    if kind == "ties":
+        x = torch.round(x).clamp(-2, 2)
+    x, _ = placed(x, dtype, 1, 1)
+    t = torch.randint(-1, V, (N,), generator=g, device=DEV)
+    if kind != "nan":
+        return check(x, t, k, 1.0)
+    x[::4, V // 3] = float("nan")                            # one NaN: its row's statistics, and no other's
+    logp, ent, _, ti, tl = forward(x, t, k)
+    assert bool(ent[::4].isnan().all()) and bool(logp[::4][t[::4] >= 0].isnan().all()) and bool((logp[::4][t[::4] < 0] == 0).all()) and bool(tl[::4].isnan().all())
+    best = torch.sort(x.float().nan_to_num(nan=-INF, neginf=-INF), dim=1, descending=True, stable=True)[1][:, :k]
+    assert torch.equal(ti, best) or k == V - 1
+    some = torch.arange(N, device=DEV) % 4 != 0
+    log, _, H, _, L, mean_d = plain(x[some], 1.0)
+    want = torch.where(t[some] < 0, 0.0, log.gather(1, t[some].clamp(min=0).unsqueeze(1))[:, 0])
+    close(logp[some], want, L + 6 * U * want.abs())
+    close(ent[some], H, 2 * L * (1 + mean_d) + 4 * U * H)
+    want = log.gather(1, best[some])
+    close(tl[some], want, L.unsqueeze(1) + 8 * U * want.abs())
