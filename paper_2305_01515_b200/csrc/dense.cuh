@@ -12,7 +12,7 @@ namespace mts {
 // hash and does not change with these).
 enum DenseKernelId {
   K_RECURRENCE_FWD = K_COUNT, K_RECURRENCE_BWD, K_RELPOS_FWD, K_RELPOS_BWD, K_ADAMW, K_ADAMW_STATE, K_NORM_FWD, K_NORM_BWD, K_LOGPROBS_FWD,
-  K_LOGPROBS_BWD, K_DISTILL, K_ALL_COUNT
+  K_LOGPROBS_BWD, K_DISTILL, K_ROWS_FROM_8BIT, K_ALL_COUNT
 };
 
 inline bool known_dtype(int32_t dtype) {

@@ -706,7 +706,7 @@ extern "C" int mts_rows_from_8bit(const uint8_t* codes, int64_t codes_stride, co
     int log_threads = 0;
     while (log_threads < 8 && 1 << log_threads < pieces) ++log_threads;
     const int64_t blocks = ceil_div(N, 256 >> log_threads);
-    LaunchScope scope(K_NORM_FWD, s);
+    LaunchScope scope(K_ROWS_FROM_8BIT, s);
     if (vector && pieces <= 256) rows_from_8bit<T, true, 1><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);
     else if (vector) rows_from_8bit<T, true, 4><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);
     else rows_from_8bit<T, false, 4><<<(unsigned)blocks, 256, 0, s>>>(codes, codes_stride, scales, group, groups, D, static_cast<T*>(out), out_stride, N, log_threads);

@@ -32,7 +32,7 @@ static const char* const kKernelNames[K_ALL_COUNT] = {
     "cache_probe_replace", "cache_lists", "cache_scatter_slots", "cache_save_victims", "cache_fetch_misses",
     "cache_write_victims", "cache_flush", "other", "recurrence_forward", "recurrence_backward", "relpos_bias_forward",
     "relpos_bias_backward", "adamw_step", "adamw_state", "rms_norm_forward", "rms_norm_backward", "logprobs_forward",
-    "logprobs_backward", "distill_loss"};
+    "logprobs_backward", "distill_loss", "rows_from_8bit"};
 
 struct TraceRecord { int kernel; cudaEvent_t start, stop; };
 

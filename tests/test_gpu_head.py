@@ -345,3 +345,18 @@ def test_the_example_scores_a_catalogue():
     best, logp = tower.recommend(indices, 5)
     assert best.shape == (12, 5) and bool((logp[:, :-1] >= logp[:, 1:]).all()) and bool(((best >= 0) & (best < 701)).all())
     tower.close()
+
+
+def test_the_trace_tells_the_heads_kernels_apart():
+    x, w, t = torch.randn(5, 64, device=DEV).requires_grad_(), torch.ones(64, device=DEV), torch.zeros(5, dtype=torch.int64, device=DEV)
+    mb.trace_enable(True)
+    try:
+        codes, scales = hd.rms_norm_8bit(x.detach(), w)
+        hd.rows_from_8bit(codes, scales)
+        hd.rms_norm(x, w).sum().backward()
+        hd.log_probs(x, t).logp.sum().backward()
+        hd.distill_loss_and_grad(x, t.unsqueeze(1), torch.zeros(5, 1, device=DEV))
+        launches = {k: v[1] for k, v in mb.trace_report().items()}
+    finally:
+        mb.trace_enable(False)
+    assert launches == {"rms_norm_forward": 2, "rows_from_8bit": 1, "rms_norm_backward": 1, "logprobs_forward": 1, "logprobs_backward": 1, "distill_loss": 1}
