@@ -122,13 +122,6 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     m = most;
     base = base_of(m, c);
   };
-  const auto add_listed = [&](float x) {
-    if (x > m_listed) {
-      listed = scaled_to(listed, m_listed, x, c);
-      m_listed = x;
-    }
-    listed += power(x, m_listed, base_of(m_listed, c), c);
-  };
 
   if (warp == (own_warp ? warps : 0)) {
     // the teacher's row.  `place`: an item's number of elements from the first batch's begin, so that its batch is place / E; -1: not used
@@ -162,7 +155,12 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     }
     if (REST) bits_ready();                                    // the others may look at the bits and places
     const float t_rest = REST ? a.rest[n] : -INFINITY;
-    for (int k = lane; k < a.K; k += 32) score[k] = place[k] >= 0 ? to_f32(r.row[place[k] - r.shift]) : 0.f;
+    for (int k = lane; k < a.K; k += 32) {
+      score[k] = place[k] >= 0 ? to_f32(r.row[place[k] - r.shift]) : 0.f;
+      if (REST && place[k] >= 0) m_listed = fmaxf(m_listed, score[k]);
+    }
+    if (REST) m_listed = warp_max(m_listed);
+    const float base_listed = base_of(m_listed, c);
     most = warp_max(most);
     // Exponents relative to the best listed one, whose product with the scale need not be a number of fp32 (nor lose digits); where the rest has more, relative to that.
     const float top = most == -INFINITY ? 0.f : most;
@@ -193,7 +191,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     }
     if (edge != -INFINITY) {
       if (REST && room.edges_listed >> lane & 1) {
-        add_listed(edge);
+        listed += power(edge, m_listed, base_listed, c);
       } else {
         if (edge > m) rescale(edge);
         others = others + Pair(power(edge, m, base, c), 0.f);
@@ -233,7 +231,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           if (places >> e & 1) {
-            add_listed(v[e]);
+            listed += power(v[e], m_listed, base_listed, c);
             v[e] = -INFINITY;
           }
           top = fmaxf(top, v[e]);
@@ -314,11 +312,22 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
       }
     }
   }
-  const DistillSums nobody = {-INFINITY, 0.f, -INFINITY, 0.f};
+  const auto some_of = [&](const DistillSums* sums, int count) {
+    DistillSums mine = {-INFINITY, 0.f, -INFINITY, 0.f};
+    if (lane < count) {
+      mine.m = sums[lane].m;
+      mine.sum = sums[lane].sum;
+      if (REST) {
+        mine.m_listed = sums[lane].m_listed;
+        mine.listed = sums[lane].listed;
+      }
+    }
+    return join_lanes<REST>(mine, c);
+  };
   DistillSums s = join_lanes<REST>({m, others.sum(), m_listed, listed}, c);
   if (lane == 0) room.of_warp[warp] = s;
   __syncthreads();
-  s = join_lanes<REST>(lane < everyone / 32 ? room.of_warp[lane] : nobody, c);
+  s = some_of(room.of_warp, everyone / 32);
   if (parts > 1) {
     cluster_wait();
     if (tid < parts) {
@@ -328,7 +337,7 @@ distill_loss(const T* logits, T* grad, const DistillCall a) {
     }
     cluster_arrive();
     cluster_wait();                                            // (and no block writes over scores that another still reads)
-    s = join_lanes<REST>(lane < parts ? room.of_part[lane] : nobody, c);
+    s = some_of(room.of_part, parts);
   }
   // of all items, and what of it the ones that are not listed have (all, where they are not told apart)
   m = REST ? fmaxf(s.m, s.m_listed) : s.m;
