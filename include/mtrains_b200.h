@@ -769,8 +769,10 @@ int mts_logprobs_forward(const void* logits, int64_t row_stride, int32_t dtype, 
                          float* top_logp, void* stream);
 /* Its gradient, for gradients of logp and of entropy (fp32 [N], either may be NULL: 0):
  *   grad_logits[n, v] = scale (grad_logp ([v = target] - p_v) - grad_entropy p_v (log p_v + entropy))
+ * (also at the target of a row in which every item is ruled out: p is 0 there, the target's place gets scale grad_logp).
  * stats and entropy as the forward left them (entropy may be NULL without grad_entropy).  A row without a target takes grad_logp as 0.  A row
- * whose gradients are 0 gets zeros whatever its scores and its target hold; another whose target is >= V gets NaN.  grad_logits may be the memory of logits (same stride).  Errors as above. */
+ * whose gradients are 0 gets zeros whatever its scores and its target hold; a grad_logp other than 0 with a target >= V makes its row NaN.
+ * grad_logits may be the memory of logits (same stride).  Errors as above. */
 int mts_logprobs_backward(const void* logits, int64_t row_stride, int32_t dtype, int64_t N, int64_t V, float scale,
                           const int64_t* targets, const float* stats, const float* entropy, const float* grad_logp,
                           const float* grad_entropy, void* grad_logits, int64_t grad_stride, void* stream);

@@ -86,8 +86,8 @@ __device__ __forceinline__ void bits_ready() { asm volatile("bar.sync 1;" ::: "m
 // difference, or relative to the row's largest, would lose its digits where the listed ones have almost everything.  Bits in shared memory, eight to a thread's group, say which batches hold a listed item; the pass
 // leaves these out, and they are added afterwards item by item.
 // The gradient is written as if nothing were listed, and the listed places once more.
-// us: 4,096 x 65,536 bf16, 50 items, with gradient 215 (5.0 TB/s of its floor's bytes; 6% more reads than the scores, issue slots 47% busy: a block's warps sum, wait for each other and write in
-// turn); 2,047 x 32,003 fp16, 64 items and the rest, 75, loss alone 40; 20,000 x 5,001 fp32, 20 and the rest, 186; 64 x 20,000 fp32, loss alone, 6-8: latency.  Rows kept in shared
+// us: 4,096 x 65,536 bf16, 50 items, with gradient 209-218 (4.9-5.1 TB/s of its floor's bytes; 5% more reads than the scores, issue slots 48% busy: a block's warps sum, wait for each other and
+// write in turn); 2,047 x 32,003 fp16, 64 items and the rest, 75-77, loss alone 40; 20,000 x 5,001 fp32, 20 and the rest, 187; 64 x 20,000 fp32, loss alone, 6-8: latency.  Rows kept in shared
 // memory between the passes took longer (fewer blocks an SM), and so did clusters for many rows.
 template <typename T, bool REST>
 __global__ void __maxnreg__(64)                                // of (DISTILL_WARPS + 1) * 32 threads at most: 32 warps an SM

@@ -200,8 +200,8 @@ __device__ __noinline__ void best_of_equals(const RowBatches<T> r, int32_t b0, i
 // maxima of 32 or 64 groups of threads is a bound that at least k scores reach, and few others.  The units whose maxima reach it are read again, and a
 // score's place is the number of those found before it, where (score, index) are ordered so that the lowest index comes first among equals.
 // SHORT: rows of one group of a warp, which list the batches themselves instead of units.
-// us without and with the best: 30,011 x 5,001 fp32, 10 of them, 99 and 141 (6.1 and 4.3 TB/s); 2,048 x 131,072 bf16, 16, 93 and 104 (5.8 and 5.2); 20,000 x 4,000 fp16, 20, - and 73;
-// one row of 100,000, 20, 10.6: a chain of the cluster's exchange and three barriers.  Groups of four batches and 48 registers a thread (40 warps an SM instead of 32) took 167
+// us without and with the best: 30,011 x 5,001 fp32, 10 of them, 99 and 141-148 (6.1 and 4.1-4.3 TB/s); 2,048 x 131,072 bf16, 16, 93-95 and 104-115 (5.7 and 4.7-5.2);
+// 20,000 x 4,000 fp16, 20, - and 73; one row of 100,000, 20, 8.5-10.6: a chain of the cluster's exchange and three barriers.  Groups of four batches and 48 registers a thread (40 warps an SM instead of 32) took 167
 // for the first: eight loads on their way hide more than the warps.  Ends as masked batches of the main loop took 160.
 template <typename T, bool ONE_WARP, bool SHORT>
 __global__ void __launch_bounds__(ONE_WARP ? LOGP_ROWS * 32 : LOGP_WARPS * 32, ONE_WARP ? 8 : 2)
@@ -444,8 +444,8 @@ logprobs_forward(const T* __restrict__ logits, int64_t row_stride, int64_t N, in
   }
 }
 
-// Gradient, dx = p (alpha + beta d) + [v = target] scale g_logp: 4,099 x 50,001 bf16, rows of gradients and of scores at different places, 131-147 us (5.6-6.3 TB/s, 85-96% of
-// the copy rate); issue slots 80% busy with the shifts.  A thread takes BACK_UNROLL batches of the gradient's row (16 bytes that start on a 16-byte boundary of it) and reads the scores that lie under them.
+// Gradient, dx = p (alpha + beta d) + [v = target] scale g_logp: 4,099 x 50,001 bf16, rows of gradients and of scores at different places, 130-149 us (5.5-6.3 TB/s, 84-96% of
+// the copy rate); issue slots 87% busy with the shifts.  A thread takes BACK_UNROLL batches of the gradient's row (16 bytes that start on a 16-byte boundary of it) and reads the scores that lie under them.
 constexpr int BACK_THREADS = 256, BACK_UNROLL = 4;
 
 template <typename T>

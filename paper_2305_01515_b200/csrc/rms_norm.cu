@@ -1,6 +1,6 @@
 // Root-mean-square norm of the residual stream, forward (output in the tensors' type or in 8 bits) and backward.
 //
-//   r = round(x + residual),  c = 1 / sqrt(mean_j r_j^2 + eps),  y_j = r_j c w_j
+//   r = round(x + residual),  c = 1 / sqrt(mean_j r_j^2 + eps),  y_j = r_j c w_j;  in 8 bits code_j = e4m3(r_j w_j 448 / max |r w|), scale = c max |r w| / 448
 //   dx_j = dr_j + c (dy_j w_j - r_j a),  a = c^2 mean_j(dy_j w_j r_j),   dw_j = sum over rows of dy_j r_j c
 //
 // Memory bounds it: six operations an element forward, a dozen backward.  So a row is read once, held in registers until its sum is known, and written
@@ -210,8 +210,8 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int D, int chunk, cons
 
 // A row by blockDim.x / 32 warps, up to 1,024 columns by each, or R rows by a warp (times 32 / LANES), so that a warp has four chunks on their way
 // whatever the width; blockDim.y such sets a block.  Everything of a row is in registers between its one reading and its one writing.
-// us, with a residual: 131,072 x 1,024 bf16 162 (6.63 TB/s, the copy rate); 8,192 x 8,192 to 8 bits, groups of 128, 95 (4.8 TB/s: issue slots 71% busy with the
-// codes and their maxima); 120,007 x 256 to 8 bits 44 (4.9 TB/s); 2,000 x 32,768 106 (one block of 1,024 threads an SM, 5.0 TB/s).  100,003 x 333 fp32 without, off
+// us, with a residual: 131,072 x 1,024 bf16 162 (6.63 TB/s, the copy rate); 8,192 x 8,192 to 8 bits, groups of 128, 95 (4.8 TB/s: issue slots 72% busy with the
+// codes and their maxima); 120,007 x 256 to 8 bits 45 (4.8 TB/s); 2,000 x 32,768 106 (one block of 1,024 threads an SM, 5.0 TB/s).  100,003 x 333 fp32 without, off
 // boundaries, 52 (5.1 TB/s): single elements, and the last chunk's 179 places that hold none.
 template <typename T, bool VECTOR, int R, int I, int LANES, int THREADS, bool CODES>
 __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VECTOR && sizeof(T) == 2) || R * I <= 2 ? 4 : 2)
@@ -400,8 +400,8 @@ struct NormBackward {
 
 // As many blocks as the GPU holds walk over the rows (shaped as in the forward, with two chunks a warp while there are warps enough: three arrays are in
 // registers); each thread keeps the sums of its columns of the weight's gradient, and the blocks' sums are added by the kernel below: no atomics, so that
-// results are the same in every run.  131,072 x 1,024 bf16 with the stream's gradient: 200-207 us (5.2-5.4 TB/s of what moves); 100,003 x 333 fp32 88 (4.6).
-// Four chunks a warp and a third fewer warps took 272 us there, one chunk a warp 200 for 332 fp32 columns (112 with two).
+// results are the same in every run.  131,072 x 1,024 bf16 with the stream's gradient: 197-207 us (5.2-5.5 TB/s of what moves); 100,003 x 333 fp32 86-92 (4.3-4.6).
+// Four chunks a warp and a third fewer warps took 272 us there, one chunk a warp 200 for 332 fp32 columns (93-98 with two).
 // A thread has 80 registers where rows come in vectors of 16-bit elements and a warp has two chunks, 128 else, and spills none: no instance has a stack.  A row has 16 warps at
 // most; where two chunks for each do not hold it they have four or eight.  Where the arrays of these do not fit (HELD false) they are read again for the second part,
 // from L1 or L2 where the row has just passed.  us: 10,000 x 5,000 bf16 117 (3 arrays, 2.6 TB/s), 6,000 x 16,384 242 (with the stream's gradient, 3.3), 3,000 x 32,768 264 and 332
